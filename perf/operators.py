@@ -302,7 +302,7 @@ def _quantise(x):
     x = x.unflatten(-1, (-1, GROUP))
     lo, hi = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
     ok = (hi <= LIMIT) & (lo >= -LIMIT)
-    scale = torch.where(ok, (hi - lo) / 15, math.nan).half()
+    scale = torch.where(ok, (hi - lo) / torch.full_like(hi, 15.0), math.nan).half()
     centre = (lo + 8 * scale.float()).half()
     inv = torch.where(scale > 0, 1 / scale.float(), 0.0)
     u = torch.where(ok, (((x - centre.float()) * inv).round() + 8).clamp(0, 15), 8.0).to(torch.uint8).flatten(-2)
@@ -467,7 +467,7 @@ def _handles(s):
         s["workspace"] = kv4.attend_workspace(s["pages"], case["q_heads"], len(_list(case["lengths"])),
                                               s["q"].shape[0], s["max_q"])
     elif case["op"] != "append":
-        s["workspace"] = kv4.pages_workspace(s["pages"], len(_list(case["lengths"])))
+        s["workspace"] = kv4.pages_workspace(s["pages"])
 
 
 def _own(s):
