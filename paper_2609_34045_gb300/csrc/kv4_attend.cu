@@ -1,0 +1,154 @@
+// Attention over the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_attend.
+//
+// A warp per query row (token, head): 32 keys at a time, a lane's key's score from its codes, the running maximum and
+// sum of the softmax, then each lane's channels of the weighted values.
+#include <math.h>
+
+#include "kv4.cuh"
+
+namespace kfl {
+namespace {
+
+struct AttendParams {
+  Kv4Pool pool;
+  Kv4Map map;
+  int layer;
+  HeadsView q, out;
+  float *lse;
+  const int32_t *users, *q_start;
+  int n_seqs, n_tokens, max_q, n_heads, group;
+  float scale;
+  int window;
+  int32_t *status;
+};
+
+template <class T>
+__global__ void __launch_bounds__(128) kv4_attend_kernel(const AttendParams p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float s_q[4][128];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hd = p.pool.head_dim;
+  const int s = blockIdx.y / p.max_q, i = blockIdx.y % p.max_q;
+  const int head = blockIdx.x * 4 + warp;
+  if (head >= p.n_heads) return;
+  const int first = p.q_start ? p.q_start[s] : s, count = (p.q_start ? p.q_start[s + 1] : s + 1) - first;
+  if (i >= count || first < 0 || first + i >= p.n_tokens) return;
+  const int64_t t = first + i;
+  const int user = p.users ? p.users[s] : s;
+  const bool known = user >= 0 && user < p.map.n_users;
+  if (!known && lane == 0) report(p.status, KFL_BAD_USER);
+  const int length = known ? min(max(0, p.map.lengths[user]), p.map.max_pages << p.pool.log2_tokens) : 0;
+  const int end = length - count + i + 1;  // keys below it are seen
+  const int begin = p.window > 0 ? max(0, end - p.window) : 0;
+  const T *q = reinterpret_cast<const T *>(p.q.row(t, head));
+  for (int c = lane; c < hd; c += 32) s_q[warp][c] = to_f32(q[c]) * p.scale;
+  __syncwarp();
+  float top = -INFINITY, sum = 0.f, acc[4] = {};
+  for (int k0 = begin; k0 < end; k0 += 32) {
+    const int key = k0 + lane;
+    const uint8_t *block = nullptr;
+    int slot = 0;
+    if (key < end) {
+      const int page = p.map.table[(int64_t)user * p.map.max_pages + (key >> p.pool.log2_tokens)];
+      if (page < 0 || page >= p.pool.n_pages)
+        report(p.status, KFL_BAD_PAGE);
+      else
+        block = p.pool.block(page, p.layer, head / p.group), slot = key & (p.pool.page_tokens() - 1);
+    }
+    float score = -INFINITY;
+    const int groups = hd / KV4_GROUP;
+    if (block) {
+      score = 0.f;
+      for (int g = 0; g < groups; ++g) {
+        const __half2 par = *reinterpret_cast<const __half2 *>(block + 2 * p.pool.code_bytes() + (slot * groups + g) * 4);
+        for (int w = 0; w < 8; ++w) {
+          const uint32_t codes = *reinterpret_cast<const uint32_t *>(block + slot * (hd / 2) + g * 32 + w * 4);
+          for (int j = 0; j < 8; ++j)
+            score = fmaf(fmaf((float)((int)((codes >> (4 * j)) & 15) - 8), __low2float(par), __high2float(par)),
+                         s_q[warp][g * 64 + w * 8 + j], score);
+        }
+      }
+    }
+    float m = score;
+    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    const float now = fmaxf(top, m);
+    const float base = now == -INFINITY ? 0.f : now;
+    const float keep = expf(top - base);
+    const float weight = block ? expf(score - base) : 0.f;
+    top = now;
+    sum *= keep;
+    for (int c = 0; c < 4; ++c) acc[c] *= keep;
+    for (int j = 0; j < 32; ++j) {
+      const uint64_t at = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(block), j);
+      const float w = __shfl_sync(0xffffffffu, weight, j);
+      const int sl = __shfl_sync(0xffffffffu, slot, j);
+      if (!at) continue;
+      const uint8_t *b = reinterpret_cast<const uint8_t *>(at);
+      sum += w;
+      for (int c = 0; c < hd / 32; ++c) {
+        const int ch = lane + 32 * c;
+        const int byte = b[p.pool.code_bytes() + sl * (hd / 2) + ch / 2];
+        const __half2 par = *reinterpret_cast<const __half2 *>(b + 2 * p.pool.code_bytes() + p.pool.param_bytes() +
+                                                               (sl * groups + ch / KV4_GROUP) * 4);
+        acc[c] = fmaf(w, fmaf((float)((ch & 1 ? byte >> 4 : byte & 15) - 8), __low2float(par), __high2float(par)), acc[c]);
+      }
+    }
+  }
+  T *out = reinterpret_cast<T *>(p.out.row(t, head));
+  for (int c = 0; c < hd / 32; ++c) out[lane + 32 * c] = from_f32<T>(sum == 0.f ? 0.f : acc[c] / sum);
+  if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : top + logf(sum);
+}
+
+int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_seqs, int n_tokens, int max_q,
+                 bool bytes) {
+  const int rc = check_pool(pool, bytes, me);
+  if (rc != KFL_OK) return rc;
+  if (n_heads < 1 || n_heads % pool->n_kv_heads || n_heads / pool->n_kv_heads > 128)
+    return bad_arg(me, "the query heads are a multiple of n_kv_heads, at most 128 per KV head");
+  if (n_seqs < 0 || n_tokens < 0 || max_q < 1) return bad_arg(me, "n_seqs, n_tokens and max_q are not negative");
+  return KFL_OK;
+}
+
+}  // namespace
+}  // namespace kfl
+
+using namespace kfl;
+
+extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_heads, int n_seqs, int n_tokens,
+                                              int max_q, size_t *out) {
+  const char *me = "kfl_kv4_attend_workspace_bytes";
+  const int rc = check_attend(me, pool, n_heads, n_seqs, n_tokens, max_q, false);
+  if (rc != KFL_OK) return rc;
+  if (!out) return bad_arg(me, "NULL pointer");
+  *out = 16;
+  return KFL_OK;
+}
+
+extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
+                              const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start,
+                              int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace,
+                              size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  const char *me = "kfl_kv4_attend";
+  if (!heads_valid(q) || !heads_valid(out)) return bad_arg(me, "q and out are needed");
+  int rc = check_attend(me, pool, q->n_heads, n_seqs, n_tokens, max_q, true);
+  if (rc == KFL_OK) rc = check_map(map, me);
+  if (rc == KFL_OK) rc = check_layer(pool, layer, me);
+  if (rc != KFL_OK) return rc;
+  if (q->n_heads != out->n_heads || q->dtype != out->dtype || q->dtype == KFL_DT_FP32)
+    return bad_arg(me, "q and out have the same heads and are both bf16 or both fp16");
+  if (!std::isfinite(scale) || window < 0) return bad_arg(me, "scale is finite, window not negative");
+  if (!q_start && n_tokens != n_seqs) return bad_arg(me, "without q_start every sequence has one token");
+  size_t need = 0;
+  rc = kfl_kv4_attend_workspace_bytes(pool, q->n_heads, n_seqs, n_tokens, max_q, &need);
+  if (rc != KFL_OK) return rc;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < need)
+    return bad_arg(me, "a 16-byte aligned workspace of kfl_kv4_attend_workspace_bytes is needed");
+  if (n_seqs == 0 || n_tokens == 0) return KFL_OK;
+  AttendParams p = {pool_of(*pool), map_of(*map), layer, view_of(*q), view_of(*out), lse, users, q_start, n_seqs,
+                    n_tokens, q_start ? max_q : 1, q->n_heads, q->n_heads / pool->n_kv_heads, scale, window, status};
+  const dim3 grid((q->n_heads + 3) / 4, n_seqs * p.max_q);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = q->dtype == KFL_DT_BF16 ? launch_chained(kv4_attend_kernel<__nv_bfloat16>, grid, 128, 0, s, p)
+                                                : launch_chained(kv4_attend_kernel<__half>, grid, 128, 0, s, p);
+  return cuda_result(e, me);
+}

@@ -1,0 +1,295 @@
+"""Python binding of ``include/kafila_rope.h`` and ``include/kafila_kv4.h``: rotary positions and the 4-bit
+paged KV cache (argument marshalling only, as in ``stage``).
+
+Functions named ``kfl_*`` call the C entry point of that name on CUDA tensors.  ``rope_plan``, ``pool`` and
+``page_map`` describe buffers that the caller keeps; ``attend_workspace`` and ``pages_workspace`` allocate the
+scratch that those calls want.  Rows of heads are tensors ``[token][head][head_dim]`` of any strides whose last
+is 1.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import stage
+from .stage import KflError  # noqa: F401
+
+KFL_BAD_POSITION, KFL_BAD_USER, KFL_BAD_PAGE, KFL_NO_PAGES = 1, 2, 4, 8
+LAYOUTS = {"half": 0, "interleaved": 1}
+SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class kfl_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_heads", C.c_int), ("dtype", C.c_int)]
+
+
+class kfl_rope_cfg(C.Structure):
+    _fields_ = [("rope_dim", C.c_int), ("scaling", C.c_int), ("theta", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("original_ctx", C.c_double), ("magnitude", C.c_double)]
+
+
+class kfl_rope_plan(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("n_pos", C.c_int), ("rope_dim", C.c_int), ("layout", C.c_int)]
+
+
+class kfl_kv4_pool(C.Structure):
+    _fields_ = [("pages", C.c_void_p)] + [(n, C.c_int) for n in ("n_pages", "page_tokens", "n_layers", "n_kv_heads",
+                                                                 "head_dim")]
+
+
+class kfl_kv4_map(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lengths", C.c_void_p), ("refs", C.c_void_p), ("n_users", C.c_int),
+                ("max_pages", C.c_int)]
+
+
+_lib = _signed = None
+
+
+def lib() -> C.CDLL:
+    """The library of ``stage.lib()`` with the signatures of these entry points."""
+    global _lib, _signed
+    L = stage.lib()
+    if _signed is not L:
+        vp, i, f, P = C.c_void_p, C.c_int, C.c_float, C.POINTER
+        heads, plan, pl, mp, sz = P(kfl_heads), P(kfl_rope_plan), P(kfl_kv4_pool), P(kfl_kv4_map), P(C.c_size_t)
+        for name, args in {
+            "kfl_rope_table": [P(kfl_rope_cfg), i, vp, vp],
+            "kfl_rope": [plan, heads, heads, heads, heads, vp, i, i, i, vp, vp],
+            "kfl_kv4_page_bytes": [pl, sz],
+            "kfl_kv4_append": [pl, mp, i, heads, heads, vp, vp, i, plan, vp, vp],
+            "kfl_kv4_read": [pl, mp, i, vp, vp, i, heads, heads, vp, vp],
+            "kfl_kv4_attend": [pl, mp, i, heads, heads, vp, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
+            "kfl_kv4_attend_workspace_bytes": [pl, i, i, i, i, sz],
+            "kfl_kv4_pages_workspace_bytes": [pl, sz],
+            "kfl_kv4_reserve": [pl, mp, vp, vp, i, vp, vp, vp],
+            "kfl_kv4_fork": [pl, mp, vp, vp, i, vp, vp, vp],
+            "kfl_kv4_free": [pl, mp, vp, i, vp, vp],
+            "kfl_kv4_compact": [pl, mp, vp, vp, vp, vp, vp, vp],
+            "kfl_kv4_copy_pages": [pl, vp, vp, i, vp, vp],
+        }.items():
+            fn = getattr(L, name)
+            fn.argtypes, fn.restype = args, i
+        _lib = _signed = L
+    return L
+
+
+def _check(rc: int, where: str) -> None:
+    if rc < 0:
+        detail = stage.kfl_last_error_detail()
+        raise KflError(rc, detail if detail.startswith(where) else where)
+
+
+def _at(t):
+    """Address of a CUDA tensor (None: NULL)."""
+    return None if t is None else t.data_ptr()
+
+
+def _int32(t, where, n=None):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
+        raise ValueError(f"{where} is a contiguous int32 tensor" + (f" of {n}" if n is not None else ""))
+    return t.data_ptr()
+
+
+def _heads(t, where, head_dim=None):
+    if t is None:
+        return None
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or (strides[2] != 1 and shape[2] != 1) or (head_dim is not None and shape[2] != head_dim):
+        raise ValueError(f"{where} is [token][head][head_dim] with contiguous channels")
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"{where} is bf16, fp16 or fp32")
+    return kfl_heads(t.data_ptr(), strides[0], strides[1], shape[1], dtype)
+
+
+# ---- rotary positions ----------------------------------------------------------------------------
+
+def kfl_rope_table(n_pos: int, rope_dim: int, theta: float, scaling: str = "plain", factor: float = 1.0,
+                   low: float = 0.0, high: float = 0.0, original_ctx: float = 0.0, magnitude: float = 0.0, out=None,
+                   cuda_stream: int | None = None):
+    """cos and sin of positions [0, n_pos): fp32 [n_pos][rope_dim / 2][2] (``out``, or a new tensor)."""
+    if out is None:
+        out = torch.empty(max(n_pos, 0), max(rope_dim // 2, 0), 2, dtype=torch.float32, device="cuda")
+    cfg = kfl_rope_cfg(rope_dim, SCALINGS[scaling], theta, factor, low, high, original_ctx, magnitude)
+    _check(lib().kfl_rope_table(C.byref(cfg), n_pos, _at(out), cuda_stream), "kfl_rope_table")
+    return out
+
+
+def rope_plan(table, layout: str = "half") -> kfl_rope_plan:
+    """A rotation by a table of kfl_rope_table; keeps the tensor alive."""
+    if table.dtype != torch.float32 or not table.is_contiguous() or table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("a rotation's table is a contiguous fp32 [n_pos][rope_dim / 2][2]")
+    plan = kfl_rope_plan(table.data_ptr(), table.shape[0], 2 * table.shape[1], LAYOUTS[layout])
+    plan.table = table
+    return plan
+
+
+def kfl_rope(plan: kfl_rope_plan, q, q_out, k, k_out, positions, inverse: bool = False, status=None,
+             cuda_stream: int | None = None) -> None:
+    """Rotates q into q_out and k into k_out ([token][head][head_dim]; k and k_out may be None; an output may be
+    its input) by int32 positions [token].  Asynchronous."""
+    n, _, hd = q.shape
+    a, b, c, d = _heads(q, "q"), _heads(q_out, "q_out", hd), _heads(k, "k", hd), _heads(k_out, "k_out", hd)
+    for x, name in ((q_out, "q_out"), (k, "k"), (k_out, "k_out")):
+        if x is not None and x.shape[0] != n:
+            raise ValueError(f"{name} has as many tokens as q")
+    _check(lib().kfl_rope(C.byref(plan), C.byref(a), C.byref(b), c and C.byref(c), d and C.byref(d),
+                          _int32(positions, "positions", n), n, hd, int(inverse), _int32(status, "status", 1),
+                          cuda_stream), "kfl_rope")
+
+
+# ---- the cache -----------------------------------------------------------------------------------
+
+def pool(pages, page_tokens: int, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int | None = None):
+    """A pool in the uint8 tensor ``pages`` (or, for the calls that move no bytes, ``n_pages`` of none)."""
+    page_bytes = n_layers * n_kv_heads * (page_tokens * head_dim * 9 // 8)
+    if pages is not None:
+        if pages.dtype != torch.uint8 or not pages.is_contiguous() or page_bytes < 1 or pages.numel() % page_bytes:
+            raise ValueError(f"the pages are a contiguous uint8 tensor of whole pages ({page_bytes} bytes)")
+        n_pages = pages.numel() // page_bytes
+    p = kfl_kv4_pool(_at(pages), n_pages, page_tokens, n_layers, n_kv_heads, head_dim)
+    p.tensor = pages
+    return p
+
+
+def page_map(table, lengths, refs) -> kfl_kv4_map:
+    """Who holds which pages: int32 table [n_users][max_pages], lengths [n_users], refs [n_pages]."""
+    m = kfl_kv4_map(_int32(table, "table"), _int32(lengths, "lengths", table.shape[0]), _int32(refs, "refs"),
+                    table.shape[0], table.shape[1])
+    m.tensors = (table, lengths, refs)
+    return m
+
+
+def _covers(p, m):
+    if m.tensors[2].numel() < p.n_pages:
+        raise ValueError(f"refs is a contiguous int32 tensor of {p.n_pages}")
+    return C.byref(p), C.byref(m)
+
+
+def kfl_kv4_page_bytes(p) -> int:
+    out = C.c_size_t(0)
+    _check(lib().kfl_kv4_page_bytes(C.byref(p), C.byref(out)), "kfl_kv4_page_bytes")
+    return out.value
+
+
+def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=None,
+                   cuda_stream: int | None = None) -> None:
+    """Rows of k and v ([token][KV head][head_dim]) of one layer into the users' pages at int32 positions [token];
+    k rotated first where ``rope`` is a rope_plan.  users None: row t is user t's.  Asynchronous."""
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError("k and v have the same tokens")
+    a, b = _heads(k, "k", p.head_dim), _heads(v, "v", p.head_dim)
+    _check(lib().kfl_kv4_append(C.byref(p), C.byref(m), layer, C.byref(a), C.byref(b), _int32(users, "users", n),
+                                _int32(positions, "positions", n), n, rope and C.byref(rope),
+                                _int32(status, "status", 1), cuda_stream), "kfl_kv4_append")
+
+
+def kfl_kv4_read(p, m, layer: int, users, positions, k_out, v_out, status=None, cuda_stream: int | None = None) -> None:
+    """The values that the cache holds for rows (users[t], positions[t]) of one layer.  Asynchronous."""
+    n = k_out.shape[0]
+    if v_out.shape[0] != n:
+        raise ValueError("k_out and v_out have the same tokens")
+    a, b = _heads(k_out, "k_out", p.head_dim), _heads(v_out, "v_out", p.head_dim)
+    _check(lib().kfl_kv4_read(C.byref(p), C.byref(m), layer, _int32(users, "users", n),
+                              _int32(positions, "positions", n), n, C.byref(a), C.byref(b),
+                              _int32(status, "status", 1), cuda_stream), "kfl_kv4_read")
+
+
+def kfl_kv4_attend_workspace_bytes(p, n_heads: int, n_seqs: int, n_tokens: int, max_q: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().kfl_kv4_attend_workspace_bytes(C.byref(p), n_heads, n_seqs, n_tokens, max_q, C.byref(out)),
+           "kfl_kv4_attend_workspace_bytes")
+    return out.value
+
+
+def attend_workspace(p, n_heads: int, n_seqs: int, n_tokens: int, max_q: int = 1):
+    """The zeroed workspace of kfl_kv4_attend for these sizes."""
+    return torch.zeros(kfl_kv4_attend_workspace_bytes(p, n_heads, n_seqs, n_tokens, max_q), dtype=torch.uint8,
+                       device="cuda")
+
+
+def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None, max_q: int = 1, scale=None,
+                   window: int = 0, lse=None, status=None, cuda_stream: int | None = None) -> None:
+    """Attention of q's rows over the users' cached rows of one layer, into out (bf16 or fp16
+    [token][query head][head_dim]).  Without q_start (int32 [sequence + 1]) every row is a sequence; without users
+    (int32 [sequence]) sequence s is user s.  lse: fp32 [token][query head].  Asynchronous."""
+    n, n_heads, hd = q.shape
+    if out.shape[0] != n:
+        raise ValueError("q and out have the same tokens")
+    if users is not None:
+        n_seqs = users.numel()
+    elif q_start is not None:
+        n_seqs = q_start.numel() - 1
+    else:
+        n_seqs = n
+    if users is None and n_seqs > m.n_users:
+        raise ValueError("more sequences than users")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
+        raise ValueError("lse is a contiguous fp32 [token][query head]")
+    a, b = _heads(q, "q", p.head_dim), _heads(out, "out", p.head_dim)
+    _check(lib().kfl_kv4_attend(C.byref(p), C.byref(m), layer, C.byref(a), C.byref(b), _at(lse),
+                                _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
+                                1.0 / math.sqrt(hd) if scale is None else scale, window, workspace.data_ptr(),
+                                workspace.numel(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
+
+
+# ---- pages ---------------------------------------------------------------------------------------
+
+def pages_workspace(p):
+    """Scratch of the calls that hand out or move pages."""
+    out = C.c_size_t(0)
+    _check(lib().kfl_kv4_pages_workspace_bytes(C.byref(p), C.byref(out)), "kfl_kv4_pages_workspace_bytes")
+    return torch.empty(out.value, dtype=torch.uint8, device="cuda")
+
+
+def _scratch(p, workspace):
+    """Address of a workspace that covers the pool's pages."""
+    if workspace.numel() < 12 * p.n_pages:
+        raise ValueError("the workspace is one of pages_workspace for this pool")
+    return workspace.data_ptr()
+
+
+def kfl_kv4_reserve(p, m, users, n_new, workspace, status=None, cuda_stream: int | None = None) -> None:
+    """Room for n_new[i] more tokens of user users[i] (int32): pages and lengths.  Asynchronous."""
+    n = users.numel()
+    a, b = _covers(p, m)
+    _check(lib().kfl_kv4_reserve(a, b, _int32(users, "users"), _int32(n_new, "n_new", n), n, _scratch(p, workspace),
+                                 _int32(status, "status", 1), cuda_stream), "kfl_kv4_reserve")
+
+
+def kfl_kv4_fork(p, m, src, dst, workspace, status=None, cuda_stream: int | None = None) -> None:
+    """User dst[i] goes on from where src[i] is (int32), all at once.  Asynchronous."""
+    n = dst.numel()
+    a, b = _covers(p, m)
+    _check(lib().kfl_kv4_fork(a, b, _int32(src, "src", n), _int32(dst, "dst"), n, _scratch(p, workspace),
+                              _int32(status, "status", 1), cuda_stream), "kfl_kv4_fork")
+
+
+def kfl_kv4_free(p, m, users, status=None, cuda_stream: int | None = None) -> None:
+    """Gives back the pages of the users (int32).  Asynchronous."""
+    a, b = _covers(p, m)
+    _check(lib().kfl_kv4_free(a, b, _int32(users, "users"), users.numel(), _int32(status, "status", 1), cuda_stream),
+           "kfl_kv4_free")
+
+
+def kfl_kv4_compact(p, m, table_out, refs_out, n_live, workspace, status=None, cuda_stream: int | None = None) -> None:
+    """Live pages to the lowest numbers; the new table and references into table_out and refs_out (the map's own
+    tensors or others), the number of live pages into n_live (int32, may be None).  Asynchronous."""
+    a, b = _covers(p, m)
+    _check(lib().kfl_kv4_compact(a, b, _int32(table_out, "table_out", m.n_users * m.max_pages),
+                                 _int32(refs_out, "refs_out", p.n_pages), _int32(n_live, "n_live", 1),
+                                 _scratch(p, workspace), _int32(status, "status", 1), cuda_stream), "kfl_kv4_compact")
+
+
+def kfl_kv4_copy_pages(p, src, dst, status=None, cuda_stream: int | None = None) -> None:
+    """Copies page src[i] to page dst[i] (int32).  Asynchronous."""
+    n = src.numel()
+    _check(lib().kfl_kv4_copy_pages(C.byref(p), _int32(src, "src"), _int32(dst, "dst", n), n,
+                                    _int32(status, "status", 1), cuda_stream), "kfl_kv4_copy_pages")
