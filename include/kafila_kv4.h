@@ -81,6 +81,7 @@ int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, co
  *             KV head h / (n_heads / n_kv_heads), at most 128 heads per KV head; out does not overlap q
  *   scale     of the scores (normally 1 / sqrt(head_dim))
  *   lse       NULL, or device fp32 [n_tokens][n_heads]: the natural log of the sum of exp(scores)
+ *   max_pages * page_tokens at most 2^26
  *   workspace device memory of kfl_kv4_attend_workspace_bytes for the same sizes (or larger ones), 16-byte
  *             aligned, zeroed before its first use and left as it has to be found.  Calls that may overlap
  *             (other streams, no ordering) need one each.

@@ -39,6 +39,7 @@ typedef struct {
 #define KFL_BAD_USER 2     /* a user outside [0, n_users), or named twice in one call */
 #define KFL_BAD_PAGE 4     /* a page number outside [0, n_pages) */
 #define KFL_NO_PAGES 8     /* the pool has no free page left, or the user's table row is full */
+#define KFL_TIMED_OUT 16   /* a bounded wait inside a kernel gave up: the call's outputs are not valid */
 
 /* ---- pairs of channels ---- */
 #define KFL_ROPE_HALF 0        /* (i, i + rope_dim / 2) */

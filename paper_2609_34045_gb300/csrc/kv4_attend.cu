@@ -4,23 +4,12 @@
 // sum of the softmax, then each lane's channels of the weighted values.
 #include <math.h>
 
-#include "kv4.cuh"
+#include <algorithm>
+
+#include "kv4_attend.cuh"
 
 namespace kfl {
 namespace {
-
-struct AttendParams {
-  Kv4Pool pool;
-  Kv4Map map;
-  int layer;
-  HeadsView q, out;
-  float *lse;
-  const int32_t *users, *q_start;
-  int n_seqs, n_tokens, max_q, n_heads, group;
-  float scale;
-  int window;
-  int32_t *status;
-};
 
 template <class T>
 __global__ void __launch_bounds__(128) kv4_attend_kernel(const AttendParams p) {
@@ -109,6 +98,11 @@ int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_se
   return KFL_OK;
 }
 
+// The workspace: tickets (zero between calls), then partial results.
+size_t ticket_bytes(const kfl_kv4_pool *pool, int n_seqs) {
+  return ((size_t)std::min(n_seqs, FEW_SEQS) * pool->n_kv_heads * 4 + 127) / 128 * 128;
+}
+
 }  // namespace
 }  // namespace kfl
 
@@ -120,7 +114,8 @@ extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_he
   const int rc = check_attend(me, pool, n_heads, n_seqs, n_tokens, max_q, false);
   if (rc != KFL_OK) return rc;
   if (!out) return bad_arg(me, "NULL pointer");
-  *out = 16;
+  const int cols = (int)std::min<int64_t>((int64_t)max_q * (n_heads / pool->n_kv_heads), FEW_ROWS);
+  *out = ticket_bytes(pool, n_seqs) + attend_few_partials(pool->head_dim, cols);
   return KFL_OK;
 }
 
@@ -144,10 +139,31 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < need)
     return bad_arg(me, "a 16-byte aligned workspace of kfl_kv4_attend_workspace_bytes is needed");
   if (n_seqs == 0 || n_tokens == 0) return KFL_OK;
-  AttendParams p = {pool_of(*pool), map_of(*map), layer, view_of(*q), view_of(*out), lse, users, q_start, n_seqs,
-                    n_tokens, q_start ? max_q : 1, q->n_heads, q->n_heads / pool->n_kv_heads, scale, window, status};
-  const dim3 grid((q->n_heads + 3) / 4, n_seqs * p.max_q);
+  if (((int64_t)map->max_pages * pool->page_tokens) > (1 << 26)) return bad_arg(me, "max_pages * page_tokens is at most 2^26");
+  AttendParams p = {};
+  p.pool = pool_of(*pool), p.map = map_of(*map), p.layer = layer;
+  p.q = view_of(*q), p.out = view_of(*out);
+  p.q_wide = rows_aligned16(*q), p.out_wide = rows_aligned16(*out), p.bf16 = q->dtype == KFL_DT_BF16;
+  p.lse = lse, p.users = users, p.q_start = q_start;
+  p.n_seqs = n_seqs, p.n_tokens = n_tokens, p.max_q = q_start ? max_q : 1;
+  p.n_heads = q->n_heads, p.group = q->n_heads / pool->n_kv_heads;
+  p.scale = scale, p.window = window, p.status = status;
+  p.tickets = static_cast<unsigned *>(workspace);
+  p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + ticket_bytes(pool, n_seqs));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const int64_t rows = (int64_t)p.max_q * p.group;
+  if (rows <= FEW_ROWS) {
+    int dev = 0, n_sm = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+    for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
+      p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
+      p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
+      e = launch_attend_few(p, (int)rows, n_sm, s);
+    }
+    return cuda_result(e, me);
+  }
+  const dim3 grid((q->n_heads + 3) / 4, n_seqs * p.max_q);
   const cudaError_t e = q->dtype == KFL_DT_BF16 ? launch_chained(kv4_attend_kernel<__nv_bfloat16>, grid, 128, 0, s, p)
                                                 : launch_chained(kv4_attend_kernel<__half>, grid, 128, 0, s, p);
   return cuda_result(e, me);

@@ -1,0 +1,772 @@
+// Attention over the 4-bit paged KV cache for few query rows per KV head (decode steps, short drafts).
+//
+// Mathematics.  For a KV head's query rows (token, head of its group) j and its keys t:
+//   x_tj = scale log2(e) sum_g [ s_tg sum_c (u_tc - 8) q_jc + c_tg sum_c q_jc ]        (g: groups of 64 channels)
+//   o_j = sum_t 2^(x_tj - m_j) [ s'_tg (u'_tc - 8) + c'_tg ] / sum_t 2^(x_tj - m_j)
+// The codes enter the matrix products as they are: an fp16 with the nibble in its mantissa is 16 (64 + u), exactly.
+// For the scores the 72 too many are taken off by the accumulator's start value -1152 sum q; for the values
+// the weights 2^(x - m) s' are the fp16 operand and 72 times their own sum (a product with ones) is taken off at
+// the end.  The scales so cost one factor per key and group, not per element, a group that reads as NaN
+// reaches exactly the rows that see it, and codes behind a user's end (any bits) are finite.
+//
+// What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
+// keeps up.  At 6.77 TB/s an SM gets 42 elements a clock; with 0.875 (K) and 1.0 (V) instructions per element
+// for the nibbles and some 0.7 for the rest it has to issue about 2 of 4 instructions a clock.
+//
+// Layout.  S^T = K Q^T and O^T = V^T P^T with m16n8k16: keys and channels fill M = 16, the query rows N = 8, nothing
+// is padded at 8 rows.  The matrix unit's k order is ours to choose, so a lane's K words hold whole fragments
+// in natural byte order, and V's pairs of tokens come together by one byte permute per eight codes.
+//
+// Work split.  The tiles (64 keys of one sequence and KV head) of all sequences form one list; one block per SM takes
+// an equal piece, its warps equal pieces of that.  A warp streams its tiles through two slots of its own
+// (bulk copies of whole page blocks), with no barrier between warps until the end.  What a warp holds of a
+// (sequence, head) that it does not own alone is merged within the block, then over blocks by the last to arrive;
+// every sum is taken in list order, so results do not depend on arrival.
+#include <algorithm>
+
+#include "kv4_attend.cuh"
+
+namespace kfl {
+namespace {
+
+constexpr int TILE = 64;  // keys
+
+template <int HD, int NT>
+struct Few {
+  // 12 warps of at most 168 registers; with 16 query rows 8 warps of 255
+  static constexpr int WARPS = NT == 1 ? 12 : 8;
+  static constexpr int THREADS = WARPS * 32;
+  static constexpr int COLS = 8 * NT;
+  static constexpr int GROUPS = HD / KV4_GROUP;
+  static constexpr int TILE_BYTES = TILE * HD * 9 / 8;
+  static constexpr int SLOTS = HD == 128 ? 2 : 3;
+  static constexpr int PARTIAL = COLS * HD + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
+  static constexpr int RING_BYTES = WARPS * SLOTS * TILE_BYTES;
+  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + 4 * WARPS * 4 + 16;
+  static_assert(PARTIAL * 4 <= TILE_BYTES, "a slot holds a warp's partial result");
+  static_assert(SMEM <= 232448, "shared memory of a block");
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float half_lo(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)x)); }
+__device__ __forceinline__ float half_hi(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)(x >> 16))); }
+
+// Nibbles I of both halves of a word as fp16 pairs 16 (64 + u).
+template <int I>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
+  const uint32_t v = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(v), "r"(0x00F000F0u), "r"(0x64006400u));
+  return r;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+
+// A place in the list of tiles.
+struct Cursor {
+  int seq, head, tile;   // tile: within the segment (sequence, KV head)
+  int n_tiles, first_tile;
+  int user, length, first, count;
+};
+
+// (user, length, first token, tokens) of a sequence; its tiles start at key first_tile * 64
+__device__ __forceinline__ int first_tile_of(int length, int count, int window) {
+  return window > 0 ? max(0, length - count + 1 - window) / TILE : 0;
+}
+
+__device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, const int *prefix, int window) {
+  const int4 v = info[c.seq];
+  c.user = v.x, c.length = v.y, c.first = v.z, c.count = v.w;
+  c.n_tiles = prefix[c.seq + 1] - prefix[c.seq];
+  c.first_tile = first_tile_of(v.y, v.w, window);
+}
+
+__device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, int n_seqs, int heads, const int4 *info,
+                                            const int *prefix, int window) {
+  int lo = 0, hi = n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)prefix[mid + 1] * heads > flat)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  c.seq = lo;
+  enter_sequence(c, info, prefix, window);
+  const int64_t rest = flat - (int64_t)prefix[lo] * heads;
+  c.head = (int)(rest / c.n_tiles);
+  c.tile = (int)(rest - (int64_t)c.head * c.n_tiles);
+}
+
+__device__ __forceinline__ void next_tile(Cursor &c, int n_seqs, int heads, const int4 *info, const int *prefix,
+                                          int window) {
+  if (++c.tile < c.n_tiles) return;
+  c.tile = 0;
+  if (++c.head < heads) return;
+  c.head = 0;
+  do {
+    if (++c.seq >= n_seqs) return;
+    enter_sequence(c, info, prefix, window);
+  } while (c.n_tiles == 0);
+}
+
+// One output row's channels from lane `lane`'s HD / 32 values.
+template <int HD>
+__device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c, int col, int lane, const float (&v)[HD / 32],
+                                          float top, float sum) {
+  const int64_t t = c.first + col / p.group;
+  const int head = c.head * p.group + col % p.group;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(t, head)) + lane * (HD / 32);
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    const float y = sum == 0.f ? 0.f : v[i] * inv;
+    out[i] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+  }
+  if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
+}
+
+// A column of several partial results, `n` of them at at(i) (in order): merged by one warp.
+template <int HD, int COLS, class At>
+__device__ __forceinline__ void merge_column(int n, int col, int lane, const At &at, float (&v)[HD / 32], float &top,
+                                             float &sum) {
+  top = -INFINITY, sum = 0.f;
+  for (int i = 0; i < n; ++i) top = fmaxf(top, at(i)[COLS * HD + col]);
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int j = 0; j < HD / 32; ++j) v[j] = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const float *part = at(i);
+    const float w = ex2(part[COLS * HD + col] - base);
+    sum = fmaf(part[COLS * HD + COLS + col], w, sum);
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) v[j] = fmaf(part[col * HD + lane * (HD / 32) + j], w, v[j]);
+  }
+}
+
+template <int HD, int NT>
+__global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel(const AttendParams p) {
+  using F = Few<HD, NT>;
+  constexpr int G = F::GROUPS, COLS = F::COLS, W = F::WARPS;
+  extern __shared__ __align__(128) uint8_t smem[];
+  int4 *info = reinterpret_cast<int4 *>(smem + F::RING_BYTES);
+  int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(prefix + FEW_SEQS + 4);
+  int *part_seg = reinterpret_cast<int *>(bars + W * F::SLOTS);  // [2 W]: segment of each partial result, or -1
+  int *part_place = part_seg + 2 * W;
+  int *n_parts = part_place + 2 * W, *last_flags = n_parts + 1;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
+  pdl_launch_dependents();
+  if (tid < W * F::SLOTS) mbar_init(smem_addr(bars + tid), 1);
+  if (tid < 2 * W) part_seg[tid] = -1;
+  fence_mbar_init();
+  pdl_wait();
+
+  // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros)
+  for (int s = tid; s < p.n_seqs; s += F::THREADS) {
+    const int user = p.users ? p.users[s] : p.seq0 + s;
+    int first = p.q_start ? p.q_start[s] : p.seq0 + s, count = p.q_start ? p.q_start[s + 1] - first : 1;
+    int length = 0;
+    if (first < 0 || count < 0 || count > p.max_q || first > p.n_tokens - count) {
+      if (blockIdx.x == 0) report(p.status, KFL_BAD_POSITION);
+      count = 0;
+    }
+    if (user < 0 || user >= p.map.n_users) {
+      if (blockIdx.x == 0) report(p.status, KFL_BAD_USER);
+    } else {
+      length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
+    }
+    const int tiles = count == 0 ? 0 : max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
+    info[s] = make_int4(user, length, first, count);
+    prefix[s + 1] = tiles;
+  }
+  if (tid == 0) prefix[0] = 0;
+  __syncthreads();
+  if (warp == 0) {
+    int before = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+      int v = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, v, off);
+        if (lane >= off) v += o;
+      }
+      if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + v;
+      before += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+  const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
+  // at least a tile for every warp of a block: fewer blocks, fewer merges
+  const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)W);
+  const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
+  if (c0 >= c1) return;
+  const int64_t w0 = c0 + (c1 - c0) * warp / W, w1 = c0 + (c1 - c0) * (warp + 1) / W;
+
+  const uint32_t ring = smem_addr(smem) + warp * F::SLOTS * F::TILE_BYTES;
+  const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
+  const int pb = min(TILE, 1 << lp);                 // tokens of a page block as it lies in a slot
+  const int sub_bytes = pb * HD * 9 / 8;
+  const int n_blocks = TILE / pb;                    // page blocks of a slot
+  const uint64_t policy = policy_evict_normal();
+
+  // ---- copies: lane i brings page block i of a tile (of a page of 128, lane i part i: codes and parameters of K and V)
+  Cursor fetch;
+  int fetch_page = -1;
+  bool fetch_ok = w0 < w1;
+  int64_t fetch_at = w0;
+  unsigned fetch_slot = 0;
+  if (fetch_ok) locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
+  const auto load_page = [&]() {  // the page of this lane's block of the tile at `fetch`
+    fetch_page = -2;              // none: behind the sequence's end
+    const int key = (fetch.first_tile + fetch.tile) * TILE + (lp == 7 ? 0 : lane << lp);
+    if (lane < (lp == 7 ? 1 : n_blocks) && key < fetch.length)
+      fetch_page = p.map.table[(int64_t)fetch.user * p.map.max_pages + (key >> lp)];
+  };
+  unsigned valid[F::SLOTS] = {};  // which of a slot's page blocks are there
+  bool dead = false;              // a wait gave up: no more copies, no results
+  const auto issue = [&]() {
+    int page = lp == 7 ? __shfl_sync(0xffffffffu, fetch_page, 0) : fetch_page;
+    const bool mine = lane < (lp == 7 ? 4 : n_blocks);
+    const bool there = mine && page >= 0 && page < p.pool.n_pages;
+    if (mine && page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+    unsigned have = __ballot_sync(0xffffffffu, there);
+    const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
+    if (lane == 0) mbar_arrive_expect_tx(bar, lp == 7 ? (have ? F::TILE_BYTES : 0) : __popc(have) * sub_bytes);
+    __syncwarp();
+    if (there) {
+      const uint8_t *src = p.pool.block(page, p.layer, fetch.head);
+      if (lp == 7) {
+        constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;
+        const int half = (fetch.first_tile + fetch.tile) & 1;
+        const int bytes = lane < 2 ? CODES : PARAMS;
+        const int from = lane < 2 ? (2 * lane + half) * CODES : 4 * CODES + (2 * (lane - 2) + half) * PARAMS;
+        const int to = lane < 2 ? lane * CODES : 2 * CODES + (lane - 2) * PARAMS;
+        bulk_g2s(dst + to, src + from, bytes, bar, policy);
+      } else {
+        bulk_g2s(dst + lane * sub_bytes, src, sub_bytes, bar, policy);
+      }
+    }
+    if (lp == 7) have = have ? 1u : 0u;
+#pragma unroll
+    for (int i = 0; i < F::SLOTS; ++i)
+      if (i == (int)fetch_slot) valid[i] = have;
+    fetch_slot = fetch_slot + 1 == F::SLOTS ? 0 : fetch_slot + 1;
+    if (++fetch_at < w1) {
+      next_tile(fetch, p.n_seqs, heads, info, prefix, p.window);
+      load_page();
+    } else {
+      fetch_ok = false;
+    }
+  };
+  if (fetch_ok) load_page();
+#pragma unroll
+  for (int i = 0; i < F::SLOTS; ++i)
+    if (fetch_ok) issue();
+
+  // ---- this warp's tiles
+  uint32_t q[NT][G][2][2][2];     // B fragments: [group][word of a lane][half of its pairs][register]
+  float seed[NT][G][2], qs[NT][G][2], cf[NT][2];
+  float o[NT][G][4][4], ones[NT][G][4], top[NT][2], sum[NT][2], centre[NT][G][2];
+  float v_unit = 0.f;             // the value scales' reference, a power of two
+  Cursor at;
+  if (w0 < w1) locate_tile(at, w0, p.n_seqs, heads, info, prefix, p.window);
+  unsigned slot = 0, phase = 0;
+  int rows = 0;
+  float *block_ws = p.partials + (size_t)blockIdx.x * (W + 2) * F::PARTIAL;
+  const float log2_scale = fabsf(p.scale) * 1.44269504089f;
+  for (int64_t flat = w0; flat < w1; ++flat) {
+    if (flat == w0 || at.tile == 0) {
+      // ---- a new (sequence, head): its query rows as fp16 (a power of two per row brings the largest to [2^14, 2^15))
+      rows = at.count * p.group;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x[G][16], big = 0.f;
+        const int col = n * 8 + gid;
+        const bool there = col < rows;
+        const char *src = there ? p.q.row(at.first + col / p.group, at.head * p.group + col % p.group) : nullptr;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const uint16_t *e = reinterpret_cast<const uint16_t *>(src) + g * 64 + tig * 16;
+          uint32_t w[8];
+          if (!there) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 0;
+          } else if (p.q_wide) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(e), b = *reinterpret_cast<const uint4 *>(e + 8);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = e[2 * i] | ((uint32_t)e[2 * i + 1] << 16);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint16_t h = (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
+            const float f = p.bf16 ? bf16_to_f32(h) : f16_to_f32(h);
+            x[g][i] = p.scale > 0.f ? f : p.scale < 0.f ? -f : 0.f;
+            big = fmaxf(big, fabsf(x[g][i]));
+          }
+        }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        float inv;
+        const float unit = xchunk_scale(big, &inv);
+        float total_g[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          total_g[g] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t pair = pack_half2(x[g][8 * j + i] * inv, x[g][8 * j + i + 4] * inv);
+              q[n][g][j][i >> 1][i & 1] = pair;
+              total_g[g] += half_lo(pair) + half_hi(pair);
+            }
+          total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], 1);
+          total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], 2);
+        }
+        // (columns of the accumulators: 2 tig, 2 tig + 1; the factor 16 of the codes is taken off with the scale)
+        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale * 0.0625f, 1e-37f);  // (not 0: -inf times it stays)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int from = (2 * tig + c) * 4;
+          cf[n][c] = __shfl_sync(0xffffffffu, factor, from);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float t = __shfl_sync(0xffffffffu, total_g[g], from);
+            qs[n][g][c] = 16.f * t;
+            seed[n][g][c] = -1152.f * t;
+            centre[n][g][c] = 0.f;
+          }
+          top[n][c] = -INFINITY, sum[n][c] = 0.f;
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            ones[n][g][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][g][i][j] = 0.f;
+          }
+        }
+      }
+      v_unit = 0.f;
+    }
+
+    // ---- one tile
+    if (!dead && !mbar_wait(bar0 + slot * 8, phase)) {
+      dead = true, fetch_ok = false;
+      if (lane == 0) report(p.status, KFL_TIMED_OUT);
+      for (int i = 0; i < F::SLOTS; ++i) mbar_wait(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
+    }
+    dead = __any_sync(0xffffffffu, dead);
+    if (!dead) {
+      const uint32_t base = ring + slot * F::TILE_BYTES;
+      const int key0 = (at.first_tile + at.tile) * TILE;
+      unsigned have = 0;
+#pragma unroll
+      for (int i = 0; i < F::SLOTS; ++i)
+        if (i == (int)slot) have = valid[i];
+      // some rows do not see all of the tile: its last keys, a window's first ones, a missing page
+      const int all_end = at.length - at.count + 1;
+      const bool masked = key0 + TILE > all_end || have != (1u << n_blocks) - 1 ||
+                          (p.window > 0 && key0 < at.length - p.window);
+      float x[NT][4][4];
+      uint32_t vpar[4][2][G];  // (scale, centre) of the lane's two keys of each subtile, as they are stored
+      const int key_lane = (gid >> 1) + 4 * (gid & 1);  // matrix row gid is this key of a subtile, row gid + 8 key_lane + 8
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        const int b = 16 * st / pb, r0 = 16 * st - b * pb;
+        const uint32_t kb = base + b * sub_bytes;
+        const uint32_t kp = kb + pb * HD, vp = kp + pb * (HD / 16);
+        uint2 kw[2][G];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int g = 0; g < G; ++g) kw[h][g] = lds64(kb + (r0 + key_lane + 8 * h) * (HD / 2) + g * 32 + tig * 8);
+        float ks[2][G], kc[2][G];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t off = (r0 + key_lane + 8 * h) * (G * 4);
+          uint32_t pk[G], pv[G];
+          if constexpr (G == 2) {
+            const uint2 a = lds64(kp + off), c = lds64(vp + off);
+            pk[0] = a.x, pk[G - 1] = a.y, pv[0] = c.x, pv[G - 1] = c.y;
+          } else {
+            pk[0] = lds32(kp + off), pv[0] = lds32(vp + off);
+          }
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            ks[h][g] = half_lo(pk[g]), kc[h][g] = half_hi(pk[g]);
+            vpar[st][h][g] = pv[g];
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[n][st][i] = 0.f;
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          float acc[NT][4];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            acc[n][0] = acc[n][2] = seed[n][g][0];
+            acc[n][1] = acc[n][3] = seed[n][g][1];
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t lo = j ? kw[0][g].y : kw[0][g].x, hi = j ? kw[1][g].y : kw[1][g].x;
+            const uint32_t a0 = code_pair<0>(lo), a1 = code_pair<0>(hi), a2 = code_pair<1>(lo), a3 = code_pair<1>(hi);
+            const uint32_t a4 = code_pair<2>(lo), a5 = code_pair<2>(hi), a6 = code_pair<3>(lo), a7 = code_pair<3>(hi);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
+              mma16816(acc[n], a4, a5, a6, a7, q[n][g][j][1][0], q[n][g][j][1][1]);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[n][st][i] = fmaf(ks[i >> 1][g], acc[n][i], fmaf(kc[i >> 1][g], qs[n][g][i & 1], x[n][st][i]));
+        }
+      }
+      unsigned hidden[NT] = {};  // a bit per score of this lane
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int k = 16 * st + key_lane + 8 * (i >> 1);
+              const int end = all_end + min((n * 8 + 2 * tig + (i & 1)) / p.group, at.count - 1);
+              const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> (k / pb) & 1);
+              if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
+            }
+        // parameters that no row sees may be anything
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+              const int k = 16 * st + key_lane + 8 * h;
+              if (key0 + k >= at.length || !(have >> (k / pb) & 1)) vpar[st][h][g] = 0;
+            }
+      }
+      // ---- running maximum, and a common unit of the value scales (their weights are fp16)
+      __half2 v_most = __float2half2_rn(0.f);  // (hmax2 passes over NaN)
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int g = 0; g < G; ++g) v_most = __hmax2(v_most, *reinterpret_cast<const __half2 *>(&vpar[st][h][g]));
+      float v_max = __low2float(v_most);
+      bool grows = v_max > v_unit;
+      float now[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float m = fmaxf(x[n][0][c], x[n][0][c + 2]);
+#pragma unroll
+          for (int st = 1; st < 4; ++st) m = fmaxf(m, fmaxf(x[n][st][c], x[n][st][c + 2]));
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+          now[n][c] = fmaxf(m, top[n][c]);
+          grows = grows || now[n][c] > top[n][c];
+        }
+      if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) v_max = fmaxf(v_max, __shfl_xor_sync(0xffffffffu, v_max, off));
+        float shrink = 1.f;
+        if (v_max > v_unit) {
+          // the power of two above the largest (at least the least fp16, so that its inverse is finite)
+          const float unit = __uint_as_float((__float_as_uint(v_max) & 0x7F800000u) + 0x00800000u);
+          shrink = v_unit / unit;
+          v_unit = unit;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float keep[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            keep[c] = now[n][c] == -INFINITY ? 1.f : ex2((top[n][c] - now[n][c]) * cf[n][c]);
+            top[n][c] = now[n][c];
+            sum[n][c] *= keep[c];
+#pragma unroll
+            for (int g = 0; g < G; ++g) centre[n][g][c] *= keep[c];
+            keep[c] *= shrink;
+          }
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              ones[n][g][i] *= keep[i & 1];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[n][g][i][j] *= keep[j & 1];
+            }
+          }
+        }
+      }
+      const float weight_unit = v_unit > 0.f ? 16384.f / v_unit : 0.f;
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        const int b = 16 * st / pb, r0 = 16 * st - b * pb;
+        const uint32_t vb = base + b * sub_bytes + pb * (HD / 2) + (r0 + tig) * (HD / 2) + gid * 4;
+        uint32_t pf[NT][G][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float pr[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float m = top[n][i & 1] == -INFINITY ? 0.f : top[n][i & 1] * cf[n][i & 1];
+            pr[i] = ex2(fmaf(x[n][st][i], cf[n][i & 1], -m));
+            sum[n][i & 1] += pr[i];
+          }
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float s = half_lo(vpar[st][i >> 1][g]), c = half_hi(vpar[st][i >> 1][g]);
+              if (masked && (hidden[n] >> (4 * st + i) & 1)) s = c = 0.f;
+              centre[n][g][i & 1] = fmaf(pr[i], c, centre[n][g][i & 1]);
+              w[i] = pr[i] * (s * weight_unit);
+            }
+            pf[n][g][0] = transpose8x8(pack_half2(w[0], w[1]));
+            pf[n][g][1] = transpose8x8(pack_half2(w[2], w[3]));
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const uint32_t wa = lds32(vb + g * 32), wb = lds32(vb + g * 32 + 4 * (HD / 2));
+          const uint32_t wc = lds32(vb + g * 32 + 8 * (HD / 2)), wd = lds32(vb + g * 32 + 12 * (HD / 2));
+          const uint32_t l0 = __byte_perm(wa, wb, 0x5410), h0 = __byte_perm(wa, wb, 0x7632);
+          const uint32_t l1 = __byte_perm(wc, wd, 0x5410), h1 = __byte_perm(wc, wd, 0x7632);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint32_t b0 = pf[n][g][0], b1 = pf[n][g][1];
+            mma16816(o[n][g][0], code_pair<0>(l0), code_pair<0>(h0), code_pair<0>(l1), code_pair<0>(h1), b0, b1);
+            mma16816(o[n][g][1], code_pair<1>(l0), code_pair<1>(h0), code_pair<1>(l1), code_pair<1>(h1), b0, b1);
+            mma16816(o[n][g][2], code_pair<2>(l0), code_pair<2>(h0), code_pair<2>(l1), code_pair<2>(h1), b0, b1);
+            mma16816(o[n][g][3], code_pair<3>(l0), code_pair<3>(h0), code_pair<3>(l1), code_pair<3>(h1), b0, b1);
+            mma16816(ones[n][g], 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, b0, b1);
+          }
+        }
+      }
+    }
+    __syncwarp();  // (every lane has read the slot)
+    if (fetch_ok) issue();
+    if (++slot == F::SLOTS) slot = 0, phase ^= 1;
+
+    // ---- the end of a (sequence, head), or of this warp's piece of it
+    const bool ends = at.tile + 1 == at.n_tiles;
+    if (ends || flat + 1 == w1) {
+      const int64_t seg_first = flat - at.tile;
+      const bool alone = ends && seg_first >= w0;
+      const float unit = v_unit * (1.f / 16384.f);
+      // a result that others continue goes to global memory while the ring is in use, else into the ring
+      const bool last = flat + 1 == w1;
+      float *part = last ? reinterpret_cast<float *>(smem + (size_t)warp * F::SLOTS * F::TILE_BYTES)
+                         : block_ws + (size_t)warp * F::PARTIAL;
+      if (!alone && lane == 0) part_seg[2 * warp + last] = at.seq * heads + at.head;
+      __syncwarp();
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = n * 8 + 2 * tig + c;
+          float l = sum[n][c];
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+          const float m = top[n][c] == -INFINITY ? -INFINITY : top[n][c] * cf[n][c];
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            float cen = centre[n][g][c];
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) cen += __shfl_xor_sync(0xffffffffu, cen, off);
+            // channels 64 g + 8 gid + 0..7 of this column
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], 0.0625f, -72.f * ones[n][g][c]), unit, cen);
+            if (alone) {
+              if (col < rows && !dead) {
+                uint16_t h[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const float y = l == 0.f ? 0.f : v[i] * inv;
+                  h[i] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+                }
+                uint16_t *out = reinterpret_cast<uint16_t *>(
+                                    p.out.row(at.first + col / p.group, at.head * p.group + col % p.group)) +
+                                64 * g + 8 * gid;
+                if (p.out_wide) {
+                  *reinterpret_cast<uint4 *>(out) =
+                      make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                                 h[6] | (uint32_t)h[7] << 16);
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) out[i] = h[i];
+                }
+              }
+            } else {
+              float4 *to = reinterpret_cast<float4 *>(part + col * HD + 64 * g + 8 * gid);
+              to[0] = make_float4(v[0], v[1], v[2], v[3]);
+              to[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+          }
+          if (gid == 0) {
+            if (!alone) {
+              part[COLS * HD + col] = m;
+              part[COLS * HD + COLS + col] = l;
+            } else if (p.lse && col < rows && !dead) {
+              p.lse[(int64_t)(at.first + col / p.group) * p.n_heads + at.head * p.group + col % p.group] =
+                  l == 0.f ? -INFINITY : 0.69314718056f * m + logf(l);
+            }
+          }
+        }
+      }
+    }
+    if (flat + 1 < w1) next_tile(at, p.n_seqs, heads, info, prefix, p.window);
+  }
+
+  // ---- partial results of this block, in list order ([warp][0: its first segment's, 1: its last's], without the
+  // places that hold none): those of a segment are neighbours
+  __syncthreads();
+  if (warp == 0) {
+    const int id = lane < 2 * W ? part_seg[lane] : -1;
+    const unsigned there = __ballot_sync(0xffffffffu, id >= 0);
+    __syncwarp();
+    if (id >= 0) {
+      const int k = __popc(there & ((1u << lane) - 1));
+      part_seg[k] = id, part_place[k] = lane;
+    }
+    if (lane == 0) *n_parts = __popc(there);
+  }
+  __syncthreads();
+  const auto place = [&](int k) {
+    const int e = part_place[k];
+    return e & 1 ? reinterpret_cast<const float *>(smem + (size_t)(e >> 1) * F::SLOTS * F::TILE_BYTES)
+                 : block_ws + (size_t)(e >> 1) * F::PARTIAL;
+  };
+  int cut[2] = {-1, -1};  // segments that other blocks have parts of: the block's first, its last
+  Cursor seg;
+  for (int e = 0, f; e < *n_parts; e = f) {
+    const int id = part_seg[e];
+    for (f = e + 1; f < *n_parts && part_seg[f] == id;) ++f;
+    seg.seq = id / heads;
+    enter_sequence(seg, info, prefix, p.window);
+    seg.head = id % heads;
+    const int64_t sa = (int64_t)prefix[seg.seq] * heads + (int64_t)seg.head * seg.n_tiles, sb = sa + seg.n_tiles;
+    const bool whole = sa >= c0 && sb <= c1;
+    const int where = sa < c0 ? 0 : 1;
+    if (!whole) cut[where] = id;
+    const auto nth = [&](int i) { return place(e + i); };
+    for (int col = warp; col < seg.count * p.group; col += W) {
+      float v[HD / 32], top_c, sum_c;
+      merge_column<HD, COLS>(f - e, col, lane, nth, v, top_c, sum_c);
+      if (whole) {
+        store_row<HD>(p, seg, col, lane, v, top_c, sum_c);
+      } else {
+        float *to = block_ws + (size_t)(W + where) * F::PARTIAL;
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) to[col * HD + lane * (HD / 32) + j] = v[j];
+        if (lane == 0) to[COLS * HD + col] = top_c, to[COLS * HD + COLS + col] = sum_c;
+      }
+    }
+  }
+  if (cut[0] < 0 && cut[1] < 0) return;
+  __threadfence();
+  __syncthreads();
+  for (int i = 0; i < 2; ++i) {
+    if (cut[i] < 0) continue;
+    seg.seq = cut[i] / heads;
+    enter_sequence(seg, info, prefix, p.window);
+    seg.head = cut[i] % heads;
+    const int64_t sa = (int64_t)prefix[seg.seq] * heads + (int64_t)seg.head * seg.n_tiles, sb = sa + seg.n_tiles;
+    const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
+    if (tid == 0) {
+      const unsigned before = atom_add_acq_rel(p.tickets + cut[i], 1u);
+      last_flags[i] = before == (unsigned)(to - from);
+      if (last_flags[i]) atomicExch(p.tickets + cut[i], 0u);  // as the next call has to find it
+    }
+    __syncthreads();
+    if (!last_flags[i]) continue;
+    const auto block_part = [&](int k) {
+      const int64_t b = from + k;
+      return static_cast<const float *>(p.partials + ((size_t)b * (W + 2) + W + (sa < b * quota ? 0 : 1)) * F::PARTIAL);
+    };
+    for (int col = warp; col < seg.count * p.group; col += W) {
+      float v[HD / 32], top_c, sum_c;
+      merge_column<HD, COLS>(to - from + 1, col, lane, block_part, v, top_c, sum_c);
+      store_row<HD>(p, seg, col, lane, v, top_c, sum_c);
+    }
+  }
+}
+
+template <int HD, int NT>
+cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
+  using F = Few<HD, NT>;
+  static SmemOptIn opt_in;
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_few_kernel<HD, NT>);
+  const cudaError_t e = opt_in(kernel, F::SMEM);
+  if (e != cudaSuccess) return e;
+  // as many blocks as the longest contexts could fill
+  const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
+  const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
+  return launch_chained(kv4_attend_few_kernel<HD, NT>, grid, F::THREADS, F::SMEM, s, p);
+}
+
+}  // namespace
+
+size_t attend_few_partials(int head_dim, int cols) {
+  const size_t floats = head_dim == 128 ? (cols <= 8 ? (size_t)Few<128, 1>::PARTIAL * (Few<128, 1>::WARPS + 2)
+                                                     : (size_t)Few<128, 2>::PARTIAL * (Few<128, 2>::WARPS + 2))
+                                        : (cols <= 8 ? (size_t)Few<64, 1>::PARTIAL * (Few<64, 1>::WARPS + 2)
+                                                     : (size_t)Few<64, 2>::PARTIAL * (Few<64, 2>::WARPS + 2));
+  return FEW_BLOCKS * floats * sizeof(float);
+}
+
+cudaError_t launch_attend_few(const AttendParams &p, int cols, int n_sm, cudaStream_t s) {
+  if (p.pool.head_dim == 128) return cols <= 8 ? launch<128, 1>(p, n_sm, s) : launch<128, 2>(p, n_sm, s);
+  return cols <= 8 ? launch<64, 1>(p, n_sm, s) : launch<64, 2>(p, n_sm, s);
+}
+
+}  // namespace kfl

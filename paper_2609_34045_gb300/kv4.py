@@ -16,7 +16,7 @@ import torch
 from . import stage
 from .stage import KflError  # noqa: F401
 
-KFL_BAD_POSITION, KFL_BAD_USER, KFL_BAD_PAGE, KFL_NO_PAGES = 1, 2, 4, 8
+KFL_BAD_POSITION, KFL_BAD_USER, KFL_BAD_PAGE, KFL_NO_PAGES, KFL_TIMED_OUT = 1, 2, 4, 8, 16
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
