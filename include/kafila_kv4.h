@@ -84,7 +84,7 @@ int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, co
  *   max_pages * page_tokens at most 2^26
  *   workspace device memory of kfl_kv4_attend_workspace_bytes for the same sizes (or larger ones), 16-byte
  *             aligned, zeroed before its first use and left as it has to be found.  Calls that may overlap
- *             (other streams, no ordering) need one each.
+ *             (other streams, no ordering) need one each; after KFL_TIMED_OUT it is zeroed again.
  * A page out of range is reported in status and its rows count as not cached.
  * Precision: fp16 products of the exact codes with fp32 sums for few query rows per KV head; values rounded to
  * fp16 for prompts; softmax weights rounded to fp16; sums and softmax statistics in fp32.

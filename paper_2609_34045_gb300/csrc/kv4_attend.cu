@@ -1,7 +1,7 @@
 // Attention over the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_attend.
 //
-// A warp per query row (token, head): 32 keys at a time, a lane's key's score from its codes, the running maximum and
-// sum of the softmax, then each lane's channels of the weighted values.
+// Up to 16 query rows per KV head (a decode step's group, a few drafted tokens of a small group) go to the kernel that
+// streams the cache (kv4_attend_few.cu), more to the one that multiplies 128 rows at a time (kv4_attend_prompt.cu).
 #include <math.h>
 
 #include <algorithm>
@@ -10,83 +10,6 @@
 
 namespace kfl {
 namespace {
-
-template <class T>
-__global__ void __launch_bounds__(128) kv4_attend_kernel(const AttendParams p) {
-  pdl_launch_dependents();
-  pdl_wait();
-  __shared__ float s_q[4][128];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hd = p.pool.head_dim;
-  const int s = blockIdx.y / p.max_q, i = blockIdx.y % p.max_q;
-  const int head = blockIdx.x * 4 + warp;
-  if (head >= p.n_heads) return;
-  const int first = p.q_start ? p.q_start[s] : s, count = (p.q_start ? p.q_start[s + 1] : s + 1) - first;
-  if (i >= count || first < 0 || first + i >= p.n_tokens) return;
-  const int64_t t = first + i;
-  const int user = p.users ? p.users[s] : s;
-  const bool known = user >= 0 && user < p.map.n_users;
-  if (!known && lane == 0) report(p.status, KFL_BAD_USER);
-  const int length = known ? min(max(0, p.map.lengths[user]), p.map.max_pages << p.pool.log2_tokens) : 0;
-  const int end = length - count + i + 1;  // keys below it are seen
-  const int begin = p.window > 0 ? max(0, end - p.window) : 0;
-  const T *q = reinterpret_cast<const T *>(p.q.row(t, head));
-  for (int c = lane; c < hd; c += 32) s_q[warp][c] = to_f32(q[c]) * p.scale;
-  __syncwarp();
-  float top = -INFINITY, sum = 0.f, acc[4] = {};
-  for (int k0 = begin; k0 < end; k0 += 32) {
-    const int key = k0 + lane;
-    const uint8_t *block = nullptr;
-    int slot = 0;
-    if (key < end) {
-      const int page = p.map.table[(int64_t)user * p.map.max_pages + (key >> p.pool.log2_tokens)];
-      if (page < 0 || page >= p.pool.n_pages)
-        report(p.status, KFL_BAD_PAGE);
-      else
-        block = p.pool.block(page, p.layer, head / p.group), slot = key & (p.pool.page_tokens() - 1);
-    }
-    float score = -INFINITY;
-    const int groups = hd / KV4_GROUP;
-    if (block) {
-      score = 0.f;
-      for (int g = 0; g < groups; ++g) {
-        const __half2 par = *reinterpret_cast<const __half2 *>(block + 2 * p.pool.code_bytes() + (slot * groups + g) * 4);
-        for (int w = 0; w < 8; ++w) {
-          const uint32_t codes = *reinterpret_cast<const uint32_t *>(block + slot * (hd / 2) + g * 32 + w * 4);
-          for (int j = 0; j < 8; ++j)
-            score = fmaf(fmaf((float)((int)((codes >> (4 * j)) & 15) - 8), __low2float(par), __high2float(par)),
-                         s_q[warp][g * 64 + w * 8 + j], score);
-        }
-      }
-    }
-    float m = score;
-    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-    const float now = fmaxf(top, m);
-    const float base = now == -INFINITY ? 0.f : now;
-    const float keep = expf(top - base);
-    const float weight = block ? expf(score - base) : 0.f;
-    top = now;
-    sum *= keep;
-    for (int c = 0; c < 4; ++c) acc[c] *= keep;
-    for (int j = 0; j < 32; ++j) {
-      const uint64_t at = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(block), j);
-      const float w = __shfl_sync(0xffffffffu, weight, j);
-      const int sl = __shfl_sync(0xffffffffu, slot, j);
-      if (!at) continue;
-      const uint8_t *b = reinterpret_cast<const uint8_t *>(at);
-      sum += w;
-      for (int c = 0; c < hd / 32; ++c) {
-        const int ch = lane + 32 * c;
-        const int byte = b[p.pool.code_bytes() + sl * (hd / 2) + ch / 2];
-        const __half2 par = *reinterpret_cast<const __half2 *>(b + 2 * p.pool.code_bytes() + p.pool.param_bytes() +
-                                                               (sl * groups + ch / KV4_GROUP) * 4);
-        acc[c] = fmaf(w, fmaf((float)((ch & 1 ? byte >> 4 : byte & 15) - 8), __low2float(par), __high2float(par)), acc[c]);
-      }
-    }
-  }
-  T *out = reinterpret_cast<T *>(p.out.row(t, head));
-  for (int c = 0; c < hd / 32; ++c) out[lane + 32 * c] = from_f32<T>(sum == 0.f ? 0.f : acc[c] / sum);
-  if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : top + logf(sum);
-}
 
 int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_seqs, int n_tokens, int max_q,
                  bool bytes) {
@@ -100,7 +23,7 @@ int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_se
 
 // The workspace: tickets (zero between calls), then partial results.
 size_t ticket_bytes(const kfl_kv4_pool *pool, int n_seqs) {
-  return ((size_t)std::min(n_seqs, FEW_SEQS) * pool->n_kv_heads * 4 + 127) / 128 * 128;
+  return (std::max<size_t>((size_t)std::min(n_seqs, FEW_SEQS) * pool->n_kv_heads, FEW_BLOCKS) * 4 + 127) / 128 * 128;
 }
 
 }  // namespace
@@ -114,8 +37,9 @@ extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_he
   const int rc = check_attend(me, pool, n_heads, n_seqs, n_tokens, max_q, false);
   if (rc != KFL_OK) return rc;
   if (!out) return bad_arg(me, "NULL pointer");
-  const int cols = (int)std::min<int64_t>((int64_t)max_q * (n_heads / pool->n_kv_heads), FEW_ROWS);
-  *out = ticket_bytes(pool, n_seqs) + attend_few_partials(pool->head_dim, cols);
+  const int64_t rows = (int64_t)max_q * (n_heads / pool->n_kv_heads);
+  *out = ticket_bytes(pool, n_seqs) +
+         (rows <= FEW_ROWS ? attend_few_partials(pool->head_dim, (int)rows) : attend_prompt_partials(pool->head_dim, rows));
   return KFL_OK;
 }
 
@@ -152,19 +76,13 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + ticket_bytes(pool, n_seqs));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)p.max_q * p.group;
-  if (rows <= FEW_ROWS) {
-    int dev = 0, n_sm = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
-    for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
-      p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
-      p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
-      e = launch_attend_few(p, (int)rows, n_sm, s);
-    }
-    return cuda_result(e, me);
+  int dev = 0, n_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+  for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
+    p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
+    p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
+    e = rows <= FEW_ROWS ? launch_attend_few(p, (int)rows, n_sm, s) : launch_attend_prompt(p, n_sm, s);
   }
-  const dim3 grid((q->n_heads + 3) / 4, n_seqs * p.max_q);
-  const cudaError_t e = q->dtype == KFL_DT_BF16 ? launch_chained(kv4_attend_kernel<__nv_bfloat16>, grid, 128, 0, s, p)
-                                                : launch_chained(kv4_attend_kernel<__half>, grid, 128, 0, s, p);
   return cuda_result(e, me);
 }

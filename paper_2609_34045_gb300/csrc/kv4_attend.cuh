@@ -21,13 +21,29 @@ struct AttendParams {
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
   float scale;
   int window;
-  unsigned *tickets;  // [n_seqs][n_kv_heads], zero between launches
+  unsigned *tickets;  // zero between launches: [n_seqs][n_kv_heads], many rows: [FEW_BLOCKS]
   float *partials;
   int32_t *status;
 };
 
+// Waits for an mbarrier phase for two seconds at most (by the clock: a poll may itself be held for microseconds).
+__device__ __forceinline__ bool wait_2s(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < 64; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long until = global_ns() + 2000000000ull;
+  while (!mbar_try_wait(bar, parity))
+    if (global_ns() > until) return false;
+  return true;
+}
+
 // Bytes of the few-row kernel's partial results for `cols` query rows per KV head.
 size_t attend_few_partials(int head_dim, int cols);
 cudaError_t launch_attend_few(const AttendParams &p, int cols, int n_sm, cudaStream_t s);
+
+
+// Query rows of a KV head that share a decoded tile in the many-row kernel.
+inline int prompt_rows(int64_t rows) { return rows > 128 ? 256 : 128; }
+size_t attend_prompt_partials(int head_dim, int64_t rows);
+cudaError_t launch_attend_prompt(const AttendParams &p, int n_sm, cudaStream_t s);
 
 }  // namespace kfl

@@ -385,10 +385,10 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     }
 
     // ---- one tile
-    if (!dead && !mbar_wait(bar0 + slot * 8, phase)) {
+    if (!dead && !wait_2s(bar0 + slot * 8, phase)) {
       dead = true, fetch_ok = false;
       if (lane == 0) report(p.status, KFL_TIMED_OUT);
-      for (int i = 0; i < F::SLOTS; ++i) mbar_wait(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
+      for (int i = 0; i < F::SLOTS; ++i) wait_2s(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
     }
     dead = __any_sync(0xffffffffu, dead);
     if (!dead) {

@@ -1,0 +1,726 @@
+// Attention over the 4-bit paged KV cache for many query rows per KV head (prompts, long drafts), on tcgen05.
+//
+// Mathematics.  The query rows (token, head of the group) of a KV head are the M of two matrix products,
+//   S = Q K^T (128 rows x 128 keys), O += P V,  P = 2^(c S - m),
+// with fp32 accumulators in tensor memory.  K and V are decoded once per block into fp16 operands in shared memory,
+// value = centre + (code - 8) scale rounded once; P takes the place of S as the second product's fp16 operand.  The
+// maximum m of a row moves only when it has grown by 2^8 (P stays below 256, far inside fp16), so that O is rarely
+// rescaled.  A row of Q is brought into fp16's range by a power of two that its scores are multiplied back by.
+//
+// What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe.  256 rows share a decoded tile, which
+// leaves the decoding (2.2 instructions per element, four warps) and the softmax (a thread per row, some 4 instructions
+// per score) beside 2048 clocks of products per 128 keys.
+//
+// Roles.  Warps 0-3 and 4-7: softmax of the two 128-row halves, a thread per row, and their Q and output; 8-11:
+// decoding, a thread per key, raw codes straight from global memory a tile ahead; 12: products.  While one
+// half's softmax runs, the other half's products do.
+//
+// Work split.  The (sequence, KV head, 256 rows) x (128 keys) tiles in sight form one list that the blocks share
+// equally; a row block cut between thread blocks is merged by the last to arrive, in list order.
+#include <algorithm>
+
+#include "kv4_attend.cuh"
+#include "prefill_tc.cuh"
+
+namespace kfl {
+namespace {
+
+constexpr int PT_KEYS = 128;                 // keys of a tile
+constexpr int PT_THREADS = 13 * 32;
+constexpr float PT_GROW = 8.f;               // log2 of how far a row's maximum may outgrow its reference
+
+template <int HD>
+struct Prompt {
+  static constexpr int KB = HD / 64;                       // 64-channel blocks of 128-byte rows
+  static constexpr int TILE = 128 * HD * 2;                // bytes of 128 rows in fp16
+  static constexpr int Q_AT = 0, K_AT = 2 * TILE, V_AT = 4 * TILE;
+  static constexpr int INFO_AT = 6 * TILE;                 // int4[FEW_SEQS], then int prefix[FEW_SEQS + 4]
+  static constexpr int FLAG_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;  // uint4 [4][1 + KB]: keys of a tile
+  static constexpr int BAR_AT = FLAG_AT + 4 * (1 + KB) * 16;
+  static constexpr int SMEM = BAR_AT + 20 * 8 + 32;
+  static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
+};
+
+// Barriers, in 8-byte places behind BAR_AT.
+enum { B_KFULL = 0, B_KFREE = 2, B_VFULL = 4, B_VFREE = 6, B_Q = 8, B_S = 10, B_P = 12, B_O = 14, B_READ = 16, B_DRAIN = 18, B_COUNT = 19 };
+
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory descriptor of an operand whose N (channels) lies contiguous, 128-byte swizzled: rows of 64 channels, one
+// per K (key), groups of 8 rows 1024 bytes apart (the stride byte offset), the next 64 channels `next` bytes on (the
+// leading byte offset).
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t addr, uint32_t next) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(next >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+__device__ __forceinline__ float pt_ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pt_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// A run of one row block's tiles: what a thread block works on at a time.
+struct Piece {
+  int seq, head, block;          // block: of rows_per_block query rows
+  int user, length, first, count;
+  int row0, rows;                // its query rows
+  int tile0, n_tiles;            // its first tile (of 128 keys) and how many it sees (at least one)
+  int from, to;                  // this thread block's run of them
+  int64_t flat;                  // place of its first tile in the list
+};
+
+struct List {
+  const int4 *info;
+  const int *prefix;
+  int n_seqs, heads, group, window, rows_per_block;
+};
+
+__device__ __forceinline__ void tiles_of_block(int length, int count, int block, const List &l, int &tile0, int &n) {
+  const int rows = count * l.group;
+  const int tok0 = block * l.rows_per_block / l.group;
+  const int tok1 = (min(rows, (block + 1) * l.rows_per_block) - 1) / l.group;
+  const int end = length - count + tok1 + 1;
+  const int begin = l.window > 0 ? max(0, length - count + tok0 + 1 - l.window) : 0;
+  tile0 = begin / PT_KEYS;
+  n = max(1, (max(end, 0) + PT_KEYS - 1) / PT_KEYS - tile0);
+}
+
+__device__ __forceinline__ void open_piece(Piece &pc, const List &l, int skip, int64_t limit) {
+  // the block's tiles from `skip` on, as far as the list's place `limit`
+  pc.row0 = pc.block * l.rows_per_block;
+  pc.rows = min(l.rows_per_block, pc.count * l.group - pc.row0);
+  tiles_of_block(pc.length, pc.count, pc.block, l, pc.tile0, pc.n_tiles);
+  pc.from = skip;
+  pc.to = (int)min((int64_t)pc.n_tiles, limit - pc.flat);
+}
+
+__device__ __forceinline__ void open_sequence(Piece &pc, const List &l) {
+  const int4 v = l.info[pc.seq];
+  pc.user = v.x, pc.length = v.y, pc.first = v.z, pc.count = v.w;
+}
+
+// The piece at place `at` of the list (at < limit).
+__device__ void find_piece(Piece &pc, const List &l, int64_t at, int64_t limit) {
+  int lo = 0, hi = l.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)l.prefix[mid + 1] * l.heads > at)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  pc.seq = lo;
+  open_sequence(pc, l);
+  const int64_t start = (int64_t)l.prefix[lo] * l.heads;
+  const int per_head = l.prefix[lo + 1] - l.prefix[lo];
+  pc.head = (int)((at - start) / per_head);
+  pc.flat = start + (int64_t)pc.head * per_head;
+  for (pc.block = 0;; ++pc.block) {
+    int tile0, n;
+    tiles_of_block(pc.length, pc.count, pc.block, l, tile0, n);
+    if (pc.flat + n > at) break;
+    pc.flat += n;
+  }
+  open_piece(pc, l, (int)(at - pc.flat), limit);
+}
+
+__device__ void next_piece(Piece &pc, const List &l, int64_t limit) {  // (the list goes on to `limit`)
+  pc.flat += pc.n_tiles;
+  if (++pc.block * l.rows_per_block >= pc.count * l.group) {
+    pc.block = 0;
+    if (++pc.head == l.heads) {
+      pc.head = 0;
+      do {
+        ++pc.seq;
+        open_sequence(pc, l);
+      } while (pc.count == 0);
+    }
+  }
+  open_piece(pc, l, 0, limit);
+}
+
+// Codes and parameters of one row in fp16 [channel], in the order that the words' nibbles come in (0 4 1 5 2 6 3 7 of
+// every eight), as a row of the swizzled operand.
+template <int HD>
+__device__ __forceinline__ void decode_row(const uint4 (&raw)[HD / 32], const uint32_t (&par)[HD / 64], uint32_t tile, int row) {
+#pragma unroll
+  for (int j = 0; j < HD / 8; ++j) {
+    const uint32_t w = j % 4 == 0 ? raw[j / 4].x : j % 4 == 1 ? raw[j / 4].y : j % 4 == 2 ? raw[j / 4].z : raw[j / 4].w;
+    const uint32_t s = __byte_perm(par[j / 8], 0, 0x1010), c = __byte_perm(par[j / 8], 0, 0x3232);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = i == 0 ? w << 4 : i == 1 ? w : i == 2 ? w >> 4 : w >> 8;
+      asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v[i]) : "r"(x), "r"(0x00F000F0u), "r"(0x64006400u));  // 16 (64 + u)
+      v[i] = hfma2(hfma2(v[i], 0x2C002C00u, 0xD480D480u), s, c);                                          // / 16 - 72: exact
+    }
+    const uint32_t at = tile + (j / 8) * (128 * 128) + row * 128 + (((j & 7) ^ (row & 7)) << 4);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const AttendParams p, int rows_per_block) {
+  using F = Prompt<HD>;
+  constexpr int KB = F::KB;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+  const uint32_t base = smem_addr(smem);
+  int4 *info = reinterpret_cast<int4 *>(smem + F::INFO_AT);
+  int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
+  uint4 *flags = reinterpret_cast<uint4 *>(smem + F::FLAG_AT);  // [4][0: page there, 1 + g: group g reads as NaN]
+  volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + F::BAR_AT + 20 * 8);  // TMEM, abort, last
+  const uint32_t bars = base + F::BAR_AT;
+  const auto bar = [&](int b) { return bars + 8 * b; };
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
+  const List list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
+  pdl_launch_dependents();
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(B_KFULL + i), 4);
+      mbar_init(bar(B_VFULL + i), 4);
+      mbar_init(bar(B_KFREE + i), 1);
+      mbar_init(bar(B_VFREE + i), 1);
+      mbar_init(bar(B_Q + i), 4);
+      mbar_init(bar(B_S + i), 1);
+      mbar_init(bar(B_P + i), 4);
+      mbar_init(bar(B_O + i), 1);
+      mbar_init(bar(B_READ + i), 4);
+    }
+    mbar_init(bar(B_DRAIN), 1);
+    words[1] = 0;
+    prefix[0] = 0;
+  }
+  fence_mbar_init();
+  if (warp == 12) tmem_alloc(base + F::BAR_AT + 20 * 8, 512);
+  pdl_wait();
+
+  // ---- the list: every sequence's tiles per head, summed
+  for (int s = warp; s < p.n_seqs; s += PT_THREADS / 32) {
+    const int user = p.users ? p.users[s] : p.seq0 + s;
+    const int first = p.q_start ? p.q_start[s] : p.seq0 + s;
+    int count = p.q_start ? p.q_start[s + 1] - first : 1, length = 0;
+    if (first < 0 || count < 0 || count > p.max_q || first > p.n_tokens - count) {
+      if (blockIdx.x == 0 && lane == 0) report(p.status, KFL_BAD_POSITION);
+      count = 0;
+    }
+    if (user < 0 || user >= p.map.n_users) {
+      if (blockIdx.x == 0 && lane == 0) report(p.status, KFL_BAD_USER);
+    } else {
+      length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
+    }
+    int tiles = 0;
+    for (int b = lane; b * rows_per_block < count * p.group; b += 32) {
+      int tile0, n;
+      tiles_of_block(length, count, b, list, tile0, n);
+      tiles += n;
+    }
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
+    if (lane == 0) info[s] = make_int4(user, length, first, count), prefix[s + 1] = tiles;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = words[0];
+  if (warp == 0) {
+    int before = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+      int v = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, v, off);
+        if (lane >= off) v += o;
+      }
+      if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + v;
+      before += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+  const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
+  const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+  const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
+  const size_t slot_floats = (size_t)rows_per_block * (HD + 2);
+
+  // a wait that gives up ends every role's loop
+  const auto wait = [&](int b, uint32_t parity) {
+    if (words[1]) return false;
+    if (wait_2s(bar(b), parity)) return true;
+    words[1] = 1;
+    report(p.status, KFL_TIMED_OUT);
+    return false;
+  };
+
+  if (c0 < c1 && warp < 8) {
+    // ---- softmax: a thread per query row
+    const int half = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
+    const uint32_t t_s = tmem + lanes + half * 128, t_o = tmem + lanes + 256 + half * 128;
+    const uint32_t q_tile = base + F::Q_AT + half * F::TILE;
+    const float log2_scale = fabsf(p.scale) * 1.44269504089f;
+    uint32_t done = 0;  // tiles of this half so far
+    bool ok = true;
+    unsigned tile = 0;  // tiles of the thread block so far (places of the flags)
+    Piece pc;
+    find_piece(pc, list, c0, c1);
+    for (;;) {
+      const int n = pc.to - pc.from;
+      if (half * 128 < pc.rows) {
+        const int r = half * 128 + row;
+        const bool there = r < pc.rows;
+        const int token = (pc.row0 + (there ? r : 0)) / p.group, head = pc.head * p.group + (pc.row0 + (there ? r : 0)) % p.group;
+        const int end = there ? pc.length - pc.count + token + 1 : pc.length;  // keys below it are seen
+        const int begin = p.window > 0 ? end - p.window : 0;
+        // its query, in fp16 and the words' channel order
+        float unit, inv;
+        {
+          const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q.row(pc.first + token, head));
+          uint32_t w[HD / 2];
+#pragma unroll
+          for (int i = 0; i < HD / 8; ++i) {
+            if (!there) {
+              w[4 * i] = w[4 * i + 1] = w[4 * i + 2] = w[4 * i + 3] = 0;
+            } else if (p.q_wide) {
+              const uint4 v = *reinterpret_cast<const uint4 *>(src + 8 * i);
+              w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[4 * i + j] = src[8 * i + 2 * j] | ((uint32_t)src[8 * i + 2 * j + 1] << 16);
+            }
+          }
+          const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
+          float big = 0.f;
+#pragma unroll
+          for (int i = 0; i < HD / 2; ++i) {
+            const float a = p.bf16 ? bf16_lo(w[i]) : f16_to_f32((uint16_t)w[i]);
+            const float b = p.bf16 ? bf16_hi(w[i]) : f16_to_f32((uint16_t)(w[i] >> 16));
+            big = fmaxf(big, fmaxf(fabsf(a), fabsf(b)));
+          }
+          unit = xchunk_scale(big, &inv);
+#pragma unroll
+          for (int i = 0; i < HD / 8; ++i) {
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t v = w[4 * i + j];
+              f[2 * j] = (p.bf16 ? bf16_lo(v) : f16_to_f32((uint16_t)v)) * inv * sign;
+              f[2 * j + 1] = (p.bf16 ? bf16_hi(v) : f16_to_f32((uint16_t)(v >> 16))) * inv * sign;
+            }
+            if (p.scale == 0.f)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = 0.f;
+            const uint32_t at = q_tile + (i / 8) * (128 * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(pt_pack(f[0], f[4])),
+                         "r"(pt_pack(f[1], f[5])), "r"(pt_pack(f[2], f[6])), "r"(pt_pack(f[3], f[7]))
+                         : "memory");
+          }
+        }
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_Q + half));
+        const float cf = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);
+        float top = -INFINITY, sum = 0.f;  // top: the reference, in scores times cf
+        unsigned poison = 0;               // groups of which this row sees a NaN
+        const auto see_poison = [&](int t) {
+          const uint4 *f = flags + ((tile + t) & 3) * (1 + KB) + 1;
+          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
+#pragma unroll
+          for (int g = 0; g < KB; ++g) {
+            const uint4 v = f[g];
+            if ((v.x | v.y | v.z | v.w) == 0) continue;
+            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+            for (int k = 0; k < PT_KEYS; ++k)
+              if ((bits[k >> 5] >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison |= 1u << g;
+          }
+        };
+        // rows of this warp: the least end and the greatest begin decide whether a tile is seen whole
+        const int least = __reduce_min_sync(0xffffffffu, end);
+        const int greatest = __reduce_max_sync(0xffffffffu, begin);
+        for (int t = 0; t < n && ok; ++t) {
+          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
+          ok = wait(B_S + half, done & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          if (t > 0) see_poison(t - 1);
+          const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
+          const bool masked = key0 + PT_KEYS > least || (p.window > 0 && key0 < greatest) ||
+                              (there4.x & there4.y & there4.z & there4.w) != 0xffffffffu;
+          const uint32_t pages[4] = {there4.x, there4.y, there4.z, there4.w};
+          uint32_t x[32];
+          float most = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_ld32(t_s + 32 * c, x);
+            if (masked) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const int key = key0 + 32 * c + i;
+                if (key >= end || key < begin || !(pages[c] >> i & 1)) x[i] = 0xff800000u;
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) most = fmaxf(most, __uint_as_float(x[i]));
+          }
+          most = most == -INFINITY ? most : most * cf;
+          float keep = 1.f;
+          const bool grows = most > top + PT_GROW || (top == -INFINITY && most > top);
+          if (grows) {
+            keep = pt_ex2(top - most);
+            top = most;
+            sum *= keep;
+          }
+          if (t > 0 && __any_sync(0xffffffffu, grows)) {
+            ok = wait(B_O + half, (done - 1) & 1);  // the last tile's product
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < HD / 16; ++c) {
+              uint32_t o[16];
+              tmem_ld16(t_o + 16 * c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+              tmem_st16(t_o + 16 * c, o);
+            }
+            tmem_wait_st();
+          }
+          const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_ld32(t_s + 32 * c, x);
+            if (masked) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const int key = key0 + 32 * c + i;
+                if (key >= end || key < begin || !(pages[c] >> i & 1)) x[i] = 0xff800000u;
+              }
+            }
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float a = pt_ex2(fmaf(__uint_as_float(x[2 * i]), cf, -ref));
+              const float b = pt_ex2(fmaf(__uint_as_float(x[2 * i + 1]), cf, -ref));
+              sum += a + b;
+              w[i] = pt_pack(a, b);
+            }
+            tmem_st16(t_s + 16 * c, w);  // (over scores that have been read)
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_P + half));
+          ++done;
+        }
+        // ---- the piece's end: O, divided and stored, or handed on
+        ok = ok && wait(B_O + half, (done - 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        see_poison(n - 1);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_READ + half));  // (the tiles' flags have been read)
+        const bool whole = pc.from == 0 && pc.to == pc.n_tiles;
+        const float inv_sum = sum == 0.f ? 0.f : 1.f / sum;
+        float *part = p.partials + ((size_t)blockIdx.x * 2 + (pc.from > 0 ? 0 : 1)) * slot_floats + (size_t)r * (HD + 2);
+        uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head));
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t x[32];
+          tmem_ld32(t_o + 32 * c, x);
+          if (!there) continue;
+          const bool nan = poison >> (c / 2) & 1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v[8];  // (back in the channels' own order)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[j] = __uint_as_float(x[8 * i + 2 * (j & 3) + (j >> 2)]);
+              if (nan) v[j] = __uint_as_float(0x7fc00000u);
+            }
+            if (whole) {
+              uint16_t h[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const float y = sum == 0.f ? 0.f : v[j] * inv_sum;
+                h[j] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+              }
+              if (p.out_wide) {
+                *reinterpret_cast<uint4 *>(out + 32 * c + 8 * i) =
+                    make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                               h[6] | (uint32_t)h[7] << 16);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) out[32 * c + 8 * i + j] = h[j];
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; j += 2) *reinterpret_cast<float2 *>(part + 2 + 32 * c + 8 * i + j) = make_float2(v[j], v[j + 1]);
+            }
+          }
+        }
+        if (there) {
+          if (!whole)
+            *reinterpret_cast<float2 *>(part) = make_float2(top, sum);
+          else if (p.lse)
+            p.lse[(int64_t)(pc.first + token) * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
+        }
+        tc_fence_before();
+      }
+      tile += n;
+      if (pc.flat + pc.to >= c1) break;
+      next_piece(pc, list, c1);
+    }
+  } else if (c0 < c1 && warp < 12) {
+    // ---- decoding: a thread per key
+    const int row = tid - 256, wq = warp - 8;
+    unsigned tile = 0;
+    bool ok = true;
+    Piece pc;
+    find_piece(pc, list, c0, c1);
+    uint4 kr[HD / 32];
+    uint32_t kp[KB];
+    int page = -1;
+    const auto page_of = [&](int key) {
+      if (key >= pc.length) return -2;
+      return p.map.table[(int64_t)pc.user * p.map.max_pages + (key >> lp)];
+    };
+    const auto load_row = [&](int key, int which, uint4 (&r)[HD / 32], uint32_t (&par)[KB]) {
+      const int slot = key & (p.pool.page_tokens() - 1);
+      const uint8_t *b = p.pool.block(page, p.layer, pc.head);
+      const uint4 *codes = reinterpret_cast<const uint4 *>(b + which * p.pool.code_bytes() + slot * (HD / 2));
+      const uint32_t *params = reinterpret_cast<const uint32_t *>(b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes()) + slot * KB;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) r[i] = codes[i];
+#pragma unroll
+      for (int i = 0; i < KB; ++i) par[i] = params[i];
+    };
+    for (;;) {
+      for (int t = pc.from; t < pc.to && ok; ++t, ++tile) {
+        const int buf = tile & 1;
+        const uint32_t parity = (tile >> 1 & 1) ^ 1;
+        const int key = (pc.tile0 + t) * PT_KEYS + row;
+        page = page_of(key);
+        const bool there = page >= 0 && page < p.pool.n_pages;
+        if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+        uint4 vr[HD / 32];
+        uint32_t vp[KB];
+        if (there) {
+          load_row(key, 0, kr, kp);
+          load_row(key, 1, vr, vp);
+        } else {
+#pragma unroll
+          for (int i = 0; i < HD / 32; ++i) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < KB; ++i) kp[i] = vp[i] = 0;
+        }
+        uint32_t *flag = reinterpret_cast<uint32_t *>(flags + (tile & 3) * (1 + KB)) + wq;
+        const unsigned have = __ballot_sync(0xffffffffu, there);
+        unsigned bad[KB];
+#pragma unroll
+        for (int g = 0; g < KB; ++g) {
+          // (a NaN or an infinity in scale or centre: all exponent bits set)
+          const bool nan = (vp[g] & 0x7c00u) == 0x7c00u || (vp[g] & 0x7c000000u) == 0x7c000000u;
+          bad[g] = __ballot_sync(0xffffffffu, nan);
+          if (nan) vp[g] = 0;
+        }
+        ok = wait(B_KFREE + buf, parity);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) {
+          flag[0] = have;
+#pragma unroll
+          for (int g = 0; g < KB; ++g) flag[4 * (1 + g)] = bad[g];
+        }
+        decode_row<HD>(kr, kp, base + F::K_AT + buf * F::TILE, row);
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_KFULL + buf));
+        ok = wait(B_VFREE + buf, parity);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        decode_row<HD>(vr, vp, base + F::V_AT + buf * F::TILE, row);
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_VFULL + buf));
+      }
+      if (!ok || pc.flat + pc.to >= c1) break;
+      next_piece(pc, list, c1);
+    }
+  } else if (c0 < c1) {
+    // ---- products, issued by an elected lane
+    constexpr uint32_t idesc_s = idesc_kind_f16(128, PT_KEYS, false);
+    constexpr uint32_t idesc_o = idesc_kind_f16(128, HD, false) | (1u << 16);  // B is N-major
+    unsigned tile = 0, done[2] = {}, pieces[2] = {};
+    int before = 0;
+    bool ok = true;
+    Piece pc;
+    find_piece(pc, list, c0, c1);
+    const auto scores = [&](int half, int buf) {
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = (k / 4) * (128 * 128) + (k % 4) * 32;
+          mma_bf16_ss(tmem + half * 128, sdesc_k_sw128(base + F::Q_AT + half * F::TILE + off),
+                      sdesc_k_sw128(base + F::K_AT + buf * F::TILE + off), idesc_s, k > 0);
+        }
+        mma_commit(bar(B_S + half));
+      }
+      __syncwarp();
+    };
+    for (; ok;) {
+      const int halves = pc.rows > 128 ? 2 : 1, n = pc.to - pc.from;
+      // the halves that worked on the last piece have read its flags (decoding runs ahead), and the ones that work
+      // on this one have their queries in place
+      for (int h = 0; h < before; ++h) ok = ok && wait(B_READ + h, (pieces[h] - 1) & 1);
+      for (int h = 0; h < halves; ++h) ok = ok && wait(B_Q + h, pieces[h]++ & 1);
+      before = halves;
+      ok = ok && wait(B_KFULL + (tile & 1), tile >> 1 & 1);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      for (int h = 0; h < halves; ++h) scores(h, tile & 1);
+      if (elect_one()) mma_commit(bar(B_KFREE + (tile & 1)));
+      __syncwarp();
+      for (int t = 0; t < n && ok; ++t, ++tile) {
+        const int buf = tile & 1;
+        const bool more = t + 1 < n;
+        ok = wait(B_VFULL + buf, tile >> 1 & 1);
+        for (int h = 0; h < halves && ok; ++h) {
+          ok = wait(B_P + h, done[h]++ & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < PT_KEYS / 16; ++k)
+              mma_ts(tmem + 256 + h * 128, tmem + h * 128 + 8 * k,
+                     sdesc_mn_sw128(base + F::V_AT + buf * F::TILE + k * 2048, KB == 2 ? 128 * 128 : 1024), idesc_o, t > 0 || k > 0);
+            mma_commit(bar(B_O + h));
+          }
+          __syncwarp();
+          if (more) {
+            if (h == 0) ok = wait(B_KFULL + (buf ^ 1), (tile + 1) >> 1 & 1);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            scores(h, buf ^ 1);
+          }
+        }
+        if (!ok) break;
+        if (elect_one()) {
+          mma_commit(bar(B_VFREE + buf));
+          if (more) mma_commit(bar(B_KFREE + (buf ^ 1)));
+        }
+        __syncwarp();
+      }
+      if (!ok || pc.flat + pc.to >= c1) break;
+      next_piece(pc, list, c1);
+    }
+    // every product has to be done before the tensor memory goes
+    if (elect_one()) mma_commit(bar(B_DRAIN));
+    __syncwarp();
+    wait_2s(bar(B_DRAIN), 0);
+  }
+  tc_fence_before();
+  __threadfence();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 12) tmem_dealloc(tmem, 512);
+  if (c0 >= c1 || words[1]) return;
+
+  // ---- row blocks that other thread blocks have parts of: this one's first, its last
+  for (int i = 0; i < 2; ++i) {
+    Piece pc;
+    find_piece(pc, list, i == 0 ? c0 : c1 - 1, c1);
+    const int64_t sa = pc.flat, sb = sa + pc.n_tiles;
+    if (!(i == 0 ? sa < c0 : sb > c1 && sa >= c0)) continue;
+    const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
+    __syncthreads();
+    if (tid == 0) {
+      unsigned *ticket = p.tickets + from;  // (a row block that is cut begins in one thread block, as its last one)
+      const unsigned before = atom_add_acq_rel(ticket, 1u);
+      words[2] = before == (unsigned)(to - from);
+      if (words[2]) atomicExch(ticket, 0u);
+    }
+    __syncthreads();
+    if (!words[2]) continue;
+    const auto part_of = [&](int b, int r) {
+      return p.partials + ((size_t)b * 2 + (sa < b * quota ? 0 : 1)) * slot_floats + (size_t)r * (HD + 2);
+    };
+    // a warp per row, lanes over its channels
+    for (int r = warp; r < pc.rows; r += PT_THREADS / 32) {
+      const int token = (pc.row0 + r) / p.group, head = pc.head * p.group + (pc.row0 + r) % p.group;
+      float top = -INFINITY, sum = 0.f, v[HD / 32] = {};
+      for (int b = from; b <= to; ++b) top = fmaxf(top, part_of(b, r)[0]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      for (int b = from; b <= to; ++b) {
+        const float *part = part_of(b, r);
+        const float w = pt_ex2(part[0] - ref);
+        sum = fmaf(part[1], w, sum);
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) v[j] = fmaf(part[1] == 0.f ? 0.f : part[2 + lane + 32 * j], w, v[j]);
+      }
+      uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head));
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) {
+        const float y = sum == 0.f ? 0.f : v[j] / sum;
+        out[lane + 32 * j] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+      }
+      if (p.lse && lane == 0)
+        p.lse[(int64_t)(pc.first + token) * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
+    }
+  }
+}
+
+template <int HD>
+cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
+  static SmemOptIn opt_in;
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_prompt_kernel<HD>);
+  const int smem = Prompt<HD>::SMEM + 1024;
+  const cudaError_t e = opt_in(kernel, smem);
+  if (e != cudaSuccess) return e;
+  return launch_chained(kv4_attend_prompt_kernel<HD>, std::min(n_sm, FEW_BLOCKS), PT_THREADS, smem, s, p,
+                        prompt_rows(p.max_q * p.group));
+}
+
+}  // namespace
+
+size_t attend_prompt_partials(int head_dim, int64_t rows) {
+  return (size_t)FEW_BLOCKS * 2 * prompt_rows(rows) * (head_dim + 2) * sizeof(float);
+}
+
+cudaError_t launch_attend_prompt(const AttendParams &p, int n_sm, cudaStream_t s) {
+  return p.pool.head_dim == 128 ? launch<128>(p, n_sm, s) : launch<64>(p, n_sm, s);
+}
+
+}  // namespace kfl
