@@ -72,13 +72,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 __device__ __forceinline__ float half_lo(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)x)); }
 __device__ __forceinline__ float half_hi(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)(x >> 16))); }
 
-// Nibbles I of both halves of a word as fp16 pairs 16 (64 + u).
-template <int I>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-  const uint32_t v = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(v), "r"(0x00F000F0u), "r"(0x64006400u));
-  return r;
+// The nibbles of a word's bytes 0 and 2 as two fp16 pairs, exactly: the low ones as u, the high ones as 16 (64 + u).  A byte
+// and its high nibble in the mantissa of fp16 1024 differ by the low one; the difference runs beside the logic unit, which
+// bounds this kernel (64 of its operations a clock, against 128 others).
+__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t &low, uint32_t &high) {
+  uint32_t both;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(both) : "r"(w), "r"(0x00FF00FFu), "r"(0x64006400u));
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(high) : "r"(w), "r"(0x00F000F0u), "r"(0x64006400u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(low) : "r"(both), "r"(high));
 }
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
@@ -155,22 +156,45 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
   if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
 }
 
-// A column of several partial results, `n` of them at at(i) (in order): merged by one warp.
+// A column of several partial results, `n` of them at at(i), in order: merged by one warp.  Lanes take the parts' maxima
+// and sums, 32 at a time; then every lane its channels of all parts, the loads of eight together.
 template <int HD, int COLS, class At>
 __device__ __forceinline__ void merge_column(int n, int col, int lane, const At &at, float (&v)[HD / 32], float &top,
                                              float &sum) {
-  top = -INFINITY, sum = 0.f;
-  for (int i = 0; i < n; ++i) top = fmaxf(top, at(i)[COLS * HD + col]);
-  const float base = top == -INFINITY ? 0.f : top;
+  constexpr int C = HD / 32;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, at(i)[COLS * HD + col]);
 #pragma unroll
-  for (int j = 0; j < HD / 32; ++j) v[j] = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const float *part = at(i);
-    const float w = ex2(part[COLS * HD + col] - base);
-    sum = fmaf(part[COLS * HD + COLS + col], w, sum);
+  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  top = m;
+  const float base = m == -INFINITY ? 0.f : m;
+  float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < HD / 32; ++j) v[j] = fmaf(part[col * HD + lane * (HD / 32) + j], w, v[j]);
+  for (int j = 0; j < C; ++j) v[j] = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float w = 0.f;
+    if (i0 + lane < n) {
+      const float *part = at(i0 + lane) + COLS * HD + col;
+      w = ex2(part[0] - base);
+      s = fmaf(part[COLS], w, s);
+    }
+    const int here = min(32, n - i0);
+#pragma unroll 8
+    for (int i = 0; i < here; ++i) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      const float *part = at(i0 + i) + col * HD + lane * C;
+      if constexpr (C == 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(part);
+        v[0] = fmaf(x.x, wi, v[0]), v[1] = fmaf(x.y, wi, v[1]), v[2] = fmaf(x.z, wi, v[2]), v[3] = fmaf(x.w, wi, v[3]);
+      } else {
+        const float2 x = *reinterpret_cast<const float2 *>(part);
+        v[0] = fmaf(x.x, wi, v[0]), v[1] = fmaf(x.y, wi, v[1]);
+      }
+    }
   }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  sum = s;
 }
 
 template <int HD, int NT>
@@ -235,49 +259,49 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 
   const uint32_t ring = smem_addr(smem) + warp * F::SLOTS * F::TILE_BYTES;
   const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
-  const int pb = min(TILE, 1 << lp);                 // tokens of a page block as it lies in a slot
-  const int sub_bytes = pb * HD * 9 / 8;
-  const int n_blocks = TILE / pb;                    // page blocks of a slot
+  constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;  // of a tile's K or V, as in a block of 64 tokens
+  const int lb = min(lp, 6);                         // log2 of a page's tokens in a tile
   const uint64_t policy = policy_evict_normal();
 
-  // ---- copies: lane i brings page block i of a tile (of a page of 128, lane i part i: codes and parameters of K and V)
+  // ---- copies: a page of 64 tokens is a tile as it stands; of others a page's part of the tile comes in four (codes and
+  // parameters of K and V), a lane each
   Cursor fetch;
   int fetch_page = -1;
   bool fetch_ok = w0 < w1;
   int64_t fetch_at = w0;
   unsigned fetch_slot = 0;
   if (fetch_ok) locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
-  const auto load_page = [&]() {  // the page of this lane's block of the tile at `fetch`
+  const auto load_page = [&]() {  // the page of this lane's copy for the tile at `fetch`
     fetch_page = -2;              // none: behind the sequence's end
-    const int key = (fetch.first_tile + fetch.tile) * TILE + (lp == 7 ? 0 : lane << lp);
-    if (lane < (lp == 7 ? 1 : n_blocks) && key < fetch.length)
+    const int key = (fetch.first_tile + fetch.tile) * TILE + (lane >> 2 << lb);
+    if (lane < (lp == 6 ? 1 : 4 * TILE >> lb) && key < fetch.length)
       fetch_page = p.map.table[(int64_t)fetch.user * p.map.max_pages + (key >> lp)];
   };
-  unsigned valid[F::SLOTS] = {};  // which of a slot's page blocks are there
+  unsigned valid[F::SLOTS] = {};  // which 16 keys of a slot's tile are there, a bit each
   bool dead = false;              // a wait gave up: no more copies, no results
   const auto issue = [&]() {
-    int page = lp == 7 ? __shfl_sync(0xffffffffu, fetch_page, 0) : fetch_page;
-    const bool mine = lane < (lp == 7 ? 4 : n_blocks);
-    const bool there = mine && page >= 0 && page < p.pool.n_pages;
-    if (mine && page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-    unsigned have = __ballot_sync(0xffffffffu, there);
+    const bool there = fetch_page >= 0 && fetch_page < p.pool.n_pages;
+    if (fetch_page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+    const unsigned lanes = __ballot_sync(0xffffffffu, there);
+    unsigned have = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
     const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
-    if (lane == 0) mbar_arrive_expect_tx(bar, lp == 7 ? (have ? F::TILE_BYTES : 0) : __popc(have) * sub_bytes);
+    if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / 4));
     __syncwarp();
     if (there) {
-      const uint8_t *src = p.pool.block(page, p.layer, fetch.head);
-      if (lp == 7) {
-        constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;
-        const int half = (fetch.first_tile + fetch.tile) & 1;
-        const int bytes = lane < 2 ? CODES : PARAMS;
-        const int from = lane < 2 ? (2 * lane + half) * CODES : 4 * CODES + (2 * (lane - 2) + half) * PARAMS;
-        const int to = lane < 2 ? lane * CODES : 2 * CODES + (lane - 2) * PARAMS;
-        bulk_g2s(dst + to, src + from, bytes, bar, policy);
+      const uint8_t *src = p.pool.block(fetch_page, p.layer, fetch.head);
+      if (lp == 6) {
+        bulk_g2s(dst, src, F::TILE_BYTES, bar, policy);
       } else {
-        bulk_g2s(dst + lane * sub_bytes, src, sub_bytes, bar, policy);
+        // part 0, 1: codes of K, V; 2, 3: parameters.  A page of 128 holds two tiles
+        const int part = lane & 3, block = lane >> 2, half = lp == 7 ? (fetch.first_tile + fetch.tile) & 1 : 0;
+        const int size = part < 2 ? CODES : PARAMS, from0 = part < 2 ? 0 : 2 * CODES, nth = part & 1;
+        const int bytes = size >> (6 - lb);
+        bulk_g2s(dst + from0 + nth * size + block * bytes,
+                 src + (lp == 7 ? 2 * from0 + nth * 2 * size + half * size : (from0 + nth * size) >> (6 - lb)), bytes, bar, policy);
       }
     }
-    if (lp == 7) have = have ? 1u : 0u;
 #pragma unroll
     for (int i = 0; i < F::SLOTS; ++i)
       if (i == (int)fetch_slot) valid[i] = have;
@@ -341,32 +365,38 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
         float inv;
         const float unit = xchunk_scale(big, &inv);
-        float total_g[G];
+        float total_g[G], start_g[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          total_g[g] = 0.f;
+          total_g[g] = start_g[g] = 0.f;
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t pair = pack_half2(x[g][8 * j + i] * inv, x[g][8 * j + i + 4] * inv);
+              // (even channels meet u and odd ones 16 (64 + u): 16 times the query for the even ones)
+              const float r = i & 1 ? inv * 0.0625f : inv;
+              const uint32_t pair = pack_half2(x[g][8 * j + i] * r, x[g][8 * j + i + 4] * r);
               q[n][g][j][i >> 1][i & 1] = pair;
-              total_g[g] += half_lo(pair) + half_hi(pair);
+              const float t = half_lo(pair) + half_hi(pair);
+              total_g[g] += i & 1 ? 16.f * t : t;
+              start_g[g] -= i & 1 ? 1152.f * t : 8.f * t;
             }
-          total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], 1);
-          total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], 2);
+#pragma unroll
+          for (int off = 1; off < 4; off <<= 1) {
+            total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], off);
+            start_g[g] += __shfl_xor_sync(0xffffffffu, start_g[g], off);
+          }
         }
-        // (columns of the accumulators: 2 tig, 2 tig + 1; the factor 16 of the codes is taken off with the scale)
-        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale * 0.0625f, 1e-37f);  // (not 0: -inf times it stays)
+        // (columns of the accumulators: 2 tig, 2 tig + 1)
+        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);  // (not 0: -inf times it stays)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int from = (2 * tig + c) * 4;
           cf[n][c] = __shfl_sync(0xffffffffu, factor, from);
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const float t = __shfl_sync(0xffffffffu, total_g[g], from);
-            qs[n][g][c] = 16.f * t;
-            seed[n][g][c] = -1152.f * t;
+            qs[n][g][c] = __shfl_sync(0xffffffffu, total_g[g], from);
+            seed[n][g][c] = __shfl_sync(0xffffffffu, start_g[g], from);
             centre[n][g][c] = 0.f;
           }
           top[n][c] = -INFINITY, sum[n][c] = 0.f;
@@ -400,25 +430,24 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         if (i == (int)slot) have = valid[i];
       // some rows do not see all of the tile: its last keys, a window's first ones, a missing page
       const int all_end = at.length - at.count + 1;
-      const bool masked = key0 + TILE > all_end || have != (1u << n_blocks) - 1 ||
+      const bool masked = key0 + TILE > all_end || have != 0xf ||
                           (p.window > 0 && key0 < at.length - p.window);
       float x[NT][4][4];
       uint32_t vpar[4][2][G];  // (scale, centre) of the lane's two keys of each subtile, as they are stored
       const int key_lane = (gid >> 1) + 4 * (gid & 1);  // matrix row gid is this key of a subtile, row gid + 8 key_lane + 8
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
-        const int b = 16 * st / pb, r0 = 16 * st - b * pb;
-        const uint32_t kb = base + b * sub_bytes;
-        const uint32_t kp = kb + pb * HD, vp = kp + pb * (HD / 16);
+        const uint32_t kb = base + 16 * st * (HD / 2);
+        const uint32_t kp = base + 2 * CODES + 16 * st * (G * 4), vp = kp + PARAMS;
         uint2 kw[2][G];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int g = 0; g < G; ++g) kw[h][g] = lds64(kb + (r0 + key_lane + 8 * h) * (HD / 2) + g * 32 + tig * 8);
+          for (int g = 0; g < G; ++g) kw[h][g] = lds64(kb + (key_lane + 8 * h) * (HD / 2) + g * 32 + tig * 8);
         float ks[2][G], kc[2][G];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t off = (r0 + key_lane + 8 * h) * (G * 4);
+          const uint32_t off = (key_lane + 8 * h) * (G * 4);
           uint32_t pk[G], pv[G];
           if constexpr (G == 2) {
             const uint2 a = lds64(kp + off), c = lds64(vp + off);
@@ -448,8 +477,9 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint32_t lo = j ? kw[0][g].y : kw[0][g].x, hi = j ? kw[1][g].y : kw[1][g].x;
-            const uint32_t a0 = code_pair<0>(lo), a1 = code_pair<0>(hi), a2 = code_pair<1>(lo), a3 = code_pair<1>(hi);
-            const uint32_t a4 = code_pair<2>(lo), a5 = code_pair<2>(hi), a6 = code_pair<3>(lo), a7 = code_pair<3>(hi);
+            uint32_t a0, a1, a2, a3, a4, a5, a6, a7;
+            code_pairs(lo, a0, a2), code_pairs(hi, a1, a3);
+            code_pairs(lo >> 8, a4, a6), code_pairs(hi >> 8, a5, a7);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
@@ -473,7 +503,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * st + key_lane + 8 * (i >> 1);
               const int end = all_end + min((n * 8 + 2 * tig + (i & 1)) / p.group, at.count - 1);
-              const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> (k / pb) & 1);
+              const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> st & 1);
               if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
             }
         // parameters that no row sees may be anything
@@ -484,7 +514,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               const int k = 16 * st + key_lane + 8 * h;
-              if (key0 + k >= at.length || !(have >> (k / pb) & 1)) vpar[st][h][g] = 0;
+              if (key0 + k >= at.length || !(have >> st & 1)) vpar[st][h][g] = 0;
             }
       }
       // ---- running maximum, and a common unit of the value scales (their weights are fp16)
@@ -546,8 +576,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       const float weight_unit = v_unit > 0.f ? 16384.f / v_unit : 0.f;
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
-        const int b = 16 * st / pb, r0 = 16 * st - b * pb;
-        const uint32_t vb = base + b * sub_bytes + pb * (HD / 2) + (r0 + tig) * (HD / 2) + gid * 4;
+        const uint32_t vb = base + CODES + (16 * st + tig) * (HD / 2) + gid * 4;
         uint32_t pf[NT][G][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -576,15 +605,24 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         for (int g = 0; g < G; ++g) {
           const uint32_t wa = lds32(vb + g * 32), wb = lds32(vb + g * 32 + 4 * (HD / 2));
           const uint32_t wc = lds32(vb + g * 32 + 8 * (HD / 2)), wd = lds32(vb + g * 32 + 12 * (HD / 2));
-          const uint32_t l0 = __byte_perm(wa, wb, 0x5410), h0 = __byte_perm(wa, wb, 0x7632);
-          const uint32_t l1 = __byte_perm(wc, wd, 0x5410), h1 = __byte_perm(wc, wd, 0x7632);
+          // [byte 0 or 1 of the tokens' words' lower, upper half][which two tokens]: the pairs of two tiles of 16 channels
+          uint32_t x0[2][2], x1[2][2], y0[2][2], y1[2][2];  // low and high nibbles of: lower half, upper half
+          code_pairs(__byte_perm(wa, wb, 0x5410), x0[0][0], x1[0][0]);
+          code_pairs(__byte_perm(wa, wb, 0x5511), x0[1][0], x1[1][0]);
+          code_pairs(__byte_perm(wa, wb, 0x7632), y0[0][0], y1[0][0]);
+          code_pairs(__byte_perm(wa, wb, 0x7733), y0[1][0], y1[1][0]);
+          code_pairs(__byte_perm(wc, wd, 0x5410), x0[0][1], x1[0][1]);
+          code_pairs(__byte_perm(wc, wd, 0x5511), x0[1][1], x1[1][1]);
+          code_pairs(__byte_perm(wc, wd, 0x7632), y0[0][1], y1[0][1]);
+          code_pairs(__byte_perm(wc, wd, 0x7733), y0[1][1], y1[1][1]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const uint32_t b0 = pf[n][g][0], b1 = pf[n][g][1];
-            mma16816(o[n][g][0], code_pair<0>(l0), code_pair<0>(h0), code_pair<0>(l1), code_pair<0>(h1), b0, b1);
-            mma16816(o[n][g][1], code_pair<1>(l0), code_pair<1>(h0), code_pair<1>(l1), code_pair<1>(h1), b0, b1);
-            mma16816(o[n][g][2], code_pair<2>(l0), code_pair<2>(h0), code_pair<2>(l1), code_pair<2>(h1), b0, b1);
-            mma16816(o[n][g][3], code_pair<3>(l0), code_pair<3>(h0), code_pair<3>(l1), code_pair<3>(h1), b0, b1);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              mma16816(o[n][g][2 * j], x0[j][0], y0[j][0], x0[j][1], y0[j][1], b0, b1);
+              mma16816(o[n][g][2 * j + 1], x1[j][0], y1[j][0], x1[j][1], y1[j][1], b0, b1);
+            }
             mma16816(ones[n][g], 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, b0, b1);
           }
         }
@@ -625,7 +663,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], 0.0625f, -72.f * ones[n][g][c]), unit, cen);
+              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 0.0625f : 1.f, (i & 1 ? -72.f : -8.f) * ones[n][g][c]),
+                          unit, cen);
             if (alone) {
               if (col < rows && !dead) {
                 uint16_t h[8];

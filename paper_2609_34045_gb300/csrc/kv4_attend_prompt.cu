@@ -87,6 +87,59 @@ __device__ __forceinline__ uint32_t pt_pack(float lo, float hi) {
   return r;
 }
 
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
+// Two lanes' worth of fp32 in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// A row's 128 scores: w the weights 2^(score cf - top) in fp16 pairs, `most` the largest score, `sum` the weights' sum.
+// Sixteen scores at a time, the next ones on their way meanwhile.
+__device__ __forceinline__ void weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[64], float &most, float &sum) {
+  uint32_t x[2][16];
+  tmem_ld16(t_s, x[0]);
+  const float2 scale = {cf, cf}, from = {-top, -top};
+  float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
+  float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    tmem_wait_ld();
+    if (c < 7) tmem_ld16(t_s + 16 * (c + 1), x[(c + 1) & 1]);
+    uint32_t(&v)[16] = x[c & 1];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float2 a = {__uint_as_float(v[i]), __uint_as_float(v[i + 1])};
+      m[i >> 1 & 1] = fmaxf(m[i >> 1 & 1], fmaxf(a.x, a.y));
+      float2 e = fma2(a, scale, from);
+      e = {pt_ex2(e.x), pt_ex2(e.y)};
+      s[i >> 1 & 1] = add2(s[i >> 1 & 1], e);
+      w[8 * c + i / 2] = pt_pack(e.x, e.y);
+    }
+  }
+  most = fmaxf(m[0], m[1]);
+  sum = s[0].x + s[0].y + (s[1].x + s[1].y);
+}
+
 // A run of one row block's tiles: what a thread block works on at a time.
 struct Piece {
   int seq, head, block;          // block: of rows_per_block query rows
@@ -374,67 +427,81 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
           const bool masked = key0 + PT_KEYS > least || (p.window > 0 && key0 < greatest) ||
                               (there4.x & there4.y & there4.z & there4.w) != 0xffffffffu;
-          const uint32_t pages[4] = {there4.x, there4.y, there4.z, there4.w};
-          uint32_t x[32];
-          float most = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tmem_ld32(t_s + 32 * c, x);
-            if (masked) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const int key = key0 + 32 * c + i;
-                if (key >= end || key < begin || !(pages[c] >> i & 1)) x[i] = 0xff800000u;
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) most = fmaxf(most, __uint_as_float(x[i]));
-          }
-          most = most == -INFINITY ? most : most * cf;
-          float keep = 1.f;
-          const bool grows = most > top + PT_GROW || (top == -INFINITY && most > top);
-          if (grows) {
-            keep = pt_ex2(top - most);
-            top = most;
-            sum *= keep;
-          }
-          if (t > 0 && __any_sync(0xffffffffu, grows)) {
-            ok = wait(B_O + half, (done - 1) & 1);  // the last tile's product
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < HD / 16; ++c) {
-              uint32_t o[16];
-              tmem_ld16(t_o + 16 * c, o);
+          const auto sees = [&](int c, int i) {  // column 16 c + i
+            const uint32_t pages = c < 2 ? there4.x : c < 4 ? there4.y : c < 6 ? there4.z : there4.w;
+            const int key = key0 + 16 * c + i;
+            return key < end && key >= begin && (pages >> ((c & 1) * 16 + i) & 1);
+          };
+          // The weights are taken against the reference that the row has, and its scores' maximum beside them; they stay in
+          // registers until that shows whether the reference holds.  Where it does not (the first tile, a row that
+          // outgrew it by 2^8, scores that are masked) the scores, still in place, are read again.
+          uint32_t w[64];
+          float most = -INFINITY, part_sum = 0.f;
+          bool again = masked || t == 0;
+          if (!again) {
+            weigh_scores(t_s, cf, top, w, most, part_sum);
+            most *= cf;
+            again = __any_sync(0xffffffffu, most > top + PT_GROW || top == -INFINITY);
+          } else {
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              uint32_t x[16];
+              tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
-              tmem_st16(t_o + 16 * c, o);
+              for (int i = 0; i < 16; ++i)
+                if (!masked || sees(c, i)) most = fmaxf(most, __uint_as_float(x[i]));
             }
-            tmem_wait_st();
+            most = most == -INFINITY ? most : most * cf;
           }
-          const float ref = top == -INFINITY ? 0.f : top;
+          if (again) {
+            float keep = 1.f;
+            if (most > top + PT_GROW || (top == -INFINITY && most > top)) {
+              keep = pt_ex2(top - most);
+              top = most;
+              sum *= keep;
+            }
+            if (t > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
+              ok = wait(B_O + half, (done - 1) & 1);  // the last tile's product
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < HD / 16; ++c) {
+                uint32_t o[16];
+                tmem_ld16(t_o + 16 * c, o);
+                tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tmem_ld32(t_s + 32 * c, x);
-            if (masked) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const int key = key0 + 32 * c + i;
-                if (key >= end || key < begin || !(pages[c] >> i & 1)) x[i] = 0xff800000u;
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+                tmem_st16(t_o + 16 * c, o);
               }
+              tmem_wait_st();
             }
-            uint32_t w[16];
+            const float ref = top == -INFINITY ? 0.f : top;
+            part_sum = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              uint32_t x[16], y[8];
+              tmem_ld16(t_s + 16 * c, x);
+              tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float a = pt_ex2(fmaf(__uint_as_float(x[2 * i]), cf, -ref));
-              const float b = pt_ex2(fmaf(__uint_as_float(x[2 * i + 1]), cf, -ref));
-              sum += a + b;
-              w[i] = pt_pack(a, b);
+              for (int i = 0; i < 16; i += 2) {
+                float a = fmaf(__uint_as_float(x[i]), cf, -ref), b = fmaf(__uint_as_float(x[i + 1]), cf, -ref);
+                if (masked) {
+                  if (!sees(c, i)) a = -INFINITY;
+                  if (!sees(c, i + 1)) b = -INFINITY;
+                }
+                a = pt_ex2(a), b = pt_ex2(b);
+                part_sum += a + b;
+                y[i / 2] = pt_pack(a, b);
+              }
+              tmem_st8(t_s + 8 * c, y);  // (over scores that have been read)
             }
-            tmem_st16(t_s + 16 * c, w);  // (over scores that have been read)
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_st16(t_s + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
           }
+          sum += part_sum;
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -501,22 +568,26 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       next_piece(pc, list, c1);
     }
   } else if (c0 < c1 && warp < 12) {
-    // ---- decoding: a thread per key
+    // ---- decoding: a thread per key.  A tile's rows are loaded while the tile before is decoded, its page number one
+    // tile earlier still
     const int row = tid - 256, wq = warp - 8;
-    unsigned tile = 0;
     bool ok = true;
     Piece pc;
     find_piece(pc, list, c0, c1);
-    uint4 kr[HD / 32];
-    uint32_t kp[KB];
-    int page = -1;
-    const auto page_of = [&](int key) {
-      if (key >= pc.length) return -2;
-      return p.map.table[(int64_t)pc.user * p.map.max_pages + (key >> lp)];
+    int t_next = pc.from;
+    int page = -2, slot = 0, head = 0;  // of the next tile's row (a page of -2: behind the user's rows)
+    const auto find_page = [&]() {
+      const int key = (pc.tile0 + t_next) * PT_KEYS + row;
+      page = key < pc.length ? p.map.table[(int64_t)pc.user * p.map.max_pages + (key >> lp)] : -2;
+      slot = key & (p.pool.page_tokens() - 1), head = pc.head;
     };
-    const auto load_row = [&](int key, int which, uint4 (&r)[HD / 32], uint32_t (&par)[KB]) {
-      const int slot = key & (p.pool.page_tokens() - 1);
-      const uint8_t *b = p.pool.block(page, p.layer, pc.head);
+    const auto load_row = [&](int which, bool there, uint4 (&r)[HD / 32], uint32_t (&par)[KB]) {
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) r[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < KB; ++i) par[i] = 0;
+      if (!there) return;
+      const uint8_t *b = p.pool.block(page, p.layer, head);
       const uint4 *codes = reinterpret_cast<const uint4 *>(b + which * p.pool.code_bytes() + slot * (HD / 2));
       const uint32_t *params = reinterpret_cast<const uint32_t *>(b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes()) + slot * KB;
 #pragma unroll
@@ -524,57 +595,61 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
 #pragma unroll
       for (int i = 0; i < KB; ++i) par[i] = params[i];
     };
-    for (;;) {
-      for (int t = pc.from; t < pc.to && ok; ++t, ++tile) {
-        const int buf = tile & 1;
-        const uint32_t parity = (tile >> 1 & 1) ^ 1;
-        const int key = (pc.tile0 + t) * PT_KEYS + row;
-        page = page_of(key);
-        const bool there = page >= 0 && page < p.pool.n_pages;
-        if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-        uint4 vr[HD / 32];
-        uint32_t vp[KB];
-        if (there) {
-          load_row(key, 0, kr, kp);
-          load_row(key, 1, vr, vp);
-        } else {
+    const auto scan = [&](const uint32_t (&par)[KB], unsigned (&bad)[KB]) {
 #pragma unroll
-          for (int i = 0; i < HD / 32; ++i) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < KB; ++i) kp[i] = vp[i] = 0;
+      for (int g = 0; g < KB; ++g)  // (a NaN or an infinity in scale or centre: all exponent bits set)
+        bad[g] = __ballot_sync(0xffffffffu, (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u);
+    };
+    uint4 now[HD / 32], later[HD / 32];  // a row of K or V, and of the other one after it
+    uint32_t now_p[KB], later_p[KB];
+    const unsigned n = (unsigned)(c1 - c0);
+    find_page();
+    bool there = page >= 0 && page < p.pool.n_pages;
+    if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+    load_row(0, there, now, now_p);
+#pragma unroll 1
+    for (unsigned i = 0; i < 2 * n; ++i) {  // K and V of tile i / 2
+      const unsigned tile = i >> 1, which = i & 1;
+      const int buf = tile & 1;
+      uint32_t *flag = reinterpret_cast<uint32_t *>(flags + (tile & 3) * (1 + KB)) + wq;
+      unsigned have = 0;
+      if (!which) {
+        have = __ballot_sync(0xffffffffu, there);
+        load_row(1, there, later, later_p);
+        if (tile + 1 < n) {  // on to the next tile's page
+          if (++t_next == pc.to) {
+            next_piece(pc, list, c1);
+            t_next = pc.from;
+          }
+          find_page();
         }
-        uint32_t *flag = reinterpret_cast<uint32_t *>(flags + (tile & 3) * (1 + KB)) + wq;
-        const unsigned have = __ballot_sync(0xffffffffu, there);
+      } else if (tile + 1 < n) {
+        there = page >= 0 && page < p.pool.n_pages;
+        if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+        load_row(0, there, later, later_p);
+      }
+      ok = wait((which ? B_VFREE : B_KFREE) + buf, (tile >> 1 & 1) ^ 1);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (which) {
         unsigned bad[KB];
+        scan(now_p, bad);
 #pragma unroll
         for (int g = 0; g < KB; ++g) {
-          // (a NaN or an infinity in scale or centre: all exponent bits set)
-          const bool nan = (vp[g] & 0x7c00u) == 0x7c00u || (vp[g] & 0x7c000000u) == 0x7c000000u;
-          bad[g] = __ballot_sync(0xffffffffu, nan);
-          if (nan) vp[g] = 0;
+          if (lane == 0) flag[4 * (1 + g)] = bad[g];
+          if (bad[g] >> lane & 1) now_p[g] = 0;
         }
-        ok = wait(B_KFREE + buf, parity);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) {
-          flag[0] = have;
-#pragma unroll
-          for (int g = 0; g < KB; ++g) flag[4 * (1 + g)] = bad[g];
-        }
-        decode_row<HD>(kr, kp, base + F::K_AT + buf * F::TILE, row);
-        fence_async_proxy();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_KFULL + buf));
-        ok = wait(B_VFREE + buf, parity);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        decode_row<HD>(vr, vp, base + F::V_AT + buf * F::TILE, row);
-        fence_async_proxy();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_VFULL + buf));
+      } else if (lane == 0) {
+        flag[0] = have;
       }
-      if (!ok || pc.flat + pc.to >= c1) break;
-      next_piece(pc, list, c1);
+      decode_row<HD>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, row);
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar((which ? B_VFULL : B_KFULL) + buf));
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) now[j] = later[j];
+#pragma unroll
+      for (int j = 0; j < KB; ++j) now_p[j] = later_p[j];
     }
   } else if (c0 < c1) {
     // ---- products, issued by an elected lane
