@@ -11,9 +11,10 @@
 // leaves the decoding (2.2 instructions per element, four warps) and the softmax (a thread per row, some 4 instructions
 // per score) beside 2048 clocks of products per 128 keys.
 //
-// Roles.  Warps 0-3 and 4-7: softmax of the two 128-row halves, a thread per row, and their Q and output; 8-11:
-// decoding, a thread per key, raw codes straight from global memory a tile ahead; 12: products.  While one
-// half's softmax runs, the other half's products do.
+// Roles.  Warps 0-7 and 8-15: softmax of the two 128-row halves, two threads per row with 64 keys each, and their Q and
+// output; 16-22: decoding, a thread per key, 32 keys of K or V at a time in turn, raw codes straight from global memory
+// ahead of their turn; 23: products.  While one half's softmax runs, the other half's products do.  A thread per row took
+// 2000 clocks a tile, as long as both halves' products, and left the tensor pipe waiting.
 //
 // Work split.  The (sequence, KV head, 256 rows) x (128 keys) tiles in sight form one list that the blocks share
 // equally; a row block cut between thread blocks is merged by the last to arrive, in list order.
@@ -26,7 +27,10 @@ namespace kfl {
 namespace {
 
 constexpr int PT_KEYS = 128;                 // keys of a tile
-constexpr int PT_THREADS = 13 * 32;
+constexpr int PT_SOFTMAX = 16;               // warps 0 to 15
+constexpr int PT_DECODERS = 7;               // 16 to 22
+constexpr int PT_MMA_WARP = PT_SOFTMAX + PT_DECODERS;
+constexpr int PT_THREADS = (PT_MMA_WARP + 1) * 32;
 constexpr float PT_GROW = 8.f;               // log2 of how far a row's maximum may outgrow its reference
 
 template <int HD>
@@ -36,7 +40,8 @@ struct Prompt {
   static constexpr int Q_AT = 0, K_AT = 2 * TILE, V_AT = 4 * TILE;
   static constexpr int INFO_AT = 6 * TILE;                 // int4[FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int FLAG_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;  // uint4 [4][1 + KB]: keys of a tile
-  static constexpr int BAR_AT = FLAG_AT + 4 * (1 + KB) * 16;
+  static constexpr int PAIR_AT = FLAG_AT + 4 * (1 + KB) * 16;  // float [2 halves][2][128]: what a row's two threads exchange
+  static constexpr int BAR_AT = PAIR_AT + 2 * 2 * 128 * 4;
   static constexpr int SMEM = BAR_AT + 20 * 8 + 32;
   static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
 };
@@ -87,12 +92,6 @@ __device__ __forceinline__ uint32_t pt_pack(float lo, float hi) {
   return r;
 }
 
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
-               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-
 // Two lanes' worth of fp32 in one instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;
@@ -113,31 +112,45 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// A row's 128 scores: w the weights 2^(score cf - top) in fp16 pairs, `most` the largest score, `sum` the weights' sum.
-// Sixteen scores at a time, the next ones on their way meanwhile.
-__device__ __forceinline__ void weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[64], float &most, float &sum) {
+// 64 scores of a row: w the weights 2^(score cf - top) in fp16 pairs, `most` the largest of them (infinity if fp16 cannot
+// hold it), `sum` their sum.  Sixteen scores at a time, the next ones on their way meanwhile.
+__device__ __forceinline__ void weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[32], float &most, float &sum) {
   uint32_t x[2][16];
   tmem_ld16(t_s, x[0]);
   const float2 scale = {cf, cf}, from = {-top, -top};
   float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
-  float m[2] = {-INFINITY, -INFINITY};
+  __half2 m[2] = {__float2half2_rn(0.f), __float2half2_rn(0.f)};
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
+  for (int c = 0; c < 4; ++c) {
     tmem_wait_ld();
-    if (c < 7) tmem_ld16(t_s + 16 * (c + 1), x[(c + 1) & 1]);
+    if (c < 3) tmem_ld16(t_s + 16 * (c + 1), x[(c + 1) & 1]);
     uint32_t(&v)[16] = x[c & 1];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       const float2 a = {__uint_as_float(v[i]), __uint_as_float(v[i + 1])};
-      m[i >> 1 & 1] = fmaxf(m[i >> 1 & 1], fmaxf(a.x, a.y));
       float2 e = fma2(a, scale, from);
       e = {pt_ex2(e.x), pt_ex2(e.y)};
       s[i >> 1 & 1] = add2(s[i >> 1 & 1], e);
       w[8 * c + i / 2] = pt_pack(e.x, e.y);
+      m[i >> 1 & 1] = __hmax2(m[i >> 1 & 1], *reinterpret_cast<const __half2 *>(&w[8 * c + i / 2]));
     }
   }
-  most = fmaxf(m[0], m[1]);
+  m[0] = __hmax2(m[0], m[1]);
+  most = fmaxf(__low2float(m[0]), __high2float(m[0]));
   sum = s[0].x + s[0].y + (s[1].x + s[1].y);
+}
+
+// A barrier of the 256 threads of a half (1 or 2); with or: whether any of them says so.
+__device__ __forceinline__ void half_sync(int half) { named_bar_sync(1 + half, 256); }
+__device__ __forceinline__ bool half_any(int half, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(1 + half)
+      : "memory");
+  return r != 0;
 }
 
 // A run of one row block's tiles: what a thread block works on at a time.
@@ -180,8 +193,9 @@ __device__ __forceinline__ void open_sequence(Piece &pc, const List &l) {
   pc.user = v.x, pc.length = v.y, pc.first = v.z, pc.count = v.w;
 }
 
-// The piece at place `at` of the list (at < limit).
+// The piece at place `at` of the list (at < limit).  The whole warp calls it: lanes count the tiles of a block each.
 __device__ void find_piece(Piece &pc, const List &l, int64_t at, int64_t limit) {
+  const int lane = threadIdx.x & 31;
   int lo = 0, hi = l.n_seqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -195,13 +209,27 @@ __device__ void find_piece(Piece &pc, const List &l, int64_t at, int64_t limit) 
   const int64_t start = (int64_t)l.prefix[lo] * l.heads;
   const int per_head = l.prefix[lo + 1] - l.prefix[lo];
   pc.head = (int)((at - start) / per_head);
-  pc.flat = start + (int64_t)pc.head * per_head;
-  for (pc.block = 0;; ++pc.block) {
-    int tile0, n;
-    tiles_of_block(pc.length, pc.count, pc.block, l, tile0, n);
-    if (pc.flat + n > at) break;
-    pc.flat += n;
+  int rest = (int)(at - start - (int64_t)pc.head * per_head), before = 0;
+  const int n_blocks = (pc.count * l.group + l.rows_per_block - 1) / l.rows_per_block;
+  for (int b0 = 0;; b0 += 32) {
+    int tile0, n = 0;
+    if (b0 + lane < n_blocks) tiles_of_block(pc.length, pc.count, b0 + lane, l, tile0, n);
+    int sum = n;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, sum, off);
+      if (lane >= off) sum += o;
+    }
+    const unsigned here = __ballot_sync(0xffffffffu, before + sum > rest);
+    if (here != 0 || b0 + 32 >= n_blocks) {
+      const int i = here ? __ffs(here) - 1 : 31;
+      pc.block = b0 + i;
+      before += __shfl_sync(0xffffffffu, sum - n, i);
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
   }
+  pc.flat = start + (int64_t)pc.head * per_head + before;
   open_piece(pc, l, (int)(at - pc.flat), limit);
 }
 
@@ -253,7 +281,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + F::BAR_AT + 20 * 8);  // TMEM, abort, last
   const uint32_t bars = base + F::BAR_AT;
   const auto bar = [&](int b) { return bars + 8 * b; };
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
   const List list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
   pdl_launch_dependents();
@@ -263,18 +291,18 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       mbar_init(bar(B_VFULL + i), 4);
       mbar_init(bar(B_KFREE + i), 1);
       mbar_init(bar(B_VFREE + i), 1);
-      mbar_init(bar(B_Q + i), 4);
+      mbar_init(bar(B_Q + i), 8);
       mbar_init(bar(B_S + i), 1);
-      mbar_init(bar(B_P + i), 4);
+      mbar_init(bar(B_P + i), 8);
       mbar_init(bar(B_O + i), 1);
-      mbar_init(bar(B_READ + i), 4);
+      mbar_init(bar(B_READ + i), 8);
     }
     mbar_init(bar(B_DRAIN), 1);
     words[1] = 0;
     prefix[0] = 0;
   }
   fence_mbar_init();
-  if (warp == 12) tmem_alloc(base + F::BAR_AT + 20 * 8, 512);
+  if (warp == PT_MMA_WARP) tmem_alloc(base + F::BAR_AT + 20 * 8, 512);
   pdl_wait();
 
   // ---- the list: every sequence's tiles per head, summed
@@ -323,8 +351,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
   const size_t slot_floats = (size_t)rows_per_block * (HD + 2);
 
-  // a wait that gives up ends every role's loop
+  // a wait that gives up lets no later one last
   const auto wait = [&](int b, uint32_t parity) {
+    if (mbar_try_wait(bar(b), parity)) return true;
     if (words[1]) return false;
     if (wait_2s(bar(b), parity)) return true;
     words[1] = 1;
@@ -332,15 +361,19 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     return false;
   };
 
-  if (c0 < c1 && warp < 8) {
-    // ---- softmax: a thread per query row
-    const int half = warp >> 2, row = tid & 127;
+  if (c0 < c1 && warp < PT_SOFTMAX) {
+    // ---- softmax: two threads per query row, each with 64 of a tile's keys and half of the row's channels.  They meet in
+    // barriers of the half, so where a wait has given up they go on to the list's end (no wait lasts then), their
+    // results being of no account
+    const int half = warp >> 3, part = warp >> 2 & 1, row = tid & 127;
+    constexpr int CH = HD / 2;                          // channels of a thread
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
-    const uint32_t t_s = tmem + lanes + half * 128, t_o = tmem + lanes + 256 + half * 128;
+    const uint32_t t_s = tmem + lanes + half * 128 + part * 64, t_p = tmem + lanes + half * 128 + part * 32;
+    const uint32_t t_o = tmem + lanes + 256 + half * 128 + part * CH;
     const uint32_t q_tile = base + F::Q_AT + half * F::TILE;
+    float *pair = reinterpret_cast<float *>(smem + F::PAIR_AT) + half * 256;  // [part][row]
     const float log2_scale = fabsf(p.scale) * 1.44269504089f;
     uint32_t done = 0;  // tiles of this half so far
-    bool ok = true;
     unsigned tile = 0;  // tiles of the thread block so far (places of the flags)
     Piece pc;
     find_piece(pc, list, c0, c1);
@@ -355,10 +388,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         // its query, in fp16 and the words' channel order
         float unit, inv;
         {
-          const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q.row(pc.first + token, head));
-          uint32_t w[HD / 2];
+          const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q.row(pc.first + token, head)) + part * CH;
+          uint32_t w[CH / 2];
 #pragma unroll
-          for (int i = 0; i < HD / 8; ++i) {
+          for (int i = 0; i < CH / 8; ++i) {
             if (!there) {
               w[4 * i] = w[4 * i + 1] = w[4 * i + 2] = w[4 * i + 3] = 0;
             } else if (p.q_wide) {
@@ -372,14 +405,16 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
           float big = 0.f;
 #pragma unroll
-          for (int i = 0; i < HD / 2; ++i) {
+          for (int i = 0; i < CH / 2; ++i) {
             const float a = p.bf16 ? bf16_lo(w[i]) : f16_to_f32((uint16_t)w[i]);
             const float b = p.bf16 ? bf16_hi(w[i]) : f16_to_f32((uint16_t)(w[i] >> 16));
             big = fmaxf(big, fmaxf(fabsf(a), fabsf(b)));
           }
-          unit = xchunk_scale(big, &inv);
+          pair[part * 128 + row] = big;
+          half_sync(half);
+          unit = xchunk_scale(fmaxf(big, pair[(part ^ 1) * 128 + row]), &inv);
 #pragma unroll
-          for (int i = 0; i < HD / 8; ++i) {
+          for (int i = 0; i < CH / 8; ++i) {
             float f[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -390,7 +425,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             if (p.scale == 0.f)
 #pragma unroll
               for (int j = 0; j < 8; ++j) f[j] = 0.f;
-            const uint32_t at = q_tile + (i / 8) * (128 * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4);
+            const int chunk = part * (CH / 8) + i;
+            const uint32_t at = q_tile + (chunk / 8) * (128 * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(pt_pack(f[0], f[4])),
                          "r"(pt_pack(f[1], f[5])), "r"(pt_pack(f[2], f[6])), "r"(pt_pack(f[3], f[7]))
                          : "memory");
@@ -400,51 +436,43 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_Q + half));
         const float cf = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);
-        float top = -INFINITY, sum = 0.f;  // top: the reference, in scores times cf
-        unsigned poison = 0;               // groups of which this row sees a NaN
+        float top = -INFINITY, sum = 0.f;  // top: the reference, in scores times cf; sum: of this thread's weights
+        bool poison = false;               // whether this row sees a NaN in the group of the thread's channels
         const auto see_poison = [&](int t) {
-          const uint4 *f = flags + ((tile + t) & 3) * (1 + KB) + 1;
+          const uint4 v = flags[((tile + t) & 3) * (1 + KB) + 1 + (KB == 2 ? part : 0)];
+          if ((v.x | v.y | v.z | v.w) == 0) return;
           const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
-#pragma unroll
-          for (int g = 0; g < KB; ++g) {
-            const uint4 v = f[g];
-            if ((v.x | v.y | v.z | v.w) == 0) continue;
-            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
-            for (int k = 0; k < PT_KEYS; ++k)
-              if ((bits[k >> 5] >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison |= 1u << g;
+#pragma unroll 1
+          for (int k = 0; k < PT_KEYS; ++k) {
+            const uint32_t bits = k < 32 ? v.x : k < 64 ? v.y : k < 96 ? v.z : v.w;
+            if ((bits >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison = true;
           }
         };
         // rows of this warp: the least end and the greatest begin decide whether a tile is seen whole
         const int least = __reduce_min_sync(0xffffffffu, end);
         const int greatest = __reduce_max_sync(0xffffffffu, begin);
-        for (int t = 0; t < n && ok; ++t) {
-          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
-          ok = wait(B_S + half, done & 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
+        for (int t = 0; t < n; ++t) {
+          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS + part * 64;  // of this thread's keys
+          wait(B_S + half, done & 1);
+          __syncwarp();
           tc_fence_after();
           if (t > 0) see_poison(t - 1);
-          const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
-          const bool masked = key0 + PT_KEYS > least || (p.window > 0 && key0 < greatest) ||
-                              (there4.x & there4.y & there4.z & there4.w) != 0xffffffffu;
+          const uint2 there2 = reinterpret_cast<const uint2 *>(flags + ((tile + t) & 3) * (1 + KB))[part];
+          const bool masked = key0 + 64 > least || (p.window > 0 && key0 < greatest) || (there2.x & there2.y) != 0xffffffffu;
           const auto sees = [&](int c, int i) {  // column 16 c + i
-            const uint32_t pages = c < 2 ? there4.x : c < 4 ? there4.y : c < 6 ? there4.z : there4.w;
             const int key = key0 + 16 * c + i;
-            return key < end && key >= begin && (pages >> ((c & 1) * 16 + i) & 1);
+            return key < end && key >= begin && ((c < 2 ? there2.x : there2.y) >> ((c & 1) * 16 + i) & 1);
           };
-          // The weights are taken against the reference that the row has, and its scores' maximum beside them; they stay in
-          // registers until that shows whether the reference holds.  Where it does not (the first tile, a row that
-          // outgrew it by 2^8, scores that are masked) the scores, still in place, are read again.
-          uint32_t w[64];
-          float most = -INFINITY, part_sum = 0.f;
-          bool again = masked || t == 0;
-          if (!again) {
-            weigh_scores(t_s, cf, top, w, most, part_sum);
-            most *= cf;
-            again = __any_sync(0xffffffffu, most > top + PT_GROW || top == -INFINITY);
-          } else {
+          // The weights are taken against the reference that the row has; they stay in registers until all threads of the
+          // half find that it holds.  Where it does not (the first tile, a row that outgrew it by 2^8, scores that
+          // are masked) the scores, still in place, are read again.
+          uint32_t w[32];
+          float most = 0.f, part_sum = 0.f;
+          if (!masked && t > 0) weigh_scores(t_s, cf, top, w, most, part_sum);
+          if (half_any(half, masked || t == 0 || most > 256.f || top == -INFINITY)) {
+            most = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < 4; ++c) {
               uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
@@ -452,9 +480,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
               for (int i = 0; i < 16; ++i)
                 if (!masked || sees(c, i)) most = fmaxf(most, __uint_as_float(x[i]));
             }
+            pair[part * 128 + row] = most;
+            half_sync(half);
+            most = fmaxf(most, pair[(part ^ 1) * 128 + row]);
             most = most == -INFINITY ? most : most * cf;
-          }
-          if (again) {
             float keep = 1.f;
             if (most > top + PT_GROW || (top == -INFINITY && most > top)) {
               keep = pt_ex2(top - most);
@@ -462,12 +491,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
               sum *= keep;
             }
             if (t > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
-              ok = wait(B_O + half, (done - 1) & 1);  // the last tile's product
-              ok = __all_sync(0xffffffffu, ok);
-              if (!ok) break;
+              wait(B_O + half, (done - 1) & 1);  // the last tile's product
+              __syncwarp();
               tc_fence_after();
 #pragma unroll 1
-              for (int c = 0; c < HD / 16; ++c) {
+              for (int c = 0; c < CH / 16; ++c) {
                 uint32_t o[16];
                 tmem_ld16(t_o + 16 * c, o);
                 tmem_wait_ld();
@@ -479,9 +507,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             }
             const float ref = top == -INFINITY ? 0.f : top;
             part_sum = 0.f;
-#pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
-              uint32_t x[16], y[8];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
 #pragma unroll
@@ -493,15 +521,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
                 }
                 a = pt_ex2(a), b = pt_ex2(b);
                 part_sum += a + b;
-                y[i / 2] = pt_pack(a, b);
+                w[8 * c + i / 2] = pt_pack(a, b);
               }
-              tmem_st8(t_s + 8 * c, y);  // (over scores that have been read)
             }
-          } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_st16(t_s + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
+            half_sync(half);  // (the second threads' weights go where the first ones' scores are)
           }
           sum += part_sum;
+          tmem_st16(t_p, reinterpret_cast<uint32_t(&)[16]>(w[0]));
+          tmem_st16(t_p + 16, reinterpret_cast<uint32_t(&)[16]>(w[16]));
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -509,30 +536,34 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           ++done;
         }
         // ---- the piece's end: O, divided and stored, or handed on
-        ok = ok && wait(B_O + half, (done - 1) & 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
+        wait(B_O + half, (done - 1) & 1);
+        __syncwarp();
         tc_fence_after();
         see_poison(n - 1);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_READ + half));  // (the tiles' flags have been read)
+        pair[part * 128 + row] = sum;
+        half_sync(half);
+        sum += pair[(part ^ 1) * 128 + row];
+        half_sync(half);  // (before the next piece's exchange)
         const bool whole = pc.from == 0 && pc.to == pc.n_tiles;
         const float inv_sum = sum == 0.f ? 0.f : 1.f / sum;
-        float *part = p.partials + ((size_t)blockIdx.x * 2 + (pc.from > 0 ? 0 : 1)) * slot_floats + (size_t)r * (HD + 2);
-        uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head));
-#pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-          uint32_t x[32];
-          tmem_ld32(t_o + 32 * c, x);
+        float *slot = p.partials + ((size_t)blockIdx.x * 2 + (pc.from > 0 ? 0 : 1)) * slot_floats;
+        float *to = slot + (size_t)r * HD + part * CH;
+        uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head)) + part * CH;
+#pragma unroll 1
+        for (int c = 0; c < CH / 16; ++c) {
+          uint32_t x[16];
+          tmem_ld16(t_o + 16 * c, x);
+          tmem_wait_ld();
           if (!there) continue;
-          const bool nan = poison >> (c / 2) & 1;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             float v[8];  // (back in the channels' own order)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               v[j] = __uint_as_float(x[8 * i + 2 * (j & 3) + (j >> 2)]);
-              if (nan) v[j] = __uint_as_float(0x7fc00000u);
+              if (poison) v[j] = __uint_as_float(0x7fc00000u);
             }
             if (whole) {
               uint16_t h[8];
@@ -542,22 +573,22 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
                 h[j] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
               }
               if (p.out_wide) {
-                *reinterpret_cast<uint4 *>(out + 32 * c + 8 * i) =
+                *reinterpret_cast<uint4 *>(out + 16 * c + 8 * i) =
                     make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
                                h[6] | (uint32_t)h[7] << 16);
               } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) out[32 * c + 8 * i + j] = h[j];
+                for (int j = 0; j < 8; ++j) out[16 * c + 8 * i + j] = h[j];
               }
             } else {
-#pragma unroll
-              for (int j = 0; j < 8; j += 2) *reinterpret_cast<float2 *>(part + 2 + 32 * c + 8 * i + j) = make_float2(v[j], v[j + 1]);
+              *reinterpret_cast<float4 *>(to + 16 * c + 8 * i) = make_float4(v[0], v[1], v[2], v[3]);
+              *reinterpret_cast<float4 *>(to + 16 * c + 8 * i + 4) = make_float4(v[4], v[5], v[6], v[7]);
             }
           }
         }
-        if (there) {
+        if (there && part == 0) {
           if (!whole)
-            *reinterpret_cast<float2 *>(part) = make_float2(top, sum);
+            *reinterpret_cast<float2 *>(slot + (size_t)rows_per_block * HD + 2 * r) = make_float2(top, sum);
           else if (p.lse)
             p.lse[(int64_t)(pc.first + token) * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
         }
@@ -567,149 +598,144 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       if (pc.flat + pc.to >= c1) break;
       next_piece(pc, list, c1);
     }
-  } else if (c0 < c1 && warp < 12) {
-    // ---- decoding: a thread per key.  A tile's rows are loaded while the tile before is decoded, its page number one
-    // tile earlier still
-    const int row = tid - 256, wq = warp - 8;
-    bool ok = true;
+  } else if (c0 < c1 && warp < PT_MMA_WARP) {
+    // ---- decoding: a warp takes 32 keys of a tile's K or V, the warps in turn.  Its next keys' rows are loaded while
+    // it decodes these, their page numbers one turn earlier still
+    const unsigned n = (unsigned)(c1 - c0) * 8;  // turns: (tile, K or V, quarter)
     Piece pc;
     find_piece(pc, list, c0, c1);
     int t_next = pc.from;
-    int page = -2, slot = 0, head = 0;  // of the next tile's row (a page of -2: behind the user's rows)
-    const auto find_page = [&]() {
-      const int key = (pc.tile0 + t_next) * PT_KEYS + row;
+    unsigned tile_next = 0;
+    int page = -2, slot = 0, head = 0;  // of the row of this warp's next turn (a page of -2: behind the user's rows)
+    const auto find_page = [&](unsigned turn) {
+      for (; tile_next < turn >> 3; ++tile_next)
+        if (++t_next == pc.to) {
+          next_piece(pc, list, c1);
+          t_next = pc.from;
+        }
+      const int key = (pc.tile0 + t_next) * PT_KEYS + (turn & 3) * 32 + lane;
       page = key < pc.length ? p.map.table[(int64_t)pc.user * p.map.max_pages + (key >> lp)] : -2;
       slot = key & (p.pool.page_tokens() - 1), head = pc.head;
     };
-    const auto load_row = [&](int which, bool there, uint4 (&r)[HD / 32], uint32_t (&par)[KB]) {
+    uint4 now[HD / 32], later[HD / 32];
+    uint32_t now_p[KB], later_p[KB];
+    const auto load_row = [&](int which, bool there) {
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) r[i] = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < HD / 32; ++i) later[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < KB; ++i) par[i] = 0;
+      for (int i = 0; i < KB; ++i) later_p[i] = 0;
       if (!there) return;
       const uint8_t *b = p.pool.block(page, p.layer, head);
       const uint4 *codes = reinterpret_cast<const uint4 *>(b + which * p.pool.code_bytes() + slot * (HD / 2));
       const uint32_t *params = reinterpret_cast<const uint32_t *>(b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes()) + slot * KB;
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) r[i] = codes[i];
+      for (int i = 0; i < HD / 32; ++i) later[i] = codes[i];
 #pragma unroll
-      for (int i = 0; i < KB; ++i) par[i] = params[i];
+      for (int i = 0; i < KB; ++i) later_p[i] = params[i];
     };
-    const auto scan = [&](const uint32_t (&par)[KB], unsigned (&bad)[KB]) {
-#pragma unroll
-      for (int g = 0; g < KB; ++g)  // (a NaN or an infinity in scale or centre: all exponent bits set)
-        bad[g] = __ballot_sync(0xffffffffu, (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u);
+    unsigned turn = warp - PT_SOFTMAX;
+    bool there = false;
+    const auto load_turn = [&](unsigned t) {  // its page is known
+      there = page >= 0 && page < p.pool.n_pages;
+      if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+      load_row(t >> 2 & 1, there);
     };
-    uint4 now[HD / 32], later[HD / 32];  // a row of K or V, and of the other one after it
-    uint32_t now_p[KB], later_p[KB];
-    const unsigned n = (unsigned)(c1 - c0);
-    find_page();
-    bool there = page >= 0 && page < p.pool.n_pages;
-    if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-    load_row(0, there, now, now_p);
+    if (turn < n) {
+      find_page(turn);
+      load_turn(turn);
+      if (turn + PT_DECODERS < n) find_page(turn + PT_DECODERS);
+    }
 #pragma unroll 1
-    for (unsigned i = 0; i < 2 * n; ++i) {  // K and V of tile i / 2
-      const unsigned tile = i >> 1, which = i & 1;
-      const int buf = tile & 1;
-      uint32_t *flag = reinterpret_cast<uint32_t *>(flags + (tile & 3) * (1 + KB)) + wq;
-      unsigned have = 0;
-      if (!which) {
-        have = __ballot_sync(0xffffffffu, there);
-        load_row(1, there, later, later_p);
-        if (tile + 1 < n) {  // on to the next tile's page
-          if (++t_next == pc.to) {
-            next_piece(pc, list, c1);
-            t_next = pc.from;
-          }
-          find_page();
-        }
-      } else if (tile + 1 < n) {
-        there = page >= 0 && page < p.pool.n_pages;
-        if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-        load_row(0, there, later, later_p);
-      }
-      ok = wait((which ? B_VFREE : B_KFREE) + buf, (tile >> 1 & 1) ^ 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      if (which) {
-        unsigned bad[KB];
-        scan(now_p, bad);
-#pragma unroll
-        for (int g = 0; g < KB; ++g) {
-          if (lane == 0) flag[4 * (1 + g)] = bad[g];
-          if (bad[g] >> lane & 1) now_p[g] = 0;
-        }
-      } else if (lane == 0) {
-        flag[0] = have;
-      }
-      decode_row<HD>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, row);
-      fence_async_proxy();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar((which ? B_VFULL : B_KFULL) + buf));
+    for (; turn < n; turn += PT_DECODERS) {
+      const unsigned tile = turn >> 3;
+      const int which = turn >> 2 & 1, buf = tile & 1, quarter = turn & 3;
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) now[j] = later[j];
 #pragma unroll
       for (int j = 0; j < KB; ++j) now_p[j] = later_p[j];
+      uint32_t *flag = reinterpret_cast<uint32_t *>(flags + (tile & 3) * (1 + KB)) + quarter;
+      const unsigned have = __ballot_sync(0xffffffffu, there);
+      if (turn + PT_DECODERS < n) {
+        load_turn(turn + PT_DECODERS);
+        if (turn + 2 * PT_DECODERS < n) find_page(turn + 2 * PT_DECODERS);
+      }
+      if (!__all_sync(0xffffffffu, wait((which ? B_VFREE : B_KFREE) + buf, (tile >> 1 & 1) ^ 1))) break;
+      if (which) {
+#pragma unroll
+        for (int g = 0; g < KB; ++g) {  // (a NaN or an infinity in scale or centre: all exponent bits set)
+          const bool nan = (now_p[g] & 0x7c00u) == 0x7c00u || (now_p[g] & 0x7c000000u) == 0x7c000000u;
+          const unsigned bad = __ballot_sync(0xffffffffu, nan);
+          if (lane == 0) flag[4 * (1 + g)] = bad;
+          if (nan) now_p[g] = 0;
+        }
+      } else if (lane == 0) {
+        flag[0] = have;
+      }
+      decode_row<HD>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, quarter * 32 + lane);
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar((which ? B_VFULL : B_KFULL) + buf));
     }
   } else if (c0 < c1) {
-    // ---- products, issued by an elected lane
+    // ---- products, issued by an elected lane.  Descriptors are the same in every lane and known to be: through
+    // shuffles, or the compiler moves them lane by lane, which takes longer than a product
     constexpr uint32_t idesc_s = idesc_kind_f16(128, PT_KEYS, false);
     constexpr uint32_t idesc_o = idesc_kind_f16(128, HD, false) | (1u << 16);  // B is N-major
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), at = __shfl_sync(0xffffffffu, base, 0);
     unsigned tile = 0, done[2] = {}, pieces[2] = {};
     int before = 0;
     bool ok = true;
     Piece pc;
     find_piece(pc, list, c0, c1);
     const auto scores = [&](int half, int buf) {
+      const uint64_t q = sdesc_k_sw128(at + F::Q_AT + half * F::TILE), k = sdesc_k_sw128(at + F::K_AT + buf * F::TILE);
       if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k / 4) * (128 * 128) + (k % 4) * 32;
-          mma_bf16_ss(tmem + half * 128, sdesc_k_sw128(base + F::Q_AT + half * F::TILE + off),
-                      sdesc_k_sw128(base + F::K_AT + buf * F::TILE + off), idesc_s, k > 0);
+        for (int i = 0; i < HD / 16; ++i) {
+          constexpr int BLOCK = 128 * 128 >> 4;
+          const int off = (i / 4) * BLOCK + (i % 4) * 2;  // (descriptors count 16 bytes)
+          mma_bf16_ss(tm + half * 128, q + off, k + off, idesc_s, i > 0);
         }
         mma_commit(bar(B_S + half));
       }
       __syncwarp();
     };
-    for (; ok;) {
-      const int halves = pc.rows > 128 ? 2 : 1, n = pc.to - pc.from;
+    const auto values = [&](int half, int buf, bool first) {
+      const uint64_t v = sdesc_mn_sw128(at + F::V_AT + buf * F::TILE, KB == 2 ? 128 * 128 : 1024);
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < PT_KEYS / 16; ++i)
+          mma_ts(tm + 256 + half * 128, tm + half * 128 + 8 * i, v + i * 128, idesc_o, !first || i > 0);
+        mma_commit(bar(B_O + half));
+      }
+      __syncwarp();
+    };
+    for (;;) {
+      const int halves = __shfl_sync(0xffffffffu, pc.rows > 128 ? 2 : 1, 0), n = __shfl_sync(0xffffffffu, pc.to - pc.from, 0);
       // the halves that worked on the last piece have read its flags (decoding runs ahead), and the ones that work
       // on this one have their queries in place
       for (int h = 0; h < before; ++h) ok = ok && wait(B_READ + h, (pieces[h] - 1) & 1);
       for (int h = 0; h < halves; ++h) ok = ok && wait(B_Q + h, pieces[h]++ & 1);
       before = halves;
       ok = ok && wait(B_KFULL + (tile & 1), tile >> 1 & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
+      if (!(ok = __all_sync(0xffffffffu, ok))) break;
       tc_fence_after();
-      for (int h = 0; h < halves; ++h) scores(h, tile & 1);
-      if (elect_one()) mma_commit(bar(B_KFREE + (tile & 1)));
+      const int buf0 = __shfl_sync(0xffffffffu, (int)(tile & 1), 0);
+      for (int h = 0; h < halves; ++h) scores(h, buf0);
+      if (elect_one()) mma_commit(bar(B_KFREE + buf0));
       __syncwarp();
-      for (int t = 0; t < n && ok; ++t, ++tile) {
-        const int buf = tile & 1;
+      for (int t = 0; t < n; ++t, ++tile) {
+        const int buf = __shfl_sync(0xffffffffu, (int)(tile & 1), 0);
         const bool more = t + 1 < n;
-        ok = wait(B_VFULL + buf, tile >> 1 & 1);
-        for (int h = 0; h < halves && ok; ++h) {
-          ok = wait(B_P + h, done[h]++ & 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
+        ok = wait(B_VFULL + buf, tile >> 1 & 1) && (!more || wait(B_KFULL + (buf ^ 1), (tile + 1) >> 1 & 1));
 #pragma unroll
-            for (int k = 0; k < PT_KEYS / 16; ++k)
-              mma_ts(tmem + 256 + h * 128, tmem + h * 128 + 8 * k,
-                     sdesc_mn_sw128(base + F::V_AT + buf * F::TILE + k * 2048, KB == 2 ? 128 * 128 : 1024), idesc_o, t > 0 || k > 0);
-            mma_commit(bar(B_O + h));
-          }
-          __syncwarp();
-          if (more) {
-            if (h == 0) ok = wait(B_KFULL + (buf ^ 1), (tile + 1) >> 1 & 1);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            tc_fence_after();
-            scores(h, buf ^ 1);
-          }
+        for (int h = 0; h < 2; ++h) {
+          if (h >= halves) break;
+          ok = ok && wait(B_P + h, done[h]++ & 1);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          tc_fence_after();
+          values(h, buf, t == 0);
+          if (more) scores(h, buf ^ 1);
         }
         if (!ok) break;
         if (elect_one()) {
@@ -730,7 +756,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   __threadfence();
   __syncthreads();
   tc_fence_after();
-  if (warp == 12) tmem_dealloc(tmem, 512);
+  if (warp == PT_MMA_WARP) tmem_dealloc(tmem, 512);
   if (c0 >= c1 || words[1]) return;
 
   // ---- row blocks that other thread blocks have parts of: this one's first, its last
@@ -749,29 +775,35 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     }
     __syncthreads();
     if (!words[2]) continue;
-    const auto part_of = [&](int b, int r) {
-      return p.partials + ((size_t)b * 2 + (sa < b * quota ? 0 : 1)) * slot_floats + (size_t)r * (HD + 2);
-    };
-    // a warp per row, lanes over its channels
-    for (int r = warp; r < pc.rows; r += PT_THREADS / 32) {
+    const auto slot_of = [&](int b) { return p.partials + ((size_t)b * 2 + (sa < b * quota ? 0 : 1)) * slot_floats; };
+    // eight lanes per row, every row of a warp's four at once
+    constexpr int C = HD / 8;
+    const int sub = lane & 7;
+    for (int r = warp * 4 + (lane >> 3); r < pc.rows; r += PT_THREADS / 8) {
       const int token = (pc.row0 + r) / p.group, head = pc.head * p.group + (pc.row0 + r) % p.group;
-      float top = -INFINITY, sum = 0.f, v[HD / 32] = {};
-      for (int b = from; b <= to; ++b) top = fmaxf(top, part_of(b, r)[0]);
+      float top = -INFINITY, sum = 0.f, v[C] = {};
+      for (int b = from; b <= to; ++b) top = fmaxf(top, slot_of(b)[(size_t)rows_per_block * HD + 2 * r]);
       const float ref = top == -INFINITY ? 0.f : top;
       for (int b = from; b <= to; ++b) {
-        const float *part = part_of(b, r);
-        const float w = pt_ex2(part[0] - ref);
-        sum = fmaf(part[1], w, sum);
+        const float *slot = slot_of(b);
+        const float *stats = slot + (size_t)rows_per_block * HD + 2 * r;
+        const float w = pt_ex2(stats[0] - ref);
+        sum = fmaf(stats[1], w, sum);
+        const float4 *x = reinterpret_cast<const float4 *>(slot + (size_t)r * HD + sub * C);
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) v[j] = fmaf(part[1] == 0.f ? 0.f : part[2 + lane + 32 * j], w, v[j]);
+        for (int j = 0; j < C / 4; ++j) {
+          const float4 y = x[j];
+          v[4 * j] = fmaf(y.x, w, v[4 * j]), v[4 * j + 1] = fmaf(y.y, w, v[4 * j + 1]);
+          v[4 * j + 2] = fmaf(y.z, w, v[4 * j + 2]), v[4 * j + 3] = fmaf(y.w, w, v[4 * j + 3]);
+        }
       }
-      uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head));
+      uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head)) + sub * C;
 #pragma unroll
-      for (int j = 0; j < HD / 32; ++j) {
+      for (int j = 0; j < C; ++j) {
         const float y = sum == 0.f ? 0.f : v[j] / sum;
-        out[lane + 32 * j] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+        out[j] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
       }
-      if (p.lse && lane == 0)
+      if (p.lse && sub == 0)
         p.lse[(int64_t)(pc.first + token) * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
     }
   }
