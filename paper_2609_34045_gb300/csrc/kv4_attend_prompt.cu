@@ -4,8 +4,8 @@
 //   S = Q K^T (128 rows x 128 keys), O += P V,  P = 2^(c S - m),
 // with fp32 accumulators in tensor memory.  K and V are decoded once per block into fp16 operands in shared memory,
 // value = centre + (code - 8) scale rounded once; P takes the place of S as the second product's fp16 operand.  The
-// maximum m of a row moves only when it has grown by 2^8 (P stays below 256, far inside fp16), so that O is rarely
-// rescaled.  A row of Q is brought into fp16's range by a power of two that its scores are multiplied back by.
+// reference m of a row is the maximum of its first tiles and moves only when a tile's weights sum to more than 2^14 (P stays
+// inside fp16), so that O is rarely rescaled and the maximum not looked for.  A row of Q is brought into fp16's range by a power of two that its scores are multiplied back by.
 //
 // What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe.  256 rows share a decoded tile, which
 // leaves the decoding (2.2 instructions per element, four warps) and the softmax (a thread per row, some 4 instructions
@@ -31,7 +31,7 @@ constexpr int PT_SOFTMAX = 16;               // warps 0 to 15
 constexpr int PT_DECODERS = 7;               // 16 to 22
 constexpr int PT_MMA_WARP = PT_SOFTMAX + PT_DECODERS;
 constexpr int PT_THREADS = (PT_MMA_WARP + 1) * 32;
-constexpr float PT_GROW = 8.f;               // log2 of how far a row's maximum may outgrow its reference
+constexpr float PT_MOST = 16384.f;           // a row's weights in a tile may sum up to this: none is near fp16's end
 
 template <int HD>
 struct Prompt {
@@ -40,7 +40,8 @@ struct Prompt {
   static constexpr int Q_AT = 0, K_AT = 2 * TILE, V_AT = 4 * TILE;
   static constexpr int INFO_AT = 6 * TILE;                 // int4[FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int FLAG_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;  // uint4 [4][1 + KB]: keys of a tile
-  static constexpr int PAIR_AT = FLAG_AT + 4 * (1 + KB) * 16;  // float [2 halves][2][128]: what a row's two threads exchange
+  static constexpr int ODD_AT = FLAG_AT + 4 * (1 + KB) * 16;    // uint32 [4][2]: a byte per 32 keys, K and V: not as usual
+  static constexpr int PAIR_AT = ODD_AT + 4 * 2 * 4;  // float [2 halves][2][128]: what a row's two threads exchange
   static constexpr int BAR_AT = PAIR_AT + 2 * 2 * 128 * 4;
   static constexpr int SMEM = BAR_AT + 20 * 8 + 32;
   static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
@@ -112,43 +113,37 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// 64 scores of a row: w the weights 2^(score cf - top) in fp16 pairs, `most` the largest of them (infinity if fp16 cannot
-// hold it), `sum` their sum.  Sixteen scores at a time, the next ones on their way meanwhile.
-__device__ __forceinline__ void weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[32], float &most, float &sum) {
-  uint32_t x[2][16];
-  tmem_ld16(t_s, x[0]);
+// 64 scores of a row: w the weights 2^(score cf - top) in fp16 pairs; returns their sum (taken in fp32 before the rounding:
+// above PT_MOST one of them may have outgrown fp16).  Sixteen at a time: a load from tensor memory takes some 50 clocks, which
+// the other warps fill, and more of them in flight would cost registers that the tile loop has not got.
+__device__ __forceinline__ float weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[32]) {
   const float2 scale = {cf, cf}, from = {-top, -top};
   float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
-  __half2 m[2] = {__float2half2_rn(0.f), __float2half2_rn(0.f)};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
+    uint32_t v[16];
+    tmem_ld16(t_s + 16 * c, v);
     tmem_wait_ld();
-    if (c < 3) tmem_ld16(t_s + 16 * (c + 1), x[(c + 1) & 1]);
-    uint32_t(&v)[16] = x[c & 1];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-      const float2 a = {__uint_as_float(v[i]), __uint_as_float(v[i + 1])};
-      float2 e = fma2(a, scale, from);
+      float2 e = fma2({__uint_as_float(v[i]), __uint_as_float(v[i + 1])}, scale, from);
       e = {pt_ex2(e.x), pt_ex2(e.y)};
       s[i >> 1 & 1] = add2(s[i >> 1 & 1], e);
       w[8 * c + i / 2] = pt_pack(e.x, e.y);
-      m[i >> 1 & 1] = __hmax2(m[i >> 1 & 1], *reinterpret_cast<const __half2 *>(&w[8 * c + i / 2]));
     }
   }
-  m[0] = __hmax2(m[0], m[1]);
-  most = fmaxf(__low2float(m[0]), __high2float(m[0]));
-  sum = s[0].x + s[0].y + (s[1].x + s[1].y);
+  return s[0].x + s[0].y + (s[1].x + s[1].y);
 }
 
-// A barrier of the 256 threads of a half (1 or 2); with or: whether any of them says so.
-__device__ __forceinline__ void half_sync(int half) { named_bar_sync(1 + half, 256); }
-__device__ __forceinline__ bool half_any(int half, bool x) {
+// A barrier of the two warps that share 32 rows (pair 0 to 7); with any: whether any of their threads says so.
+__device__ __forceinline__ void pair_sync(int pair) { named_bar_sync(1 + pair, 64); }
+__device__ __forceinline__ bool pair_any(int pair, bool x) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "barrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)x), "r"(1 + half)
+      : "r"((uint32_t)x), "r"(1 + pair)
       : "memory");
   return r != 0;
 }
@@ -278,6 +273,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   int4 *info = reinterpret_cast<int4 *>(smem + F::INFO_AT);
   int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
   uint4 *flags = reinterpret_cast<uint4 *>(smem + F::FLAG_AT);  // [4][0: page there, 1 + g: group g reads as NaN]
+  volatile uint32_t *odd = reinterpret_cast<volatile uint32_t *>(smem + F::ODD_AT);
   volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + F::BAR_AT + 20 * 8);  // TMEM, abort, last
   const uint32_t bars = base + F::BAR_AT;
   const auto bar = [&](int b) { return bars + 8 * b; };
@@ -368,9 +364,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     const int half = warp >> 3, part = warp >> 2 & 1, row = tid & 127;
     constexpr int CH = HD / 2;                          // channels of a thread
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
-    const uint32_t t_s = tmem + lanes + half * 128 + part * 64, t_p = tmem + lanes + half * 128 + part * 32;
+    const uint32_t t_s = tmem + lanes + half * 128 + part * 64;
     const uint32_t t_o = tmem + lanes + 256 + half * 128 + part * CH;
     const uint32_t q_tile = base + F::Q_AT + half * F::TILE;
+    const int twins = half * 4 + (warp & 3);
     float *pair = reinterpret_cast<float *>(smem + F::PAIR_AT) + half * 256;  // [part][row]
     const float log2_scale = fabsf(p.scale) * 1.44269504089f;
     uint32_t done = 0;  // tiles of this half so far
@@ -411,7 +408,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             big = fmaxf(big, fmaxf(fabsf(a), fabsf(b)));
           }
           pair[part * 128 + row] = big;
-          half_sync(half);
+          pair_sync(twins);
           unit = xchunk_scale(fmaxf(big, pair[(part ^ 1) * 128 + row]), &inv);
 #pragma unroll
           for (int i = 0; i < CH / 8; ++i) {
@@ -456,21 +453,25 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           wait(B_S + half, done & 1);
           __syncwarp();
           tc_fence_after();
-          if (t > 0) see_poison(t - 1);
-          const uint2 there2 = reinterpret_cast<const uint2 *>(flags + ((tile + t) & 3) * (1 + KB))[part];
-          const bool masked = key0 + 64 > least || (p.window > 0 && key0 < greatest) || (there2.x & there2.y) != 0xffffffffu;
-          const auto sees = [&](int c, int i) {  // column 16 c + i
-            const int key = key0 + 16 * c + i;
-            return key < end && key >= begin && ((c < 2 ? there2.x : there2.y) >> ((c & 1) * 16 + i) & 1);
-          };
-          // The weights are taken against the reference that the row has; they stay in registers until all threads of the
-          // half find that it holds.  Where it does not (the first tile, a row that outgrew it by 2^8, scores that
+          const bool masked = key0 + 64 > least || (p.window > 0 && key0 < greatest);
+          // (what the decoding has to say of the tiles comes while the scores are weighed: shared memory, busy with the
+          // products' operands, takes hundreds of clocks)
+          const uint32_t odd_k = odd[2 * ((tile + t) & 3)] >> (16 * part) & 0xffff, odd_v = t > 0 ? odd[2 * ((tile + t - 1) & 3) + 1] : 0;
+          // The weights are taken against the reference that the row has; they stay in registers until both threads of the
+          // row find that it holds.  Where it does not (the first tile, a row that outgrew it, scores that
           // are masked) the scores, still in place, are read again.
           uint32_t w[32];
-          float most = 0.f, part_sum = 0.f;
-          if (!masked && t > 0) weigh_scores(t_s, cf, top, w, most, part_sum);
-          if (half_any(half, masked || t == 0 || most > 256.f || top == -INFINITY)) {
-            most = -INFINITY;
+          float part_sum = 0.f;
+          if (!masked && t > 0) part_sum = weigh_scores(t_s, cf, top, w);
+          if (odd_v) see_poison(t - 1);
+          if (pair_any(twins, masked || odd_k || t == 0 || part_sum > PT_MOST || top == -INFINITY)) {
+            const bool pick = masked || odd_k;
+            const uint2 there2 = reinterpret_cast<const uint2 *>(flags + ((tile + t) & 3) * (1 + KB))[part];
+            const auto sees = [&](int c, int i) {  // column 16 c + i
+              const int key = key0 + 16 * c + i;
+              return key < end && key >= begin && ((c < 2 ? there2.x : there2.y) >> ((c & 1) * 16 + i) & 1);
+            };
+            float most = -INFINITY;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               uint32_t x[16];
@@ -478,14 +479,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
               tmem_wait_ld();
 #pragma unroll
               for (int i = 0; i < 16; ++i)
-                if (!masked || sees(c, i)) most = fmaxf(most, __uint_as_float(x[i]));
+                if (!pick || sees(c, i)) most = fmaxf(most, __uint_as_float(x[i]));
             }
             pair[part * 128 + row] = most;
-            half_sync(half);
+            pair_sync(twins);
             most = fmaxf(most, pair[(part ^ 1) * 128 + row]);
             most = most == -INFINITY ? most : most * cf;
             float keep = 1.f;
-            if (most > top + PT_GROW || (top == -INFINITY && most > top)) {
+            if (most > top) {
               keep = pt_ex2(top - most);
               top = most;
               sum *= keep;
@@ -515,7 +516,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
 #pragma unroll
               for (int i = 0; i < 16; i += 2) {
                 float a = fmaf(__uint_as_float(x[i]), cf, -ref), b = fmaf(__uint_as_float(x[i + 1]), cf, -ref);
-                if (masked) {
+                if (pick) {
                   if (!sees(c, i)) a = -INFINITY;
                   if (!sees(c, i + 1)) b = -INFINITY;
                 }
@@ -524,11 +525,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
                 w[8 * c + i / 2] = pt_pack(a, b);
               }
             }
-            half_sync(half);  // (the second threads' weights go where the first ones' scores are)
+            pair_sync(twins);  // (before the next exchange)
           }
           sum += part_sum;
-          tmem_st16(t_p, reinterpret_cast<uint32_t(&)[16]>(w[0]));
-          tmem_st16(t_p + 16, reinterpret_cast<uint32_t(&)[16]>(w[16]));
+          tmem_st16(t_s, reinterpret_cast<uint32_t(&)[16]>(w[0]));
+          tmem_st16(t_s + 16, reinterpret_cast<uint32_t(&)[16]>(w[16]));
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -543,9 +544,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_READ + half));  // (the tiles' flags have been read)
         pair[part * 128 + row] = sum;
-        half_sync(half);
+        pair_sync(twins);
         sum += pair[(part ^ 1) * 128 + row];
-        half_sync(half);  // (before the next piece's exchange)
+        pair_sync(twins);  // (before the next piece's exchange)
         const bool whole = pc.from == 0 && pc.to == pc.n_tiles;
         const float inv_sum = sum == 0.f ? 0.f : 1.f / sum;
         float *slot = p.partials + ((size_t)blockIdx.x * 2 + (pc.from > 0 ? 0 : 1)) * slot_floats;
@@ -620,11 +621,13 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     uint4 now[HD / 32], later[HD / 32];
     uint32_t now_p[KB], later_p[KB];
     const auto load_row = [&](int which, bool there) {
+      if (!there) {
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) later[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < HD / 32; ++i) later[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < KB; ++i) later_p[i] = 0;
-      if (!there) return;
+        for (int i = 0; i < KB; ++i) later_p[i] = 0;
+        return;
+      }
       const uint8_t *b = p.pool.block(page, p.layer, head);
       const uint4 *codes = reinterpret_cast<const uint4 *>(b + which * p.pool.code_bytes() + slot * (HD / 2));
       const uint32_t *params = reinterpret_cast<const uint32_t *>(b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes()) + slot * KB;
@@ -660,17 +663,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         if (turn + 2 * PT_DECODERS < n) find_page(turn + 2 * PT_DECODERS);
       }
       if (!__all_sync(0xffffffffu, wait((which ? B_VFREE : B_KFREE) + buf, (tile >> 1 & 1) ^ 1))) break;
+      unsigned any = which ? 0 : ~have;
       if (which) {
 #pragma unroll
         for (int g = 0; g < KB; ++g) {  // (a NaN or an infinity in scale or centre: all exponent bits set)
           const bool nan = (now_p[g] & 0x7c00u) == 0x7c00u || (now_p[g] & 0x7c000000u) == 0x7c000000u;
           const unsigned bad = __ballot_sync(0xffffffffu, nan);
           if (lane == 0) flag[4 * (1 + g)] = bad;
+          any |= bad;
           if (nan) now_p[g] = 0;
         }
       } else if (lane == 0) {
         flag[0] = have;
       }
+      if (lane == 0) reinterpret_cast<volatile uint8_t *>(odd + 2 * (tile & 3) + which)[quarter] = any != 0;
       decode_row<HD>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, quarter * 32 + lane);
       fence_async_proxy();
       __syncwarp();
@@ -705,7 +711,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       if (elect_one()) {
 #pragma unroll
         for (int i = 0; i < PT_KEYS / 16; ++i)
-          mma_ts(tm + 256 + half * 128, tm + half * 128 + 8 * i, v + i * 128, idesc_o, !first || i > 0);
+          mma_ts(tm + 256 + half * 128, tm + half * 128 + (i / 4) * 64 + (i % 4) * 8, v + i * 128, idesc_o, !first || i > 0);
         mma_commit(bar(B_O + half));
       }
       __syncwarp();
