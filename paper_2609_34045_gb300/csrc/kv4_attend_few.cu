@@ -23,6 +23,7 @@
 // (sequence, head) that it does not own alone is merged within the block, then over blocks by the last to arrive;
 // every sum is taken in list order, so results do not depend on arrival.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4_attend.cuh"
 
@@ -123,9 +124,9 @@ __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, int n_seqs,
   }
   c.seq = lo;
   enter_sequence(c, info, prefix, window);
-  const int64_t rest = flat - (int64_t)prefix[lo] * heads;
-  c.head = (int)(rest / c.n_tiles);
-  c.tile = (int)(rest - (int64_t)c.head * c.n_tiles);
+  const int rest = (int)(flat - (int64_t)prefix[lo] * heads);  // (below heads * 2^20)
+  c.head = rest / c.n_tiles;
+  c.tile = rest - c.head * c.n_tiles;
 }
 
 __device__ __forceinline__ void next_tile(Cursor &c, int n_seqs, int heads, const int4 *info, const int *prefix,
@@ -179,16 +180,19 @@ __device__ __forceinline__ void merge_column(int n, int col, int lane, const At 
       s = fmaf(part[COLS], w, s);
     }
     const int here = min(32, n - i0);
-#pragma unroll 8
-    for (int i = 0; i < here; ++i) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float *part = at(i0 + i) + col * HD + lane * C;
-      if constexpr (C == 4) {
-        const float4 x = *reinterpret_cast<const float4 *>(part);
-        v[0] = fmaf(x.x, wi, v[0]), v[1] = fmaf(x.y, wi, v[1]), v[2] = fmaf(x.z, wi, v[2]), v[3] = fmaf(x.w, wi, v[3]);
-      } else {
-        const float2 x = *reinterpret_cast<const float2 *>(part);
-        v[0] = fmaf(x.x, wi, v[0]), v[1] = fmaf(x.y, wi, v[1]);
+    for (int i = 0; i < here; i += 8) {
+      using Vec = typename std::conditional<C == 4, float4, float2>::type;
+      Vec x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        x[k] = *reinterpret_cast<const Vec *>(at(i0 + min(i + k, here - 1)) + col * HD + lane * C);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float wi = __shfl_sync(0xffffffffu, w, (i + k) & 31);  // (0 behind the last)
+        const float *y = reinterpret_cast<const float *>(&x[k]);
+        if (i + k < here)
+#pragma unroll
+          for (int j = 0; j < C; ++j) v[j] = fmaf(y[j], wi, v[j]);
       }
     }
   }
@@ -313,18 +317,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       fetch_ok = false;
     }
   };
+  Cursor at = fetch;
   if (fetch_ok) load_page();
-#pragma unroll
-  for (int i = 0; i < F::SLOTS; ++i)
-    if (fetch_ok) issue();
 
   // ---- this warp's tiles
   uint32_t q[NT][G][2][2][2];     // B fragments: [group][word of a lane][half of its pairs][register]
   float seed[NT][G][2], qs[NT][G][2], cf[NT][2];
   float o[NT][G][4][4], ones[NT][G][4], top[NT][2], sum[NT][2], centre[NT][G][2];
   float v_unit = 0.f;             // the value scales' reference, a power of two
-  Cursor at;
-  if (w0 < w1) locate_tile(at, w0, p.n_seqs, heads, info, prefix, p.window);
   unsigned slot = 0, phase = 0;
   int rows = 0;
   float *block_ws = p.partials + (size_t)blockIdx.x * (W + 2) * F::PARTIAL;
@@ -332,73 +332,76 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   for (int64_t flat = w0; flat < w1; ++flat) {
     if (flat == w0 || at.tile == 0) {
       // ---- a new (sequence, head): its query rows as fp16 (a power of two per row brings the largest to [2^14, 2^15))
+      // 16 channels of each group for column gid; under way before the first tiles' copies, whose page numbers come first
+      uint32_t raw[NT][G][8];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int col = n * 8 + gid;
+          const bool there = col < at.count * p.group;
+          const uint16_t *e = reinterpret_cast<const uint16_t *>(
+                                  there ? p.q.row(at.first + col / p.group, at.head * p.group + col % p.group) : nullptr) +
+                              tig * 16;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            if (!there) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) raw[n][g][i] = 0;
+            } else if (p.q_wide) {
+              const uint4 a = *reinterpret_cast<const uint4 *>(e + 64 * g), b = *reinterpret_cast<const uint4 *>(e + 64 * g + 8);
+              raw[n][g][0] = a.x, raw[n][g][1] = a.y, raw[n][g][2] = a.z, raw[n][g][3] = a.w;
+              raw[n][g][4] = b.x, raw[n][g][5] = b.y, raw[n][g][6] = b.z, raw[n][g][7] = b.w;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) raw[n][g][i] = e[64 * g + 2 * i] | ((uint32_t)e[64 * g + 2 * i + 1] << 16);
+            }
+          }
+        }
+      if (flat == w0 && fetch_ok) issue();
       rows = at.count * p.group;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[G][16], big = 0.f;
-        const int col = n * 8 + gid;
-        const bool there = col < rows;
-        const char *src = there ? p.q.row(at.first + col / p.group, at.head * p.group + col % p.group) : nullptr;
+        // (magnitudes of either type order as their bits)
+        uint32_t big2 = 0;
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const uint16_t *e = reinterpret_cast<const uint16_t *>(src) + g * 64 + tig * 16;
-          uint32_t w[8];
-          if (!there) {
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0;
-          } else if (p.q_wide) {
-            const uint4 a = *reinterpret_cast<const uint4 *>(e), b = *reinterpret_cast<const uint4 *>(e + 8);
-            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = e[2 * i] | ((uint32_t)e[2 * i + 1] << 16);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint16_t h = (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
-            const float f = p.bf16 ? bf16_to_f32(h) : f16_to_f32(h);
-            x[g][i] = p.scale > 0.f ? f : p.scale < 0.f ? -f : 0.f;
-            big = fmaxf(big, fabsf(x[g][i]));
-          }
-        }
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          for (int i = 0; i < 8; ++i) big2 = __vmaxu2(big2, raw[n][g][i] & 0x7FFF7FFFu);
+        uint32_t big1 = max(big2 & 0xffff, big2 >> 16);
+        big1 = max(big1, __shfl_xor_sync(0xffffffffu, big1, 1));
+        big1 = max(big1, __shfl_xor_sync(0xffffffffu, big1, 2));
         float inv;
-        const float unit = xchunk_scale(big, &inv);
-        float total_g[G], start_g[G];
+        const float unit = xchunk_scale(p.bf16 ? bf16_to_f32((uint16_t)big1) : f16_to_f32((uint16_t)big1), &inv);
+        inv = p.scale > 0.f ? inv : p.scale < 0.f ? -inv : 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          total_g[g] = start_g[g] = 0.f;
+          float even[4] = {}, odd[4] = {};  // sums over the channels, as products with ones: in the accumulators' columns
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              // (even channels meet u and odd ones 16 (64 + u): 16 times the query for the even ones)
-              const float r = i & 1 ? inv * 0.0625f : inv;
-              const uint32_t pair = pack_half2(x[g][8 * j + i] * r, x[g][8 * j + i + 4] * r);
-              q[n][g][j][i >> 1][i & 1] = pair;
-              const float t = half_lo(pair) + half_hi(pair);
-              total_g[g] += i & 1 ? 16.f * t : t;
-              start_g[g] -= i & 1 ? 1152.f * t : 8.f * t;
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                // (even channels meet u and odd ones 16 (64 + u): 16 times the query for the even ones)
+                const uint32_t two = __byte_perm(raw[n][g][4 * j + h], raw[n][g][4 * j + h + 2], k ? 0x7632 : 0x5410);
+                const float lo = p.bf16 ? bf16_lo(two) : half_lo(two), hi = p.bf16 ? bf16_hi(two) : half_hi(two);
+                const float r = k ? inv * 0.0625f : inv;
+                q[n][g][j][h][k] = pack_half2(lo * r, hi * r);
+              }
+              mma16816(even, 0x3C003C00u, 0x3C003C00u, 0, 0, q[n][g][j][h][0], q[n][g][j][h][1]);
+              mma16816(odd, 0, 0, 0x3C003C00u, 0x3C003C00u, q[n][g][j][h][0], q[n][g][j][h][1]);
             }
 #pragma unroll
-          for (int off = 1; off < 4; off <<= 1) {
-            total_g[g] += __shfl_xor_sync(0xffffffffu, total_g[g], off);
-            start_g[g] += __shfl_xor_sync(0xffffffffu, start_g[g], off);
+          for (int c = 0; c < 2; ++c) {
+            qs[n][g][c] = fmaf(16.f, odd[c], even[c]);
+            seed[n][g][c] = fmaf(-1152.f, odd[c], -8.f * even[c]);
+            centre[n][g][c] = 0.f;
           }
         }
         // (columns of the accumulators: 2 tig, 2 tig + 1)
         const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);  // (not 0: -inf times it stays)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int from = (2 * tig + c) * 4;
-          cf[n][c] = __shfl_sync(0xffffffffu, factor, from);
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            qs[n][g][c] = __shfl_sync(0xffffffffu, total_g[g], from);
-            seed[n][g][c] = __shfl_sync(0xffffffffu, start_g[g], from);
-            centre[n][g][c] = 0.f;
-          }
+          cf[n][c] = __shfl_sync(0xffffffffu, factor, (2 * tig + c) * 4);
           top[n][c] = -INFINITY, sum[n][c] = 0.f;
         }
 #pragma unroll
@@ -412,6 +415,10 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         }
       }
       v_unit = 0.f;
+      if (flat == w0)
+#pragma unroll
+        for (int i = 1; i < F::SLOTS; ++i)
+          if (fetch_ok) issue();
     }
 
     // ---- one tile
