@@ -26,6 +26,17 @@ struct AttendParams {
   int32_t *status;
 };
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
 // Waits for an mbarrier phase for two seconds at most (by the clock: a poll may itself be held for microseconds).
 __device__ __forceinline__ bool wait_2s(uint32_t bar, uint32_t parity) {
   for (int i = 0; i < 64; ++i)

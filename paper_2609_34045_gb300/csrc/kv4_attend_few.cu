@@ -43,7 +43,7 @@ struct Few {
   static constexpr int SLOTS = HD == 128 ? 2 : 3;
   static constexpr int PARTIAL = COLS * HD + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
   static constexpr int RING_BYTES = WARPS * SLOTS * TILE_BYTES;
-  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + 4 * WARPS * 4 + 16;
+  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (6 * WARPS + 4) * 4;
   static_assert(PARTIAL * 4 <= TILE_BYTES, "a slot holds a warp's partial result");
   static_assert(SMEM <= 232448, "shared memory of a block");
 };
@@ -70,8 +70,8 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ float half_lo(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)x)); }
-__device__ __forceinline__ float half_hi(uint32_t x) { return __half2float(__ushort_as_half((uint16_t)(x >> 16))); }
+__device__ __forceinline__ float half_lo(uint32_t x) { return __low2float(*reinterpret_cast<const __half2 *>(&x)); }
+__device__ __forceinline__ float half_hi(uint32_t x) { return __high2float(*reinterpret_cast<const __half2 *>(&x)); }
 
 // The nibbles of a word's bytes 0 and 2 as two fp16 pairs, exactly: the low ones as u, the high ones as 16 (64 + u).  A byte
 // and its high nibble in the mantissa of fp16 1024 differ by the low one; the difference runs beside the logic unit, which
@@ -157,48 +157,65 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
   if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
 }
 
-// A column of several partial results, `n` of them at at(i), in order: merged by one warp.  Lanes take the parts' maxima
-// and sums, 32 at a time; then every lane its channels of all parts, the loads of eight together.
-template <int HD, int COLS, class At>
-__device__ __forceinline__ void merge_column(int n, int col, int lane, const At &at, float (&v)[HD / 32], float &top,
-                                             float &sum) {
-  constexpr int C = HD / 32;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, at(i)[COLS * HD + col]);
+// NC columns from `col` on of several partial results, `n` of them at at(i), in order: merged by one warp.  Lanes take the
+// parts' maxima and sums, 32 at a time; then every lane its channels of all parts, 16 loads together.
+template <int HD, int COLS, int NC, class At>
+__device__ __forceinline__ void merge_columns(int n, int col, int lane, const At &at, float (&v)[NC][HD / 32], float (&top)[NC],
+                                              float (&sum)[NC]) {
+  constexpr int C = HD / 32, AHEAD = 16 / NC;
+  using Vec = typename std::conditional<C == 4, float4, float2>::type;
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  top = m;
-  const float base = m == -INFINITY ? 0.f : m;
-  float s = 0.f;
+  for (int c = 0; c < NC; ++c) {
+    top[c] = -INFINITY, sum[c] = 0.f;
 #pragma unroll
-  for (int j = 0; j < C; ++j) v[j] = 0.f;
+    for (int j = 0; j < C; ++j) v[c][j] = 0.f;
+  }
+  for (int i = lane; i < n; i += 32) {
+    const float *part = at(i) + COLS * HD + col;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) top[c] = fmaxf(top[c], part[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], off));
   for (int i0 = 0; i0 < n; i0 += 32) {
-    float w = 0.f;
-    if (i0 + lane < n) {
-      const float *part = at(i0 + lane) + COLS * HD + col;
-      w = ex2(part[0] - base);
-      s = fmaf(part[COLS], w, s);
-    }
     const int here = min(32, n - i0);
-    for (int i = 0; i < here; i += 8) {
-      using Vec = typename std::conditional<C == 4, float4, float2>::type;
-      Vec x[8];
+    float w[NC] = {};
+    if (lane < here) {
+      const float *part = at(i0 + lane) + COLS * HD + col;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        x[k] = *reinterpret_cast<const Vec *>(at(i0 + min(i + k, here - 1)) + col * HD + lane * C);
+      for (int c = 0; c < NC; ++c) {
+        w[c] = ex2(part[c] - (top[c] == -INFINITY ? 0.f : top[c]));
+        sum[c] = fmaf(part[COLS + c], w[c], sum[c]);
+      }
+    }
+#pragma unroll 1
+    for (int i = 0; i < here; i += AHEAD) {
+      Vec x[AHEAD][NC];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float wi = __shfl_sync(0xffffffffu, w, (i + k) & 31);  // (0 behind the last)
-        const float *y = reinterpret_cast<const float *>(&x[k]);
-        if (i + k < here)
+      for (int k = 0; k < AHEAD; ++k) {
+        const float *part = at(i0 + min(i + k, here - 1)) + col * HD + lane * C;
 #pragma unroll
-          for (int j = 0; j < C; ++j) v[j] = fmaf(y[j], wi, v[j]);
+        for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * HD);
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        if (i + k >= here) break;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float wi = __shfl_sync(0xffffffffu, w[c], i + k);
+          const float *y = reinterpret_cast<const float *>(&x[k][c]);
+#pragma unroll
+          for (int j = 0; j < C; ++j) v[c][j] = fmaf(y[j], wi, v[c][j]);
+        }
       }
     }
   }
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  sum = s;
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], off);
 }
 
 template <int HD, int NT>
@@ -211,7 +228,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   uint64_t *bars = reinterpret_cast<uint64_t *>(prefix + FEW_SEQS + 4);
   int *part_seg = reinterpret_cast<int *>(bars + W * F::SLOTS);  // [2 W]: segment of each partial result, or -1
   int *part_place = part_seg + 2 * W;
-  int *n_parts = part_place + 2 * W, *last_flags = n_parts + 1;
+  int *group_at = part_place + 2 * W, *n_groups = group_at + 2 * W + 1;
+  volatile int *cut = n_groups + 1;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
   pdl_launch_dependents();
@@ -265,6 +283,9 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
   constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;  // of a tile's K or V, as in a block of 64 tokens
   const int lb = min(lp, 6);                         // log2 of a page's tokens in a tile
+  const int block_bytes = p.pool.block_bytes();
+  const size_t page_bytes = p.pool.page_bytes();
+  const uint8_t *layer_pages = p.pool.pages + (size_t)p.layer * heads * block_bytes;
   const uint64_t policy = policy_evict_normal();
 
   // ---- copies: a page of 64 tokens is a tile as it stands; of others a page's part of the tile comes in four (codes and
@@ -287,14 +308,17 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     const bool there = fetch_page >= 0 && fetch_page < p.pool.n_pages;
     if (fetch_page != -2 && !there) report(p.status, KFL_BAD_PAGE);
     const unsigned lanes = __ballot_sync(0xffffffffu, there);
-    unsigned have = 0;
+    unsigned have = lanes & 1 ? 0xf : 0;
+    if (lp < 6) {
+      have = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
+      for (int i = 0; i < 4; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
+    }
     const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
     if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / 4));
     __syncwarp();
     if (there) {
-      const uint8_t *src = p.pool.block(fetch_page, p.layer, fetch.head);
+      const uint8_t *src = layer_pages + fetch_page * page_bytes + (unsigned)(fetch.head * block_bytes);
       if (lp == 6) {
         bulk_g2s(dst, src, F::TILE_BYTES, bar, policy);
       } else {
@@ -496,8 +520,12 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[n][st][i] = fmaf(ks[i >> 1][g], acc[n][i], fmaf(kc[i >> 1][g], qs[n][g][i & 1], x[n][st][i]));
+            for (int i = 0; i < 4; i += 2) {
+              const float s = ks[i >> 1][g], c = kc[i >> 1][g];
+              const float2 t = fma2({c, c}, {qs[n][g][0], qs[n][g][1]}, {x[n][st][i], x[n][st][i + 1]});
+              const float2 r = fma2({s, s}, {acc[n][i], acc[n][i + 1]}, t);
+              x[n][st][i] = r.x, x[n][st][i + 1] = r.y;
+            }
         }
       }
       unsigned hidden[NT] = {};  // a bit per score of this lane
@@ -581,6 +609,11 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         }
       }
       const float weight_unit = v_unit > 0.f ? 16384.f / v_unit : 0.f;
+      float ref[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) ref[n][c] = top[n][c] == -INFINITY ? 0.f : -top[n][c] * cf[n][c];
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
         const uint32_t vb = base + CODES + (16 * st + tig) * (HD / 2) + gid * 4;
@@ -588,21 +621,26 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float pr[4];
+          const float2 scale = {cf[n][0], cf[n][1]}, from = {ref[n][0], ref[n][1]};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float m = top[n][i & 1] == -INFINITY ? 0.f : top[n][i & 1] * cf[n][i & 1];
-            pr[i] = ex2(fmaf(x[n][st][i], cf[n][i & 1], -m));
-            sum[n][i & 1] += pr[i];
+          for (int i = 0; i < 4; i += 2) {
+            const float2 e = fma2({x[n][st][i], x[n][st][i + 1]}, scale, from);
+            pr[i] = ex2(e.x), pr[i + 1] = ex2(e.y);
+            sum[n][0] += pr[i], sum[n][1] += pr[i + 1];
           }
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             float w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float s = half_lo(vpar[st][i >> 1][g]), c = half_hi(vpar[st][i >> 1][g]);
-              if (masked && (hidden[n] >> (4 * st + i) & 1)) s = c = 0.f;
-              centre[n][g][i & 1] = fmaf(pr[i], c, centre[n][g][i & 1]);
-              w[i] = pr[i] * (s * weight_unit);
+            for (int i = 0; i < 4; i += 2) {
+              float s0 = half_lo(vpar[st][i >> 1][g]) * weight_unit, d0 = half_hi(vpar[st][i >> 1][g]), s1 = s0, d1 = d0;
+              if (masked) {
+                if (hidden[n] >> (4 * st + i) & 1) s0 = d0 = 0.f;
+                if (hidden[n] >> (4 * st + i + 1) & 1) s1 = d1 = 0.f;
+              }
+              const float2 t = fma2({pr[i], pr[i + 1]}, {d0, d1}, {centre[n][g][0], centre[n][g][1]});
+              centre[n][g][0] = t.x, centre[n][g][1] = t.y;
+              w[i] = pr[i] * s0, w[i + 1] = pr[i + 1] * s1;
             }
             pf[n][g][0] = transpose8x8(pack_half2(w[0], w[1]));
             pf[n][g][1] = transpose8x8(pack_half2(w[2], w[3]));
@@ -714,76 +752,87 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   }
 
   // ---- partial results of this block, in list order ([warp][0: its first segment's, 1: its last's], without the
-  // places that hold none): those of a segment are neighbours
+  // places that hold none): those of a segment are neighbours, a group
   __syncthreads();
   if (warp == 0) {
     const int id = lane < 2 * W ? part_seg[lane] : -1;
     const unsigned there = __ballot_sync(0xffffffffu, id >= 0);
-    __syncwarp();
-    if (id >= 0) {
-      const int k = __popc(there & ((1u << lane) - 1));
-      part_seg[k] = id, part_place[k] = lane;
+    const unsigned before = there & ((1u << lane) - 1);
+    const int last_id = __shfl_sync(0xffffffffu, id, before ? 31 - __clz(before) : 0);
+    const bool opens = id >= 0 && (before == 0 || last_id != id);
+    const unsigned groups = __ballot_sync(0xffffffffu, opens);
+    if (id >= 0) part_place[__popc(before)] = lane;
+    if (opens) {
+      const int k = __popc(groups & ((1u << lane) - 1));
+      part_seg[k] = id, group_at[k] = __popc(before);
     }
-    if (lane == 0) *n_parts = __popc(there);
+    if (lane == 0) n_groups[0] = __popc(groups), group_at[__popc(groups)] = __popc(there);
   }
   __syncthreads();
-  const auto place = [&](int k) {
-    const int e = part_place[k];
-    return e & 1 ? reinterpret_cast<const float *>(smem + (size_t)(e >> 1) * F::SLOTS * F::TILE_BYTES)
-                 : block_ws + (size_t)(e >> 1) * F::PARTIAL;
+  // a segment's places in the list, and how it stands to this block's: whole, or begun (0) or continued (1) elsewhere
+  const auto segment = [&](int id, Cursor &c, int64_t &sa, int64_t &sb) {
+    c.seq = id / heads, c.head = id - c.seq * heads;
+    enter_sequence(c, info, prefix, p.window);
+    sa = (int64_t)prefix[c.seq] * heads + c.head * c.n_tiles, sb = sa + c.n_tiles;
   };
-  int cut[2] = {-1, -1};  // segments that other blocks have parts of: the block's first, its last
   Cursor seg;
-  for (int e = 0, f; e < *n_parts; e = f) {
-    const int id = part_seg[e];
-    for (f = e + 1; f < *n_parts && part_seg[f] == id;) ++f;
-    seg.seq = id / heads;
-    enter_sequence(seg, info, prefix, p.window);
-    seg.head = id % heads;
-    const int64_t sa = (int64_t)prefix[seg.seq] * heads + (int64_t)seg.head * seg.n_tiles, sb = sa + seg.n_tiles;
+  int64_t sa, sb;
+  for (int u = warp; u < n_groups[0] * (COLS / 4); u += W) {
+    const int k = u / (COLS / 4), col = u % (COLS / 4) * 4;
+    segment(part_seg[k], seg, sa, sb);
+    const int rows_here = seg.count * p.group;
+    if (col >= rows_here) continue;
+    const int e = group_at[k];
+    const auto nth = [&](int i) {
+      const int at = part_place[e + i];
+      return at & 1 ? reinterpret_cast<const float *>(smem + (size_t)(at >> 1) * F::SLOTS * F::TILE_BYTES)
+                    : block_ws + (at >> 1) * F::PARTIAL;
+    };
+    float v[4][HD / 32], top4[4], sum4[4];
+    merge_columns<HD, COLS, 4>(group_at[k + 1] - e, col, lane, nth, v, top4, sum4);
     const bool whole = sa >= c0 && sb <= c1;
-    const int where = sa < c0 ? 0 : 1;
-    if (!whole) cut[where] = id;
-    const auto nth = [&](int i) { return place(e + i); };
-    for (int col = warp; col < seg.count * p.group; col += W) {
-      float v[HD / 32], top_c, sum_c;
-      merge_column<HD, COLS>(f - e, col, lane, nth, v, top_c, sum_c);
-      if (whole) {
-        store_row<HD>(p, seg, col, lane, v, top_c, sum_c);
-      } else {
-        float *to = block_ws + (size_t)(W + where) * F::PARTIAL;
+    float *to = block_ws + (W + (sa < c0 ? 0 : 1)) * F::PARTIAL;
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) to[col * HD + lane * (HD / 32) + j] = v[j];
-        if (lane == 0) to[COLS * HD + col] = top_c, to[COLS * HD + COLS + col] = sum_c;
+    for (int c = 0; c < 4; ++c) {
+      if (whole) {
+        if (col + c < rows_here) store_row<HD>(p, seg, col + c, lane, v[c], top4[c], sum4[c]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) to[(col + c) * HD + lane * (HD / 32) + j] = v[c][j];
+        if (lane == 0) to[COLS * HD + col + c] = top4[c], to[COLS * HD + COLS + col + c] = sum4[c];
       }
     }
   }
-  if (cut[0] < 0 && cut[1] < 0) return;
-  __threadfence();
   __syncthreads();
-  for (int i = 0; i < 2; ++i) {
-    if (cut[i] < 0) continue;
-    seg.seq = cut[i] / heads;
-    enter_sequence(seg, info, prefix, p.window);
-    seg.head = cut[i] % heads;
-    const int64_t sa = (int64_t)prefix[seg.seq] * heads + (int64_t)seg.head * seg.n_tiles, sb = sa + seg.n_tiles;
-    const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
-    if (tid == 0) {
-      const unsigned before = atom_add_acq_rel(p.tickets + cut[i], 1u);
-      last_flags[i] = before == (unsigned)(to - from);
-      if (last_flags[i]) atomicExch(p.tickets + cut[i], 0u);  // as the next call has to find it
+  // ---- segments that other blocks have parts of, the first and the last group at most: the last block to arrive merges
+  if (lane == 0 && warp < 2) {
+    cut[warp] = -1;
+    if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
+      const int id = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
+      segment(id, seg, sa, sb);
+      if (sa < c0 || sb > c1) {
+        const unsigned others = (unsigned)((sb - 1) / quota - sa / quota);
+        if (atom_add_acq_rel(p.tickets + id, 1u) == others) {
+          atomicExch(p.tickets + id, 0u);  // as the next call has to find it
+          cut[warp] = id;
+        }
+      }
     }
-    __syncthreads();
-    if (!last_flags[i]) continue;
+  }
+  __syncthreads();
+  for (int u = warp; u < 2 * COLS; u += W) {
+    const int id = cut[u / COLS], col = u % COLS;
+    if (id < 0) continue;
+    segment(id, seg, sa, sb);
+    if (col >= seg.count * p.group) continue;
+    const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
     const auto block_part = [&](int k) {
       const int64_t b = from + k;
       return static_cast<const float *>(p.partials + ((size_t)b * (W + 2) + W + (sa < b * quota ? 0 : 1)) * F::PARTIAL);
     };
-    for (int col = warp; col < seg.count * p.group; col += W) {
-      float v[HD / 32], top_c, sum_c;
-      merge_column<HD, COLS>(to - from + 1, col, lane, block_part, v, top_c, sum_c);
-      store_row<HD>(p, seg, col, lane, v, top_c, sum_c);
-    }
+    float v[1][HD / 32], top1[1], sum1[1];
+    merge_columns<HD, COLS, 1>(to - from + 1, col, lane, block_part, v, top1, sum1);
+    store_row<HD>(p, seg, col, lane, v[0], top1[0], sum1[0]);
   }
 }
 
