@@ -43,7 +43,7 @@ struct Few {
   static constexpr int SLOTS = HD == 128 ? 2 : 3;
   static constexpr int PARTIAL = COLS * HD + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
   static constexpr int RING_BYTES = WARPS * SLOTS * TILE_BYTES;
-  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (6 * WARPS + 4) * 4;
+  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (6 * WARPS + 8) * 4;
   static_assert(PARTIAL * 4 <= TILE_BYTES, "a slot holds a warp's partial result");
   static_assert(SMEM <= 232448, "shared memory of a block");
 };
@@ -54,6 +54,14 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same from a start value of its own.
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1, const float (&c)[4]) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t r;
@@ -158,7 +166,8 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
 }
 
 // NC columns from `col` on of several partial results, `n` of them at at(i), in order: merged by one warp.  Lanes take the
-// parts' maxima and sums, 32 at a time; then every lane its channels of all parts, 16 loads together.
+// parts' maxima and sums, 32 at a time; every lane takes its channels of all parts, 16 loads together, the first of them
+// under way with the maxima.
 template <int HD, int COLS, int NC, class At>
 __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At &at, float (&v)[NC][HD / 32], float (&top)[NC],
                                               float (&sum)[NC]) {
@@ -170,45 +179,52 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
 #pragma unroll
     for (int j = 0; j < C; ++j) v[c][j] = 0.f;
   }
-  for (int i = lane; i < n; i += 32) {
-    const float *part = at(i) + COLS * HD + col;
+  Vec x[AHEAD][NC];
+  const auto load = [&](int i) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) top[c] = fmaxf(top[c], part[c]);
+    for (int k = 0; k < AHEAD; ++k) {
+      const float *part = at(min(i + k, n - 1)) + col * HD + lane * C;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * HD);
+    }
+  };
+  load(0);
+  float m[NC], l[NC];  // of part `lane`
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m[c] = -INFINITY, l[c] = 0.f;
+    if (lane < n) m[c] = at(lane)[COLS * HD + col + c], l[c] = at(lane)[COLS * HD + COLS + col + c];
+    top[c] = m[c];
   }
+  for (int i = lane + 32; i < n; i += 32)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) top[c] = fmaxf(top[c], at(i)[COLS * HD + col + c]);
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], off));
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const int here = min(32, n - i0);
-    float w[NC] = {};
-    if (lane < here) {
-      const float *part = at(i0 + lane) + COLS * HD + col;
+#pragma unroll 1
+  for (int i = 0; i < n; i += AHEAD) {
+    if ((i & 31) == 0) {  // the next 32 parts' weights
+      if (i > 0 && i + lane < n)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) m[c] = at(i + lane)[COLS * HD + col + c], l[c] = at(i + lane)[COLS * HD + COLS + col + c];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        w[c] = ex2(part[c] - (top[c] == -INFINITY ? 0.f : top[c]));
-        sum[c] = fmaf(part[COLS + c], w[c], sum[c]);
+        m[c] = i + lane < n ? ex2(m[c] - (top[c] == -INFINITY ? 0.f : top[c])) : 0.f;
+        if (i + lane < n) sum[c] = fmaf(l[c], m[c], sum[c]);
       }
     }
-#pragma unroll 1
-    for (int i = 0; i < here; i += AHEAD) {
-      Vec x[AHEAD][NC];
+    if (i > 0) load(i);
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const float *part = at(i0 + min(i + k, here - 1)) + col * HD + lane * C;
+    for (int k = 0; k < AHEAD; ++k) {
+      if (i + k >= n) break;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * HD);
-      }
+      for (int c = 0; c < NC; ++c) {
+        const float wi = __shfl_sync(0xffffffffu, m[c], (i + k) & 31);
+        const float *y = reinterpret_cast<const float *>(&x[k][c]);
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        if (i + k >= here) break;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const float wi = __shfl_sync(0xffffffffu, w[c], i + k);
-          const float *y = reinterpret_cast<const float *>(&x[k][c]);
-#pragma unroll
-          for (int j = 0; j < C; ++j) v[c][j] = fmaf(y[j], wi, v[c][j]);
-        }
+        for (int j = 0; j < C; ++j) v[c][j] = fmaf(y[j], wi, v[c][j]);
       }
     }
   }
@@ -229,7 +245,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   int *part_seg = reinterpret_cast<int *>(bars + W * F::SLOTS);  // [2 W]: segment of each partial result, or -1
   int *part_place = part_seg + 2 * W;
   int *group_at = part_place + 2 * W, *n_groups = group_at + 2 * W + 1;
-  volatile int *cut = n_groups + 1;
+  volatile int *cut = n_groups + 1, *span = cut + 2;  // of the segments that this block merges: blocks
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
   pdl_launch_dependents();
@@ -291,16 +307,18 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   // ---- copies: a page of 64 tokens is a tile as it stands; of others a page's part of the tile comes in four (codes and
   // parameters of K and V), a lane each
   Cursor fetch;
-  int fetch_page = -1;
-  bool fetch_ok = w0 < w1;
-  int64_t fetch_at = w0;
+  int fetch_page = -2, fetch_left = (int)(w1 - w0);  // tiles to bring (a page of -2: behind the sequence's end)
   unsigned fetch_slot = 0;
-  if (fetch_ok) locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
+  const int lane_key = lane >> 2 << lb;              // of this lane's copy, in the tile
+  const bool copies = lane < (lp == 6 ? 1 : 4 * TILE >> lb);
+  const int32_t *fetch_row = nullptr;
+  if (fetch_left > 0) {
+    locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
+    fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
+  }
   const auto load_page = [&]() {  // the page of this lane's copy for the tile at `fetch`
-    fetch_page = -2;              // none: behind the sequence's end
-    const int key = (fetch.first_tile + fetch.tile) * TILE + (lane >> 2 << lb);
-    if (lane < (lp == 6 ? 1 : 4 * TILE >> lb) && key < fetch.length)
-      fetch_page = p.map.table[(int64_t)fetch.user * p.map.max_pages + (key >> lp)];
+    const int key = (fetch.first_tile + fetch.tile) * TILE + lane_key;
+    fetch_page = copies && key < fetch.length ? fetch_row[key >> lp] : -2;
   };
   unsigned valid[F::SLOTS] = {};  // which 16 keys of a slot's tile are there, a bit each
   bool dead = false;              // a wait gave up: no more copies, no results
@@ -334,19 +352,19 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     for (int i = 0; i < F::SLOTS; ++i)
       if (i == (int)fetch_slot) valid[i] = have;
     fetch_slot = fetch_slot + 1 == F::SLOTS ? 0 : fetch_slot + 1;
-    if (++fetch_at < w1) {
+    if (--fetch_left > 0) {
+      const int seq = fetch.seq;
       next_tile(fetch, p.n_seqs, heads, info, prefix, p.window);
+      if (fetch.seq != seq) fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
       load_page();
-    } else {
-      fetch_ok = false;
     }
   };
   Cursor at = fetch;
-  if (fetch_ok) load_page();
+  if (fetch_left > 0) load_page();
 
   // ---- this warp's tiles
   uint32_t q[NT][G][2][2][2];     // B fragments: [group][word of a lane][half of its pairs][register]
-  float seed[NT][G][2], qs[NT][G][2], cf[NT][2];
+  float seed[NT][G][4], qs[NT][G][2], cf[NT][2];
   float o[NT][G][4][4], ones[NT][G][4], top[NT][2], sum[NT][2], centre[NT][G][2];
   float v_unit = 0.f;             // the value scales' reference, a power of two
   unsigned slot = 0, phase = 0;
@@ -380,7 +398,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             }
           }
         }
-      if (flat == w0 && fetch_ok) issue();
+      if (flat == w0) issue();
       rows = at.count * p.group;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -417,7 +435,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             qs[n][g][c] = fmaf(16.f, odd[c], even[c]);
-            seed[n][g][c] = fmaf(-1152.f, odd[c], -8.f * even[c]);
+            seed[n][g][c] = seed[n][g][c + 2] = fmaf(-1152.f, odd[c], -8.f * even[c]);
             centre[n][g][c] = 0.f;
           }
         }
@@ -442,12 +460,12 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       if (flat == w0)
 #pragma unroll
         for (int i = 1; i < F::SLOTS; ++i)
-          if (fetch_ok) issue();
+          if (fetch_left > 0) issue();
     }
 
     // ---- one tile
     if (!dead && !wait_2s(bar0 + slot * 8, phase)) {
-      dead = true, fetch_ok = false;
+      dead = true, fetch_left = 0;
       if (lane == 0) report(p.status, KFL_TIMED_OUT);
       for (int i = 0; i < F::SLOTS; ++i) wait_2s(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
     }
@@ -493,18 +511,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           }
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[n][st][i] = 0.f;
-        }
-#pragma unroll
         for (int g = 0; g < G; ++g) {
           float acc[NT][4];
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            acc[n][0] = acc[n][2] = seed[n][g][0];
-            acc[n][1] = acc[n][3] = seed[n][g][1];
-          }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint32_t lo = j ? kw[0][g].y : kw[0][g].x, hi = j ? kw[1][g].y : kw[1][g].x;
@@ -513,18 +521,20 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             code_pairs(lo >> 8, a4, a6), code_pairs(hi >> 8, a5, a7);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
+              if (j == 0)
+                mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1], seed[n][g]);
+              else
+                mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
               mma16816(acc[n], a4, a5, a6, a7, q[n][g][j][1][0], q[n][g][j][1][1]);
             }
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-              const float s = ks[i >> 1][g], c = kc[i >> 1][g];
-              const float2 t = fma2({c, c}, {qs[n][g][0], qs[n][g][1]}, {x[n][st][i], x[n][st][i + 1]});
-              const float2 r = fma2({s, s}, {acc[n][i], acc[n][i + 1]}, t);
-              x[n][st][i] = r.x, x[n][st][i + 1] = r.y;
+            for (int i = 0; i < 4; ++i) {
+              const float t = kc[i >> 1][g] * qs[n][g][i & 1];
+              x[n][st][i] = g == 0 ? fmaf(ks[i >> 1][g], acc[n][i], t)
+                                  : fmaf(ks[i >> 1][g], acc[n][i], fmaf(kc[i >> 1][g], qs[n][g][i & 1], x[n][st][i]));
             }
         }
       }
@@ -638,8 +648,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
                 if (hidden[n] >> (4 * st + i) & 1) s0 = d0 = 0.f;
                 if (hidden[n] >> (4 * st + i + 1) & 1) s1 = d1 = 0.f;
               }
-              const float2 t = fma2({pr[i], pr[i + 1]}, {d0, d1}, {centre[n][g][0], centre[n][g][1]});
-              centre[n][g][0] = t.x, centre[n][g][1] = t.y;
+              centre[n][g][0] = fmaf(pr[i], d0, centre[n][g][0]);
+              centre[n][g][1] = fmaf(pr[i + 1], d1, centre[n][g][1]);
               w[i] = pr[i] * s0, w[i + 1] = pr[i + 1] * s1;
             }
             pf[n][g][0] = transpose8x8(pack_half2(w[0], w[1]));
@@ -674,7 +684,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       }
     }
     __syncwarp();  // (every lane has read the slot)
-    if (fetch_ok) issue();
+    if (fetch_left > 0) issue();
     if (++slot == F::SLOTS) slot = 0, phase ^= 1;
 
     // ---- the end of a (sequence, head), or of this warp's piece of it
@@ -806,32 +816,31 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   __syncthreads();
   // ---- segments that other blocks have parts of, the first and the last group at most: the last block to arrive merges
   if (lane == 0 && warp < 2) {
-    cut[warp] = -1;
+    int id = -1;
     if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
-      const int id = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
-      segment(id, seg, sa, sb);
+      const int mine = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
+      segment(mine, seg, sa, sb);
       if (sa < c0 || sb > c1) {
-        const unsigned others = (unsigned)((sb - 1) / quota - sa / quota);
-        if (atom_add_acq_rel(p.tickets + id, 1u) == others) {
-          atomicExch(p.tickets + id, 0u);  // as the next call has to find it
-          cut[warp] = id;
+        const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
+        if (atom_add_acq_rel(p.tickets + mine, 1u) == (unsigned)(to - from)) {
+          atomicExch(p.tickets + mine, 0u);  // as the next call has to find it
+          id = mine, span[2 * warp] = from, span[2 * warp + 1] = to - from + 1;
         }
       }
     }
+    cut[warp] = id;
   }
   __syncthreads();
   for (int u = warp; u < 2 * COLS; u += W) {
-    const int id = cut[u / COLS], col = u % COLS;
+    const int which = u / COLS, id = cut[which], col = u % COLS;
     if (id < 0) continue;
     segment(id, seg, sa, sb);
     if (col >= seg.count * p.group) continue;
-    const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
-    const auto block_part = [&](int k) {
-      const int64_t b = from + k;
-      return static_cast<const float *>(p.partials + ((size_t)b * (W + 2) + W + (sa < b * quota ? 0 : 1)) * F::PARTIAL);
-    };
+    // (the block where the segment begins has it as its last part, the others as their first)
+    const float *first = p.partials + ((size_t)span[2 * which] * (W + 2) + W) * F::PARTIAL;
+    const auto block_part = [&](int k) { return first + (size_t)(k * (W + 2) + (k == 0)) * F::PARTIAL; };
     float v[1][HD / 32], top1[1], sum1[1];
-    merge_columns<HD, COLS, 1>(to - from + 1, col, lane, block_part, v, top1, sum1);
+    merge_columns<HD, COLS, 1>(span[2 * which + 1], col, lane, block_part, v, top1, sum1);
     store_row<HD>(p, seg, col, lane, v[0], top1[0], sum1[0]);
   }
 }
