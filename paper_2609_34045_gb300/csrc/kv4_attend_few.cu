@@ -31,6 +31,7 @@ namespace kfl {
 namespace {
 
 constexpr int TILE = 64;  // keys
+constexpr int SUB = 2;    // groups of 16 keys that are worked on at once
 
 template <int HD, int NT>
 struct Few {
@@ -470,24 +471,27 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       for (int i = 0; i < F::SLOTS; ++i) wait_2s(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
     }
     dead = __any_sync(0xffffffffu, dead);
-    if (!dead) {
-      const uint32_t base = ring + slot * F::TILE_BYTES;
-      const int key0 = (at.first_tile + at.tile) * TILE;
-      unsigned have = 0;
+    unsigned have = 0;
 #pragma unroll
-      for (int i = 0; i < F::SLOTS; ++i)
-        if (i == (int)slot) have = valid[i];
+    for (int i = 0; i < F::SLOTS; ++i)
+      if (i == (int)slot) have = valid[i];
+    // in steps of 16 SUB keys: the tile at once is more code than the instruction cache next to the scheduler holds
+#pragma unroll 1
+    for (int s0 = 0; s0 < 4 && !dead; s0 += SUB, have >>= SUB) {
+      const uint32_t base = ring + slot * F::TILE_BYTES + 16 * s0 * (HD / 2);
+      const uint32_t base_p = ring + slot * F::TILE_BYTES + 2 * CODES + 16 * s0 * (G * 4);
+      const int key0 = (at.first_tile + at.tile) * TILE + 16 * s0;
       // some rows do not see all of the tile: its last keys, a window's first ones, a missing page
       const int all_end = at.length - at.count + 1;
-      const bool masked = key0 + TILE > all_end || have != 0xf ||
+      const bool masked = key0 + 16 * SUB > all_end || (have & ((1 << SUB) - 1)) != (1 << SUB) - 1 ||
                           (p.window > 0 && key0 < at.length - p.window);
-      float x[NT][4][4];
-      uint32_t vpar[4][2][G];  // (scale, centre) of the lane's two keys of each subtile, as they are stored
+      float x[NT][SUB][4];
+      uint32_t vpar[SUB][2][G];  // (scale, centre) of the lane's two keys of each subtile, as they are stored
       const int key_lane = (gid >> 1) + 4 * (gid & 1);  // matrix row gid is this key of a subtile, row gid + 8 key_lane + 8
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
+      for (int st = 0; st < SUB; ++st) {
         const uint32_t kb = base + 16 * st * (HD / 2);
-        const uint32_t kp = base + 2 * CODES + 16 * st * (G * 4), vp = kp + PARAMS;
+        const uint32_t kp = base_p + 16 * st * (G * 4), vp = kp + PARAMS;
         uint2 kw[2][G];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -543,7 +547,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int st = 0; st < 4; ++st)
+          for (int st = 0; st < SUB; ++st)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * st + key_lane + 8 * (i >> 1);
@@ -553,7 +557,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             }
         // parameters that no row sees may be anything
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
+        for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       // ---- running maximum, and a common unit of the value scales (their weights are fp16)
       __half2 v_most = __float2half2_rn(0.f);  // (hmax2 passes over NaN)
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < SUB; ++st)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -579,7 +583,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         for (int c = 0; c < 2; ++c) {
           float m = fmaxf(x[n][0][c], x[n][0][c + 2]);
 #pragma unroll
-          for (int st = 1; st < 4; ++st) m = fmaxf(m, fmaxf(x[n][st][c], x[n][st][c + 2]));
+          for (int st = 1; st < SUB; ++st) m = fmaxf(m, fmaxf(x[n][st][c], x[n][st][c + 2]));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
           now[n][c] = fmaxf(m, top[n][c]);
@@ -625,7 +629,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
         for (int c = 0; c < 2; ++c) ref[n][c] = top[n][c] == -INFINITY ? 0.f : -top[n][c] * cf[n][c];
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
+      for (int st = 0; st < SUB; ++st) {
         const uint32_t vb = base + CODES + (16 * st + tig) * (HD / 2) + gid * 4;
         uint32_t pf[NT][G][2];
 #pragma unroll
