@@ -791,61 +791,59 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   };
   Cursor seg;
   int64_t sa, sb;
-  for (int u = warp; u < n_groups[0] * (COLS / 4); u += W) {
-    const int k = u / (COLS / 4), col = u % (COLS / 4) * 4;
-    segment(part_seg[k], seg, sa, sb);
-    const int rows_here = seg.count * p.group;
-    if (col >= rows_here) continue;
-    const int e = group_at[k];
-    const auto nth = [&](int i) {
-      const int at = part_place[e + i];
-      return at & 1 ? reinterpret_cast<const float *>(smem + (size_t)(at >> 1) * F::SLOTS * F::TILE_BYTES)
-                    : block_ws + (at >> 1) * F::PARTIAL;
-    };
-    float v[4][HD / 32], top4[4], sum4[4];
-    merge_columns<HD, COLS, 4>(group_at[k + 1] - e, col, lane, nth, v, top4, sum4);
-    const bool whole = sa >= c0 && sb <= c1;
-    float *to = block_ws + (W + (sa < c0 ? 0 : 1)) * F::PARTIAL;
+  constexpr int NC = 2;  // columns of a warp at a time
+  // first the block's own partial results, then those that blocks have left to this one as the last to arrive: the same
+  // code, which costs more the first time than what it does
+#pragma unroll 1
+  for (int across = 0; across < 2; ++across) {
+    for (int u = warp; u < (across ? 2 : n_groups[0]) * (COLS / NC); u += W) {
+      const int k = u / (COLS / NC), col = u % (COLS / NC) * NC, id = across ? cut[k] : part_seg[k];
+      if (id < 0) continue;
+      segment(id, seg, sa, sb);
+      const int rows_here = seg.count * p.group;
+      if (col >= rows_here) continue;
+      const int first = across ? span[2 * k] : group_at[k], n = across ? span[2 * k + 1] : group_at[k + 1] - first;
+      const auto nth = [&](int i) {
+        // (of a segment that is cut, the block where it begins has it as its last part, the others as their first)
+        if (across) return static_cast<const float *>(p.partials + ((size_t)(first + i) * (W + 2) + W + (i == 0)) * F::PARTIAL);
+        const int at = part_place[first + i];
+        return at & 1 ? reinterpret_cast<const float *>(smem + (size_t)(at >> 1) * F::SLOTS * F::TILE_BYTES)
+                      : static_cast<const float *>(block_ws + (at >> 1) * F::PARTIAL);
+      };
+      float v[NC][HD / 32], tops[NC], sums[NC];
+      merge_columns<HD, COLS, NC>(n, col, lane, nth, v, tops, sums);
+      const bool whole = across || (sa >= c0 && sb <= c1);
+      float *to = block_ws + (W + (sa < c0 ? 0 : 1)) * F::PARTIAL;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (whole) {
-        if (col + c < rows_here) store_row<HD>(p, seg, col + c, lane, v[c], top4[c], sum4[c]);
-      } else {
+      for (int c = 0; c < NC; ++c) {
+        if (whole) {
+          if (col + c < rows_here) store_row<HD>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) to[(col + c) * HD + lane * (HD / 32) + j] = v[c][j];
-        if (lane == 0) to[COLS * HD + col + c] = top4[c], to[COLS * HD + COLS + col + c] = sum4[c];
-      }
-    }
-  }
-  __syncthreads();
-  // ---- segments that other blocks have parts of, the first and the last group at most: the last block to arrive merges
-  if (lane == 0 && warp < 2) {
-    int id = -1;
-    if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
-      const int mine = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
-      segment(mine, seg, sa, sb);
-      if (sa < c0 || sb > c1) {
-        const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
-        if (atom_add_acq_rel(p.tickets + mine, 1u) == (unsigned)(to - from)) {
-          atomicExch(p.tickets + mine, 0u);  // as the next call has to find it
-          id = mine, span[2 * warp] = from, span[2 * warp + 1] = to - from + 1;
+          for (int j = 0; j < HD / 32; ++j) to[(col + c) * HD + lane * (HD / 32) + j] = v[c][j];
+          if (lane == 0) to[COLS * HD + col + c] = tops[c], to[COLS * HD + COLS + col + c] = sums[c];
         }
       }
     }
-    cut[warp] = id;
-  }
-  __syncthreads();
-  for (int u = warp; u < 2 * COLS; u += W) {
-    const int which = u / COLS, id = cut[which], col = u % COLS;
-    if (id < 0) continue;
-    segment(id, seg, sa, sb);
-    if (col >= seg.count * p.group) continue;
-    // (the block where the segment begins has it as its last part, the others as their first)
-    const float *first = p.partials + ((size_t)span[2 * which] * (W + 2) + W) * F::PARTIAL;
-    const auto block_part = [&](int k) { return first + (size_t)(k * (W + 2) + (k == 0)) * F::PARTIAL; };
-    float v[1][HD / 32], top1[1], sum1[1];
-    merge_columns<HD, COLS, 1>(span[2 * which + 1], col, lane, block_part, v, top1, sum1);
-    store_row<HD>(p, seg, col, lane, v[0], top1[0], sum1[0]);
+    if (across) break;
+    __syncthreads();
+    // ---- segments that other blocks have parts of: the first and the last group at most
+    if (lane == 0 && warp < 2) {
+      int id = -1;
+      if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
+        const int mine = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
+        segment(mine, seg, sa, sb);
+        if (sa < c0 || sb > c1) {
+          const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
+          if (atom_add_acq_rel(p.tickets + mine, 1u) == (unsigned)(to - from)) {
+            atomicExch(p.tickets + mine, 0u);  // as the next call has to find it
+            id = mine, span[2 * warp] = from, span[2 * warp + 1] = to - from + 1;
+          }
+        }
+      }
+      cut[warp] = id;
+    }
+    __syncthreads();
   }
 }
 
