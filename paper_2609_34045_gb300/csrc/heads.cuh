@@ -57,8 +57,9 @@ inline bool rows_aligned16(const kfl_heads &h) {
   const HeadsView v = view_of(h);
   return ((reinterpret_cast<uintptr_t>(h.data) | (uintptr_t)v.token_bytes | (uintptr_t)v.head_bytes) & 15) == 0;
 }
-inline bool heads_valid(const kfl_heads *h) {
-  return h && h->data && h->n_heads >= 1 && h->n_heads <= (1 << 16) && h->dtype >= KFL_DT_BF16 &&
+// (a call without tokens may come without data)
+inline bool heads_valid(const kfl_heads *h, int n_tokens) {
+  return h && (h->data || n_tokens == 0) && h->n_heads >= 1 && h->n_heads <= (1 << 16) && h->dtype >= KFL_DT_BF16 &&
          h->dtype <= KFL_DT_FP32 && reinterpret_cast<uintptr_t>(h->data) % dtype_size(h->dtype) == 0;
 }
 inline bool rope_valid(const kfl_rope_plan *r) {

@@ -232,7 +232,7 @@ int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv
   if (rc == KFL_OK) rc = check_map(map, me);
   if (rc == KFL_OK) rc = check_layer(pool, layer, me);
   if (rc != KFL_OK) return rc;
-  if (!heads_valid(k) || !heads_valid(v)) return bad_arg(me, "k and v are needed");
+  if (!heads_valid(k, n_tokens) || !heads_valid(v, n_tokens)) return bad_arg(me, "k and v are needed");
   if (k->n_heads != pool->n_kv_heads || v->n_heads != pool->n_kv_heads || k->dtype != v->dtype)
     return bad_arg(me, "k and v have the pool's heads and one type");
   if (rope && (!rope_valid(rope) || rope->rope_dim > pool->head_dim)) return bad_arg(me, "not a rotation of these heads");

@@ -48,7 +48,7 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
                               int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace,
                               size_t workspace_bytes, int32_t *status, void *cuda_stream) {
   const char *me = "kfl_kv4_attend";
-  if (!heads_valid(q) || !heads_valid(out)) return bad_arg(me, "q and out are needed");
+  if (!heads_valid(q, n_tokens) || !heads_valid(out, n_tokens)) return bad_arg(me, "q and out are needed");
   int rc = check_attend(me, pool, q->n_heads, n_seqs, n_tokens, max_q, true);
   if (rc == KFL_OK) rc = check_map(map, me);
   if (rc == KFL_OK) rc = check_layer(pool, layer, me);

@@ -203,8 +203,8 @@ extern "C" int kfl_rope(const kfl_rope_plan *plan, const kfl_heads *q, const kfl
   using namespace kfl;
   const char *me = "kfl_rope";
   if (!rope_valid(plan)) return bad_arg(me, "not a rotation (16-byte aligned table, even rope_dim of 2..512, layout)");
-  if (!heads_valid(q) || !heads_valid(q_out)) return bad_arg(me, "q and q_out are needed");
-  if (!k != !k_out || (k && (!heads_valid(k) || !heads_valid(k_out)))) return bad_arg(me, "k and k_out go together");
+  if (!heads_valid(q, n_tokens) || !heads_valid(q_out, n_tokens)) return bad_arg(me, "q and q_out are needed");
+  if (!k != !k_out || (k && (!heads_valid(k, n_tokens) || !heads_valid(k_out, n_tokens)))) return bad_arg(me, "k and k_out go together");
   if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype) return bad_arg(me, "q and q_out differ");
   if (k && (k->n_heads != k_out->n_heads || k->dtype != k_out->dtype || k->dtype != q->dtype))
     return bad_arg(me, "k and k_out differ, or k has another type than q");
