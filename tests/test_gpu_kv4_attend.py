@@ -1,6 +1,7 @@
 """Attention over the 4-bit paged cache against the 64-bit oracle.
 
-Tolerances.  An output's own rounding is at most 2^-9 (bf16) or 2^-11 (fp16) of it.  Beside it every term p v is off by the
+Tolerances.  An output's own rounding is at most 2^-8 (bf16; half of it is allowed for, the rest falls to the slack of the next
+term) or 2^-11 (fp16) of it.  Beside it every term p v is off by the
 rounding of its weight to fp16 (2^-12 at most, as with v in prompts) and by the error of its score: in the few-row kernel
 fp32 sums of exact codes, below 1e-4; in prompts the rounding of k to fp16, 2^-12 of each of head_dim random terms, below
 2^-9 at six deviations for the scores of these cases (|scale q k| of a few).  Together: at most 2^-8 of the weighted mean
