@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 
 import torch
 
@@ -25,6 +26,11 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 class kfl_heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
                 ("n_heads", C.c_int), ("dtype", C.c_int)]
+
+
+# the same as packed bytes, in a third of a ctypes structure's time: a decode step's kernel is over in less than its
+# arguments take
+_pack_heads = struct.Struct("@Pqqii").pack
 
 
 class kfl_rope_cfg(C.Structure):
@@ -55,7 +61,7 @@ def lib() -> C.CDLL:
     L = stage.lib()
     if _signed is not L:
         vp, i, f, P = C.c_void_p, C.c_int, C.c_float, C.POINTER
-        heads, plan, pl, mp, sz = P(kfl_heads), P(kfl_rope_plan), P(kfl_kv4_pool), P(kfl_kv4_map), P(C.c_size_t)
+        heads, plan, pl, mp, sz = vp, P(kfl_rope_plan), P(kfl_kv4_pool), P(kfl_kv4_map), P(C.c_size_t)
         for name, args in {
             "kfl_rope_table": [P(kfl_rope_cfg), i, vp, vp],
             "kfl_rope": [plan, heads, heads, heads, heads, vp, i, i, i, vp, vp],
@@ -99,13 +105,16 @@ def _int32(t, where, n=None):
 def _heads(t, where, head_dim=None):
     if t is None:
         return None
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 3 or (strides[2] != 1 and shape[2] != 1) or (head_dim is not None and shape[2] != head_dim):
-        raise ValueError(f"{where} is [token][head][head_dim] with contiguous channels")
+    if t.dim() != 3:
+        raise ValueError(f"{where} is [token][head][head_dim]")
+    _, n_heads, hd = t.shape
+    per_token, per_head, one = t.stride()
+    if (one != 1 and hd != 1) or (head_dim is not None and hd != head_dim):
+        raise ValueError(f"{where} has contiguous channels, as many as the others")
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{where} is bf16, fp16 or fp32")
-    return kfl_heads(t.data_ptr(), strides[0], strides[1], shape[1], dtype)
+    return _pack_heads(t.data_ptr(), per_token, per_head, n_heads, dtype)
 
 
 # ---- rotary positions ----------------------------------------------------------------------------
@@ -139,7 +148,7 @@ def kfl_rope(plan: kfl_rope_plan, q, q_out, k, k_out, positions, inverse: bool =
     for x, name in ((q_out, "q_out"), (k, "k"), (k_out, "k_out")):
         if x is not None and x.shape[0] != n:
             raise ValueError(f"{name} has as many tokens as q")
-    _check(lib().kfl_rope(C.byref(plan), C.byref(a), C.byref(b), c and C.byref(c), d and C.byref(d),
+    _check(lib().kfl_rope(C.byref(plan), a, b, c, d,
                           _int32(positions, "positions", n), n, hd, int(inverse), _int32(status, "status", 1),
                           cuda_stream), "kfl_rope")
 
@@ -186,7 +195,7 @@ def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=N
     if v.shape[0] != n:
         raise ValueError("k and v have the same tokens")
     a, b = _heads(k, "k", p.head_dim), _heads(v, "v", p.head_dim)
-    _check(lib().kfl_kv4_append(C.byref(p), C.byref(m), layer, C.byref(a), C.byref(b), _int32(users, "users", n),
+    _check(lib().kfl_kv4_append(C.byref(p), C.byref(m), layer, a, b, _int32(users, "users", n),
                                 _int32(positions, "positions", n), n, rope and C.byref(rope),
                                 _int32(status, "status", 1), cuda_stream), "kfl_kv4_append")
 
@@ -198,7 +207,7 @@ def kfl_kv4_read(p, m, layer: int, users, positions, k_out, v_out, status=None, 
         raise ValueError("k_out and v_out have the same tokens")
     a, b = _heads(k_out, "k_out", p.head_dim), _heads(v_out, "v_out", p.head_dim)
     _check(lib().kfl_kv4_read(C.byref(p), C.byref(m), layer, _int32(users, "users", n),
-                              _int32(positions, "positions", n), n, C.byref(a), C.byref(b),
+                              _int32(positions, "positions", n), n, a, b,
                               _int32(status, "status", 1), cuda_stream), "kfl_kv4_read")
 
 
@@ -234,7 +243,7 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
         raise ValueError("lse is a contiguous fp32 [token][query head]")
     a, b = _heads(q, "q", p.head_dim), _heads(out, "out", p.head_dim)
-    _check(lib().kfl_kv4_attend(C.byref(p), C.byref(m), layer, C.byref(a), C.byref(b), _at(lse),
+    _check(lib().kfl_kv4_attend(C.byref(p), C.byref(m), layer, a, b, _at(lse),
                                 _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
                                 1.0 / math.sqrt(hd) if scale is None else scale, window, workspace.data_ptr(),
                                 workspace.numel(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
