@@ -24,45 +24,52 @@ struct RowsParams {
   int32_t *status;
 };
 
-// The page and slot of row t, or a page of -1 (reported once per row).
-__device__ __forceinline__ int locate(const RowsParams &p, int64_t t, int pos, bool reports, int &slot) {
-  const int user = p.users ? p.users[t] : (int)t;
-  int bad = 0, page = -1;
-  if (user < 0 || user >= p.map.n_users) {
+// Where row t goes: its place in the table (NULL: out of range, reported once per row), its slot in the page.
+__device__ __forceinline__ const int32_t *place(const RowsParams &p, int user, int pos, bool reports, int &slot) {
+  int bad = 0;
+  if (user < 0 || user >= p.map.n_users)
     bad = KFL_BAD_USER;
-  } else if (pos < 0 || (pos >> p.pool.log2_tokens) >= p.map.max_pages || (p.cos_sin && pos >= p.n_pos)) {
+  else if (pos < 0 || (pos >> p.pool.log2_tokens) >= p.map.max_pages || (p.cos_sin && pos >= p.n_pos))
     bad = KFL_BAD_POSITION;
-  } else {
-    page = p.map.table[(int64_t)user * p.map.max_pages + (pos >> p.pool.log2_tokens)];
-    if (page < 0 || page >= p.pool.n_pages) bad = page == -1 ? KFL_BAD_POSITION : KFL_BAD_PAGE, page = -1;
-  }
   if (bad && reports) report(p.status, bad);
   slot = pos & (p.pool.page_tokens() - 1);
-  return page;
+  return bad ? nullptr : p.map.table + (int64_t)user * p.map.max_pages + (pos >> p.pool.log2_tokens);
+}
+__device__ __forceinline__ bool page_ok(const RowsParams &p, int page, bool reports) {
+  if (page >= 0 && page < p.pool.n_pages) return true;
+  if (reports) report(p.status, page == -1 ? KFL_BAD_POSITION : KFL_BAD_PAGE);
+  return false;
 }
 
+// Eight channels as they lie in memory.
+template <class T>
+struct alignas(16) Raw8 {
+  T e[8];
+};
 template <class T, bool WIDE>
-__device__ __forceinline__ void load8(const T *p, float (&x)[8]) {
+__device__ __forceinline__ Raw8<T> load_raw(const T *p) {
+  Raw8<T> r;
   if constexpr (WIDE) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 8; i += W) {
-      const Pack<T, W> w = *reinterpret_cast<const Pack<T, W> *>(p + i);
-#pragma unroll
-      for (int j = 0; j < W; ++j) x[i + j] = to_f32(w.e[j]);
-    }
+    for (int i = 0; i < 8; i += W) *reinterpret_cast<Pack<T, W> *>(r.e + i) = *reinterpret_cast<const Pack<T, W> *>(p + i);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f32(p[i]);
+    for (int i = 0; i < 8; ++i) r.e[i] = p[i];
   }
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = to_f32(r.e[i]);
 }
 
-// Channels [c, c + 8) of a k row, rotated.
+// x, channels [c, c + 8) of a k row, rotated.
 template <class T, bool WIDE>
-__device__ __forceinline__ void load8_rotated(const RowsParams &p, const T *row, int c, int pos, float (&x)[8]) {
-  load8<T, WIDE>(row + c, x);
+__device__ __forceinline__ void rotate8(const RowsParams &p, const T *row, int c, int pos, float (&x)[8]) {
   const int half = p.rope_half;
-  if (!p.cos_sin || c >= 2 * half) return;
+  if (c >= 2 * half) return;
   const float2 *cs = p.cos_sin + (int64_t)pos * half;
   if (p.rope_layout == KFL_ROPE_INTERLEAVED) {
 #pragma unroll
@@ -75,7 +82,7 @@ __device__ __forceinline__ void load8_rotated(const RowsParams &p, const T *row,
   } else if (half % 8 == 0) {  // the eight channels have their partners in eight others
     float y[8];
     const bool second = c >= half;
-    load8<T, WIDE>(row + (second ? c - half : c + half), y);
+    unpack8(load_raw<T, WIDE>(row + (second ? c - half : c + half)), y);
     const float4 *f4 = reinterpret_cast<const float4 *>(cs + (second ? c - half : c));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -129,40 +136,59 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], int lane, uin
   return w;
 }
 
-template <class T, bool WIDE>
+// U rows a thread, in flight together.
+template <class T, bool WIDE, int U>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_append_kernel(const RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int lanes = p.pool.head_dim / 8;  // threads of a row
-  const int64_t unit = (int64_t)blockIdx.x * (ROW_THREADS / lanes) + threadIdx.x / lanes;
+  const int lanes = p.pool.head_dim / 8, rows = ROW_THREADS / lanes;  // threads of a row, rows of a block at a time
   const int64_t n_units = (int64_t)p.n_tokens * p.pool.n_kv_heads;
   const int c = threadIdx.x % lanes * 8;
-  // (a block's last threads repeat the last row without storing it: the shuffles take whole warps)
-  const int64_t u = min(unit, n_units - 1);
-  const int64_t t = u / p.pool.n_kv_heads;
-  const int head = (int)(u % p.pool.n_kv_heads);
-  const int pos = p.positions[t];
-  int slot;
-  const int page = locate(p, t, pos, head == 0 && c == 0 && unit < n_units, slot);
-  float x[8], y[8];
-  load8<T, WIDE>(reinterpret_cast<const T *>(p.v.row(t, head)) + c, y);
-  const T *k_row = reinterpret_cast<const T *>(p.k.row(t, head));
-  if (page >= 0)
-    load8_rotated<T, WIDE>(p, k_row, c, pos, x);
-  else
-    load8<T, WIDE>(k_row + c, x);
-  uint32_t kp, vp;
-  const uint32_t kw = quantise8(x, threadIdx.x & 31, kp);
-  const uint32_t vw = quantise8(y, threadIdx.x & 31, vp);
-  if (unit >= n_units || page < 0) return;
-  uint8_t *block = p.pool.block(page, p.layer, head);
-  const int row = slot * (p.pool.head_dim / 2) + c / 2;
-  *reinterpret_cast<uint32_t *>(block + row) = kw;
-  *reinterpret_cast<uint32_t *>(block + p.pool.code_bytes() + row) = vw;
-  if (c % KV4_GROUP == 0) {
-    uint8_t *params = block + 2 * p.pool.code_bytes() + (slot * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
-    *reinterpret_cast<uint32_t *>(params) = kp;
-    *reinterpret_cast<uint32_t *>(params + p.pool.param_bytes()) = vp;
+  Raw8<T> k_raw[U], v_raw[U];
+  int pos[U], user[U], head[U];
+  bool mine[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t unit = ((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes;
+    // (threads behind the last row repeat it without storing it: the shuffles take whole warps)
+    mine[j] = unit < n_units;
+    const int64_t u = min(unit, n_units - 1), t = u / p.pool.n_kv_heads;
+    head[j] = (int)(u - t * p.pool.n_kv_heads);
+    pos[j] = p.positions[t];
+    user[j] = p.users ? p.users[t] : (int)t;
+    v_raw[j] = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.v.row(t, head[j])) + c);
+    k_raw[j] = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.k.row(t, head[j])) + c);
+  }
+  int slot[U], page[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const bool reports = head[j] == 0 && c == 0 && mine[j];
+    const int32_t *at = place(p, user[j], pos[j], reports, slot[j]);
+    page[j] = at ? *at : -2;
+    if (at && !page_ok(p, page[j], reports)) page[j] = -2;
+    mine[j] = mine[j] && page[j] >= 0;
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t unit = min(((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes, n_units - 1);
+    const T *row = reinterpret_cast<const T *>(p.k.row(unit / p.pool.n_kv_heads, head[j]));
+    float x[8];
+    unpack8(k_raw[j], x);
+    if (p.cos_sin && mine[j]) rotate8<T, WIDE>(p, row, c, pos[j], x);
+    uint32_t kp, vp;
+    const uint32_t kw = quantise8(x, threadIdx.x & 31, kp);
+    unpack8(v_raw[j], x);
+    const uint32_t vw = quantise8(x, threadIdx.x & 31, vp);
+    if (!mine[j]) continue;
+    uint8_t *block = p.pool.block(page[j], p.layer, head[j]);
+    const int at = slot[j] * (p.pool.head_dim / 2) + c / 2;
+    *reinterpret_cast<uint32_t *>(block + at) = kw;
+    *reinterpret_cast<uint32_t *>(block + p.pool.code_bytes() + at) = vw;
+    if (c % KV4_GROUP == 0) {
+      uint8_t *params = block + 2 * p.pool.code_bytes() + (slot[j] * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
+      *reinterpret_cast<uint32_t *>(params) = kp;
+      *reinterpret_cast<uint32_t *>(params + p.pool.param_bytes()) = vp;
+    }
   }
 }
 
@@ -189,40 +215,70 @@ __device__ __forceinline__ void store_values(uint32_t w, uint32_t params, T *dst
   }
 }
 
-template <class T, bool WIDE>
+template <class T, bool WIDE, int U>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int lanes = p.pool.head_dim / 8;
-  const int64_t unit = (int64_t)blockIdx.x * (ROW_THREADS / lanes) + threadIdx.x / lanes;
-  if (unit >= (int64_t)p.n_tokens * p.pool.n_kv_heads) return;
+  const int lanes = p.pool.head_dim / 8, rows = ROW_THREADS / lanes;
+  const int64_t n_units = (int64_t)p.n_tokens * p.pool.n_kv_heads;
   const int c = threadIdx.x % lanes * 8;
-  const int64_t t = unit / p.pool.n_kv_heads;
-  const int head = (int)(unit % p.pool.n_kv_heads);
-  int slot;
-  const int page = locate(p, t, p.positions[t], head == 0 && c == 0, slot);
-  if (page < 0) return;
-  const uint8_t *block = p.pool.block(page, p.layer, head);
-  const int row = slot * (p.pool.head_dim / 2) + c / 2;
-  const uint8_t *params = block + 2 * p.pool.code_bytes() + (slot * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
-  const uint32_t kw = *reinterpret_cast<const uint32_t *>(block + row);
-  const uint32_t vw = *reinterpret_cast<const uint32_t *>(block + p.pool.code_bytes() + row);
-  const uint32_t kp = *reinterpret_cast<const uint32_t *>(params);
-  const uint32_t vp = *reinterpret_cast<const uint32_t *>(params + p.pool.param_bytes());
-  store_values<T, WIDE>(kw, kp, reinterpret_cast<T *>(p.k.row(t, head)) + c);
-  store_values<T, WIDE>(vw, vp, reinterpret_cast<T *>(p.v.row(t, head)) + c);
+  int64_t t[U];
+  int head[U], page[U], slot[U], user[U], pos[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t unit = ((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes;
+    t[j] = unit < n_units ? unit / p.pool.n_kv_heads : -1;
+    if (t[j] < 0) continue;
+    head[j] = (int)(unit - t[j] * p.pool.n_kv_heads);
+    pos[j] = p.positions[t[j]];
+    user[j] = p.users ? p.users[t[j]] : (int)t[j];
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    if (t[j] < 0) continue;
+    const int32_t *at = place(p, user[j], pos[j], head[j] == 0 && c == 0, slot[j]);
+    if (at)
+      page[j] = *at;
+    else
+      t[j] = -1;
+  }
+  uint32_t kw[U], vw[U], kp[U], vp[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    if (t[j] >= 0 && !page_ok(p, page[j], head[j] == 0 && c == 0)) t[j] = -1;
+    if (t[j] < 0) continue;
+    const uint8_t *block = p.pool.block(page[j], p.layer, head[j]);
+    const int at = slot[j] * (p.pool.head_dim / 2) + c / 2;
+    const uint8_t *params = block + 2 * p.pool.code_bytes() + (slot[j] * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
+    kw[j] = *reinterpret_cast<const uint32_t *>(block + at);
+    vw[j] = *reinterpret_cast<const uint32_t *>(block + p.pool.code_bytes() + at);
+    kp[j] = *reinterpret_cast<const uint32_t *>(params);
+    vp[j] = *reinterpret_cast<const uint32_t *>(params + p.pool.param_bytes());
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    if (t[j] < 0) continue;
+    store_values<T, WIDE>(kw[j], kp[j], reinterpret_cast<T *>(p.k.row(t[j], head[j])) + c);
+    store_values<T, WIDE>(vw[j], vp[j], reinterpret_cast<T *>(p.v.row(t[j], head[j])) + c);
+  }
 }
 
-template <class T>
-cudaError_t launch_rows(const RowsParams &p, bool reads, bool wide, cudaStream_t s) {
-  const int rows = ROW_THREADS / (p.pool.head_dim / 8);
+template <class T, bool WIDE, int U>
+cudaError_t launch_units(const RowsParams &p, bool reads, cudaStream_t s) {
+  const int rows = ROW_THREADS / (p.pool.head_dim / 8) * U;
   const int64_t grid = ((int64_t)p.n_tokens * p.pool.n_kv_heads + rows - 1) / rows;
   if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  if (reads)
-    return wide ? launch_chained(kv4_read_kernel<T, true>, (unsigned)grid, ROW_THREADS, 0, s, p)
-                : launch_chained(kv4_read_kernel<T, false>, (unsigned)grid, ROW_THREADS, 0, s, p);
-  return wide ? launch_chained(kv4_append_kernel<T, true>, (unsigned)grid, ROW_THREADS, 0, s, p)
-              : launch_chained(kv4_append_kernel<T, false>, (unsigned)grid, ROW_THREADS, 0, s, p);
+  return reads ? launch_chained(kv4_read_kernel<T, WIDE, U>, (unsigned)grid, ROW_THREADS, 0, s, p)
+               : launch_chained(kv4_append_kernel<T, WIDE, U>, (unsigned)grid, ROW_THREADS, 0, s, p);
+}
+
+// Rows that fill the SMs many times over: two or four a thread.  Few, or off 16 bytes: one, spread as widely as they go.
+template <class T>
+cudaError_t launch_rows(const RowsParams &p, bool reads, bool wide, cudaStream_t s) {
+  const int64_t threads = (int64_t)p.n_tokens * p.pool.n_kv_heads * (p.pool.head_dim / 8);
+  if (!wide) return launch_units<T, false, 1>(p, reads, s);
+  if (threads < 8 * 152 * 2048) return launch_units<T, true, 1>(p, reads, s);
+  return reads ? launch_units<T, true, 4>(p, reads, s) : launch_units<T, true, 2>(p, reads, s);
 }
 
 int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer,

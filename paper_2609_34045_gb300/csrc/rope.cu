@@ -35,10 +35,6 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeParams p) 
   pdl_wait();
   const int64_t t = blockIdx.x;
   const int pos = p.positions[t];
-  if (pos < 0 || pos >= p.n_pos) {
-    if (blockIdx.y == 0 && threadIdx.x == 0) report(p.status, KFL_BAD_POSITION);
-    return;
-  }
   using Vec = Pack<T, V>;
   const int item = threadIdx.x % p.n_items, head0 = threadIdx.x / p.n_items;
   const bool turns = item < p.n_rot;
@@ -52,6 +48,26 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeParams p) 
     b = a + V;
   }
   const bool has_b = b < p.head_dim;
+  const int first = blockIdx.y * p.heads_per_block;
+  const int last = min(p.n_heads, first + p.heads_per_block);
+  Vec x[ROPE_AHEAD], y[ROPE_AHEAD];
+  const auto load = [&](int h0) {
+#pragma unroll
+    for (int j = 0; j < ROPE_AHEAD; ++j) {
+      const int h = h0 + j * p.heads_per_step;
+      if (h >= last) break;
+      const int which = h >= p.n_q;
+      if (!turns && !p.copies[which]) continue;
+      const T *src = reinterpret_cast<const T *>(p.in[which].row(t, h - (which ? p.n_q : 0)));
+      x[j] = *reinterpret_cast<const Vec *>(src + a);
+      if (has_b) y[j] = *reinterpret_cast<const Vec *>(src + b);
+    }
+  };
+  load(first + head0);  // (under way before the position is known)
+  if (pos < 0 || pos >= p.n_pos) {
+    if (blockIdx.y == 0 && threadIdx.x == 0) report(p.status, KFL_BAD_POSITION);
+    return;
+  }
   float2 cs[V];
   if (turns) {
     const float2 *row = p.cos_sin + (int64_t)pos * p.rope_half + item * V;
@@ -65,20 +81,8 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeParams p) 
       }
     }
   }
-  const int first = blockIdx.y * p.heads_per_block;
-  const int last = min(p.n_heads, first + p.heads_per_block);
   for (int h0 = first + head0; h0 < last; h0 += ROPE_AHEAD * p.heads_per_step) {
-    Vec x[ROPE_AHEAD], y[ROPE_AHEAD];
-#pragma unroll
-    for (int j = 0; j < ROPE_AHEAD; ++j) {
-      const int h = h0 + j * p.heads_per_step;
-      if (h >= last) break;
-      const int which = h >= p.n_q;
-      if (!turns && !p.copies[which]) continue;
-      const T *src = reinterpret_cast<const T *>(p.in[which].row(t, h - (which ? p.n_q : 0)));
-      x[j] = *reinterpret_cast<const Vec *>(src + a);
-      if (has_b) y[j] = *reinterpret_cast<const Vec *>(src + b);
-    }
+    if (h0 != first + head0) load(h0);
 #pragma unroll
     for (int j = 0; j < ROPE_AHEAD; ++j) {
       const int h = h0 + j * p.heads_per_step;
@@ -137,10 +141,11 @@ cudaError_t launch_rope(RopeParams &p, bool wide, bool half, int n_tokens, cudaS
   const int rest = (p.copies[0] || p.copies[1]) ? (p.head_dim - 2 * p.rope_half) / V : 0;
   p.n_items = p.n_rot + (rest + 1) / 2;
   // Few tokens: a head or two per thread, so that the rows spread over the SMs (4 tokens of 72 heads of 128: 36
-  // blocks).  Many: one block per token, its heads in equal steps.
-  const int most = std::max(1, (n_tokens < 304 ? 64 : ROPE_THREADS) / p.n_items);
-  p.heads_per_block = n_tokens < 304 ? std::min(p.n_heads, most) : p.n_heads;
-  const int steps = (p.heads_per_block + most - 1) / most;
+  // blocks).  Many: a block per token with up to four heads per thread, whose loads are in flight together.
+  const bool few = n_tokens < 304;
+  const int most = std::max(1, (few ? 64 : ROPE_THREADS) / p.n_items);
+  p.heads_per_block = few ? std::min(p.n_heads, most) : p.n_heads;
+  const int steps = std::max((p.heads_per_block + most - 1) / most, few ? 1 : std::min(p.heads_per_block, ROPE_AHEAD));
   p.heads_per_step = (p.heads_per_block + steps - 1) / steps;
   const dim3 grid(n_tokens, (p.n_heads + p.heads_per_block - 1) / p.heads_per_block);
   const int threads = p.heads_per_step * p.n_items;
