@@ -58,7 +58,7 @@ int kfl_kv4_page_bytes(const kfl_kv4_pool *pool, size_t *out);
  * behind them (or a user or page out of range) is reported in status and not written.  Rows of one call are
  * distinct places; a page that several users hold is written for all of them (kfl_kv4_fork leaves no
  * such page to be written).  Lengths are kfl_kv4_reserve's to change.
- * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer), KFL_ERR_CUDA. */
+ * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer, n_tokens * n_kv_heads of 2^31 and more), KFL_ERR_CUDA. */
 int kfl_kv4_append(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *k,
                    const kfl_heads *v, const int32_t *users, const int32_t *positions, int n_tokens,
                    const kfl_rope_plan *rope, int32_t *status, void *cuda_stream);

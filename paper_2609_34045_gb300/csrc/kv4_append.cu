@@ -1,10 +1,11 @@
 // Rows into and out of the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_append, kfl_kv4_read.
 //
-// Memory bound: a 16-bit value read and 4.5 bits written (or the reverse), some 10 flops.  Eight channels of one
-// row to a thread (one 16-byte load, one 4-byte word of codes), eight threads to a group of 64, whose ends
-// meet in three shuffles; a thread has its k and its v in flight together.  The rotation's partner channels
-// are read once more, from L1, rather than exchanged: the partner may lie in any other thread or
-// in the same one, depending on layout and rope_dim.
+// Memory bound in bytes (a 16-bit value read and 4.5 bits written, or the reverse), if the instructions per value stay
+// below some 12: at 41 (eight channels a thread, integer divisions of 64 bits, a code's clamp and shift one by one) 16384 rows
+// of 8 heads took 49 us against 13 for their bytes.  So sixteen channels of a k row and of its v row to a thread, four
+// threads to a group of 64, whose ends meet in two shuffles; a code is six operations, its place in the word the last of
+// them.  The rotation's partner channels are read once more, from L1, rather than exchanged: the partner may lie in any other
+// thread or in the same one, depending on layout and rope_dim.
 #include "kv4.cuh"
 
 namespace kfl {
@@ -41,59 +42,60 @@ __device__ __forceinline__ bool page_ok(const RowsParams &p, int page, bool repo
   return false;
 }
 
-// Eight channels as they lie in memory.
+// Sixteen channels as they lie in memory.
+constexpr int CH = 16;
 template <class T>
-struct alignas(16) Raw8 {
-  T e[8];
+struct alignas(16) Raw {
+  T e[CH];
 };
 template <class T, bool WIDE>
-__device__ __forceinline__ Raw8<T> load_raw(const T *p) {
-  Raw8<T> r;
+__device__ __forceinline__ Raw<T> load_raw(const T *p) {
+  Raw<T> r;
   if constexpr (WIDE) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 8; i += W) *reinterpret_cast<Pack<T, W> *>(r.e + i) = *reinterpret_cast<const Pack<T, W> *>(p + i);
+    for (int i = 0; i < CH; i += W) *reinterpret_cast<Pack<T, W> *>(r.e + i) = *reinterpret_cast<const Pack<T, W> *>(p + i);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.e[i] = p[i];
+    for (int i = 0; i < CH; ++i) r.e[i] = p[i];
   }
   return r;
 }
 template <class T>
-__device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&x)[8]) {
+__device__ __forceinline__ void unpack(const Raw<T> &r, float (&x)[CH]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = to_f32(r.e[i]);
+  for (int i = 0; i < CH; ++i) x[i] = to_f32(r.e[i]);
 }
 
-// x, channels [c, c + 8) of a k row, rotated.
+// x, channels [c, c + 16) of a k row, rotated.
 template <class T, bool WIDE>
-__device__ __forceinline__ void rotate8(const RowsParams &p, const T *row, int c, int pos, float (&x)[8]) {
+__device__ __forceinline__ void rotate(const RowsParams &p, const T *row, int c, int pos, float (&x)[CH]) {
   const int half = p.rope_half;
   if (c >= 2 * half) return;
   const float2 *cs = p.cos_sin + (int64_t)pos * half;
   if (p.rope_layout == KFL_ROPE_INTERLEAVED) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
+    for (int i = 0; i < CH; i += 2) {
       if (c + i >= 2 * half) break;  // (rope_dim is even: a pair is inside or outside as a whole)
       const float2 f = cs[(c + i) / 2];
       const float a = x[i], b = x[i + 1];
       x[i] = rope_first(a, b, f), x[i + 1] = rope_second(a, b, f);
     }
-  } else if (half % 8 == 0) {  // the eight channels have their partners in eight others
-    float y[8];
+  } else if (half % CH == 0) {  // the sixteen channels have their partners in sixteen others
+    float y[CH];
     const bool second = c >= half;
-    unpack8(load_raw<T, WIDE>(row + (second ? c - half : c + half)), y);
+    unpack(load_raw<T, WIDE>(row + (second ? c - half : c + half)), y);
     const float4 *f4 = reinterpret_cast<const float4 *>(cs + (second ? c - half : c));
+    const float sign = second ? 1.f : -1.f;  // x cos - y sin, or x cos + y sin
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < CH / 2; ++i) {
       const float4 f = f4[i];
-      const float2 f0 = {f.x, f.y}, f1 = {f.z, f.w};
-      x[2 * i] = second ? rope_second(y[2 * i], x[2 * i], f0) : rope_first(x[2 * i], y[2 * i], f0);
-      x[2 * i + 1] = second ? rope_second(y[2 * i + 1], x[2 * i + 1], f1) : rope_first(x[2 * i + 1], y[2 * i + 1], f1);
+      x[2 * i] = __fadd_rn(__fmul_rn(x[2 * i], f.x), __fmul_rn(y[2 * i], f.y * sign));
+      x[2 * i + 1] = __fadd_rn(__fmul_rn(x[2 * i + 1], f.z), __fmul_rn(y[2 * i + 1], f.w * sign));
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < CH; ++i) {
       const int e = c + i;
       if (e >= 2 * half) break;
       x[i] = e < half ? rope_first(x[i], to_f32(row[e + half]), cs[e])
@@ -102,183 +104,161 @@ __device__ __forceinline__ void rotate8(const RowsParams &p, const T *row, int c
   }
 }
 
-// Codes of eight channels; their group is the warp's aligned eight lanes, which all call.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], int lane, uint32_t &params) {
+// Smaller and larger of two, NaN if one is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Codes of sixteen channels; their group is the warp's aligned four lanes, which all call.
+__device__ __forceinline__ uint2 quantise(const float (&x)[CH], uint32_t &params) {
   float lo = x[0], hi = x[0];
-  bool ok = true;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
-    ok = ok && fabsf(x[i]) <= KV4_LIMIT;  // (false for NaN, which fminf and fmaxf pass over)
-  }
+  for (int i = 1; i < CH; ++i) lo = min_nan(lo, x[i]), hi = max_nan(hi, x[i]);
 #pragma unroll
-  for (int off = 4; off > 0; off >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, off));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, off));
+  for (int off = 2; off > 0; off >>= 1) {
+    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, off));
+    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, off));
   }
-  ok = ((__ballot_sync(0xffffffffu, ok) >> (lane & 24)) & 0xff) == 0xff;
-  if (!ok) {
+  if (!(hi <= KV4_LIMIT && lo >= -KV4_LIMIT)) {  // (or NaN)
     params = 0x7FFF7FFFu;
-    return 0x88888888u;
+    return make_uint2(0x88888888u, 0x88888888u);
   }
   const __half scale_h = __float2half_rn(__fdiv_rn(hi - lo, 15.f));
   const float scale = __half2float(scale_h);
   const __half centre_h = __float2half_rn(__fadd_rn(lo, 8.f * scale));
   const float centre = __half2float(centre_h);
-  const float inv = scale > 0.f ? __fdiv_rn(1.f, scale) : 0.f;
-  uint32_t w = 0;
+  const float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  // clamp(rint(t) + 8, 0, 15): t is clamped first (to whole numbers: the order is of no account), and its sum with
+  // 1.5 2^23 + 8, rounded to whole numbers, has rint(t) + 8 as its last bits.  The other bits of the eight sums, one
+  // on the other at 16 times the place, are a constant.
+  constexpr uint32_t MAGIC = 0x4B400000u;
+  constexpr uint32_t REST = MAGIC * 0x11111111u;
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int u = __float2int_rn(__fmul_rn(__fsub_rn(x[i], centre), inv)) + 8;
-    w |= (uint32_t)min(15, max(0, u)) << (4 * i);
+  for (int j = 0; j < 2; ++j) {
+    w[j] = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      const float t = __fmul_rn(__fsub_rn(x[8 * j + i], centre), inv);
+      w[j] = w[j] * 16 + __float_as_uint(__fadd_rn(fminf(fmaxf(t, -8.f), 7.f), 12582920.f));
+    }
+    w[j] -= REST;
   }
   params = (uint32_t)__half_as_ushort(scale_h) | ((uint32_t)__half_as_ushort(centre_h) << 16);
-  return w;
+  return make_uint2(w[0], w[1]);
 }
 
-// U rows a thread, in flight together.
-template <class T, bool WIDE, int U>
+// The (token, head) of a unit: below 2^31 of them (checked by the host).
+struct Unit {
+  int64_t t;
+  int head;
+};
+__device__ __forceinline__ Unit unit_of(const RowsParams &p, unsigned u) {
+  const unsigned t = u / (unsigned)p.pool.n_kv_heads;
+  return {(int64_t)t, (int)(u - t * (unsigned)p.pool.n_kv_heads)};
+}
+
+template <class T, bool WIDE>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_append_kernel(const RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int lanes = p.pool.head_dim / 8, rows = ROW_THREADS / lanes;  // threads of a row, rows of a block at a time
-  const int64_t n_units = (int64_t)p.n_tokens * p.pool.n_kv_heads;
-  const int c = threadIdx.x % lanes * 8;
-  Raw8<T> k_raw[U], v_raw[U];
-  int pos[U], user[U], head[U];
-  bool mine[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t unit = ((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes;
-    // (threads behind the last row repeat it without storing it: the shuffles take whole warps)
-    mine[j] = unit < n_units;
-    const int64_t u = min(unit, n_units - 1), t = u / p.pool.n_kv_heads;
-    head[j] = (int)(u - t * p.pool.n_kv_heads);
-    pos[j] = p.positions[t];
-    user[j] = p.users ? p.users[t] : (int)t;
-    v_raw[j] = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.v.row(t, head[j])) + c);
-    k_raw[j] = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.k.row(t, head[j])) + c);
-  }
-  int slot[U], page[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const bool reports = head[j] == 0 && c == 0 && mine[j];
-    const int32_t *at = place(p, user[j], pos[j], reports, slot[j]);
-    page[j] = at ? *at : -2;
-    if (at && !page_ok(p, page[j], reports)) page[j] = -2;
-    mine[j] = mine[j] && page[j] >= 0;
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t unit = min(((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes, n_units - 1);
-    const T *row = reinterpret_cast<const T *>(p.k.row(unit / p.pool.n_kv_heads, head[j]));
-    float x[8];
-    unpack8(k_raw[j], x);
-    if (p.cos_sin && mine[j]) rotate8<T, WIDE>(p, row, c, pos[j], x);
-    uint32_t kp, vp;
-    const uint32_t kw = quantise8(x, threadIdx.x & 31, kp);
-    unpack8(v_raw[j], x);
-    const uint32_t vw = quantise8(x, threadIdx.x & 31, vp);
-    if (!mine[j]) continue;
-    uint8_t *block = p.pool.block(page[j], p.layer, head[j]);
-    const int at = slot[j] * (p.pool.head_dim / 2) + c / 2;
-    *reinterpret_cast<uint32_t *>(block + at) = kw;
-    *reinterpret_cast<uint32_t *>(block + p.pool.code_bytes() + at) = vw;
-    if (c % KV4_GROUP == 0) {
-      uint8_t *params = block + 2 * p.pool.code_bytes() + (slot[j] * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
-      *reinterpret_cast<uint32_t *>(params) = kp;
-      *reinterpret_cast<uint32_t *>(params + p.pool.param_bytes()) = vp;
-    }
+  const int lanes = p.pool.head_dim / CH, shift = p.pool.head_dim == 128 ? 3 : 2;  // threads of a row
+  const unsigned n_units = (unsigned)p.n_tokens * (unsigned)p.pool.n_kv_heads;
+  const unsigned unit = blockIdx.x * (unsigned)(ROW_THREADS >> shift) + (threadIdx.x >> shift);
+  // (threads behind the last row repeat it without storing it: the shuffles take whole warps)
+  const Unit u = unit_of(p, min(unit, n_units - 1));
+  const int c = (threadIdx.x & (lanes - 1)) * CH;
+  const int pos = p.positions[u.t], user = p.users ? p.users[u.t] : (int)u.t;
+  const T *k_row = reinterpret_cast<const T *>(p.k.row(u.t, u.head));
+  const Raw<T> v_raw = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.v.row(u.t, u.head)) + c);
+  const Raw<T> k_raw = load_raw<T, WIDE>(k_row + c);
+  const bool reports = u.head == 0 && c == 0 && unit < n_units;
+  int slot, page = -2;
+  const int32_t *at = place(p, user, pos, reports, slot);
+  if (at) page = *at;
+  float x[CH];
+  unpack(k_raw, x);
+  if (p.cos_sin && at) rotate<T, WIDE>(p, k_row, c, pos, x);
+  uint32_t kp, vp;
+  const uint2 kw = quantise(x, kp);
+  unpack(v_raw, x);
+  const uint2 vw = quantise(x, vp);
+  if (unit >= n_units || !at || !page_ok(p, page, reports)) return;
+  uint8_t *block = p.pool.block(page, p.layer, u.head);
+  const int to = slot * (p.pool.head_dim / 2) + c / 2;
+  *reinterpret_cast<uint2 *>(block + to) = kw;
+  *reinterpret_cast<uint2 *>(block + p.pool.code_bytes() + to) = vw;
+  if (c % KV4_GROUP == 0) {
+    uint8_t *params = block + 2 * p.pool.code_bytes() + (slot * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
+    *reinterpret_cast<uint32_t *>(params) = kp;
+    *reinterpret_cast<uint32_t *>(params + p.pool.param_bytes()) = vp;
   }
 }
 
 template <class T, bool WIDE>
-__device__ __forceinline__ void store_values(uint32_t w, uint32_t params, T *dst) {
-  const float scale = __half2float(__ushort_as_half((uint16_t)params));
-  const float centre = __half2float(__ushort_as_half((uint16_t)(params >> 16)));
-  T v[8];
+__device__ __forceinline__ void store_values(uint2 codes, uint32_t params, T *dst) {
+  const __half2 par = *reinterpret_cast<const __half2 *>(&params);
+  const float scale = __low2float(par), centre = __high2float(par);
+  Raw<T> v;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)  // (the product is exact: 4 by 11 bits)
-    v[i] = from_f32<T>(fmaf((float)((int)((w >> (4 * i)) & 15) - 8), scale, centre));
+  for (int i = 0; i < CH; ++i) {
+    const uint32_t w = i < 8 ? codes.x : codes.y;
+    // (2^23 + code, less 2^23 + 8: exact; so is the product, of 4 by 11 bits)
+    const float u = __uint_as_float((w >> (4 * (i & 7)) & 15) | 0x4B000000u) - 8388616.f;
+    v.e[i] = from_f32<T>(fmaf(u, scale, centre));
+  }
   if constexpr (WIDE) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 8; i += W) {
-      Pack<T, W> o;
-#pragma unroll
-      for (int j = 0; j < W; ++j) o.e[j] = v[i + j];
-      *reinterpret_cast<Pack<T, W> *>(dst + i) = o;
-    }
+    for (int i = 0; i < CH; i += W) *reinterpret_cast<Pack<T, W> *>(dst + i) = *reinterpret_cast<Pack<T, W> *>(v.e + i);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dst[i] = v[i];
+    for (int i = 0; i < CH; ++i) dst[i] = v.e[i];
   }
 }
 
-template <class T, bool WIDE, int U>
+template <class T, bool WIDE>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int lanes = p.pool.head_dim / 8, rows = ROW_THREADS / lanes;
-  const int64_t n_units = (int64_t)p.n_tokens * p.pool.n_kv_heads;
-  const int c = threadIdx.x % lanes * 8;
-  int64_t t[U];
-  int head[U], page[U], slot[U], user[U], pos[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t unit = ((int64_t)blockIdx.x * U + j) * rows + threadIdx.x / lanes;
-    t[j] = unit < n_units ? unit / p.pool.n_kv_heads : -1;
-    if (t[j] < 0) continue;
-    head[j] = (int)(unit - t[j] * p.pool.n_kv_heads);
-    pos[j] = p.positions[t[j]];
-    user[j] = p.users ? p.users[t[j]] : (int)t[j];
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    if (t[j] < 0) continue;
-    const int32_t *at = place(p, user[j], pos[j], head[j] == 0 && c == 0, slot[j]);
-    if (at)
-      page[j] = *at;
-    else
-      t[j] = -1;
-  }
-  uint32_t kw[U], vw[U], kp[U], vp[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    if (t[j] >= 0 && !page_ok(p, page[j], head[j] == 0 && c == 0)) t[j] = -1;
-    if (t[j] < 0) continue;
-    const uint8_t *block = p.pool.block(page[j], p.layer, head[j]);
-    const int at = slot[j] * (p.pool.head_dim / 2) + c / 2;
-    const uint8_t *params = block + 2 * p.pool.code_bytes() + (slot[j] * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
-    kw[j] = *reinterpret_cast<const uint32_t *>(block + at);
-    vw[j] = *reinterpret_cast<const uint32_t *>(block + p.pool.code_bytes() + at);
-    kp[j] = *reinterpret_cast<const uint32_t *>(params);
-    vp[j] = *reinterpret_cast<const uint32_t *>(params + p.pool.param_bytes());
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    if (t[j] < 0) continue;
-    store_values<T, WIDE>(kw[j], kp[j], reinterpret_cast<T *>(p.k.row(t[j], head[j])) + c);
-    store_values<T, WIDE>(vw[j], vp[j], reinterpret_cast<T *>(p.v.row(t[j], head[j])) + c);
-  }
+  const int lanes = p.pool.head_dim / CH, shift = p.pool.head_dim == 128 ? 3 : 2;
+  const unsigned unit = blockIdx.x * (unsigned)(ROW_THREADS >> shift) + (threadIdx.x >> shift);
+  if (unit >= (unsigned)p.n_tokens * (unsigned)p.pool.n_kv_heads) return;
+  const Unit u = unit_of(p, unit);
+  const int c = (threadIdx.x & (lanes - 1)) * CH;
+  const bool reports = u.head == 0 && c == 0;
+  int slot;
+  const int32_t *at = place(p, p.users ? p.users[u.t] : (int)u.t, p.positions[u.t], reports, slot);
+  if (!at) return;
+  const int page = *at;
+  if (!page_ok(p, page, reports)) return;
+  const uint8_t *block = p.pool.block(page, p.layer, u.head);
+  const int from = slot * (p.pool.head_dim / 2) + c / 2;
+  const uint8_t *params = block + 2 * p.pool.code_bytes() + (slot * (p.pool.head_dim / KV4_GROUP) + c / KV4_GROUP) * 4;
+  const uint2 kw = *reinterpret_cast<const uint2 *>(block + from);
+  const uint2 vw = *reinterpret_cast<const uint2 *>(block + p.pool.code_bytes() + from);
+  const uint32_t kp = *reinterpret_cast<const uint32_t *>(params);
+  const uint32_t vp = *reinterpret_cast<const uint32_t *>(params + p.pool.param_bytes());
+  store_values<T, WIDE>(kw, kp, reinterpret_cast<T *>(p.k.row(u.t, u.head)) + c);
+  store_values<T, WIDE>(vw, vp, reinterpret_cast<T *>(p.v.row(u.t, u.head)) + c);
 }
 
-template <class T, bool WIDE, int U>
-cudaError_t launch_units(const RowsParams &p, bool reads, cudaStream_t s) {
-  const int rows = ROW_THREADS / (p.pool.head_dim / 8) * U;
-  const int64_t grid = ((int64_t)p.n_tokens * p.pool.n_kv_heads + rows - 1) / rows;
-  if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  return reads ? launch_chained(kv4_read_kernel<T, WIDE, U>, (unsigned)grid, ROW_THREADS, 0, s, p)
-               : launch_chained(kv4_append_kernel<T, WIDE, U>, (unsigned)grid, ROW_THREADS, 0, s, p);
-}
-
-// Rows that fill the SMs many times over: two or four a thread.  Few, or off 16 bytes: one, spread as widely as they go.
 template <class T>
 cudaError_t launch_rows(const RowsParams &p, bool reads, bool wide, cudaStream_t s) {
-  const int64_t threads = (int64_t)p.n_tokens * p.pool.n_kv_heads * (p.pool.head_dim / 8);
-  if (!wide) return launch_units<T, false, 1>(p, reads, s);
-  if (threads < 8 * 152 * 2048) return launch_units<T, true, 1>(p, reads, s);
-  return reads ? launch_units<T, true, 4>(p, reads, s) : launch_units<T, true, 2>(p, reads, s);
+  const int rows = ROW_THREADS / (p.pool.head_dim / CH);
+  const unsigned grid = (unsigned)(((int64_t)p.n_tokens * p.pool.n_kv_heads + rows - 1) / rows);
+  if (reads)
+    return wide ? launch_chained(kv4_read_kernel<T, true>, grid, ROW_THREADS, 0, s, p)
+                : launch_chained(kv4_read_kernel<T, false>, grid, ROW_THREADS, 0, s, p);
+  return wide ? launch_chained(kv4_append_kernel<T, true>, grid, ROW_THREADS, 0, s, p)
+              : launch_chained(kv4_append_kernel<T, false>, grid, ROW_THREADS, 0, s, p);
 }
 
 int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer,
@@ -294,6 +274,10 @@ int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv
   if (rope && (!rope_valid(rope) || rope->rope_dim > pool->head_dim)) return bad_arg(me, "not a rotation of these heads");
   if (n_tokens < 0 || (n_tokens > 0 && !positions)) return bad_arg(me, "positions are needed");
   if (n_tokens == 0) return KFL_OK;
+  if ((int64_t)n_tokens * pool->n_kv_heads > 0x7fffffff) {
+    bad_arg(me, "more than 2^31 - 1 rows in one call");
+    return KFL_ERR_RANGE;
+  }
   RowsParams p = {};
   p.pool = pool_of(*pool), p.map = map_of(*map), p.layer = layer;
   p.k = view_of(*k), p.v = view_of(*v);
