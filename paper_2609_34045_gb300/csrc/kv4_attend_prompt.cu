@@ -27,8 +27,10 @@ namespace kfl {
 namespace {
 
 constexpr int PT_KEYS = 128;                 // keys of a tile
-constexpr int PT_SOFTMAX = 16;               // warps 0 to 15
+constexpr int PT_PARTS = 2;                  // threads of a row
+constexpr int PT_SOFTMAX = 8 * PT_PARTS;     // warps 0 to 15
 constexpr int PT_DECODERS = 7;               // 16 to 22
+constexpr int PT_COLS = PT_KEYS / PT_PARTS;   // scores of a thread
 constexpr int PT_MMA_WARP = PT_SOFTMAX + PT_DECODERS;
 constexpr int PT_THREADS = (PT_MMA_WARP + 1) * 32;
 constexpr float PT_MOST = 16384.f;           // a row's weights in a tile may sum up to this: none is near fp16's end
@@ -106,11 +108,11 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 // 64 scores of a row: w the weights 2^(score cf - top) in fp16 pairs; returns their sum (taken in fp32 before the rounding:
 // above PT_MOST one of them may have outgrown fp16).  Sixteen at a time: a load from tensor memory takes some 50 clocks, which
 // the other warps fill, and more of them in flight would cost registers that the tile loop has not got.
-__device__ __forceinline__ float weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[32]) {
+__device__ __forceinline__ float weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[PT_COLS / 2]) {
   const float2 scale = {cf, cf}, from = {-top, -top};
   float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
+  for (int c = 0; c < PT_COLS / 16; ++c) {
     uint32_t v[16];
     tmem_ld16(t_s + 16 * c, v);
     tmem_wait_ld();
@@ -277,11 +279,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       mbar_init(bar(B_VFULL + i), 4);
       mbar_init(bar(B_KFREE + i), 1);
       mbar_init(bar(B_VFREE + i), 1);
-      mbar_init(bar(B_Q + i), 8);
+      mbar_init(bar(B_Q + i), 4 * PT_PARTS);
       mbar_init(bar(B_S + i), 1);
-      mbar_init(bar(B_P + i), 8);
+      mbar_init(bar(B_P + i), 4 * PT_PARTS);
       mbar_init(bar(B_O + i), 1);
-      mbar_init(bar(B_READ + i), 8);
+      mbar_init(bar(B_READ + i), 4 * PT_PARTS);
     }
     mbar_init(bar(B_DRAIN), 1);
     words[1] = 0;
@@ -351,14 +353,22 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     // ---- softmax: two threads per query row, each with 64 of a tile's keys and half of the row's channels.  They meet in
     // barriers of the half, so where a wait has given up they go on to the list's end (no wait lasts then), their
     // results being of no account
-    const int half = warp >> 3, part = warp >> 2 & 1, row = tid & 127;
-    constexpr int CH = HD / 2;                          // channels of a thread
+    const int half = warp / (4 * PT_PARTS), part = warp / 4 % PT_PARTS, row = tid & 127;
+    constexpr int CH = HD / PT_PARTS;                          // channels of a thread
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
-    const uint32_t t_s = tmem + lanes + half * 128 + part * 64;
+    const uint32_t t_s = tmem + lanes + half * 128 + part * PT_COLS;
     const uint32_t t_o = tmem + lanes + 256 + half * 128 + part * CH;
     const uint32_t q_tile = base + F::Q_AT + half * F::TILE;
     const int twins = half * 4 + (warp & 3);
     float *pair = reinterpret_cast<float *>(smem + F::PAIR_AT) + half * 256;  // [part][row]
+    // A value of both threads of the row
+    const auto shared_by_row = [&](float x, auto join) {
+      pair[part * 128 + row] = x;
+      pair_sync(twins);
+      x = join(x, pair[(part ^ 1) * 128 + row]);
+      pair_sync(twins);  // (before the next exchange)
+      return x;
+    };
     const float log2_scale = fabsf(p.scale) * 1.44269504089f;
     uint32_t done = 0;  // tiles of this half so far
     unsigned tile = 0;  // tiles of the thread block so far (places of the flags)
@@ -397,9 +407,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             const float b = p.bf16 ? bf16_hi(w[i]) : f16_to_f32((uint16_t)(w[i] >> 16));
             big = fmaxf(big, fmaxf(fabsf(a), fabsf(b)));
           }
-          pair[part * 128 + row] = big;
-          pair_sync(twins);
-          unit = xchunk_scale(fmaxf(big, pair[(part ^ 1) * 128 + row]), &inv);
+          unit = xchunk_scale(shared_by_row(big, [](float a, float b) { return fmaxf(a, b); }), &inv);
 #pragma unroll
           for (int i = 0; i < CH / 8; ++i) {
             float f[8];
@@ -424,46 +432,50 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         if (lane == 0) mbar_arrive(bar(B_Q + half));
         const float cf = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);
         float top = -INFINITY, sum = 0.f;  // top: the reference, in scores times cf; sum: of this thread's weights
-        bool poison = false;               // whether this row sees a NaN in the group of the thread's channels
+        unsigned poison = 0;               // groups of which this row sees a NaN
         const auto see_poison = [&](int t) {
-          const uint4 v = flags[((tile + t) & 3) * (1 + KB) + 1 + (KB == 2 ? part : 0)];
-          if ((v.x | v.y | v.z | v.w) == 0) return;
           const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
 #pragma unroll 1
-          for (int k = 0; k < PT_KEYS; ++k) {
-            const uint32_t bits = k < 32 ? v.x : k < 64 ? v.y : k < 96 ? v.z : v.w;
-            if ((bits >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison = true;
+          for (int g = 0; g < KB; ++g) {
+            const uint4 v = flags[((tile + t) & 3) * (1 + KB) + 1 + g];
+#pragma unroll 1
+            for (int k = 0; k < PT_KEYS; ++k) {
+              const uint32_t bits = k < 32 ? v.x : k < 64 ? v.y : k < 96 ? v.z : v.w;
+              if ((bits >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison |= 1u << g;
+            }
           }
         };
         // rows of this warp: the least end and the greatest begin decide whether a tile is seen whole
         const int least = __reduce_min_sync(0xffffffffu, end);
         const int greatest = __reduce_max_sync(0xffffffffu, begin);
         for (int t = 0; t < n; ++t) {
-          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS + part * 64;  // of this thread's keys
+          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS + part * PT_COLS;  // of this thread's keys
           wait(B_S + half, done & 1);
           __syncwarp();
           tc_fence_after();
-          const bool masked = key0 + 64 > least || (p.window > 0 && key0 < greatest);
+          const bool masked = key0 + PT_COLS > least || (p.window > 0 && key0 < greatest);
           // (what the decoding has to say of the tiles comes while the scores are weighed: shared memory, busy with the
           // products' operands, takes hundreds of clocks)
-          const uint32_t odd_k = odd[2 * ((tile + t) & 3)] >> (16 * part) & 0xffff, odd_v = t > 0 ? odd[2 * ((tile + t - 1) & 3) + 1] : 0;
+          const uint32_t odd_k = odd[2 * ((tile + t) & 3)], odd_v = t > 0 ? odd[2 * ((tile + t - 1) & 3) + 1] : 0;
           // The weights are taken against the reference that the row has; they stay in registers until both threads of the
           // row find that it holds.  Where it does not (the first tile, a row that outgrew it, scores that
           // are masked) the scores, still in place, are read again.
-          uint32_t w[32];
+          uint32_t w[PT_COLS / 2];
           float part_sum = 0.f;
           if (!masked && t > 0) part_sum = weigh_scores(t_s, cf, top, w);
           if (odd_v) see_poison(t - 1);
           if (pair_any(twins, masked || odd_k || t == 0 || part_sum > PT_MOST || top == -INFINITY)) {
             const bool pick = masked || odd_k;
-            const uint2 there2 = reinterpret_cast<const uint2 *>(flags + ((tile + t) & 3) * (1 + KB))[part];
+            const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
             const auto sees = [&](int c, int i) {  // column 16 c + i
               const int key = key0 + 16 * c + i;
-              return key < end && key >= begin && ((c < 2 ? there2.x : there2.y) >> ((c & 1) * 16 + i) & 1);
+              const int k = part * PT_COLS + 16 * c;
+              const uint32_t pages = k < 32 ? there4.x : k < 64 ? there4.y : k < 96 ? there4.z : there4.w;
+              return key < end && key >= begin && (pages >> ((c & 1) * 16 + i) & 1);
             };
             float most = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < PT_COLS / 16; ++c) {
               uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
@@ -471,9 +483,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
               for (int i = 0; i < 16; ++i)
                 if (!pick || sees(c, i)) most = fmaxf(most, __uint_as_float(x[i]));
             }
-            pair[part * 128 + row] = most;
-            pair_sync(twins);
-            most = fmaxf(most, pair[(part ^ 1) * 128 + row]);
+            most = shared_by_row(most, [](float a, float b) { return fmaxf(a, b); });
             most = most == -INFINITY ? most : most * cf;
             float keep = 1.f;
             if (most > top) {
@@ -499,7 +509,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             const float ref = top == -INFINITY ? 0.f : top;
             part_sum = 0.f;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < PT_COLS / 16; ++c) {
               uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
@@ -515,11 +525,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
                 w[8 * c + i / 2] = pt_pack(a, b);
               }
             }
-            pair_sync(twins);  // (before the next exchange)
           }
           sum += part_sum;
-          tmem_st16(t_s, reinterpret_cast<uint32_t(&)[16]>(w[0]));
-          tmem_st16(t_s + 16, reinterpret_cast<uint32_t(&)[16]>(w[16]));
+#pragma unroll
+          for (int c = 0; c < PT_COLS / 32; ++c) tmem_st16(t_s + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -530,13 +539,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         wait(B_O + half, (done - 1) & 1);
         __syncwarp();
         tc_fence_after();
-        see_poison(n - 1);
+        if (odd[2 * ((tile + n - 1) & 3) + 1]) see_poison(n - 1);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_READ + half));  // (the tiles' flags have been read)
-        pair[part * 128 + row] = sum;
-        pair_sync(twins);
-        sum += pair[(part ^ 1) * 128 + row];
-        pair_sync(twins);  // (before the next piece's exchange)
+        sum = shared_by_row(sum, [](float a, float b) { return a + b; });
         const bool whole = pc.from == 0 && pc.to == pc.n_tiles;
         const float inv_sum = sum == 0.f ? 0.f : 1.f / sum;
         float *slot = p.partials + ((size_t)blockIdx.x * 2 + (pc.from > 0 ? 0 : 1)) * slot_floats;
@@ -554,7 +560,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               v[j] = __uint_as_float(x[8 * i + 2 * (j & 3) + (j >> 2)]);
-              if (poison) v[j] = __uint_as_float(0x7fc00000u);
+              if (poison >> ((part * CH + 16 * c) / 64) & 1) v[j] = __uint_as_float(0x7fc00000u);
             }
             if (whole) {
               uint16_t h[8];
@@ -701,7 +707,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       if (elect_one()) {
 #pragma unroll
         for (int i = 0; i < PT_KEYS / 16; ++i)
-          mma_ts(tm + 256 + half * 128, tm + half * 128 + (i / 4) * 64 + (i % 4) * 8, v + i * 128, idesc_o, !first || i > 0);
+          mma_ts(tm + 256 + half * 128, tm + half * 128 + i / (PT_COLS / 16) * PT_COLS + i % (PT_COLS / 16) * 8, v + i * 128, idesc_o, !first || i > 0);
         mma_commit(bar(B_O + half));
       }
       __syncwarp();
