@@ -777,28 +777,52 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     }
     __syncthreads();
     if (!words[2]) continue;
-    const auto slot_of = [&](int b) { return p.partials + ((size_t)b * 2 + (sa < b * quota ? 0 : 1)) * slot_floats; };
-    // eight lanes per row, every row of a warp's four at once
-    constexpr int C = HD / 8;
-    const int sub = lane & 7;
-    for (int r = warp * 4 + (lane >> 3); r < pc.rows; r += PT_THREADS / 8) {
-      const int token = (pc.row0 + r) / p.group, head = pc.head * p.group + (pc.row0 + r) % p.group;
-      float top = -INFINITY, sum = 0.f, v[C] = {};
-      for (int b = from; b <= to; ++b) top = fmaxf(top, slot_of(b)[(size_t)rows_per_block * HD + 2 * r]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      for (int b = from; b <= to; ++b) {
-        const float *slot = slot_of(b);
-        const float *stats = slot + (size_t)rows_per_block * HD + 2 * r;
-        const float w = pt_ex2(stats[0] - ref);
-        sum = fmaf(stats[1], w, sum);
-        const float4 *x = reinterpret_cast<const float4 *>(slot + (size_t)r * HD + sub * C);
+    // (the thread block where the row block begins has it as its last part, the others as their first)
+    const float *first = p.partials + ((size_t)from * 2 + 1) * slot_floats;
+    const auto slot_of = [&](int i) { return first + (i == 0 ? 0 : (size_t)(2 * i - 1) * slot_floats); };
+    // sixteen lanes per row: a part's maximum and sum to a lane, then every lane its channels of all parts, four parts'
+    // loads together
+    constexpr int C = HD / 16;
+    const int sub = lane & 15, n = to - from + 1;
+    for (int r0 = warp * 2; r0 < pc.rows; r0 += PT_THREADS / 16) {
+      const int r = min(r0 + (lane >> 4), pc.rows - 1);
+      const size_t stats = (size_t)rows_per_block * HD + 2 * r;
+      float top = -INFINITY;
+      for (int i = sub; i < n; i += 16) top = fmaxf(top, slot_of(i)[stats]);
 #pragma unroll
-        for (int j = 0; j < C / 4; ++j) {
-          const float4 y = x[j];
-          v[4 * j] = fmaf(y.x, w, v[4 * j]), v[4 * j + 1] = fmaf(y.y, w, v[4 * j + 1]);
-          v[4 * j + 2] = fmaf(y.z, w, v[4 * j + 2]), v[4 * j + 3] = fmaf(y.w, w, v[4 * j + 3]);
+      for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, v[C] = {};
+      for (int i0 = 0; i0 < n; i0 += 16) {
+        float w = 0.f;
+        if (i0 + sub < n) {
+          const float2 ms = *reinterpret_cast<const float2 *>(slot_of(i0 + sub) + stats);
+          w = pt_ex2(ms.x - ref);
+          sum = fmaf(ms.y, w, sum);
+        }
+        for (int i = 0; i < min(16, n - i0); i += 4) {
+          float4 x[4][C / 4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < C / 4; ++j)
+              x[k][j] = reinterpret_cast<const float4 *>(slot_of(min(i0 + i + k, n - 1)) + (size_t)r * HD + sub * C)[j];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float wk = __shfl_sync(0xffffffffu, w, (lane & 16) + i + k);
+            if (i0 + i + k >= n) break;
+#pragma unroll
+            for (int j = 0; j < C / 4; ++j) {
+              v[4 * j] = fmaf(x[k][j].x, wk, v[4 * j]), v[4 * j + 1] = fmaf(x[k][j].y, wk, v[4 * j + 1]);
+              v[4 * j + 2] = fmaf(x[k][j].z, wk, v[4 * j + 2]), v[4 * j + 3] = fmaf(x[k][j].w, wk, v[4 * j + 3]);
+            }
+          }
         }
       }
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      if (r0 + (lane >> 4) >= pc.rows) continue;
+      const int token = (pc.row0 + r) / p.group, head = pc.head * p.group + (pc.row0 + r) % p.group;
       uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(pc.first + token, head)) + sub * C;
 #pragma unroll
       for (int j = 0; j < C; ++j) {
