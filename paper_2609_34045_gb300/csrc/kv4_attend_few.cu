@@ -250,45 +250,52 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
   pdl_launch_dependents();
-  if (tid < W * F::SLOTS) mbar_init(smem_addr(bars + tid), 1);
-  if (tid < 2 * W) part_seg[tid] = -1;
+  if (lane < F::SLOTS) mbar_init(smem_addr(bars + warp * F::SLOTS + lane), 1);  // (each warp its own)
+  if (lane < 2) part_seg[2 * warp + lane] = -1;
   fence_mbar_init();
   pdl_wait();
 
-  // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros)
-  for (int s = tid; s < p.n_seqs; s += F::THREADS) {
+  // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros).  Up to 32
+  // sequences every warp makes the whole list, alike, and waits for no other
+  const auto tiles_of = [&](int s) {
     const int user = p.users ? p.users[s] : p.seq0 + s;
-    int first = p.q_start ? p.q_start[s] : p.seq0 + s, count = p.q_start ? p.q_start[s + 1] - first : 1;
-    int length = 0;
-    if (first < 0 || count < 0 || count > p.max_q || first > p.n_tokens - count) {
-      if (blockIdx.x == 0) report(p.status, KFL_BAD_POSITION);
-      count = 0;
-    }
-    if (user < 0 || user >= p.map.n_users) {
-      if (blockIdx.x == 0) report(p.status, KFL_BAD_USER);
-    } else {
+    const int first = p.q_start ? p.q_start[s] : p.seq0 + s;
+    int count = p.q_start ? p.q_start[s + 1] - first : 1, length = 0, bad = 0;
+    if (first < 0 || count < 0 || count > p.max_q || first > p.n_tokens - count) bad |= KFL_BAD_POSITION, count = 0;
+    if (user < 0 || user >= p.map.n_users)
+      bad |= KFL_BAD_USER;
+    else
       length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
-    }
-    const int tiles = count == 0 ? 0 : max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
+    if (bad && blockIdx.x == 0) report(p.status, bad);
     info[s] = make_int4(user, length, first, count);
-    prefix[s + 1] = tiles;
-  }
-  if (tid == 0) prefix[0] = 0;
-  __syncthreads();
-  if (warp == 0) {
-    int before = 0;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-      int v = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0;
+    return count == 0 ? 0 : max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
+  };
+  const auto warp_sum = [&](int v) {  // up to and with this lane's
 #pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, v, off);
-        if (lane >= off) v += o;
-      }
-      if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + v;
-      before += __shfl_sync(0xffffffffu, v, 31);
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, off);
+      if (lane >= off) v += o;
     }
+    return v;
+  };
+  if (lane == 0) prefix[0] = 0;
+  if (p.n_seqs <= 32) {
+    const int sum = warp_sum(lane < p.n_seqs ? tiles_of(lane) : 0);
+    if (lane < p.n_seqs) prefix[lane + 1] = sum;
+    __syncwarp();
+  } else {
+    for (int s = tid; s < p.n_seqs; s += F::THREADS) prefix[s + 1] = tiles_of(s);
+    __syncthreads();
+    if (warp == 0) {
+      int before = 0;
+      for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+        const int sum = warp_sum(s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0);
+        if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + sum;
+        before += __shfl_sync(0xffffffffu, sum, 31);
+      }
+    }
+    __syncthreads();
   }
-  __syncthreads();
   const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
   // at least a tile for every warp of a block: fewer blocks, fewer merges
   const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)W);

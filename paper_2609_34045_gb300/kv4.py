@@ -102,15 +102,16 @@ def _int32(t, where, n=None):
     return t.data_ptr()
 
 
-def _heads(t, where, head_dim=None):
+def _heads(t, where, n_tokens=None, head_dim=None):
+    """kfl_heads of a tensor [token][head][head_dim]."""
     if t is None:
         return None
     if t.dim() != 3:
         raise ValueError(f"{where} is [token][head][head_dim]")
-    _, n_heads, hd = t.shape
+    n, n_heads, hd = t.shape
     per_token, per_head, one = t.stride()
-    if (one != 1 and hd != 1) or (head_dim is not None and hd != head_dim):
-        raise ValueError(f"{where} has contiguous channels, as many as the others")
+    if (n != n_tokens and n_tokens is not None) or (hd != head_dim and head_dim is not None) or (one != 1 and hd != 1):
+        raise ValueError(f"{where} has contiguous channels, and as many tokens and channels as the others")
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{where} is bf16, fp16 or fp32")
@@ -144,12 +145,8 @@ def kfl_rope(plan: kfl_rope_plan, q, q_out, k, k_out, positions, inverse: bool =
     """Rotates q into q_out and k into k_out ([token][head][head_dim]; k and k_out may be None; an output may be
     its input) by int32 positions [token].  Asynchronous."""
     n, _, hd = q.shape
-    a, b, c, d = _heads(q, "q"), _heads(q_out, "q_out", hd), _heads(k, "k", hd), _heads(k_out, "k_out", hd)
-    for x, name in ((q_out, "q_out"), (k, "k"), (k_out, "k_out")):
-        if x is not None and x.shape[0] != n:
-            raise ValueError(f"{name} has as many tokens as q")
-    _check(lib().kfl_rope(C.byref(plan), a, b, c, d,
-                          _int32(positions, "positions", n), n, hd, int(inverse), _int32(status, "status", 1),
+    _check(lib().kfl_rope(C.byref(plan), _heads(q, "q", n, hd), _heads(q_out, "q_out", n, hd), _heads(k, "k", n, hd),
+                          _heads(k_out, "k_out", n, hd), _int32(positions, "positions", n), n, hd, int(inverse), _int32(status, "status", 1),
                           cuda_stream), "kfl_rope")
 
 
@@ -192,9 +189,7 @@ def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=N
     """Rows of k and v ([token][KV head][head_dim]) of one layer into the users' pages at int32 positions [token];
     k rotated first where ``rope`` is a rope_plan.  users None: row t is user t's.  Asynchronous."""
     n = k.shape[0]
-    if v.shape[0] != n:
-        raise ValueError("k and v have the same tokens")
-    a, b = _heads(k, "k", p.head_dim), _heads(v, "v", p.head_dim)
+    a, b = _heads(k, "k", n, p.head_dim), _heads(v, "v", n, p.head_dim)
     _check(lib().kfl_kv4_append(C.byref(p), C.byref(m), layer, a, b, _int32(users, "users", n),
                                 _int32(positions, "positions", n), n, rope and C.byref(rope),
                                 _int32(status, "status", 1), cuda_stream), "kfl_kv4_append")
@@ -203,9 +198,7 @@ def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=N
 def kfl_kv4_read(p, m, layer: int, users, positions, k_out, v_out, status=None, cuda_stream: int | None = None) -> None:
     """The values that the cache holds for rows (users[t], positions[t]) of one layer.  Asynchronous."""
     n = k_out.shape[0]
-    if v_out.shape[0] != n:
-        raise ValueError("k_out and v_out have the same tokens")
-    a, b = _heads(k_out, "k_out", p.head_dim), _heads(v_out, "v_out", p.head_dim)
+    a, b = _heads(k_out, "k_out", n, p.head_dim), _heads(v_out, "v_out", n, p.head_dim)
     _check(lib().kfl_kv4_read(C.byref(p), C.byref(m), layer, _int32(users, "users", n),
                               _int32(positions, "positions", n), n, a, b,
                               _int32(status, "status", 1), cuda_stream), "kfl_kv4_read")
@@ -230,8 +223,6 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
     [token][query head][head_dim]).  Without q_start (int32 [sequence + 1]) every row is a sequence; without users
     (int32 [sequence]) sequence s is user s.  lse: fp32 [token][query head].  Asynchronous."""
     n, n_heads, hd = q.shape
-    if out.shape[0] != n:
-        raise ValueError("q and out have the same tokens")
     if users is not None:
         n_seqs = users.numel()
     elif q_start is not None:
@@ -242,7 +233,7 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
         raise ValueError("more sequences than users")
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
         raise ValueError("lse is a contiguous fp32 [token][query head]")
-    a, b = _heads(q, "q", p.head_dim), _heads(out, "out", p.head_dim)
+    a, b = _heads(q, "q", n, p.head_dim), _heads(out, "out", n, p.head_dim)
     _check(lib().kfl_kv4_attend(C.byref(p), C.byref(m), layer, a, b, _at(lse),
                                 _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
                                 1.0 / math.sqrt(hd) if scale is None else scale, window, workspace.data_ptr(),
