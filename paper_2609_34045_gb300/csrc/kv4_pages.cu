@@ -13,6 +13,7 @@ namespace {
 
 constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_MOST = 1024;    // users of one call
+constexpr int PLAN_LIST = 4096;    // new pages of one call that are listed in shared memory; more go through the workspace
 constexpr int SCAN_PER_THREAD = 16;
 constexpr int COPY_THREADS = 256;
 
@@ -78,14 +79,15 @@ __device__ __forceinline__ void load_refs(const int32_t *refs, int at, int n, bo
   }
 }
 
-// The `want` lowest free pages into list[0..); returns how many there are (at most want).
-__device__ int find_free(const int32_t *refs, int n_pages, int want, int32_t *list) {
+// The `want` lowest free pages into list[0..); returns how many there are (at most want).  r: the references of the
+// thread's run in the first pass, loaded by the caller ahead of what it waits for in between.
+__device__ int find_free(const int32_t *refs, int n_pages, int want, int32_t *list, int (&r)[SCAN_PER_THREAD]) {
   const bool wide = (reinterpret_cast<uintptr_t>(refs) & 15) == 0;
   int found = 0;
   for (int base = 0; base < n_pages && found < want; base += PLAN_THREADS * SCAN_PER_THREAD) {
     const int at = base + threadIdx.x * SCAN_PER_THREAD;
-    int r[SCAN_PER_THREAD], mine = 0, total;
-    load_refs(refs, at, n_pages, wide, r);
+    int mine = 0, total;
+    if (base > 0) load_refs(refs, at, n_pages, wide, r);
 #pragma unroll
     for (int i = 0; i < SCAN_PER_THREAD; ++i) mine += r[i] == 0;
     int rank = found + block_scan(mine, total);
@@ -100,6 +102,9 @@ __device__ int find_free(const int32_t *refs, int n_pages, int want, int32_t *li
   __syncthreads();
   return min(found, want);
 }
+__device__ __forceinline__ void load_first_refs(const PlanParams &p, int (&r)[SCAN_PER_THREAD]) {
+  load_refs(p.map.refs, threadIdx.x * SCAN_PER_THREAD, p.pool.n_pages, (reinterpret_cast<uintptr_t>(p.map.refs) & 15) == 0, r);
+}
 
 // Whether an earlier entry of the call's list (in shared memory) names the same user.
 __device__ __forceinline__ bool named_before(const int *users, int i) {
@@ -110,10 +115,12 @@ __device__ __forceinline__ bool named_before(const int *users, int i) {
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS) kv4_reserve_kernel(const PlanParams p) {
-  __shared__ int s_user[PLAN_MOST], s_held[PLAN_MOST], s_end[PLAN_MOST];
+  __shared__ int s_user[PLAN_MOST], s_held[PLAN_MOST], s_end[PLAN_MOST], s_list[PLAN_LIST];
   pdl_launch_dependents();
   pdl_wait();
   const int i = threadIdx.x, P = p.pool.log2_tokens;
+  int first_refs[SCAN_PER_THREAD];
+  load_first_refs(p, first_refs);
   if (i < p.n) s_user[i] = p.users[i];
   __syncthreads();
   int need = 0, held = 0, length = 0, user = -1;
@@ -140,7 +147,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv4_reserve_kernel(const PlanPar
   // (more pages than the pool has do not fit however many they are: the sum stays below 2^31)
   need = min(need, p.pool.n_pages + 1);
   const int offset = block_scan(need, total);
-  const int found = find_free(p.map.refs, p.pool.n_pages, min(total, p.pool.n_pages), p.ws.src());
+  const int want = min(total, p.pool.n_pages);
+  int32_t *list = want <= PLAN_LIST ? s_list : p.ws.src();
+  const int found = find_free(p.map.refs, p.pool.n_pages, want, list, first_refs);
   const bool fits = user >= 0 && (need == 0 || offset + need <= found);
   if (user >= 0 && !fits) report(p.status, KFL_NO_PAGES);
   if (fits) p.map.lengths[user] = length;
@@ -161,7 +170,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv4_reserve_kernel(const PlanPar
         lo = mid + 1;
     }
     if (s_user[lo] < 0) continue;
-    const int page = p.ws.src()[r];
+    const int page = list[r];
     p.map.table[(int64_t)s_user[lo] * p.map.max_pages + s_held[lo] + r] = page;
     p.map.refs[page] = 1;
   }
@@ -193,11 +202,13 @@ __global__ void __launch_bounds__(256) kv4_free_kernel(const PlanParams p) {
 // The pairs' rows in steps of 32 columns: a step's old entries are all read before one of its new ones is written,
 // so that a user may be source and destination at once; columns do not hang on one another.
 __global__ void __launch_bounds__(PLAN_THREADS) kv4_fork_kernel(const PlanParams p) {
-  __shared__ int s_src[PLAN_MOST], s_dst[PLAN_MOST], s_full[PLAN_MOST], s_new[PLAN_MOST];
+  __shared__ int s_src[PLAN_MOST], s_dst[PLAN_MOST], s_full[PLAN_MOST], s_new[PLAN_MOST], s_list[PLAN_MOST];
   __shared__ int s_columns, s_count;
   pdl_launch_dependents();
   pdl_wait();
   const int i = threadIdx.x, P = p.pool.log2_tokens;
+  int first_refs[SCAN_PER_THREAD];
+  load_first_refs(p, first_refs);
   if (i == 0) s_columns = s_count = 0;
   if (i < p.n) s_dst[i] = p.other[i];
   __syncthreads();
@@ -219,15 +230,14 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv4_fork_kernel(const PlanParams
   }
   int total;
   const int rank = block_scan(need, total);
-  int32_t *list = p.ws.moved_refs();  // (free pages; the moves' own lists are written below)
-  const int found = find_free(p.map.refs, p.pool.n_pages, total, list);
+  const int found = find_free(p.map.refs, p.pool.n_pages, total, s_list, first_refs);
   int page = -1;
   if (dst >= 0 && need) {
     if (rank >= found) {
       report(p.status, KFL_NO_PAGES);
       dst = -1, columns = 0;
     } else {
-      page = list[rank];
+      page = s_list[rank];
       p.map.refs[page] = 1;
       const int end = p.map.table[(int64_t)src * p.map.max_pages + full];
       if (end < 0 || end >= p.pool.n_pages) {
