@@ -549,8 +549,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             }
         }
       }
-      unsigned hidden[NT] = {};  // a bit per score of this lane
       if (masked) {
+        unsigned hidden[NT] = {};  // a bit per score of this lane
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -562,7 +562,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> st & 1);
               if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
             }
-        // parameters that no row sees may be anything
+        // Parameters that no row sees may be anything.  A NaN that some rows see and others do not: theirs at once
+        // (through the group's centres), and gone for the products, where it would meet the others' zeros
 #pragma unroll
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
@@ -571,6 +572,15 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             for (int g = 0; g < G; ++g) {
               const int k = 16 * st + key_lane + 8 * h;
               if (key0 + k >= at.length || !(have >> st & 1)) vpar[st][h][g] = 0;
+              const uint32_t v = vpar[st][h][g];
+              if ((v & 0x7c00u) == 0x7c00u || (v & 0x7c000000u) == 0x7c000000u) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                  for (int c = 0; c < 2; ++c)
+                    if (!(hidden[n] >> (4 * st + 2 * h + c) & 1)) centre[n][g][c] = __uint_as_float(0x7fc00000u);
+                vpar[st][h][g] = 0;
+              }
             }
       }
       // ---- running maximum, and a common unit of the value scales (their weights are fp16)
@@ -654,14 +664,10 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             float w[4];
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-              float s0 = half_lo(vpar[st][i >> 1][g]) * weight_unit, d0 = half_hi(vpar[st][i >> 1][g]), s1 = s0, d1 = d0;
-              if (masked) {
-                if (hidden[n] >> (4 * st + i) & 1) s0 = d0 = 0.f;
-                if (hidden[n] >> (4 * st + i + 1) & 1) s1 = d1 = 0.f;
-              }
-              centre[n][g][0] = fmaf(pr[i], d0, centre[n][g][0]);
-              centre[n][g][1] = fmaf(pr[i + 1], d1, centre[n][g][1]);
-              w[i] = pr[i] * s0, w[i + 1] = pr[i + 1] * s1;
+              const float s = half_lo(vpar[st][i >> 1][g]) * weight_unit, d = half_hi(vpar[st][i >> 1][g]);
+              centre[n][g][0] = fmaf(pr[i], d, centre[n][g][0]);
+              centre[n][g][1] = fmaf(pr[i + 1], d, centre[n][g][1]);
+              w[i] = pr[i] * s, w[i + 1] = pr[i + 1] * s;
             }
             pf[n][g][0] = transpose8x8(pack_half2(w[0], w[1]));
             pf[n][g][1] = transpose8x8(pack_half2(w[2], w[3]));
