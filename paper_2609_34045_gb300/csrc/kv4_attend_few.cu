@@ -30,7 +30,9 @@
 namespace kfl {
 namespace {
 
-constexpr int TILE = 64;  // keys
+constexpr int LOG_TILE = 6, TILE = 1 << LOG_TILE;  // keys
+constexpr float WEIGHT_UNIT = 2048.f;  // fp16 weights: 2^(x - m) times this, at most WEIGHT_MOST times as much
+constexpr float WEIGHT_MOST = 16.f;
 constexpr int SUB = 2;    // groups of 16 keys that are worked on at once
 
 template <int HD, int NT>
@@ -306,19 +308,19 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const uint32_t ring = smem_addr(smem) + warp * F::SLOTS * F::TILE_BYTES;
   const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
   constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;  // of a tile's K or V, as in a block of 64 tokens
-  const int lb = min(lp, 6);                         // log2 of a page's tokens in a tile
+  const int lb = min(lp, LOG_TILE);                         // log2 of a page's tokens in a tile
   const int block_bytes = p.pool.block_bytes();
   const size_t page_bytes = p.pool.page_bytes();
   const uint8_t *layer_pages = p.pool.pages + (size_t)p.layer * heads * block_bytes;
   const uint64_t policy = policy_evict_normal();
 
-  // ---- copies: a page of 64 tokens is a tile as it stands; of others a page's part of the tile comes in four (codes and
+  // ---- copies: a page of a tile's size is one as it stands; of others a page's part of the tile comes in four (codes and
   // parameters of K and V), a lane each
   Cursor fetch;
   int fetch_page = -2, fetch_left = (int)(w1 - w0);  // tiles to bring (a page of -2: behind the sequence's end)
   unsigned fetch_slot = 0;
   const int lane_key = lane >> 2 << lb;              // of this lane's copy, in the tile
-  const bool copies = lane < (lp == 6 ? 1 : 4 * TILE >> lb);
+  const bool copies = lane < (lp == LOG_TILE ? 1 : 4 * TILE >> lb);
   const int32_t *fetch_row = nullptr;
   if (fetch_left > 0) {
     locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
@@ -328,32 +330,32 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     const int key = (fetch.first_tile + fetch.tile) * TILE + lane_key;
     fetch_page = copies && key < fetch.length ? fetch_row[key >> lp] : -2;
   };
+  constexpr unsigned ALL = (1u << TILE / 16) - 1;
   unsigned valid[F::SLOTS] = {};  // which 16 keys of a slot's tile are there, a bit each
   bool dead = false;              // a wait gave up: no more copies, no results
   const auto issue = [&]() {
     const bool there = fetch_page >= 0 && fetch_page < p.pool.n_pages;
     if (fetch_page != -2 && !there) report(p.status, KFL_BAD_PAGE);
     const unsigned lanes = __ballot_sync(0xffffffffu, there);
-    unsigned have = lanes & 1 ? 0xf : 0;
-    if (lp < 6) {
+    unsigned have = lanes & 1 ? ALL : 0;
+    if (lp < LOG_TILE) {
       have = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
+      for (int i = 0; i < TILE / 16; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
     }
     const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
-    if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / 4));
+    if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / (TILE / 16)));
     __syncwarp();
     if (there) {
       const uint8_t *src = layer_pages + fetch_page * page_bytes + (unsigned)(fetch.head * block_bytes);
-      if (lp == 6) {
+      if (lp == LOG_TILE) {
         bulk_g2s(dst, src, F::TILE_BYTES, bar, policy);
       } else {
-        // part 0, 1: codes of K, V; 2, 3: parameters.  A page of 128 holds two tiles
-        const int part = lane & 3, block = lane >> 2, half = lp == 7 ? (fetch.first_tile + fetch.tile) & 1 : 0;
-        const int size = part < 2 ? CODES : PARAMS, from0 = part < 2 ? 0 : 2 * CODES, nth = part & 1;
-        const int bytes = size >> (6 - lb);
-        bulk_g2s(dst + from0 + nth * size + block * bytes,
-                 src + (lp == 7 ? 2 * from0 + nth * 2 * size + half * size : (from0 + nth * size) >> (6 - lb)), bytes, bar, policy);
+        // part 0, 1: codes of K, V; 2, 3: parameters.  A larger page holds several tiles
+        const int part = lane & 3, block = lane >> 2, size = part < 2 ? CODES : PARAMS, bytes = size >> (LOG_TILE - lb);
+        const int to = (part < 2 ? 0 : 2 * CODES) + (part & 1) * size;  // as in a page of a tile's size
+        const int more = lp - LOG_TILE, nth = more > 0 ? (fetch.first_tile + fetch.tile) & ((1 << more) - 1) : 0;
+        bulk_g2s(dst + to + block * bytes, src + (more > 0 ? (to << more) + nth * size : to >> -more), bytes, bar, policy);
       }
     }
 #pragma unroll
@@ -484,7 +486,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       if (i == (int)slot) have = valid[i];
     // in steps of 16 SUB keys: the tile at once is more code than the instruction cache next to the scheduler holds
 #pragma unroll 1
-    for (int s0 = 0; s0 < 4 && !dead; s0 += SUB, have >>= SUB) {
+    for (int s0 = 0; s0 < TILE / 16 && !dead; s0 += SUB, have >>= SUB) {
       const uint32_t base = ring + slot * F::TILE_BYTES + 16 * s0 * (HD / 2);
       const uint32_t base_p = ring + slot * F::TILE_BYTES + 2 * CODES + 16 * s0 * (G * 4);
       const int key0 = (at.first_tile + at.tile) * TILE + 16 * s0;
@@ -583,7 +585,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               }
             }
       }
-      // ---- running maximum, and a common unit of the value scales (their weights are fp16)
+      // ---- weights against the reference that the columns have: it holds unless it is not there yet, a weight has outgrown
+      // it, or the value scales have outgrown their common unit (the products of the two are fp16, below 2^15)
       __half2 v_most = __float2half2_rn(0.f);  // (hmax2 passes over NaN)
 #pragma unroll
       for (int st = 0; st < SUB; ++st)
@@ -593,6 +596,30 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           for (int g = 0; g < G; ++g) v_most = __hmax2(v_most, *reinterpret_cast<const __half2 *>(&vpar[st][h][g]));
       float v_max = __low2float(v_most);
       bool grows = v_max > v_unit;
+      float pr[NT][SUB][4], part[NT][2];
+      const auto weigh = [&]() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float2 scale = {cf[n][0], cf[n][1]};
+          const float2 from = {top[n][0] == -INFINITY ? 0.f : -top[n][0] * cf[n][0],
+                               top[n][1] == -INFINITY ? 0.f : -top[n][1] * cf[n][1]};
+          part[n][0] = part[n][1] = 0.f;
+#pragma unroll
+          for (int st = 0; st < SUB; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const float2 e = fma2({x[n][st][i], x[n][st][i + 1]}, scale, from);
+              pr[n][st][i] = ex2(e.x), pr[n][st][i + 1] = ex2(e.y);
+              part[n][0] += pr[n][st][i], part[n][1] += pr[n][st][i + 1];
+            }
+        }
+      };
+      weigh();
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) grows = grows || part[n][c] > WEIGHT_MOST || top[n][c] == -INFINITY;
+      if (__any_sync(0xffffffffu, grows)) {
       float now[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -604,9 +631,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
           now[n][c] = fmaxf(m, top[n][c]);
-          grows = grows || now[n][c] > top[n][c];
         }
-      if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) v_max = fmaxf(v_max, __shfl_xor_sync(0xffffffffu, v_max, off));
         float shrink = 1.f;
@@ -638,36 +663,28 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             }
           }
         }
+        weigh();
       }
-      const float weight_unit = v_unit > 0.f ? 16384.f / v_unit : 0.f;
-      float ref[NT][2];
+      const float weight_unit = v_unit > 0.f ? WEIGHT_UNIT / v_unit : 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) ref[n][c] = top[n][c] == -INFINITY ? 0.f : -top[n][c] * cf[n][c];
+        for (int c = 0; c < 2; ++c) sum[n][c] += part[n][c];
 #pragma unroll
       for (int st = 0; st < SUB; ++st) {
         const uint32_t vb = base + CODES + (16 * st + tig) * (HD / 2) + gid * 4;
         uint32_t pf[NT][G][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          float pr[4];
-          const float2 scale = {cf[n][0], cf[n][1]}, from = {ref[n][0], ref[n][1]};
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const float2 e = fma2({x[n][st][i], x[n][st][i + 1]}, scale, from);
-            pr[i] = ex2(e.x), pr[i + 1] = ex2(e.y);
-            sum[n][0] += pr[i], sum[n][1] += pr[i + 1];
-          }
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             float w[4];
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
               const float s = half_lo(vpar[st][i >> 1][g]) * weight_unit, d = half_hi(vpar[st][i >> 1][g]);
-              centre[n][g][0] = fmaf(pr[i], d, centre[n][g][0]);
-              centre[n][g][1] = fmaf(pr[i + 1], d, centre[n][g][1]);
-              w[i] = pr[i] * s, w[i + 1] = pr[i + 1] * s;
+              centre[n][g][0] = fmaf(pr[n][st][i], d, centre[n][g][0]);
+              centre[n][g][1] = fmaf(pr[n][st][i + 1], d, centre[n][g][1]);
+              w[i] = pr[n][st][i] * s, w[i + 1] = pr[n][st][i + 1] * s;
             }
             pf[n][g][0] = transpose8x8(pack_half2(w[0], w[1]));
             pf[n][g][1] = transpose8x8(pack_half2(w[2], w[3]));
@@ -709,7 +726,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     if (ends || flat + 1 == w1) {
       const int64_t seg_first = flat - at.tile;
       const bool alone = ends && seg_first >= w0;
-      const float unit = v_unit * (1.f / 16384.f);
+      const float unit = v_unit * (1.f / WEIGHT_UNIT);
       // a result that others continue goes to global memory while the ring is in use, else into the ring
       const bool last = flat + 1 == w1;
       float *part = last ? reinterpret_cast<float *>(smem + (size_t)warp * F::SLOTS * F::TILE_BYTES)
