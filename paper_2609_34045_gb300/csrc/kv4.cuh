@@ -8,6 +8,7 @@
 namespace kfl {
 
 constexpr int KV4_GROUP = 64;          // channels that share a scale and a centre
+constexpr int KV4_MOST_HEADS = 256;    // KV heads of a pool
 constexpr float KV4_LIMIT = 32768.f;   // a group with a larger magnitude reads as NaN
 
 struct Kv4Pool {
@@ -37,7 +38,7 @@ inline int check_pool(const kfl_kv4_pool *p, bool need_pages, const char *where)
   if (!p) return bad_arg(where, "no pool");
   if (log2_page(p->page_tokens) < 0) return bad_arg(where, "page_tokens is 16, 32, 64 or 128");
   if (p->head_dim != 64 && p->head_dim != 128) return bad_arg(where, "head_dim is 64 or 128");
-  if (p->n_kv_heads < 1 || p->n_kv_heads > 256) return bad_arg(where, "n_kv_heads is 1..256");
+  if (p->n_kv_heads < 1 || p->n_kv_heads > KV4_MOST_HEADS) return bad_arg(where, "n_kv_heads is 1..256");
   if (p->n_layers < 1 || p->n_layers > (1 << 16)) return bad_arg(where, "n_layers is 1..65536");
   if (p->n_pages < 1 || p->n_pages > (1 << 20)) return bad_arg(where, "n_pages is 1..2^20");
   if (need_pages && (!p->pages || (reinterpret_cast<uintptr_t>(p->pages) & 15)))

@@ -1,7 +1,7 @@
 // Attention over the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_attend.
 //
-// Up to 16 query rows per KV head (a decode step's group, a few drafted tokens of a small group) go to the kernel that
-// streams the cache (kv4_attend_few.cu), more to the one that multiplies 128 rows at a time (kv4_attend_prompt.cu).
+// Up to 48 query rows per KV head (a decode step's group, a few drafted tokens) go to the kernel that streams the cache
+// (kv4_attend_few.cu), more to the one that multiplies 128 rows at a time (kv4_attend_prompt.cu).
 #include <math.h>
 
 #include <algorithm>
@@ -21,10 +21,10 @@ int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_se
   return KFL_OK;
 }
 
-// The workspace: tickets (zero between calls), then partial results.
-size_t ticket_bytes(const kfl_kv4_pool *pool, int n_seqs) {
-  return (std::max<size_t>((size_t)std::min(n_seqs, FEW_SEQS) * pool->n_kv_heads, FEW_BLOCKS) * 4 + 127) / 128 * 128;
-}
+// The workspace: tickets (zero between calls), then partial results.  The tickets' part is the same for every call, so
+// that no call's partial results lie where another one's tickets are.
+constexpr size_t TICKET_BYTES = (size_t)FEW_SEQS * KV4_MOST_HEADS * ((FEW_ROWS + 15) / 16) * 4;
+static_assert(TICKET_BYTES >= FEW_BLOCKS * 4 && TICKET_BYTES % 128 == 0, "tickets");
 
 }  // namespace
 }  // namespace kfl
@@ -38,8 +38,8 @@ extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_he
   if (rc != KFL_OK) return rc;
   if (!out) return bad_arg(me, "NULL pointer");
   const int64_t rows = (int64_t)max_q * (n_heads / pool->n_kv_heads);
-  *out = ticket_bytes(pool, n_seqs) +
-         (rows <= FEW_ROWS ? attend_few_partials(pool->head_dim, (int)rows) : attend_prompt_partials(pool->head_dim, rows));
+  *out = TICKET_BYTES +
+         (rows <= FEW_ROWS ? attend_few_partials(pool->head_dim, few_cols(rows)) : attend_prompt_partials(pool->head_dim, rows));
   return KFL_OK;
 }
 
@@ -72,17 +72,18 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.n_seqs = n_seqs, p.n_tokens = n_tokens, p.max_q = q_start ? max_q : 1;
   p.n_heads = q->n_heads, p.group = q->n_heads / pool->n_kv_heads;
   p.scale = scale, p.window = window, p.status = status;
-  p.tickets = static_cast<unsigned *>(workspace);
-  p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + ticket_bytes(pool, n_seqs));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)p.max_q * p.group;
+  p.most_blocks = rows <= FEW_ROWS ? (int)((rows + few_cols(rows) - 1) / few_cols(rows)) : 0;
+  p.tickets = static_cast<unsigned *>(workspace);
+  p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + TICKET_BYTES);
   int dev = 0, n_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
   for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
     p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
     p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
-    e = rows <= FEW_ROWS ? launch_attend_few(p, (int)rows, n_sm, s) : launch_attend_prompt(p, n_sm, s);
+    e = rows <= FEW_ROWS ? launch_attend_few(p, few_cols(rows), n_sm, s) : launch_attend_prompt(p, n_sm, s);
   }
   return cuda_result(e, me);
 }

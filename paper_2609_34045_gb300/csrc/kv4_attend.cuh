@@ -6,7 +6,7 @@
 
 namespace kfl {
 
-constexpr int FEW_ROWS = 16;     // most query rows per KV head of the few-row kernel
+constexpr int FEW_ROWS = 48;     // most query rows per KV head of the few-row kernel, in blocks of 8 or 16
 constexpr int FEW_SEQS = 512;    // sequences of one of its launches (their places lie in shared memory)
 constexpr int FEW_BLOCKS = 152;  // most blocks of one of its launches
 
@@ -21,7 +21,8 @@ struct AttendParams {
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
   float scale;
   int window;
-  unsigned *tickets;  // zero between launches: [n_seqs][n_kv_heads], many rows: [FEW_BLOCKS]
+  int most_blocks;    // few rows: of a KV head's query rows, in blocks of few_cols
+  unsigned *tickets;  // zero between launches: [n_seqs][n_kv_heads][most_blocks], many rows: [FEW_BLOCKS]
   float *partials;
   int32_t *status;
 };
@@ -47,7 +48,9 @@ __device__ __forceinline__ bool wait_2s(uint32_t bar, uint32_t parity) {
   return true;
 }
 
-// Bytes of the few-row kernel's partial results for `cols` query rows per KV head.
+// Query rows of a KV head that the few-row kernel works on at once.
+inline int few_cols(int64_t rows) { return rows <= 8 ? 8 : 16; }
+// Bytes of its partial results.
 size_t attend_few_partials(int head_dim, int cols);
 cudaError_t launch_attend_few(const AttendParams &p, int cols, int n_sm, cudaStream_t s);
 

@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "kv4_attend.cuh"
+#include "prefill_tc.cuh"  // hfma2
 
 namespace kfl {
 namespace {
@@ -93,6 +94,13 @@ __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t &low, uint32_t &
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(high) : "r"(w), "r"(0x00F000F0u), "r"(0x64006400u));
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(low) : "r"(both), "r"(high));
 }
+// The same for V, the high nibbles as u - 8: a sum over many keys of 64 + u, small weights of either sign in the end, would
+// lose to the matrix unit's truncation (3e-8 of the sum at every step, always downwards: 131072 keys came out 4.4e-3 off, and
+// 1.7e-3 is bf16's own rounding).  The low ones' 8 too many are few enough.
+__device__ __forceinline__ void value_pairs(uint32_t w, uint32_t &low, uint32_t &high) {
+  code_pairs(w, low, high);
+  high = hfma2(high, 0x2C002C00u, 0xD480D480u);  // / 16 - 72, exactly
+}
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
@@ -106,8 +114,8 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
 
 // A place in the list of tiles.
 struct Cursor {
-  int seq, head, tile;   // tile: within the segment (sequence, KV head)
-  int n_tiles, first_tile;
+  int seq, head, block, tile;  // block: of COLS query rows; tile: within the segment (sequence, KV head, block)
+  int blocks, n_tiles, first_tile;
   int user, length, first, count;
 };
 
@@ -116,48 +124,65 @@ __device__ __forceinline__ int first_tile_of(int length, int count, int window) 
   return window > 0 ? max(0, length - count + 1 - window) / TILE : 0;
 }
 
-__device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, const int *prefix, int window) {
+template <int COLS>
+__device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, const int *prefix, const AttendParams &p) {
   const int4 v = info[c.seq];
   c.user = v.x, c.length = v.y, c.first = v.z, c.count = v.w;
+  c.blocks = (c.count * p.group + COLS - 1) / COLS;
   c.n_tiles = prefix[c.seq + 1] - prefix[c.seq];
-  c.first_tile = first_tile_of(v.y, v.w, window);
+  if (c.blocks > 1) c.n_tiles /= c.blocks;
+  c.first_tile = first_tile_of(v.y, v.w, p.window);
 }
 
-__device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, int n_seqs, int heads, const int4 *info,
-                                            const int *prefix, int window) {
-  int lo = 0, hi = n_seqs - 1;
+template <int COLS>
+__device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 *info, const int *prefix,
+                                            const AttendParams &p) {
+  int lo = 0, hi = p.n_seqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if ((int64_t)prefix[mid + 1] * heads > flat)
+    if ((int64_t)prefix[mid + 1] * p.pool.n_kv_heads > flat)
       hi = mid;
     else
       lo = mid + 1;
   }
   c.seq = lo;
-  enter_sequence(c, info, prefix, window);
-  const int rest = (int)(flat - (int64_t)prefix[lo] * heads);  // (below heads * 2^20)
-  c.head = rest / c.n_tiles;
-  c.tile = rest - c.head * c.n_tiles;
+  enter_sequence<COLS>(c, info, prefix, p);
+  const int rest = (int)(flat - (int64_t)prefix[lo] * p.pool.n_kv_heads);  // (below heads * blocks * 2^20)
+  const int segment = rest / c.n_tiles;
+  c.tile = rest - segment * c.n_tiles;
+  c.head = segment / c.blocks;
+  c.block = segment - c.head * c.blocks;
 }
 
-__device__ __forceinline__ void next_tile(Cursor &c, int n_seqs, int heads, const int4 *info, const int *prefix,
-                                          int window) {
+template <int COLS>
+__device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const int *prefix, const AttendParams &p) {
   if (++c.tile < c.n_tiles) return;
   c.tile = 0;
-  if (++c.head < heads) return;
+  if (++c.block < c.blocks) return;
+  c.block = 0;
+  if (++c.head < p.pool.n_kv_heads) return;
   c.head = 0;
   do {
-    if (++c.seq >= n_seqs) return;
-    enter_sequence(c, info, prefix, window);
+    if (++c.seq >= p.n_seqs) return;
+    enter_sequence<COLS>(c, info, prefix, p);
   } while (c.n_tiles == 0);
 }
 
+// Query row `col` of the segment's block: the token's and the head's place.
+template <int COLS>
+__device__ __forceinline__ void row_of(const Cursor &c, int col, const AttendParams &p, int64_t &token, int &head) {
+  const int row = c.block * COLS + col, t = row / p.group;
+  token = c.first + t;
+  head = c.head * p.group + row - t * p.group;
+}
+
 // One output row's channels from lane `lane`'s HD / 32 values.
-template <int HD>
+template <int HD, int COLS>
 __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c, int col, int lane, const float (&v)[HD / 32],
                                           float top, float sum) {
-  const int64_t t = c.first + col / p.group;
-  const int head = c.head * p.group + col % p.group;
+  int64_t t;
+  int head;
+  row_of<COLS>(c, col, p, t, head);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(t, head)) + lane * (HD / 32);
 #pragma unroll
@@ -270,7 +295,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
     if (bad && blockIdx.x == 0) report(p.status, bad);
     info[s] = make_int4(user, length, first, count);
-    return count == 0 ? 0 : max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
+    return (count * p.group + COLS - 1) / COLS * max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
   };
   const auto warp_sum = [&](int v) {  // up to and with this lane's
 #pragma unroll
@@ -323,7 +348,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const bool copies = lane < (lp == LOG_TILE ? 1 : 4 * TILE >> lb);
   const int32_t *fetch_row = nullptr;
   if (fetch_left > 0) {
-    locate_tile(fetch, w0, p.n_seqs, heads, info, prefix, p.window);
+    locate_tile<COLS>(fetch, w0, info, prefix, p);
     fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
   }
   const auto load_page = [&]() {  // the page of this lane's copy for the tile at `fetch`
@@ -364,7 +389,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     fetch_slot = fetch_slot + 1 == F::SLOTS ? 0 : fetch_slot + 1;
     if (--fetch_left > 0) {
       const int seq = fetch.seq;
-      next_tile(fetch, p.n_seqs, heads, info, prefix, p.window);
+      next_tile<COLS>(fetch, info, prefix, p);
       if (fetch.seq != seq) fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
       load_page();
     }
@@ -389,9 +414,11 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int col = n * 8 + gid;
-          const bool there = col < at.count * p.group;
-          const uint16_t *e = reinterpret_cast<const uint16_t *>(
-                                  there ? p.q.row(at.first + col / p.group, at.head * p.group + col % p.group) : nullptr) +
+          const bool there = col < at.count * p.group - at.block * COLS;
+          int64_t token;
+          int head;
+          row_of<COLS>(at, col, p, token, head);
+          const uint16_t *e = reinterpret_cast<const uint16_t *>(there ? p.q.row(token, head) : nullptr) +
                               tig * 16;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
@@ -409,7 +436,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           }
         }
       if (flat == w0) issue();
-      rows = at.count * p.group;
+      rows = at.count * p.group - at.block * COLS;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         // (magnitudes of either type order as their bits)
@@ -560,7 +587,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * st + key_lane + 8 * (i >> 1);
-              const int end = all_end + min((n * 8 + 2 * tig + (i & 1)) / p.group, at.count - 1);
+              const int end = all_end + min((at.block * COLS + n * 8 + 2 * tig + (i & 1)) / p.group, at.count - 1);
               const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> st & 1);
               if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
             }
@@ -696,14 +723,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           const uint32_t wc = lds32(vb + g * 32 + 8 * (HD / 2)), wd = lds32(vb + g * 32 + 12 * (HD / 2));
           // [byte 0 or 1 of the tokens' words' lower, upper half][which two tokens]: the pairs of two tiles of 16 channels
           uint32_t x0[2][2], x1[2][2], y0[2][2], y1[2][2];  // low and high nibbles of: lower half, upper half
-          code_pairs(__byte_perm(wa, wb, 0x5410), x0[0][0], x1[0][0]);
-          code_pairs(__byte_perm(wa, wb, 0x5511), x0[1][0], x1[1][0]);
-          code_pairs(__byte_perm(wa, wb, 0x7632), y0[0][0], y1[0][0]);
-          code_pairs(__byte_perm(wa, wb, 0x7733), y0[1][0], y1[1][0]);
-          code_pairs(__byte_perm(wc, wd, 0x5410), x0[0][1], x1[0][1]);
-          code_pairs(__byte_perm(wc, wd, 0x5511), x0[1][1], x1[1][1]);
-          code_pairs(__byte_perm(wc, wd, 0x7632), y0[0][1], y1[0][1]);
-          code_pairs(__byte_perm(wc, wd, 0x7733), y0[1][1], y1[1][1]);
+          value_pairs(__byte_perm(wa, wb, 0x5410), x0[0][0], x1[0][0]);
+          value_pairs(__byte_perm(wa, wb, 0x5511), x0[1][0], x1[1][0]);
+          value_pairs(__byte_perm(wa, wb, 0x7632), y0[0][0], y1[0][0]);
+          value_pairs(__byte_perm(wa, wb, 0x7733), y0[1][0], y1[1][0]);
+          value_pairs(__byte_perm(wc, wd, 0x5410), x0[0][1], x1[0][1]);
+          value_pairs(__byte_perm(wc, wd, 0x5511), x0[1][1], x1[1][1]);
+          value_pairs(__byte_perm(wc, wd, 0x7632), y0[0][1], y1[0][1]);
+          value_pairs(__byte_perm(wc, wd, 0x7733), y0[1][1], y1[1][1]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const uint32_t b0 = pf[n][g][0], b1 = pf[n][g][1];
@@ -731,13 +758,16 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       const bool last = flat + 1 == w1;
       float *part = last ? reinterpret_cast<float *>(smem + (size_t)warp * F::SLOTS * F::TILE_BYTES)
                          : block_ws + (size_t)warp * F::PARTIAL;
-      if (!alone && lane == 0) part_seg[2 * warp + last] = at.seq * heads + at.head;
+      if (!alone && lane == 0) part_seg[2 * warp + last] = (at.seq * heads + at.head) * p.most_blocks + at.block;
       __syncwarp();
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int col = n * 8 + 2 * tig + c;
+          int64_t token;
+          int head;
+          row_of<COLS>(at, col, p, token, head);
           float l = sum[n][c];
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
@@ -752,7 +782,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 0.0625f : 1.f, (i & 1 ? -72.f : -8.f) * ones[n][g][c]),
+              v[i] = fmaf(i & 1 ? o[n][g][i & 3][c + 2 * (i >> 2)] : fmaf(-8.f, ones[n][g][c], o[n][g][i & 3][c + 2 * (i >> 2)]),
                           unit, cen);
             if (alone) {
               if (col < rows && !dead) {
@@ -762,9 +792,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
                   const float y = l == 0.f ? 0.f : v[i] * inv;
                   h[i] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
                 }
-                uint16_t *out = reinterpret_cast<uint16_t *>(
-                                    p.out.row(at.first + col / p.group, at.head * p.group + col % p.group)) +
-                                64 * g + 8 * gid;
+                uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(token, head)) + 64 * g + 8 * gid;
                 if (p.out_wide) {
                   *reinterpret_cast<uint4 *>(out) =
                       make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
@@ -785,14 +813,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               part[COLS * HD + col] = m;
               part[COLS * HD + COLS + col] = l;
             } else if (p.lse && col < rows && !dead) {
-              p.lse[(int64_t)(at.first + col / p.group) * p.n_heads + at.head * p.group + col % p.group] =
+              p.lse[token * p.n_heads + head] =
                   l == 0.f ? -INFINITY : 0.69314718056f * m + logf(l);
             }
           }
         }
       }
     }
-    if (flat + 1 < w1) next_tile(at, p.n_seqs, heads, info, prefix, p.window);
+    if (flat + 1 < w1) next_tile<COLS>(at, info, prefix, p);
   }
 
   // ---- partial results of this block, in list order ([warp][0: its first segment's, 1: its last's], without the
@@ -815,9 +843,11 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   __syncthreads();
   // a segment's places in the list, and how it stands to this block's: whole, or begun (0) or continued (1) elsewhere
   const auto segment = [&](int id, Cursor &c, int64_t &sa, int64_t &sb) {
-    c.seq = id / heads, c.head = id - c.seq * heads;
-    enter_sequence(c, info, prefix, p.window);
-    sa = (int64_t)prefix[c.seq] * heads + c.head * c.n_tiles, sb = sa + c.n_tiles;
+    const int of_head = id / p.most_blocks;
+    c.block = id - of_head * p.most_blocks;
+    c.seq = of_head / heads, c.head = of_head - c.seq * heads;
+    enter_sequence<COLS>(c, info, prefix, p);
+    sa = (int64_t)prefix[c.seq] * heads + (c.head * c.blocks + c.block) * c.n_tiles, sb = sa + c.n_tiles;
   };
   Cursor seg;
   int64_t sa, sb;
@@ -830,7 +860,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       const int k = u / (COLS / NC), col = u % (COLS / NC) * NC, id = across ? cut[k] : part_seg[k];
       if (id < 0) continue;
       segment(id, seg, sa, sb);
-      const int rows_here = seg.count * p.group;
+      const int rows_here = seg.count * p.group - seg.block * COLS;
       if (col >= rows_here) continue;
       const int first = across ? span[2 * k] : group_at[k], n = across ? span[2 * k + 1] : group_at[k + 1] - first;
       const auto nth = [&](int i) {
@@ -847,7 +877,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         if (whole) {
-          if (col + c < rows_here) store_row<HD>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
+          if (col + c < rows_here) store_row<HD, COLS>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
         } else {
 #pragma unroll
           for (int j = 0; j < HD / 32; ++j) to[(col + c) * HD + lane * (HD / 32) + j] = v[c][j];
@@ -885,7 +915,7 @@ cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   const cudaError_t e = opt_in(kernel, F::SMEM);
   if (e != cudaSuccess) return e;
   // as many blocks as the longest contexts could fill
-  const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
+  const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks * (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
   return launch_chained(kv4_attend_few_kernel<HD, NT>, grid, F::THREADS, F::SMEM, s, p);
 }

@@ -306,3 +306,43 @@ def test_offsets_behind_4_gib():
             ref, size, _ = ora.attend(q[:, h].double().numpy(), kd[:, h // 8], vd[:, h // 8], np.arange(200 - t, 200), hd ** -0.5)
             err = np.abs(out[:, h].double().cpu().numpy() - ref)
             assert (err <= 2.0 ** -9 * np.abs(ref) + 2.0 ** -8 * size).all()
+
+
+def test_one_workspace_serves_calls_of_all_smaller_sizes():
+    """Calls of other shapes leave nothing where a call looks for its tickets."""
+    c = Case([3000, 17, 2100, 64] + [90] * 60, 2, 128, 64, seed=8)
+    kv4 = c.kv4
+    pool = kv4.pool(torch.from_numpy(c.pool).cuda(), c.page, 1, 2, 128)
+    ws = kv4.attend_workspace(pool, 16, 64, 400, 200)
+    shapes = [dict(tokens=[1] * 64), dict(tokens=[6, 1, 4] + [1] * 61), dict(tokens=[2] * 64), dict(tokens=[200, 17, 50, 1] + [1] * 60), dict()]
+    alone = []
+    for kw in shapes:
+        n = sum(kw.get("tokens", [1] * 64))
+        alone.append(c.run(queries(n, 16, 128, seed=n), **kw)[0])
+    for _ in range(2):
+        for kw, want in zip(shapes + shapes[::-1], alone + alone[::-1]):
+            n = sum(kw.get("tokens", [1] * 64))
+            got, _ = c.run(queries(n, 16, 128, seed=n), workspace=ws, **kw)
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("hd,kv_heads,group,page,dtype", [(128, 2, 8, 64, BF16), (128, 2, 7, 16, FP16), (64, 2, 12, 32, BF16), (64, 1, 1, 128, FP16)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_drafts_in_blocks_of_rows(hd, kv_heads, group, page, dtype, window):
+    """Token counts whose rows fill one to three blocks of sixteen, mixed, some of them more than there are cached rows."""
+    most = 48 // group
+    tokens = [1, most, (most + 1) // 2, 0, most, min(most, 3)]
+    c = Case([5, 700, 64, 9, most - 1 if most > 1 else 1, 130], kv_heads, hd, page, seed=group)
+    c.check(queries(sum(tokens), kv_heads * group, hd, dtype), tokens=tokens, window=window)
+
+
+def test_long_contexts_keep_the_precision_of_short_ones():
+    """65536 rows of nearly even weights: the small mean of many values of either sign.  The weights' rounding to fp16 (2^-12)
+    is independent over the rows, as the values are: relative to the output 2^-12 as well, and an fp16 output's own 2^-11."""
+    n, hd = 65536, 128
+    c = Case([n], 1, hd, 128, seed=1)
+    q = queries(1, 8, hd, FP16, std=0.2)
+    got, _ = c.run(q)
+    ref, _, _ = c.expected(q)
+    err = np.linalg.norm(got.double().cpu().numpy() - ref) / np.linalg.norm(ref)
+    assert err <= 2.0 ** -11 + 2.0 ** -12
