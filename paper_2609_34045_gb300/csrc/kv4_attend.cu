@@ -1,7 +1,7 @@
 // Attention over the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_attend.
 //
-// Up to 48 query rows per KV head (a decode step's group, a few drafted tokens) go to the kernel that streams the cache
-// (kv4_attend_few.cu), more to the one that multiplies 128 rows at a time (kv4_attend_prompt.cu).
+// Few query rows per KV head (a decode step's group, some drafted tokens) go to the kernel that streams the cache, sixteen
+// rows at a time (kv4_attend_few.cu), more to the one that multiplies 128 rows at a time (kv4_attend_prompt.cu).
 #include <math.h>
 
 #include <algorithm>
@@ -10,6 +10,20 @@
 
 namespace kfl {
 namespace {
+
+// Which kernel: the first reads and decodes a tile once for every sixteen rows, the second once for all, at a larger cost
+// to begin with.  us, heads of 128, 8 KV heads, first against second:
+//   sequences x keys      24 rows        32 rows        40 rows        48 rows
+//    1 x 1000            18.0   23.3    18.2   23.8    18.2   24.1    18.3   24.9
+//    4 x 3000            34.8   33.4    34.8   33.8    39.7   34.4    40.2   35.0
+//   16 x 8192             117    121     118    122     168    123     168    124
+//   64 x 4096             219    254     221    255     321    255     323    257
+// The contexts' lengths are on the device: the third sixteen rows go by what the tables could hold.
+bool is_few(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int n_seqs, int64_t rows) {
+  if (rows <= 32) return true;
+  return rows <= FEW_ROWS && n_seqs <= 65536 &&
+         (int64_t)n_seqs * pool->n_kv_heads * map->max_pages * pool->page_tokens <= 65536;
+}
 
 int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_seqs, int n_tokens, int max_q,
                  bool bytes) {
@@ -39,7 +53,8 @@ extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_he
   if (!out) return bad_arg(me, "NULL pointer");
   const int64_t rows = (int64_t)max_q * (n_heads / pool->n_kv_heads);
   *out = TICKET_BYTES +
-         (rows <= FEW_ROWS ? attend_few_partials(pool->head_dim, few_cols(rows)) : attend_prompt_partials(pool->head_dim, rows));
+         (rows <= 32 ? attend_few_partials(pool->head_dim, few_cols(rows))
+                     : std::max(attend_few_partials(pool->head_dim, 16), attend_prompt_partials(pool->head_dim, rows)));
   return KFL_OK;
 }
 
@@ -74,7 +89,8 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.scale = scale, p.window = window, p.status = status;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)p.max_q * p.group;
-  p.most_blocks = rows <= FEW_ROWS ? (int)((rows + few_cols(rows) - 1) / few_cols(rows)) : 0;
+  const bool few = is_few(pool, map, n_seqs, rows);
+  p.most_blocks = few ? (int)((rows + few_cols(rows) - 1) / few_cols(rows)) : 0;
   p.tickets = static_cast<unsigned *>(workspace);
   p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + TICKET_BYTES);
   int dev = 0, n_sm = 0;
@@ -83,7 +99,7 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
     p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
     p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
-    e = rows <= FEW_ROWS ? launch_attend_few(p, few_cols(rows), n_sm, s) : launch_attend_prompt(p, n_sm, s);
+    e = few ? launch_attend_few(p, few_cols(rows), n_sm, s) : launch_attend_prompt(p, n_sm, s);
   }
   return cuda_result(e, me);
 }

@@ -359,24 +359,30 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   unsigned valid[F::SLOTS] = {};  // which 16 keys of a slot's tile are there, a bit each
   bool dead = false;              // a wait gave up: no more copies, no results
   const auto issue = [&]() {
-    const bool there = fetch_page >= 0 && fetch_page < p.pool.n_pages;
-    if (fetch_page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-    const unsigned lanes = __ballot_sync(0xffffffffu, there);
-    unsigned have = lanes & 1 ? ALL : 0;
-    if (lp < LOG_TILE) {
-      have = 0;
+    const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
+    unsigned have = 0;
+    if (lp == LOG_TILE) {
+      // (an elected lane of a page number that all have: one instruction and not a loop over the lanes)
+      const int page = __shfl_sync(0xffffffffu, fetch_page, 0);
+      const bool there = page >= 0 && page < p.pool.n_pages;
+      if (there) have = ALL;
+      if (elect_one()) {
+        if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+        mbar_arrive_expect_tx(bar, there ? F::TILE_BYTES : 0);
+        if (there) bulk_g2s(dst, layer_pages + (unsigned)page * page_bytes + (unsigned)(fetch.head * block_bytes), F::TILE_BYTES, bar, policy);
+      }
+      __syncwarp();
+    } else {
+      const bool there = fetch_page >= 0 && fetch_page < p.pool.n_pages;
+      if (fetch_page != -2 && !there) report(p.status, KFL_BAD_PAGE);
+      const unsigned lanes = __ballot_sync(0xffffffffu, there);
 #pragma unroll
       for (int i = 0; i < TILE / 16; ++i) have |= (lanes >> ((16 * i >> lb) * 4) & 1) << i;
-    }
-    const uint32_t bar = bar0 + fetch_slot * 8, dst = ring + fetch_slot * F::TILE_BYTES;
-    if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / (TILE / 16)));
-    __syncwarp();
-    if (there) {
-      const uint8_t *src = layer_pages + fetch_page * page_bytes + (unsigned)(fetch.head * block_bytes);
-      if (lp == LOG_TILE) {
-        bulk_g2s(dst, src, F::TILE_BYTES, bar, policy);
-      } else {
+      if (lane == 0) mbar_arrive_expect_tx(bar, __popc(have) * (F::TILE_BYTES / (TILE / 16)));
+      __syncwarp();
+      if (there) {
         // part 0, 1: codes of K, V; 2, 3: parameters.  A larger page holds several tiles
+        const uint8_t *src = layer_pages + (unsigned)fetch_page * page_bytes + (unsigned)(fetch.head * block_bytes);
         const int part = lane & 3, block = lane >> 2, size = part < 2 ? CODES : PARAMS, bytes = size >> (LOG_TILE - lb);
         const int to = (part < 2 ? 0 : 2 * CODES) + (part & 1) * size;  // as in a page of a tile's size
         const int more = lp - LOG_TILE, nth = more > 0 ? (fetch.first_tile + fetch.tile) & ((1 << more) - 1) : 0;
