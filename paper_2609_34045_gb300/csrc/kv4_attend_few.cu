@@ -3,15 +3,17 @@
 // Mathematics.  For a KV head's query rows (token, head of its group) j and its keys t:
 //   x_tj = scale log2(e) sum_g [ s_tg sum_c (u_tc - 8) q_jc + c_tg sum_c q_jc ]        (g: groups of 64 channels)
 //   o_j = sum_t 2^(x_tj - m_j) [ s'_tg (u'_tc - 8) + c'_tg ] / sum_t 2^(x_tj - m_j)
-// The codes enter the matrix products as they are: an fp16 with the nibble in its mantissa is 16 (64 + u), exactly.
-// For the scores the 72 too many are taken off by the accumulator's start value -1152 sum q; for the values
-// the weights 2^(x - m) s' are the fp16 operand and 72 times their own sum (a product with ones) is taken off at
-// the end.  The scales so cost one factor per key and group, not per element, a group that reads as NaN
-// reaches exactly the rows that see it, and codes behind a user's end (any bits) are finite.
+// The codes enter the matrix products as they are, a nibble with zeros around it being an fp16 u 2^-24 or u 2^-20.  For
+// the scores the 8 too many are taken off by the accumulator's start value -8 sum q; for the values the weights
+// 2^(x - m) s' are the fp16 operand and 8 times their own sum (a product with ones) is taken off at the end.  (An
+// offset as large as the 64 of a nibble set in the mantissa of a normal fp16 would be lost to the matrix unit's
+// truncation: 3e-8 of the sum at every step, always downwards, made 131072 keys 4.4e-3 wrong.)  The scales so cost one
+// factor per key and group, not per element, a group that reads as NaN reaches exactly the rows that see it, and
+// codes behind a user's end (any bits) are finite.
 //
 // What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
-// keeps up.  At 6.77 TB/s an SM gets 42 elements a clock; with 0.875 (K) and 1.0 (V) instructions per element
-// for the nibbles and some 0.7 for the rest it has to issue about 2 of 4 instructions a clock.
+// keeps up.  At 6.77 TB/s an SM gets 42 elements a clock, its logic units do 64 operations: 0.6 (K) and 0.75 (V) per
+// element for the nibbles and some 0.4 for the rest.
 //
 // Layout.  S^T = K Q^T and O^T = V^T P^T with m16n8k16: keys and channels fill M = 16, the query rows N = 8, nothing
 // is padded at 8 rows.  The matrix unit's k order is ours to choose, so a lane's K words hold whole fragments
@@ -26,7 +28,6 @@
 #include <type_traits>
 
 #include "kv4_attend.cuh"
-#include "prefill_tc.cuh"  // hfma2
 
 namespace kfl {
 namespace {
@@ -85,22 +86,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 __device__ __forceinline__ float half_lo(uint32_t x) { return __low2float(*reinterpret_cast<const __half2 *>(&x)); }
 __device__ __forceinline__ float half_hi(uint32_t x) { return __high2float(*reinterpret_cast<const __half2 *>(&x)); }
 
-// The nibbles of a word's bytes 0 and 2 as two fp16 pairs, exactly: the low ones as u, the high ones as 16 (64 + u).  A byte
-// and its high nibble in the mantissa of fp16 1024 differ by the low one; the difference runs beside the logic unit, which
-// bounds this kernel (64 of its operations a clock, against 128 others).
+// The nibbles of a word's bytes 0 and 2 as two fp16 pairs, as they stand: whole numbers below 2048 in the bits of an fp16
+// are that many times 2^-24 (its subnormal numbers and the first binade above), exactly, and the matrix unit takes them as
+// any others.  The low nibbles are u 2^-24, the high ones u 2^-20.
 __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t &low, uint32_t &high) {
-  uint32_t both;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(both) : "r"(w), "r"(0x00FF00FFu), "r"(0x64006400u));
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(high) : "r"(w), "r"(0x00F000F0u), "r"(0x64006400u));
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(low) : "r"(both), "r"(high));
+  low = w & 0x000F000Fu;
+  high = w & 0x00F000F0u;
 }
-// The same for V, the high nibbles as u - 8: a sum over many keys of 64 + u, small weights of either sign in the end, would
-// lose to the matrix unit's truncation (3e-8 of the sum at every step, always downwards: 131072 keys came out 4.4e-3 off, and
-// 1.7e-3 is bf16's own rounding).  The low ones' 8 too many are few enough.
-__device__ __forceinline__ void value_pairs(uint32_t w, uint32_t &low, uint32_t &high) {
-  code_pairs(w, low, high);
-  high = hfma2(high, 0x2C002C00u, 0xD480D480u);  // / 16 - 72, exactly
-}
+constexpr float LOW = 0x1p-24f, HIGH = 0x1p-20f;
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
@@ -466,7 +459,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                // (even channels meet u and odd ones 16 (64 + u): 16 times the query for the even ones)
+                // (odd channels' codes are 16 times the even ones': a sixteenth of the query)
                 const uint32_t two = __byte_perm(raw[n][g][4 * j + h], raw[n][g][4 * j + h + 2], k ? 0x7632 : 0x5410);
                 const float lo = p.bf16 ? bf16_lo(two) : half_lo(two), hi = p.bf16 ? bf16_hi(two) : half_hi(two);
                 const float r = k ? inv * 0.0625f : inv;
@@ -477,13 +470,13 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             }
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            qs[n][g][c] = fmaf(16.f, odd[c], even[c]);
-            seed[n][g][c] = seed[n][g][c + 2] = fmaf(-1152.f, odd[c], -8.f * even[c]);
+            qs[n][g][c] = LOW * fmaf(16.f, odd[c], even[c]);
+            seed[n][g][c] = seed[n][g][c + 2] = -8.f * qs[n][g][c];
             centre[n][g][c] = 0.f;
           }
         }
         // (columns of the accumulators: 2 tig, 2 tig + 1)
-        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);  // (not 0: -inf times it stays)
+        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale * (1.f / LOW), 1e-37f);  // (not 0: -inf times it stays)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           cf[n][c] = __shfl_sync(0xffffffffu, factor, (2 * tig + c) * 4);
@@ -729,14 +722,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           const uint32_t wc = lds32(vb + g * 32 + 8 * (HD / 2)), wd = lds32(vb + g * 32 + 12 * (HD / 2));
           // [byte 0 or 1 of the tokens' words' lower, upper half][which two tokens]: the pairs of two tiles of 16 channels
           uint32_t x0[2][2], x1[2][2], y0[2][2], y1[2][2];  // low and high nibbles of: lower half, upper half
-          value_pairs(__byte_perm(wa, wb, 0x5410), x0[0][0], x1[0][0]);
-          value_pairs(__byte_perm(wa, wb, 0x5511), x0[1][0], x1[1][0]);
-          value_pairs(__byte_perm(wa, wb, 0x7632), y0[0][0], y1[0][0]);
-          value_pairs(__byte_perm(wa, wb, 0x7733), y0[1][0], y1[1][0]);
-          value_pairs(__byte_perm(wc, wd, 0x5410), x0[0][1], x1[0][1]);
-          value_pairs(__byte_perm(wc, wd, 0x5511), x0[1][1], x1[1][1]);
-          value_pairs(__byte_perm(wc, wd, 0x7632), y0[0][1], y1[0][1]);
-          value_pairs(__byte_perm(wc, wd, 0x7733), y0[1][1], y1[1][1]);
+          code_pairs(__byte_perm(wa, wb, 0x5410), x0[0][0], x1[0][0]);
+          code_pairs(__byte_perm(wa, wb, 0x5511), x0[1][0], x1[1][0]);
+          code_pairs(__byte_perm(wa, wb, 0x7632), y0[0][0], y1[0][0]);
+          code_pairs(__byte_perm(wa, wb, 0x7733), y0[1][0], y1[1][0]);
+          code_pairs(__byte_perm(wc, wd, 0x5410), x0[0][1], x1[0][1]);
+          code_pairs(__byte_perm(wc, wd, 0x5511), x0[1][1], x1[1][1]);
+          code_pairs(__byte_perm(wc, wd, 0x7632), y0[0][1], y1[0][1]);
+          code_pairs(__byte_perm(wc, wd, 0x7733), y0[1][1], y1[1][1]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const uint32_t b0 = pf[n][g][0], b1 = pf[n][g][1];
@@ -788,8 +781,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = fmaf(i & 1 ? o[n][g][i & 3][c + 2 * (i >> 2)] : fmaf(-8.f, ones[n][g][c], o[n][g][i & 3][c + 2 * (i >> 2)]),
-                          unit, cen);
+              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 1.f / HIGH : 1.f / LOW, -8.f * ones[n][g][c]), unit, cen);
             if (alone) {
               if (col < rows && !dead) {
                 uint16_t h[8];
