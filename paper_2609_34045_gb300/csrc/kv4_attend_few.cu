@@ -1,4 +1,4 @@
-// Attention over the 4-bit paged KV cache for few query rows per KV head (decode steps, short drafts).
+// Attention over the 4-bit paged KV cache for few query rows per KV head (decode steps, drafts), eight or sixteen at once.
 //
 // Mathematics.  For a KV head's query rows (token, head of its group) j and its keys t:
 //   x_tj = scale log2(e) sum_g [ s_tg sum_c (u_tc - 8) q_jc + c_tg sum_c q_jc ]        (g: groups of 64 channels)
@@ -13,16 +13,19 @@
 //
 // What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
 // keeps up.  At 6.77 TB/s an SM gets 42 elements a clock, its logic units do 64 operations: 0.6 (K) and 0.75 (V) per
-// element for the nibbles and some 0.4 for the rest.
+// element for the nibbles and some 0.4 for the rest.  Measured: 32 users at 412 to 8192 keys, 64/8 heads of 128 (160 MB)
+// 50.7 us; one user at 131072 keys (151 MB) 43.4 us, 3.4 TB/s: some 30 us of tiles, which 12 warps of 168 registers work off at
+// about 0.7 of the copy rate, and 12 us of start, partial results and merge.  Clocks say that the copies are waited for in
+// one of sixty.
 //
 // Layout.  S^T = K Q^T and O^T = V^T P^T with m16n8k16: keys and channels fill M = 16, the query rows N = 8, nothing
 // is padded at 8 rows.  The matrix unit's k order is ours to choose, so a lane's K words hold whole fragments
 // in natural byte order, and V's pairs of tokens come together by one byte permute per eight codes.
 //
-// Work split.  The tiles (64 keys of one sequence and KV head) of all sequences form one list; one block per SM takes
-// an equal piece, its warps equal pieces of that.  A warp streams its tiles through two slots of its own
+// Work split.  The tiles (64 keys of one sequence, KV head and sixteen query rows) of all sequences form one list; one
+// block per SM takes an equal piece, its warps equal pieces of that.  A warp streams its tiles through two slots of its own
 // (bulk copies of whole page blocks), with no barrier between warps until the end.  What a warp holds of a
-// (sequence, head) that it does not own alone is merged within the block, then over blocks by the last to arrive;
+// segment (sequence, head, rows) that it does not own alone is merged within the block, then over blocks by the last to arrive;
 // every sum is taken in list order, so results do not depend on arrival.
 #include <algorithm>
 #include <type_traits>
@@ -35,11 +38,13 @@ namespace {
 constexpr int LOG_TILE = 6, TILE = 1 << LOG_TILE;  // keys
 constexpr float WEIGHT_UNIT = 2048.f;  // fp16 weights: 2^(x - m) times this, at most WEIGHT_MOST times as much
 constexpr float WEIGHT_MOST = 16.f;
-constexpr int SUB = 2;    // groups of 16 keys that are worked on at once
+// Groups of 16 keys that are worked on at once: 1, 2 and 4 take 54, 51 and 58 us for 32 ragged users (more steps; more code than
+// the instruction cache next to the scheduler holds)
+constexpr int SUB = 2;
 
 template <int HD, int NT>
 struct Few {
-  // 12 warps of at most 168 registers; with 16 query rows 8 warps of 255
+  // 12 warps of at most 168 registers (11: 53 us for 51; 16 spill); with 16 query rows 8 warps of 255
   static constexpr int WARPS = NT == 1 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int COLS = 8 * NT;
@@ -362,7 +367,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       if (elect_one()) {
         if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
         mbar_arrive_expect_tx(bar, there ? F::TILE_BYTES : 0);
-        if (there) bulk_g2s(dst, layer_pages + (unsigned)page * page_bytes + (unsigned)(fetch.head * block_bytes), F::TILE_BYTES, bar, policy);
+        const uint8_t *src = layer_pages + (unsigned)page * page_bytes + (unsigned)(fetch.head * block_bytes);
+        if (there) bulk_g2s(dst, src, F::TILE_BYTES, bar, policy);
       }
       __syncwarp();
     } else {
@@ -411,29 +417,29 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       // 16 channels of each group for column gid; under way before the first tiles' copies, whose page numbers come first
       uint32_t raw[NT][G][8];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int col = n * 8 + gid;
-          const bool there = col < at.count * p.group - at.block * COLS;
-          int64_t token;
-          int head;
-          row_of<COLS>(at, col, p, token, head);
-          const uint16_t *e = reinterpret_cast<const uint16_t *>(there ? p.q.row(token, head) : nullptr) +
-                              tig * 16;
+      for (int n = 0; n < NT; ++n) {
+        const int col = n * 8 + gid;
+        const bool there = col < at.count * p.group - at.block * COLS;
+        int64_t token;
+        int head;
+        row_of<COLS>(at, col, p, token, head);
+        const uint16_t *e = reinterpret_cast<const uint16_t *>(there ? p.q.row(token, head) : nullptr) +
+                            tig * 16;
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            if (!there) {
+        for (int g = 0; g < G; ++g) {
+          if (!there) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) raw[n][g][i] = 0;
-            } else if (p.q_wide) {
-              const uint4 a = *reinterpret_cast<const uint4 *>(e + 64 * g), b = *reinterpret_cast<const uint4 *>(e + 64 * g + 8);
-              raw[n][g][0] = a.x, raw[n][g][1] = a.y, raw[n][g][2] = a.z, raw[n][g][3] = a.w;
-              raw[n][g][4] = b.x, raw[n][g][5] = b.y, raw[n][g][6] = b.z, raw[n][g][7] = b.w;
-            } else {
+            for (int i = 0; i < 8; ++i) raw[n][g][i] = 0;
+          } else if (p.q_wide) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(e + 64 * g), b = *reinterpret_cast<const uint4 *>(e + 64 * g + 8);
+            raw[n][g][0] = a.x, raw[n][g][1] = a.y, raw[n][g][2] = a.z, raw[n][g][3] = a.w;
+            raw[n][g][4] = b.x, raw[n][g][5] = b.y, raw[n][g][6] = b.z, raw[n][g][7] = b.w;
+          } else {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) raw[n][g][i] = e[64 * g + 2 * i] | ((uint32_t)e[64 * g + 2 * i + 1] << 16);
-            }
+            for (int i = 0; i < 8; ++i) raw[n][g][i] = e[64 * g + 2 * i] | ((uint32_t)e[64 * g + 2 * i + 1] << 16);
           }
         }
+      }
       if (flat == w0) issue();
       rows = at.count * p.group - at.block * COLS;
 #pragma unroll
@@ -476,7 +482,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           }
         }
         // (columns of the accumulators: 2 tig, 2 tig + 1)
-        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale * (1.f / LOW), 1e-37f);  // (not 0: -inf times it stays)
+        // (not 0: -inf times it stays)
+        const float factor = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale * (1.f / LOW), 1e-37f);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           cf[n][c] = __shfl_sync(0xffffffffu, factor, (2 * tig + c) * 4);
@@ -781,7 +788,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 1.f / HIGH : 1.f / LOW, -8.f * ones[n][g][c]), unit, cen);
+              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 1.f / HIGH : 1.f / LOW, -8.f * ones[n][g][c]),
+                          unit, cen);
             if (alone) {
               if (col < rows && !dead) {
                 uint16_t h[8];
@@ -913,7 +921,8 @@ cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   const cudaError_t e = opt_in(kernel, F::SMEM);
   if (e != cudaSuccess) return e;
   // as many blocks as the longest contexts could fill
-  const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks * (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
+  const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks *
+                       (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
   return launch_chained(kv4_attend_few_kernel<HD, NT>, grid, F::THREADS, F::SMEM, s, p);
 }

