@@ -91,6 +91,15 @@ template <class T, int V>
 struct alignas(V == 1 ? sizeof(T) : 16) Pack {
   T e[V];
 };
+// Moves one as one access (assigned, its elements may be moved one by one).
+template <int V, class T>
+__device__ __forceinline__ void move_pack(T *dst, const T *src) {
+  static_assert(V == 1 || V * sizeof(T) == 16, "an element or 16 bytes");
+  if constexpr (V == 1)
+    *dst = *src;
+  else
+    *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(src);
+}
 
 // a' = a c - b s and b' = b c + a s with every product and sum rounded: the same values whatever the
 // compiler would fuse, so that a cache's codes do not hang on it.

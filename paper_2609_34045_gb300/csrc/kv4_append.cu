@@ -54,7 +54,7 @@ __device__ __forceinline__ Raw<T> load_raw(const T *p) {
   if constexpr (WIDE) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < CH; i += W) *reinterpret_cast<Pack<T, W> *>(r.e + i) = *reinterpret_cast<const Pack<T, W> *>(p + i);
+    for (int i = 0; i < CH; i += W) move_pack<W>(r.e + i, p + i);
   } else {
 #pragma unroll
     for (int i = 0; i < CH; ++i) r.e[i] = p[i];
@@ -217,7 +217,7 @@ __device__ __forceinline__ void store_values(uint2 codes, uint32_t params, T *ds
   if constexpr (WIDE) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < CH; i += W) *reinterpret_cast<Pack<T, W> *>(dst + i) = *reinterpret_cast<Pack<T, W> *>(v.e + i);
+    for (int i = 0; i < CH; i += W) move_pack<W>(dst + i, v.e + i);
   } else {
 #pragma unroll
     for (int i = 0; i < CH; ++i) dst[i] = v.e[i];
