@@ -3,9 +3,12 @@
 // Memory bound in bytes (a 16-bit value read and 4.5 bits written, or the reverse), if the instructions per value stay
 // below some 12: at 41 (eight channels a thread, integer divisions of 64 bits, a code's clamp and shift one by one) 16384 rows
 // of 8 heads took 49 us against 13 for their bytes.  So sixteen channels of a k row and of its v row to a thread, four
-// threads to a group of 64, whose ends meet in two shuffles; a code is six operations, its place in the word the last of
-// them: 36 us, and 20 for reading the rows back.  The rotation's partner channels are read once more, from L1, rather than exchanged: the partner may lie in any other
-// thread or in the same one, depending on layout and rope_dim.
+// threads to a group of 64, whose ends meet in two shuffles; a code is four operations, its place in the word the last of
+// them, and two more where a group's ends need a clamp.  19 us for these rows unrotated, 25 rotated in neighbouring
+// pairs, 31 in halves, 18 for reading them back.  The difference is the angles: 8 bytes for each pair, which the L1 looks up a
+// line at a time.  Through shared memory they cost a barrier that waits for them (29 and 28 us); with the next rows' loads
+// under way in a loop the registers leave half the warps (34 us).  The rotation's partner channels are read once more,
+// from L1, rather than exchanged: the partner may lie in any other thread or in the same one, depending on layout and rope_dim.
 #include "kv4.cuh"
 
 namespace kfl {
@@ -104,27 +107,63 @@ __device__ __forceinline__ void rotate(const RowsParams &p, const T *row, int c,
   }
 }
 
-// Smaller and larger of two, NaN if one is.
-__device__ __forceinline__ float min_nan(float a, float b) {
+// Smallest and largest of three, NaN if one is.
+__device__ __forceinline__ float min_nan(float a, float b, float c) {
   float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+// Two rounded sums or products in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// Eight codes from t = (x - centre) / scale: clamp(rint(t) + 8, 0, 15).  t is clamped first (to whole numbers: the order is
+// of no account), and its sum with 1.5 2^23 + 8, rounded to whole numbers, has rint(t) + 8 as its last bits.  The other
+// bits of the eight sums, one on the other at 16 times the place, are a constant.
+template <bool CLAMPS>
+__device__ __forceinline__ uint32_t codes8(const float *x, float centre, float inv) {
+  constexpr uint32_t MAGIC = 0x4B400000u;
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 6; i >= 0; i -= 2) {
+    float2 t = mul2(add2({x[i], x[i + 1]}, {-centre, -centre}), {inv, inv});
+    if (CLAMPS) t = {fminf(fmaxf(t.x, -8.f), 7.f), fminf(fmaxf(t.y, -8.f), 7.f)};
+    // (not add2: two-fold, the product and this sum come out as one operation, and ties go elsewhere)
+    w = w * 16 + __float_as_uint(__fadd_rn(t.y, 12582920.f));
+    w = w * 16 + __float_as_uint(__fadd_rn(t.x, 12582920.f));
+  }
+  return w - MAGIC * 0x11111111u;
 }
 
 // Codes of sixteen channels; their group is the warp's aligned four lanes, which all call.
 __device__ __forceinline__ uint2 quantise(const float (&x)[CH], uint32_t &params) {
-  float lo = x[0], hi = x[0];
+  float lo = min_nan(x[0], x[1], x[2]), hi = max_nan(x[0], x[1], x[2]);
 #pragma unroll
-  for (int i = 1; i < CH; ++i) lo = min_nan(lo, x[i]), hi = max_nan(hi, x[i]);
+  for (int i = 3; i < CH - 1; i += 2) lo = min_nan(lo, x[i], x[i + 1]), hi = max_nan(hi, x[i], x[i + 1]);
+  lo = min_nan(lo, x[CH - 1], x[CH - 1]), hi = max_nan(hi, x[CH - 1], x[CH - 1]);
 #pragma unroll
   for (int off = 2; off > 0; off >>= 1) {
-    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, off));
-    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, off));
+    const float l = __shfl_xor_sync(0xffffffffu, lo, off), h = __shfl_xor_sync(0xffffffffu, hi, off);
+    lo = min_nan(lo, l, l), hi = max_nan(hi, h, h);
   }
   if (!(hi <= KV4_LIMIT && lo >= -KV4_LIMIT)) {  // (or NaN)
     params = 0x7FFF7FFFu;
@@ -135,24 +174,12 @@ __device__ __forceinline__ uint2 quantise(const float (&x)[CH], uint32_t &params
   const __half centre_h = __float2half_rn(__fadd_rn(lo, 8.f * scale));
   const float centre = __half2float(centre_h);
   const float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
-  // clamp(rint(t) + 8, 0, 15): t is clamped first (to whole numbers: the order is of no account), and its sum with
-  // 1.5 2^23 + 8, rounded to whole numbers, has rint(t) + 8 as its last bits.  The other bits of the eight sums, one
-  // on the other at 16 times the place, are a constant.
-  constexpr uint32_t MAGIC = 0x4B400000u;
-  constexpr uint32_t REST = MAGIC * 0x11111111u;
-  uint32_t w[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    w[j] = 0;
-#pragma unroll
-    for (int i = 7; i >= 0; --i) {
-      const float t = __fmul_rn(__fsub_rn(x[8 * j + i], centre), inv);
-      w[j] = w[j] * 16 + __float_as_uint(__fadd_rn(fminf(fmaxf(t, -8.f), 7.f), 12582920.f));
-    }
-    w[j] -= REST;
-  }
   params = (uint32_t)__half_as_ushort(scale_h) | ((uint32_t)__half_as_ushort(centre_h) << 16);
-  return make_uint2(w[0], w[1]);
+  // the group's ends have the ends of t: where those need no clamp (a centre whose rounding to fp16 is far below a step),
+  // none does
+  if (__fmul_rn(__fsub_rn(lo, centre), inv) >= -8.5f && __fmul_rn(__fsub_rn(hi, centre), inv) < 7.5f)
+    return make_uint2(codes8<false>(x, centre, inv), codes8<false>(x + 8, centre, inv));
+  return make_uint2(codes8<true>(x, centre, inv), codes8<true>(x + 8, centre, inv));
 }
 
 // The (token, head) of a unit: below 2^31 of them (checked by the host).
@@ -166,7 +193,7 @@ __device__ __forceinline__ Unit unit_of(const RowsParams &p, unsigned u) {
 }
 
 template <class T, bool WIDE>
-__global__ void __launch_bounds__(ROW_THREADS) kv4_append_kernel(const RowsParams p) {
+__global__ void __launch_bounds__(ROW_THREADS, 4) kv4_append_kernel(const RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
   const int lanes = p.pool.head_dim / CH, shift = p.pool.head_dim == 128 ? 3 : 2;  // threads of a row
