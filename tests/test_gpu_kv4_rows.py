@@ -303,3 +303,22 @@ def test_on_another_stream_and_captured():
     step(torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert torch.equal(out, again) and not torch.equal(out, first)
+
+
+@pytest.mark.parametrize("offset", [0.0, 3.0, 1000.0, -20000.0])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32], ids=["bf16", "fp16", "fp32"])
+def test_groups_far_from_zero(offset, dtype):
+    """The centre's rounding to fp16 is up to many steps there: codes are clamped in some groups, not in others."""
+    hd, kv, page, n = 128, 2, 64, 70
+    kv4, pool_t, p, m, _ = cache([n], kv, hd, page)
+    x = (randn((n, 2 * kv, hd), FP32, seed=11) * torch.logspace(-3, 1, n, device="cuda")[:, None, None] + offset).to(dtype)
+    k, v = x[:, :kv], x[:, kv:]
+    users, pos = int32(np.zeros(n)), int32(np.arange(n))
+    kv4.kfl_kv4_append(p, m, 0, k, v, users, pos)
+    out = [torch.empty(n, kv, hd, dtype=FP32, device="cuda") for _ in range(2)]
+    kv4.kfl_kv4_read(p, m, 0, users, pos, *out)
+    for a, b in zip((k, v), out):
+        codes, params = ora.quantise(a.float().cpu().numpy())
+        assert torch.equal(b.cpu(), torch.from_numpy(ora.values(codes, params).astype(np.float32)))
+    if abs(offset) == 1000.0:
+        assert codes.max() == 15 and any((g == 0).sum() > 1 for g in codes.reshape(-1, 64))
