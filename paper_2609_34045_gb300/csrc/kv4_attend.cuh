@@ -21,6 +21,7 @@ struct AttendParams {
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
   float scale;
   int window;
+  unsigned group_inv;  // 2^16 / group, rounded up
   int most_blocks;    // few rows: of a KV head's query rows, in blocks of few_cols
   unsigned *tickets;  // zero between launches: [n_seqs][n_kv_heads][most_blocks], many rows: [FEW_BLOCKS]
   float *partials;

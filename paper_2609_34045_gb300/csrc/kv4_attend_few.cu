@@ -14,7 +14,7 @@
 // What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
 // keeps up.  At 6.77 TB/s an SM gets 42 elements a clock, its logic units do 64 operations: 0.6 (K) and 0.75 (V) per
 // element for the nibbles and some 0.4 for the rest.  Measured: 32 users at 412 to 8192 keys, 64/8 heads of 128 (160 MB)
-// 50.7 us; one user at 131072 keys (151 MB) 43.4 us, 3.4 TB/s: some 30 us of tiles, which 12 warps of 168 registers work off at
+// 46.4 us; one user at 131072 keys (151 MB) 42.6 us, 3.5 TB/s: some 30 us of tiles, which 12 warps of 168 registers work off at
 // about 0.7 of the copy rate, and 12 us of start, partial results and merge.  Clocks say that the copies are waited for in
 // one of sixty.
 //
@@ -51,9 +51,10 @@ struct Few {
   static constexpr int GROUPS = HD / KV4_GROUP;
   static constexpr int TILE_BYTES = TILE * HD * 9 / 8;
   static constexpr int SLOTS = HD == 128 ? 2 : 3;
-  static constexpr int PARTIAL = COLS * HD + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
+  static constexpr int COL = HD + 4;                    // floats from column to column of a partial result: other banks
+  static constexpr int PARTIAL = COLS * COL + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
   static constexpr int RING_BYTES = WARPS * SLOTS * TILE_BYTES;
-  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (6 * WARPS + 8) * 4;
+  static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (8 * WARPS + 8) * 4;
   static_assert(PARTIAL * 4 <= TILE_BYTES, "a slot holds a warp's partial result");
   static_assert(SMEM <= 232448, "shared memory of a block");
 };
@@ -108,6 +109,20 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
   return v;
+}
+
+// 1 / x, and 0 of 0: a sum of weights, which is 0 where nothing is seen, else no smaller than its reference's weight
+__device__ __forceinline__ float inverse(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return x == 0.f ? 0.f : r;
+}
+// Two outputs.
+__device__ __forceinline__ uint32_t pack_out(const AttendParams &p, float lo, float hi) {
+  uint32_t r;
+  if (!p.bf16) return pack_half2(lo, hi);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 
 // A place in the list of tiles.
@@ -166,10 +181,12 @@ __device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const int
   } while (c.n_tiles == 0);
 }
 
+// The token of a query row: row / group, for rows below 64 (group at most 128: the product's error stays below its place)
+__device__ __forceinline__ int token_of(int row, const AttendParams &p) { return (unsigned)row * p.group_inv >> 16; }
 // Query row `col` of the segment's block: the token's and the head's place.
 template <int COLS>
 __device__ __forceinline__ void row_of(const Cursor &c, int col, const AttendParams &p, int64_t &token, int &head) {
-  const int row = c.block * COLS + col, t = row / p.group;
+  const int row = c.block * COLS + col, t = token_of(row, p);
   token = c.first + t;
   head = c.head * p.group + row - t * p.group;
 }
@@ -181,12 +198,19 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
   int64_t t;
   int head;
   row_of<COLS>(c, col, p, t, head);
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = inverse(sum);
   uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(t, head)) + lane * (HD / 32);
+  uint32_t h[HD / 64];
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) {
-    const float y = sum == 0.f ? 0.f : v[i] * inv;
-    out[i] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
+  for (int i = 0; i < HD / 64; ++i) h[i] = pack_out(p, v[2 * i] * inv, v[2 * i + 1] * inv);
+  if (p.out_wide) {
+    if constexpr (HD == 128)
+      *reinterpret_cast<uint2 *>(out) = make_uint2(h[0], h[HD / 64 - 1]);
+    else
+      *reinterpret_cast<uint32_t *>(out) = h[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) out[i] = (uint16_t)(h[i / 2] >> 16 * (i & 1));
   }
   if (p.lse && lane == 0) p.lse[t * p.n_heads + head] = sum == 0.f ? -INFINITY : 0.69314718056f * top + logf(sum);
 }
@@ -197,7 +221,7 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
 template <int HD, int COLS, int NC, class At>
 __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At &at, float (&v)[NC][HD / 32], float (&top)[NC],
                                               float (&sum)[NC]) {
-  constexpr int C = HD / 32, AHEAD = 16 / NC;
+  constexpr int C = HD / 32, COL = Few<HD, COLS / 8>::COL, AHEAD = 16 / NC;
   using Vec = typename std::conditional<C == 4, float4, float2>::type;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -209,9 +233,9 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
   const auto load = [&](int i) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const float *part = at(min(i + k, n - 1)) + col * HD + lane * C;
+      const float *part = at(min(i + k, n - 1)) + col * COL + lane * C;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * HD);
+      for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * COL);
     }
   };
   load(0);
@@ -219,12 +243,12 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m[c] = -INFINITY, l[c] = 0.f;
-    if (lane < n) m[c] = at(lane)[COLS * HD + col + c], l[c] = at(lane)[COLS * HD + COLS + col + c];
+    if (lane < n) m[c] = at(lane)[COLS * COL + col + c], l[c] = at(lane)[COLS * COL + COLS + col + c];
     top[c] = m[c];
   }
   for (int i = lane + 32; i < n; i += 32)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) top[c] = fmaxf(top[c], at(i)[COLS * HD + col + c]);
+    for (int c = 0; c < NC; ++c) top[c] = fmaxf(top[c], at(i)[COLS * COL + col + c]);
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -234,7 +258,7 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
     if ((i & 31) == 0) {  // the next 32 parts' weights
       if (i > 0 && i + lane < n)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) m[c] = at(i + lane)[COLS * HD + col + c], l[c] = at(i + lane)[COLS * HD + COLS + col + c];
+        for (int c = 0; c < NC; ++c) m[c] = at(i + lane)[COLS * COL + col + c], l[c] = at(i + lane)[COLS * COL + COLS + col + c];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         m[c] = i + lane < n ? ex2(m[c] - (top[c] == -INFINITY ? 0.f : top[c])) : 0.f;
@@ -268,9 +292,9 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   int4 *info = reinterpret_cast<int4 *>(smem + F::RING_BYTES);
   int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
   uint64_t *bars = reinterpret_cast<uint64_t *>(prefix + FEW_SEQS + 4);
-  int *part_seg = reinterpret_cast<int *>(bars + W * F::SLOTS);  // [2 W]: segment of each partial result, or -1
-  int *part_place = part_seg + 2 * W;
-  int *group_at = part_place + 2 * W, *n_groups = group_at + 2 * W + 1;
+  int *part_seg = reinterpret_cast<int *>(bars + W * F::SLOTS);  // [2 W]: segment of each partial result (packed), or -1
+  int *part_place = part_seg + 2 * W, *group_seg = part_place + 2 * W;
+  int *group_at = group_seg + 2 * W, *n_groups = group_at + 2 * W + 1;
   volatile int *cut = n_groups + 1, *span = cut + 2;  // of the segments that this block merges: blocks
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
@@ -322,11 +346,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     __syncthreads();
   }
   const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
-  // at least a tile for every warp of a block: fewer blocks, fewer merges
-  const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)W);
+  // at least a tile for every warp of a block: fewer blocks, fewer merges.  (Divided in 32 bits where it fits: one chain of
+  // instructions instead of three)
+  const int64_t all = total + gridDim.x - 1;
+  const int64_t quota = max(all <= 0x7fffffff ? (int64_t)((unsigned)all / gridDim.x) : all / gridDim.x, (int64_t)W);
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
   if (c0 >= c1) return;
-  const int64_t w0 = c0 + (c1 - c0) * warp / W, w1 = c0 + (c1 - c0) * (warp + 1) / W;
+  const auto share = [&](int w) { return c0 + (c1 - c0 <= 1 << 27 ? (unsigned)(c1 - c0) * w / W : (c1 - c0) * w / W); };
+  const int64_t w0 = share(warp), w1 = share(warp + 1);
 
   const uint32_t ring = smem_addr(smem) + warp * F::SLOTS * F::TILE_BYTES;
   const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
@@ -593,7 +620,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * st + key_lane + 8 * (i >> 1);
-              const int end = all_end + min((at.block * COLS + n * 8 + 2 * tig + (i & 1)) / p.group, at.count - 1);
+              const int end = all_end + min(token_of(at.block * COLS + n * 8 + 2 * tig + (i & 1), p), at.count - 1);
               const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> st & 1);
               if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
             }
@@ -764,66 +791,76 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       const bool last = flat + 1 == w1;
       float *part = last ? reinterpret_cast<float *>(smem + (size_t)warp * F::SLOTS * F::TILE_BYTES)
                          : block_ws + (size_t)warp * F::PARTIAL;
-      if (!alone && lane == 0) part_seg[2 * warp + last] = (at.seq * heads + at.head) * p.most_blocks + at.block;
+      if (!alone && lane == 0) part_seg[2 * warp + last] = (at.seq << 10) | (at.head << 2) | at.block;
       __syncwarp();
+      // sums over the lanes that share a column
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+      for (int off = 4; off < 32; off <<= 1)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = n * 8 + 2 * tig + c;
-          int64_t token;
-          int head;
-          row_of<COLS>(at, col, p, token, head);
-          float l = sum[n][c];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-          const float m = top[n][c] == -INFINITY ? -INFINITY : top[n][c] * cf[n][c];
-          const float inv = l == 0.f ? 0.f : 1.f / l;
+          for (int c = 0; c < 2; ++c) {
+            sum[n][c] += __shfl_xor_sync(0xffffffffu, sum[n][c], off);
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            float cen = centre[n][g][c];
+            for (int g = 0; g < G; ++g) centre[n][g][c] += __shfl_xor_sync(0xffffffffu, centre[n][g][c], off);
+          }
+      // channels 64 g + 8 gid + 0..7 of column 2 tig + c: o[..][0..3][c], then o[..][0..3][c + 2]
 #pragma unroll
-            for (int off = 4; off < 32; off <<= 1) cen += __shfl_xor_sync(0xffffffffu, cen, off);
-            // channels 64 g + 8 gid + 0..7 of this column
-            float v[8];
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              v[i] = fmaf(fmaf(o[n][g][i & 3][c + 2 * (i >> 2)], i & 1 ? 1.f / HIGH : 1.f / LOW, -8.f * ones[n][g][c]),
-                          unit, cen);
-            if (alone) {
-              if (col < rows && !dead) {
-                uint16_t h[8];
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  const float y = l == 0.f ? 0.f : v[i] * inv;
-                  h[i] = p.bf16 ? f32_to_bf16_rne(y) : f32_to_f16_rn(y);
-                }
-                uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(token, head)) + 64 * g + 8 * gid;
-                if (p.out_wide) {
-                  *reinterpret_cast<uint4 *>(out) =
-                      make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                                 h[6] | (uint32_t)h[7] << 16);
-                } else {
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) out[i] = h[i];
-                }
+            for (int j = 0; j < 4; ++j)
+              o[n][g][i][j] = fmaf(fmaf(o[n][g][i][j], i & 1 ? 1.f / HIGH : 1.f / LOW, -8.f * ones[n][g][j & 1]), unit,
+                                   centre[n][g][j & 1]);
+      if (!alone) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int col = n * 8 + 2 * tig + c;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+              float4 *to = reinterpret_cast<float4 *>(part + col * F::COL + 64 * g + 8 * gid);
+              to[0] = make_float4(o[n][g][0][c], o[n][g][1][c], o[n][g][2][c], o[n][g][3][c]);
+              to[1] = make_float4(o[n][g][0][c + 2], o[n][g][1][c + 2], o[n][g][2][c + 2], o[n][g][3][c + 2]);
+            }
+            if (gid == 0) {
+              part[COLS * F::COL + col] = top[n][c] == -INFINITY ? -INFINITY : top[n][c] * cf[n][c];
+              part[COLS * F::COL + COLS + col] = sum[n][c];
+            }
+          }
+      } else if (!dead) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int col = n * 8 + 2 * tig + c;
+            if (col >= rows) continue;
+            int64_t token;
+            int head;
+            row_of<COLS>(at, col, p, token, head);
+            const float inv = inverse(sum[n][c]);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+              uint32_t h[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                h[i] = pack_out(p, o[n][g][2 * (i & 1)][c + (i & 2)] * inv, o[n][g][2 * (i & 1) + 1][c + (i & 2)] * inv);
+              uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(token, head)) + 64 * g + 8 * gid;
+              if (p.out_wide) {
+                *reinterpret_cast<uint4 *>(out) = make_uint4(h[0], h[1], h[2], h[3]);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = (uint16_t)(h[i / 2] >> 16 * (i & 1));
               }
-            } else {
-              float4 *to = reinterpret_cast<float4 *>(part + col * HD + 64 * g + 8 * gid);
-              to[0] = make_float4(v[0], v[1], v[2], v[3]);
-              to[1] = make_float4(v[4], v[5], v[6], v[7]);
             }
-          }
-          if (gid == 0) {
-            if (!alone) {
-              part[COLS * HD + col] = m;
-              part[COLS * HD + COLS + col] = l;
-            } else if (p.lse && col < rows && !dead) {
+            if (gid == 0 && p.lse)
               p.lse[token * p.n_heads + head] =
-                  l == 0.f ? -INFINITY : 0.69314718056f * m + logf(l);
-            }
+                  sum[n][c] == 0.f ? -INFINITY : 0.69314718056f * (top[n][c] * cf[n][c]) + logf(sum[n][c]);
           }
-        }
       }
     }
     if (flat + 1 < w1) next_tile<COLS>(at, info, prefix, p);
@@ -832,7 +869,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   // ---- partial results of this block, in list order ([warp][0: its first segment's, 1: its last's], without the
   // places that hold none): those of a segment are neighbours, a group
   __syncthreads();
-  if (warp == 0) {
+  {  // (every warp makes the same list, and waits for no other)
     const int id = lane < 2 * W ? part_seg[lane] : -1;
     const unsigned there = __ballot_sync(0xffffffffu, id >= 0);
     const unsigned before = there & ((1u << lane) - 1);
@@ -842,16 +879,14 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     if (id >= 0) part_place[__popc(before)] = lane;
     if (opens) {
       const int k = __popc(groups & ((1u << lane) - 1));
-      part_seg[k] = id, group_at[k] = __popc(before);
+      group_seg[k] = id, group_at[k] = __popc(before);
     }
     if (lane == 0) n_groups[0] = __popc(groups), group_at[__popc(groups)] = __popc(there);
+    __syncwarp();
   }
-  __syncthreads();
   // a segment's places in the list, and how it stands to this block's: whole, or begun (0) or continued (1) elsewhere
   const auto segment = [&](int id, Cursor &c, int64_t &sa, int64_t &sb) {
-    const int of_head = id / p.most_blocks;
-    c.block = id - of_head * p.most_blocks;
-    c.seq = of_head / heads, c.head = of_head - c.seq * heads;
+    c.seq = id >> 10, c.head = id >> 2 & 255, c.block = id & 3;
     enter_sequence<COLS>(c, info, prefix, p);
     sa = (int64_t)prefix[c.seq] * heads + (c.head * c.blocks + c.block) * c.n_tiles, sb = sa + c.n_tiles;
   };
@@ -863,7 +898,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
 #pragma unroll 1
   for (int across = 0; across < 2; ++across) {
     for (int u = warp; u < (across ? 2 : n_groups[0]) * (COLS / NC); u += W) {
-      const int k = u / (COLS / NC), col = u % (COLS / NC) * NC, id = across ? cut[k] : part_seg[k];
+      const int k = u / (COLS / NC), col = u % (COLS / NC) * NC, id = across ? cut[k] : group_seg[k];
       if (id < 0) continue;
       segment(id, seg, sa, sb);
       const int rows_here = seg.count * p.group - seg.block * COLS;
@@ -886,8 +921,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           if (col + c < rows_here) store_row<HD, COLS>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
         } else {
 #pragma unroll
-          for (int j = 0; j < HD / 32; ++j) to[(col + c) * HD + lane * (HD / 32) + j] = v[c][j];
-          if (lane == 0) to[COLS * HD + col + c] = tops[c], to[COLS * HD + COLS + col + c] = sums[c];
+          for (int j = 0; j < HD / 32; ++j) to[(col + c) * F::COL + lane * (HD / 32) + j] = v[c][j];
+          if (lane == 0) to[COLS * F::COL + col + c] = tops[c], to[COLS * F::COL + COLS + col + c] = sums[c];
         }
       }
     }
@@ -897,12 +932,13 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     if (lane == 0 && warp < 2) {
       int id = -1;
       if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
-        const int mine = part_seg[warp == 0 ? 0 : n_groups[0] - 1];
+        const int mine = group_seg[warp == 0 ? 0 : n_groups[0] - 1];
         segment(mine, seg, sa, sb);
         if (sa < c0 || sb > c1) {
           const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
-          if (atom_add_acq_rel(p.tickets + mine, 1u) == (unsigned)(to - from)) {
-            atomicExch(p.tickets + mine, 0u);  // as the next call has to find it
+          unsigned *ticket = p.tickets + (seg.seq * heads + seg.head) * p.most_blocks + seg.block;
+          if (atom_add_acq_rel(ticket, 1u) == (unsigned)(to - from)) {
+            atomicExch(ticket, 0u);  // as the next call has to find it
             id = mine, span[2 * warp] = from, span[2 * warp + 1] = to - from + 1;
           }
         }
