@@ -118,11 +118,17 @@ __device__ __forceinline__ float inverse(float x) {
   return x == 0.f ? 0.f : r;
 }
 // Two outputs.
-__device__ __forceinline__ uint32_t pack_out(const AttendParams &p, float lo, float hi) {
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
   uint32_t r;
-  if (!p.bf16) return pack_half2(lo, hi);
+  if (!BF16) return pack_half2(lo, hi);
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// a / b, in 32 bits where they fit: one chain of instructions instead of three.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (a | b) >> 32 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
 }
 
 // A place in the list of tiles.
@@ -192,7 +198,7 @@ __device__ __forceinline__ void row_of(const Cursor &c, int col, const AttendPar
 }
 
 // One output row's channels from lane `lane`'s HD / 32 values.
-template <int HD, int COLS>
+template <int HD, int COLS, bool BF16>
 __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c, int col, int lane, const float (&v)[HD / 32],
                                           float top, float sum) {
   int64_t t;
@@ -202,7 +208,7 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
   uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(t, head)) + lane * (HD / 32);
   uint32_t h[HD / 64];
 #pragma unroll
-  for (int i = 0; i < HD / 64; ++i) h[i] = pack_out(p, v[2 * i] * inv, v[2 * i + 1] * inv);
+  for (int i = 0; i < HD / 64; ++i) h[i] = pack_out<BF16>(v[2 * i] * inv, v[2 * i + 1] * inv);
   if (p.out_wide) {
     if constexpr (HD == 128)
       *reinterpret_cast<uint2 *>(out) = make_uint2(h[0], h[HD / 64 - 1]);
@@ -284,7 +290,7 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
     for (int off = 16; off > 0; off >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], off);
 }
 
-template <int HD, int NT>
+template <int HD, int NT, bool BF16>
 __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel(const AttendParams p) {
   using F = Few<HD, NT>;
   constexpr int G = F::GROUPS, COLS = F::COLS, W = F::WARPS;
@@ -346,10 +352,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     __syncthreads();
   }
   const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
-  // at least a tile for every warp of a block: fewer blocks, fewer merges.  (Divided in 32 bits where it fits: one chain of
-  // instructions instead of three)
-  const int64_t all = total + gridDim.x - 1;
-  const int64_t quota = max(all <= 0x7fffffff ? (int64_t)((unsigned)all / gridDim.x) : all / gridDim.x, (int64_t)W);
+  // at least a tile for every warp of a block: fewer blocks, fewer merges
+  const int64_t quota = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)W);
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
   if (c0 >= c1) return;
   const auto share = [&](int w) { return c0 + (c1 - c0 <= 1 << 27 ? (unsigned)(c1 - c0) * w / W : (c1 - c0) * w / W); };
@@ -481,7 +485,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         big1 = max(big1, __shfl_xor_sync(0xffffffffu, big1, 1));
         big1 = max(big1, __shfl_xor_sync(0xffffffffu, big1, 2));
         float inv;
-        const float unit = xchunk_scale(p.bf16 ? bf16_to_f32((uint16_t)big1) : f16_to_f32((uint16_t)big1), &inv);
+        const float unit = xchunk_scale(BF16 ? bf16_to_f32((uint16_t)big1) : f16_to_f32((uint16_t)big1), &inv);
         inv = p.scale > 0.f ? inv : p.scale < 0.f ? -inv : 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -494,7 +498,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               for (int k = 0; k < 2; ++k) {
                 // (odd channels' codes are 16 times the even ones': a sixteenth of the query)
                 const uint32_t two = __byte_perm(raw[n][g][4 * j + h], raw[n][g][4 * j + h + 2], k ? 0x7632 : 0x5410);
-                const float lo = p.bf16 ? bf16_lo(two) : half_lo(two), hi = p.bf16 ? bf16_hi(two) : half_hi(two);
+                const float lo = BF16 ? bf16_lo(two) : half_lo(two), hi = BF16 ? bf16_hi(two) : half_hi(two);
                 const float r = k ? inv * 0.0625f : inv;
                 q[n][g][j][h][k] = pack_half2(lo * r, hi * r);
               }
@@ -848,7 +852,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               uint32_t h[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                h[i] = pack_out(p, o[n][g][2 * (i & 1)][c + (i & 2)] * inv, o[n][g][2 * (i & 1) + 1][c + (i & 2)] * inv);
+                h[i] = pack_out<BF16>(o[n][g][2 * (i & 1)][c + (i & 2)] * inv, o[n][g][2 * (i & 1) + 1][c + (i & 2)] * inv);
               uint16_t *out = reinterpret_cast<uint16_t *>(p.out.row(token, head)) + 64 * g + 8 * gid;
               if (p.out_wide) {
                 *reinterpret_cast<uint4 *>(out) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -892,7 +896,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   };
   Cursor seg;
   int64_t sa, sb;
-  constexpr int NC = 2;  // columns of a warp at a time
+  constexpr int NC = 2 * NT;  // columns of a warp at a time
   // first the block's own partial results, then those that blocks have left to this one as the last to arrive: the same
   // code, which costs more the first time than what it does
 #pragma unroll 1
@@ -911,17 +915,17 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         return at & 1 ? reinterpret_cast<const float *>(smem + (size_t)(at >> 1) * F::SLOTS * F::TILE_BYTES)
                       : static_cast<const float *>(block_ws + (at >> 1) * F::PARTIAL);
       };
-      float v[NC][HD / 32], tops[NC], sums[NC];
+      alignas(16) float v[NC][HD / 32], tops[NC], sums[NC];
       merge_columns<HD, COLS, NC>(n, col, lane, nth, v, tops, sums);
       const bool whole = across || (sa >= c0 && sb <= c1);
       float *to = block_ws + (W + (sa < c0 ? 0 : 1)) * F::PARTIAL;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         if (whole) {
-          if (col + c < rows_here) store_row<HD, COLS>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
+          if (col + c < rows_here) store_row<HD, COLS, BF16>(p, seg, col + c, lane, v[c], tops[c], sums[c]);
         } else {
-#pragma unroll
-          for (int j = 0; j < HD / 32; ++j) to[(col + c) * F::COL + lane * (HD / 32) + j] = v[c][j];
+          using Vec = typename std::conditional<HD == 128, float4, float2>::type;
+          *reinterpret_cast<Vec *>(to + (col + c) * F::COL + lane * (HD / 32)) = *reinterpret_cast<const Vec *>(v[c]);
           if (lane == 0) to[COLS * F::COL + col + c] = tops[c], to[COLS * F::COL + COLS + col + c] = sums[c];
         }
       }
@@ -935,7 +939,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
         const int mine = group_seg[warp == 0 ? 0 : n_groups[0] - 1];
         segment(mine, seg, sa, sb);
         if (sa < c0 || sb > c1) {
-          const int from = (int)(sa / quota), to = (int)((sb - 1) / quota);
+          const int from = (int)quotient(sa, quota), to = (int)quotient(sb - 1, quota);
           unsigned *ticket = p.tickets + (seg.seq * heads + seg.head) * p.most_blocks + seg.block;
           if (atom_add_acq_rel(ticket, 1u) == (unsigned)(to - from)) {
             atomicExch(ticket, 0u);  // as the next call has to find it
@@ -949,18 +953,18 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   }
 }
 
-template <int HD, int NT>
+template <int HD, int NT, bool BF16>
 cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   using F = Few<HD, NT>;
   static SmemOptIn opt_in;
-  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_few_kernel<HD, NT>);
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_few_kernel<HD, NT, BF16>);
   const cudaError_t e = opt_in(kernel, F::SMEM);
   if (e != cudaSuccess) return e;
   // as many blocks as the longest contexts could fill
   const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks *
                        (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
-  return launch_chained(kv4_attend_few_kernel<HD, NT>, grid, F::THREADS, F::SMEM, s, p);
+  return launch_chained(kv4_attend_few_kernel<HD, NT, BF16>, grid, F::THREADS, F::SMEM, s, p);
 }
 
 }  // namespace
@@ -973,9 +977,13 @@ size_t attend_few_partials(int head_dim, int cols) {
   return FEW_BLOCKS * floats * sizeof(float);
 }
 
+template <bool BF16>
+static cudaError_t launch_type(const AttendParams &p, int cols, int n_sm, cudaStream_t s) {
+  if (p.pool.head_dim == 128) return cols <= 8 ? launch<128, 1, BF16>(p, n_sm, s) : launch<128, 2, BF16>(p, n_sm, s);
+  return cols <= 8 ? launch<64, 1, BF16>(p, n_sm, s) : launch<64, 2, BF16>(p, n_sm, s);
+}
 cudaError_t launch_attend_few(const AttendParams &p, int cols, int n_sm, cudaStream_t s) {
-  if (p.pool.head_dim == 128) return cols <= 8 ? launch<128, 1>(p, n_sm, s) : launch<128, 2>(p, n_sm, s);
-  return cols <= 8 ? launch<64, 1>(p, n_sm, s) : launch<64, 2>(p, n_sm, s);
+  return p.bf16 ? launch_type<true>(p, cols, n_sm, s) : launch_type<false>(p, cols, n_sm, s);
 }
 
 }  // namespace kfl
