@@ -148,11 +148,13 @@ __device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, cons
   const int4 v = info[c.seq];
   c.user = v.x, c.length = v.y, c.first = v.z, c.count = v.w;
   c.blocks = (c.count * p.group + COLS - 1) / COLS;
-  c.n_tiles = prefix[c.seq + 1] - prefix[c.seq];
-  if (c.blocks > 1) c.n_tiles /= c.blocks;
+  int units = prefix[c.seq + 1] - prefix[c.seq];
+  if (c.blocks > 1) units /= c.blocks;
+  c.n_tiles = units - 1;
   c.first_tile = first_tile_of(v.y, v.w, p.window);
 }
 
+// The tile of unit `flat` of the list, -1 for what comes before a segment's first (a segment of n tiles is n + 1 units).
 template <int COLS>
 __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 *info, const int *prefix,
                                             const AttendParams &p) {
@@ -167,8 +169,8 @@ __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 
   c.seq = lo;
   enter_sequence<COLS>(c, info, prefix, p);
   const int rest = (int)(flat - (int64_t)prefix[lo] * p.pool.n_kv_heads);  // (below heads * blocks * 2^20)
-  const int segment = rest / c.n_tiles;
-  c.tile = rest - segment * c.n_tiles;
+  const int segment = rest / (c.n_tiles + 1);
+  c.tile = rest - segment * (c.n_tiles + 1) - 1;
   c.head = segment / c.blocks;
   c.block = segment - c.head * c.blocks;
 }
@@ -184,7 +186,7 @@ __device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const int
   do {
     if (++c.seq >= p.n_seqs) return;
     enter_sequence<COLS>(c, info, prefix, p);
-  } while (c.n_tiles == 0);
+  } while (c.n_tiles <= 0);
 }
 
 // The token of a query row: row / group, for rows below 64 (group at most 128: the product's error stays below its place)
@@ -310,7 +312,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   fence_mbar_init();
   pdl_wait();
 
-  // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros).  Up to 32
+  // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros).  Each segment has
+  // one unit more, since its rows and results take about as long as a tile (uncounted, 32 ragged users: 42.8 us).  Up to 32
   // sequences every warp makes the whole list, alike, and waits for no other
   const auto tiles_of = [&](int s) {
     const int user = p.users ? p.users[s] : p.seq0 + s;
@@ -323,7 +326,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
     if (bad && blockIdx.x == 0) report(p.status, bad);
     info[s] = make_int4(user, length, first, count);
-    return (count * p.group + COLS - 1) / COLS * max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window));
+    return (count * p.group + COLS - 1) / COLS *
+           (max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window)) + 1);
   };
   const auto warp_sum = [&](int v) {  // up to and with this lane's
 #pragma unroll
@@ -357,7 +361,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
   if (c0 >= c1) return;
   const auto share = [&](int w) { return c0 + (c1 - c0 <= 1 << 27 ? (unsigned)(c1 - c0) * w / W : (c1 - c0) * w / W); };
-  const int64_t w0 = share(warp), w1 = share(warp + 1);
+  int64_t w0 = share(warp);
+  const int64_t w1 = share(warp + 1);
 
   const uint32_t ring = smem_addr(smem) + warp * F::SLOTS * F::TILE_BYTES;
   const uint32_t bar0 = smem_addr(bars + warp * F::SLOTS);
@@ -371,15 +376,17 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   // ---- copies: a page of a tile's size is one as it stands; of others a page's part of the tile comes in four (codes and
   // parameters of K and V), a lane each
   Cursor fetch;
-  int fetch_page = -2, fetch_left = (int)(w1 - w0);  // tiles to bring (a page of -2: behind the sequence's end)
+  int fetch_page = -2;  // (behind the sequence's end)
   unsigned fetch_slot = 0;
   const int lane_key = lane >> 2 << lb;              // of this lane's copy, in the tile
   const bool copies = lane < (lp == LOG_TILE ? 1 : 4 * TILE >> lb);
   const int32_t *fetch_row = nullptr;
-  if (fetch_left > 0) {
+  if (w0 < w1) {
     locate_tile<COLS>(fetch, w0, info, prefix, p);
+    if (fetch.tile < 0) fetch.tile = 0, ++w0;
     fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
   }
+  int64_t fetch_flat = w0;  // (w1: all are brought or under way)
   const auto load_page = [&]() {  // the page of this lane's copy for the tile at `fetch`
     const int key = (fetch.first_tile + fetch.tile) * TILE + lane_key;
     fetch_page = copies && key < fetch.length ? fetch_row[key >> lp] : -2;
@@ -423,15 +430,16 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     for (int i = 0; i < F::SLOTS; ++i)
       if (i == (int)fetch_slot) valid[i] = have;
     fetch_slot = fetch_slot + 1 == F::SLOTS ? 0 : fetch_slot + 1;
-    if (--fetch_left > 0) {
-      const int seq = fetch.seq;
+    const int seq = fetch.seq;
+    fetch_flat += fetch.tile + 1 == fetch.n_tiles ? 2 : 1;
+    if (fetch_flat < w1) {
       next_tile<COLS>(fetch, info, prefix, p);
       if (fetch.seq != seq) fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
       load_page();
     }
   };
   Cursor at = fetch;
-  if (fetch_left > 0) load_page();
+  if (fetch_flat < w1) load_page();
 
   // ---- this warp's tiles
   uint32_t q[NT][G][2][2][2];     // B fragments: [group][word of a lane][half of its pairs][register]
@@ -442,7 +450,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   int rows = 0;
   float *block_ws = p.partials + (size_t)blockIdx.x * (W + 2) * F::PARTIAL;
   const float log2_scale = fabsf(p.scale) * 1.44269504089f;
-  for (int64_t flat = w0; flat < w1; ++flat) {
+  for (int64_t flat = w0; flat < w1;) {
     if (flat == w0 || at.tile == 0) {
       // ---- a new (sequence, head): its query rows as fp16 (a power of two per row brings the largest to [2^14, 2^15))
       // 16 channels of each group for column gid; under way before the first tiles' copies, whose page numbers come first
@@ -534,12 +542,12 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       if (flat == w0)
 #pragma unroll
         for (int i = 1; i < F::SLOTS; ++i)
-          if (fetch_left > 0) issue();
+          if (fetch_flat < w1) issue();
     }
 
     // ---- one tile
     if (!dead && !wait_2s(bar0 + slot * 8, phase)) {
-      dead = true, fetch_left = 0;
+      dead = true, fetch_flat = w1;
       if (lane == 0) report(p.status, KFL_TIMED_OUT);
       for (int i = 0; i < F::SLOTS; ++i) wait_2s(bar0 + i * 8, i < (int)slot ? phase ^ 1 : phase);
     }
@@ -782,17 +790,18 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       }
     }
     __syncwarp();  // (every lane has read the slot)
-    if (fetch_left > 0) issue();
+    if (fetch_flat < w1) issue();
     if (++slot == F::SLOTS) slot = 0, phase ^= 1;
 
     // ---- the end of a (sequence, head), or of this warp's piece of it
     const bool ends = at.tile + 1 == at.n_tiles;
-    if (ends || flat + 1 == w1) {
+    const int64_t next = flat + (ends ? 2 : 1);
+    if (ends || next >= w1) {
       const int64_t seg_first = flat - at.tile;
       const bool alone = ends && seg_first >= w0;
       const float unit = v_unit * (1.f / WEIGHT_UNIT);
       // a result that others continue goes to global memory while the ring is in use, else into the ring
-      const bool last = flat + 1 == w1;
+      const bool last = next >= w1;
       float *part = last ? reinterpret_cast<float *>(smem + (size_t)warp * F::SLOTS * F::TILE_BYTES)
                          : block_ws + (size_t)warp * F::PARTIAL;
       if (!alone && lane == 0) part_seg[2 * warp + last] = (at.seq << 10) | (at.head << 2) | at.block;
@@ -867,7 +876,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           }
       }
     }
-    if (flat + 1 < w1) next_tile<COLS>(at, info, prefix, p);
+    if (next < w1) next_tile<COLS>(at, info, prefix, p);
+    flat = next;
   }
 
   // ---- partial results of this block, in list order ([warp][0: its first segment's, 1: its last's], without the
@@ -892,7 +902,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const auto segment = [&](int id, Cursor &c, int64_t &sa, int64_t &sb) {
     c.seq = id >> 10, c.head = id >> 2 & 255, c.block = id & 3;
     enter_sequence<COLS>(c, info, prefix, p);
-    sa = (int64_t)prefix[c.seq] * heads + (c.head * c.blocks + c.block) * c.n_tiles, sb = sa + c.n_tiles;
+    sa = (int64_t)prefix[c.seq] * heads + (c.head * c.blocks + c.block) * (c.n_tiles + 1) + 1, sb = sa + c.n_tiles;
   };
   Cursor seg;
   int64_t sa, sb;
@@ -970,7 +980,7 @@ cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   // as many blocks as the longest contexts could fill
   const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks *
-                       (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 1);
+                       (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 2);
   const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
   return launch_chained(kv4_attend_few_kernel<HD, NT, BF16>, grid, F::THREADS, F::SMEM, s, p);
 }
