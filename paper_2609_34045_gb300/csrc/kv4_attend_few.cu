@@ -224,12 +224,13 @@ __device__ __forceinline__ void store_row(const AttendParams &p, const Cursor &c
 }
 
 // NC columns from `col` on of several partial results, `n` of them at at(i), in order: merged by one warp.  Lanes take the
-// parts' maxima and sums, 32 at a time; every lane takes its channels of all parts, four at a time, the first of them
-// under way with the maxima.
+// parts' places, maxima and sums, 32 at a time; every lane takes its channels of all parts, four at a time, the first of them
+// under way with the maxima.  (Eight at a time take the tiles' registers: 32 ragged users 45 us for 41.)
 template <int HD, int COLS, int NC, class At>
 __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At &at, float (&v)[NC][HD / 32], float (&top)[NC],
                                               float (&sum)[NC]) {
   constexpr int C = HD / 32, COL = Few<HD, COLS / 8>::COL, AHEAD = 4;
+  static_assert(32 % AHEAD == 0, "a round stays within the 32 parts whose weights the lanes hold");
   using Vec = typename std::conditional<C == 4, float4, float2>::type;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -238,10 +239,14 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
     for (int j = 0; j < C; ++j) v[c][j] = 0.f;
   }
   Vec x[AHEAD][NC];
+  const float *mine = at(min(lane, n - 1));
   const auto load = [&](int i) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const float *part = at(min(i + k, n - 1)) + col * COL + lane * C;
+      if (i + k >= n) break;
+      const float *part = reinterpret_cast<const float *>(
+                              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), (i + k) & 31)) +
+                          col * COL + lane * C;
 #pragma unroll
       for (int c = 0; c < NC; ++c) x[k][c] = *reinterpret_cast<const Vec *>(part + c * COL);
     }
@@ -251,7 +256,7 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m[c] = -INFINITY, l[c] = 0.f;
-    if (lane < n) m[c] = at(lane)[COLS * COL + col + c], l[c] = at(lane)[COLS * COL + COLS + col + c];
+    if (lane < n) m[c] = mine[COLS * COL + col + c], l[c] = mine[COLS * COL + COLS + col + c];
     top[c] = m[c];
   }
   for (int i = lane + 32; i < n; i += 32)
@@ -264,9 +269,11 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
 #pragma unroll 1
   for (int i = 0; i < n; i += AHEAD) {
     if ((i & 31) == 0) {  // the next 32 parts' weights
-      if (i > 0 && i + lane < n)
+      if (i > 0) {
+        mine = at(min(i + lane, n - 1));
 #pragma unroll
-        for (int c = 0; c < NC; ++c) m[c] = at(i + lane)[COLS * COL + col + c], l[c] = at(i + lane)[COLS * COL + COLS + col + c];
+        for (int c = 0; c < NC; ++c) m[c] = mine[COLS * COL + col + c], l[c] = mine[COLS * COL + COLS + col + c];
+      }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         m[c] = i + lane < n ? ex2(m[c] - (top[c] == -INFINITY ? 0.f : top[c])) : 0.f;
