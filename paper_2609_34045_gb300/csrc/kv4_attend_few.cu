@@ -30,6 +30,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attn_core.cuh"  // cp_async16
 #include "kv4_attend.cuh"
 
 namespace kfl {
@@ -55,6 +56,7 @@ struct Few {
   static constexpr int PARTIAL = COLS * COL + 2 * COLS;  // floats: [col][channel], then [col] (max, sum)
   static constexpr int RING_BYTES = WARPS * SLOTS * TILE_BYTES;
   static constexpr int SMEM = RING_BYTES + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4 + WARPS * SLOTS * 8 + (8 * WARPS + 8) * 4;
+  static_assert(PARTIAL % 4 == 0, "copied in 16 bytes");
   static_assert(PARTIAL * 4 <= TILE_BYTES, "a slot holds a warp's partial result");
   static_assert(SMEM <= 232448, "shared memory of a block");
 };
@@ -913,6 +915,12 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   };
   Cursor seg;
   int64_t sa, sb;
+  // part i of a segment that is cut, from block `first` on: the block where it begins has it as its last part, the others as
+  // their first
+  const auto part_of = [&](int first, int i) {
+    return static_cast<const float *>(p.partials + ((size_t)(first + i) * (W + 2) + W + (i == 0)) * F::PARTIAL);
+  };
+  bool staged = false;
   const auto merge = [&](auto columns, int across, int groups) {
     constexpr int NC = decltype(columns)::value;
     for (int u = warp; u < groups * (COLS / NC); u += W) {
@@ -923,8 +931,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       if (col >= rows_here) continue;
       const int first = across ? span[2 * k] : group_at[k], n = across ? span[2 * k + 1] : group_at[k + 1] - first;
       const auto nth = [&](int i) {
-        // (of a segment that is cut, the block where it begins has it as its last part, the others as their first)
-        if (across) return static_cast<const float *>(p.partials + ((size_t)(first + i) * (W + 2) + W + (i == 0)) * F::PARTIAL);
+        if (across)
+          return staged ? reinterpret_cast<const float *>(smem) + (k * span[1] + i) * F::PARTIAL : part_of(first, i);
         const int at = part_place[first + i];
         return at & 1 ? reinterpret_cast<const float *>(smem + (size_t)(at >> 1) * F::SLOTS * F::TILE_BYTES)
                       : static_cast<const float *>(block_ws + (at >> 1) * F::PARTIAL);
@@ -956,25 +964,45 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     else
       merge(std::integral_constant<int, 4>(), across, groups);
     if (across) break;
-    __syncthreads();
-    // ---- segments that other blocks have parts of: the first and the last group at most
-    if (lane == 0 && warp < 2) {
-      int id = -1;
-      if (n_groups[0] > 0 && (warp == 0 || n_groups[0] > 1)) {
-        const int mine = group_seg[warp == 0 ? 0 : n_groups[0] - 1];
-        segment(mine, seg, sa, sb);
-        if (sa < c0 || sb > c1) {
-          const int from = (int)quotient(sa, quota), to = (int)quotient(sb - 1, quota);
-          unsigned *ticket = p.tickets + (seg.seq * heads + seg.head) * p.most_blocks + seg.block;
-          if (atom_add_acq_rel(ticket, 1u) == (unsigned)(to - from)) {
-            atomicExch(ticket, 0u);  // as the next call has to find it
-            id = mine, span[2 * warp] = from, span[2 * warp + 1] = to - from + 1;
-          }
-        }
-      }
-      cut[warp] = id;
+    // ---- segments that other blocks have parts of: the first and the last group at most.  (The last warps, which have
+    // fewer columns to merge)
+    const int k = W - 1 - warp;
+    int mine = -1, from = 0, to = 0;
+    if (lane == 0 && k < 2 && n_groups[0] > k) {
+      mine = group_seg[k == 0 ? 0 : n_groups[0] - 1];
+      segment(mine, seg, sa, sb);
+      if (sa < c0 || sb > c1)
+        from = (int)quotient(sa, quota), to = (int)quotient(sb - 1, quota);
+      else
+        mine = -1;
     }
     __syncthreads();
+    if (lane == 0 && k < 2) {
+      if (mine >= 0) {
+        unsigned *ticket = p.tickets + (seg.seq * heads + seg.head) * p.most_blocks + seg.block;
+        if (atom_add_acq_rel(ticket, 1u) == (unsigned)(to - from))
+          atomicExch(ticket, 0u);  // as the next call has to find it
+        else
+          mine = -1;
+      }
+      cut[k] = mine, span[2 * k] = from, span[2 * k + 1] = mine < 0 ? 0 : to - from + 1;
+    }
+    __syncthreads();
+    const int parts = span[1] + span[3];
+    if (parts == 0) return;
+    // all of them into the ring, where there is room: one round trip instead of one for every four
+    staged = parts <= F::RING_BYTES / (F::PARTIAL * 4);
+    if (staged) {
+      for (int i = warp; i < parts; i += W) {
+        const bool second = i >= span[1];
+        const float *src = part_of(span[second ? 2 : 0], second ? i - span[1] : i);
+        float *dst = reinterpret_cast<float *>(smem) + i * F::PARTIAL;
+        for (int j = 4 * lane; j < F::PARTIAL; j += 128) cp_async16(dst + j, src + j);
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      __syncthreads();
+    }
   }
 }
 
