@@ -347,9 +347,11 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     return v;
   };
   if (lane == 0) prefix[0] = 0;
+  int longest = 0;  // units of a sequence, all its blocks of rows
   if (p.n_seqs <= 32) {
-    const int sum = warp_sum(lane < p.n_seqs ? tiles_of(lane) : 0);
+    const int units = lane < p.n_seqs ? tiles_of(lane) : 0, sum = warp_sum(units);
     if (lane < p.n_seqs) prefix[lane + 1] = sum;
+    longest = __reduce_max_sync(0xffffffffu, units);
     __syncwarp();
   } else {
     for (int s = tid; s < p.n_seqs; s += F::THREADS) prefix[s + 1] = tiles_of(s);
@@ -357,16 +359,28 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     if (warp == 0) {
       int before = 0;
       for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-        const int sum = warp_sum(s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0);
+        const int units = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0, sum = warp_sum(units);
+        longest = max(longest, units);
         if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + sum;
         before += __shfl_sync(0xffffffffu, sum, 31);
       }
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      if (lane == 0) prefix[FEW_SEQS + 1] = longest;
     }
     __syncthreads();
+    longest = prefix[FEW_SEQS + 1];
   }
   const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
   // at least a tile for every warp of a block: fewer blocks, fewer merges
-  const int64_t quota = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)W);
+  int64_t quota = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)W);
+  // A segment over more blocks than the ring holds parts of is merged from global memory, at some 330 clocks a part: it gets
+  // larger pieces where those cost less, 460 clocks a tile (one KV head of 131072 keys: 27.0 us for 40.9)
+  constexpr int MOST_PARTS = F::RING_BYTES / (F::PARTIAL * 4) - 4;
+  if (longest > MOST_PARTS * p.most_blocks * quota) {
+    const int segment = longest / p.most_blocks;
+    const int64_t larger = segment / MOST_PARTS + 1;
+    if (7 * (larger - quota) < 5 * (quotient(segment, quota) - 18)) quota = larger;
+  }
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
   if (c0 >= c1) return;
   const auto share = [&](int w) { return c0 + (c1 - c0 <= 1 << 27 ? (unsigned)(c1 - c0) * w / W : (c1 - c0) * w / W); };

@@ -346,3 +346,10 @@ def test_long_contexts_keep_the_precision_of_short_ones():
     ref, _, _ = c.expected(q)
     err = np.linalg.norm(got.double().cpu().numpy() - ref) / np.linalg.norm(ref)
     assert err <= 2.0 ** -11 + 2.0 ** -12
+
+
+@pytest.mark.parametrize("hd,page,lengths", [(128, 64, [70000]), (64, 128, [50000, 20]), (128, 128, [1] * 40 + [40000])])
+def test_one_segment_over_many_blocks(hd, page, lengths):
+    """A KV head's keys split over dozens of blocks, alone and among many short users."""
+    c = Case(lengths, 1, hd, page, seed=8)
+    c.check(queries(len(lengths), 4, hd, FP16))
