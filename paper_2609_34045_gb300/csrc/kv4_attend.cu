@@ -13,16 +13,18 @@ namespace {
 
 // Which kernel: the first reads and decodes a tile once for every sixteen rows, the second once for all, at a larger cost
 // to begin with.  us, heads of 128, 8 KV heads, first against second:
-//   sequences x keys      24 rows        32 rows        40 rows        48 rows
-//    1 x 1000            18.0   23.3    18.2   23.8    18.2   24.1    18.3   24.9
-//    4 x 3000            34.8   33.4    34.8   33.8    39.7   34.4    40.2   35.0
-//   16 x 8192             117    121     118    122     168    123     168    124
-//   64 x 4096             219    254     221    255     321    255     323    257
-// The contexts' lengths are on the device: the third sixteen rows go by what the tables could hold.
+//   sequences x keys      24 rows        32 rows        48 rows        64 rows
+//    1 x 1000            14.3   23.1    14.5   23.7    14.7   24.8    14.9   28.8
+//    4 x 3000            21.2   33.3    21.4   33.7    24.6   35.0    29.8   37.8
+//    8 x 4096            33.4   56.5    33.8   57.5    45.4   59.6    55.8   65.1
+//    8 x 8192            55.4   76.8    55.9   76.8    76.6   79.6    99.7   85.2
+//   16 x 8192            99.5    121    99.8    122     141    124
+//   64 x 4096             186    253     186    254     274    257
+// The contexts' lengths are on the device: the third and fourth sixteen rows go by what the tables could hold.
 bool is_few(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int n_seqs, int64_t rows) {
   if (rows <= 32) return true;
   return rows <= FEW_ROWS && n_seqs <= 65536 &&
-         (int64_t)n_seqs * pool->n_kv_heads * map->max_pages * pool->page_tokens <= 65536;
+         (int64_t)n_seqs * pool->n_kv_heads * map->max_pages * pool->page_tokens <= (rows <= 48 ? 1 << 19 : 1 << 18);
 }
 
 int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_seqs, int n_tokens, int max_q,

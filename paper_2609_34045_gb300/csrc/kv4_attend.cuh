@@ -6,7 +6,7 @@
 
 namespace kfl {
 
-constexpr int FEW_ROWS = 48;     // most query rows per KV head of the few-row kernel, in blocks of 8 or 16
+constexpr int FEW_ROWS = 64;     // most query rows per KV head of the few-row kernel, in blocks of 8 or 16
 constexpr int FEW_SEQS = 512;    // sequences of one of its launches (their places lie in shared memory)
 constexpr int FEW_BLOCKS = 152;  // most blocks of one of its launches
 

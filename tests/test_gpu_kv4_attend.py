@@ -353,3 +353,10 @@ def test_one_segment_over_many_blocks(hd, page, lengths):
     """A KV head's keys split over dozens of blocks, alone and among many short users."""
     c = Case(lengths, 1, hd, page, seed=8)
     c.check(queries(len(lengths), 4, hd, FP16))
+
+
+@pytest.mark.parametrize("group,tokens", [(8, [8, 7, 1]), (1, [64, 49, 2]), (16, [4, 3, 4]), (5, [12, 11, 10])])
+@pytest.mark.parametrize("hd,page,window", [(128, 64, 0), (64, 16, 70)])
+def test_four_blocks_of_rows(group, tokens, hd, page, window):
+    c = Case([1000, 333, 64], 2, hd, page, seed=9)
+    c.check(queries(sum(tokens), 2 * group, hd, FP16), tokens=tokens, window=window)
