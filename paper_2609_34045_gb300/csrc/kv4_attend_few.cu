@@ -14,19 +14,20 @@
 // What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
 // keeps up.  At 6.77 TB/s an SM gets 42 elements a clock, its logic units do 64 operations: 0.6 (K) and 0.75 (V) per
 // element for the nibbles and some 0.4 for the rest.  Measured: 32 users at 412 to 8192 keys, 64/8 heads of 128 (160 MB)
-// 46.4 us; one user at 131072 keys (151 MB) 42.6 us, 3.5 TB/s: some 30 us of tiles, which 12 warps of 168 registers work off at
-// about 0.7 of the copy rate, and 12 us of start, partial results and merge.  Clocks say that the copies are waited for in
-// one of sixty.
+// 41 us; one user at 131072 keys (151 MB) 40 us, 3.8 TB/s: 25 us of tiles, which 12 warps of 168 registers work off at
+// about 0.88 of the copy rate, 4 us before them (list, queries) and 10 after (partial results, merges), most of it code
+// that runs once.
 //
 // Layout.  S^T = K Q^T and O^T = V^T P^T with m16n8k16: keys and channels fill M = 16, the query rows N = 8, nothing
 // is padded at 8 rows.  The matrix unit's k order is ours to choose, so a lane's K words hold whole fragments
 // in natural byte order, and V's pairs of tokens come together by one byte permute per eight codes.
 //
-// Work split.  The tiles (64 keys of one sequence, KV head and sixteen query rows) of all sequences form one list; one
+// Work split.  The tiles (64 keys of one sequence, KV head and sixteen query rows) of all sequences form one list, with a
+// place more for each segment (sequence, head, rows), whose start and end cost a warp as much as a tile; one
 // block per SM takes an equal piece, its warps equal pieces of that.  A warp streams its tiles through two slots of its own
 // (bulk copies of whole page blocks), with no barrier between warps until the end.  What a warp holds of a
-// segment (sequence, head, rows) that it does not own alone is merged within the block, then over blocks by the last to arrive;
-// every sum is taken in list order, so results do not depend on arrival.
+// segment that it does not own alone is merged within the block, then over blocks by the last to arrive, which brings their
+// parts to shared memory together; every sum is taken in list order, so results do not depend on arrival.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,13 +40,13 @@ namespace {
 constexpr int LOG_TILE = 6, TILE = 1 << LOG_TILE;  // keys
 constexpr float WEIGHT_UNIT = 2048.f;  // fp16 weights: 2^(x - m) times this, at most WEIGHT_MOST times as much
 constexpr float WEIGHT_MOST = 16.f;
-// Groups of 16 keys that are worked on at once: 1, 2 and 4 take 54, 51 and 58 us for 32 ragged users (more steps; more code than
-// the instruction cache next to the scheduler holds)
+// Groups of 16 keys that are worked on at once: 1, 2 and 4 took 54, 51 and 58 us for 32 ragged users, of which 10 have gone
+// since at the start and the end (more steps; more code than the instruction cache next to the scheduler holds)
 constexpr int SUB = 2;
 
 template <int HD, int NT>
 struct Few {
-  // 12 warps of at most 168 registers (11: 53 us for 51; 16 spill); with 16 query rows 8 warps of 255
+  // 12 warps of at most 168 registers (11: 2 us more for 32 ragged users; 16 spill); with 16 query rows 8 warps of 255
   static constexpr int WARPS = NT == 1 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int COLS = 8 * NT;
@@ -322,7 +323,8 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   pdl_wait();
 
   // ---- the list of tiles: each sequence's, summed (a sequence without rows has one, to write its zeros).  Each segment has
-  // one unit more, since its rows and results take about as long as a tile (uncounted, 32 ragged users: 42.8 us).  Up to 32
+  // one unit more, since its rows and results take about as long as a tile (uncounted, 32 ragged users: 42.8 us for 40.9, drafts
+  // 20.9 for 18.3).  Up to 32
   // sequences every warp makes the whole list, alike, and waits for no other
   const auto tiles_of = [&](int s) {
     const int user = p.users ? p.users[s] : p.seq0 + s;
@@ -969,7 +971,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   };
   // First the block's own partial results, then those that blocks have left to this one as the last to arrive: the same
   // code, which costs more the first time than what it does.  A warp takes two columns at a time, or four where two would
-  // need another round (32 ragged users: 43.0 us for 44.4; with four only, 136 keys 8.2 us for 7.8)
+  // need another round (32 ragged users: 1.4 us less than with two; 136 keys: 0.4 us less than with four)
 #pragma unroll 1
   for (int across = 0; across < 2; ++across) {
     const int groups = across ? 2 : n_groups[0];
