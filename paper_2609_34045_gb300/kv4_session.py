@@ -2,7 +2,7 @@
 
 ``Session`` keeps the buffers (pool, tables, workspaces, rotation) of a stage's layers for a number of users and
 runs the passes of one layer's attention: reserve room, rotate q, append k and v, attend, and for beams and leaving
-users fork, free and compact.  Everything is enqueued on one stream; nothing is read back between steps.
+users fork, free and compact.  Everything is enqueued on torch's current stream, that of its own tensors.
 
     python -m paper_2609_34045_gb300.kv4_session
 
@@ -34,7 +34,7 @@ class Session:
         self.status, self.n_live = torch.zeros(1, **int32), torch.zeros(1, **int32)
         self.pool = kv4.pool(self.pages, page_tokens, n_layers, n_kv_heads, head_dim)
         self.map = kv4.page_map(self.table, self.lengths, self.refs)
-        self.rope = kv4.rope_plan(kv4.kfl_rope_table(max_ctx, rope_dim or head_dim, theta), layout)
+        self.rope = kv4.rope_plan(kv4.kfl_rope_table(max_ctx, rope_dim or head_dim, theta, cuda_stream=self._stream()), layout)
         self.scratch = kv4.pages_workspace(self.pool)
         # attention of one token per user, and of prompts
         self.workspace = kv4.attend_workspace(self.pool, n_heads, n_users, max(max_tokens, n_users), max_tokens)
@@ -43,13 +43,19 @@ class Session:
     def _int32(values):
         return torch.tensor(values, dtype=torch.int32, device="cuda")
 
+    @staticmethod
+    def _stream():
+        """torch's current stream: the inputs, the lists made here and the outputs' memory are ordered on it, and on no other."""
+        return torch.cuda.current_stream().cuda_stream
+
     def begin(self, counts: dict) -> dict:
         """Room for counts[user] more tokens of each user, and what the layers of the pass need to know of them.  The
         lengths are read once here (a server knows them); a captured step would keep these tensors."""
         users, n = list(counts), [counts[u] for u in counts]
         before = self.lengths.tolist()
         ids = self._int32(users)
-        kv4.kfl_kv4_reserve(self.pool, self.map, ids, self._int32(n), self.scratch, status=self.status)
+        kv4.kfl_kv4_reserve(self.pool, self.map, ids, self._int32(n), self.scratch, status=self.status,
+                            cuda_stream=self._stream())
         start = [0]
         for c in n:
             start.append(start[-1] + c)
@@ -60,24 +66,27 @@ class Session:
     def attend(self, layer: int, step: dict, q, k, v, window: int = 0):
         """One layer's attention of a pass: q [token][query head][head_dim] rotated, k and v appended, the users' rows
         attended to."""
-        turned, out = torch.empty_like(q), torch.empty_like(q)
-        kv4.kfl_rope(self.rope, q, turned, None, None, step["positions"], status=self.status)
+        turned, out, stream = torch.empty_like(q), torch.empty_like(q), self._stream()
+        kv4.kfl_rope(self.rope, q, turned, None, None, step["positions"], status=self.status, cuda_stream=stream)
         kv4.kfl_kv4_append(self.pool, self.map, layer, k, v, step["row_users"], step["positions"], rope=self.rope,
-                           status=self.status)
+                           status=self.status, cuda_stream=stream)
         kv4.kfl_kv4_attend(self.pool, self.map, layer, turned, out, self.workspace, users=step["users"],
-                           q_start=step["q_start"], max_q=step["max_q"], window=window, status=self.status)
+                           q_start=step["q_start"], max_q=step["max_q"], window=window, status=self.status,
+                           cuda_stream=stream)
         return out
 
     def fork(self, src, dst):
         """User dst[i] goes on from where src[i] is, all at once."""
-        kv4.kfl_kv4_fork(self.pool, self.map, self._int32(src), self._int32(dst), self.scratch, status=self.status)
+        kv4.kfl_kv4_fork(self.pool, self.map, self._int32(src), self._int32(dst), self.scratch, status=self.status,
+                         cuda_stream=self._stream())
 
     def free(self, users):
-        kv4.kfl_kv4_free(self.pool, self.map, self._int32(users), status=self.status)
+        kv4.kfl_kv4_free(self.pool, self.map, self._int32(users), status=self.status, cuda_stream=self._stream())
 
     def compact(self):
         """Live pages to the lowest numbers; returns how many there are (on the device)."""
-        kv4.kfl_kv4_compact(self.pool, self.map, self.table, self.refs, self.n_live, self.scratch, status=self.status)
+        kv4.kfl_kv4_compact(self.pool, self.map, self.table, self.refs, self.n_live, self.scratch, status=self.status,
+                            cuda_stream=self._stream())
         return self.n_live
 
 
