@@ -242,17 +242,26 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
 
 # ---- pages ---------------------------------------------------------------------------------------
 
-def pages_workspace(p):
-    """Scratch of the calls that hand out or move pages."""
+def kfl_kv4_pages_workspace_bytes(p) -> int:
     out = C.c_size_t(0)
     _check(lib().kfl_kv4_pages_workspace_bytes(C.byref(p), C.byref(out)), "kfl_kv4_pages_workspace_bytes")
-    return torch.empty(out.value, dtype=torch.uint8, device="cuda")
+    return out.value
+
+
+def pages_workspace(p):
+    """Scratch of the calls that hand out or move pages."""
+    return torch.empty(kfl_kv4_pages_workspace_bytes(p), dtype=torch.uint8, device="cuda")
 
 
 def _scratch(p, workspace):
-    """Address of a workspace that covers the pool's pages."""
-    if workspace.numel() < 12 * p.n_pages:
-        raise ValueError("the workspace is one of pages_workspace for this pool")
+    """Address of a workspace that covers the pool's pages: as many bytes as the library asks for, which the pool's
+    description keeps for the next call's check."""
+    n_pages, need = getattr(p, "scratch", (None, 0))
+    if n_pages != p.n_pages:
+        need = kfl_kv4_pages_workspace_bytes(p)
+        p.scratch = (p.n_pages, need)
+    if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"the workspace is one of pages_workspace for this pool ({need} bytes)")
     return workspace.data_ptr()
 
 
