@@ -4,7 +4,7 @@ paged KV cache (argument marshalling only, as in ``stage``).
 Functions named ``kfl_*`` call the C entry point of that name on CUDA tensors.  ``rope_plan``, ``pool`` and
 ``page_map`` describe buffers that the caller keeps; ``attend_workspace`` and ``pages_workspace`` allocate the
 scratch that those calls want.  Rows of heads are tensors ``[token][head][head_dim]`` of any strides whose last
-is 1.
+is 1.  Every tensor lies in the memory of the current device; others are refused.
 """
 from __future__ import annotations
 
@@ -53,11 +53,12 @@ class kfl_kv4_map(C.Structure):
 
 
 _lib = _signed = None
+_several = True  # whether a tensor may be another device's (until the library is loaded: perhaps)
 
 
 def lib() -> C.CDLL:
     """The library of ``stage.lib()`` with the signatures of these entry points."""
-    global _lib, _signed
+    global _lib, _signed, _several
     L = stage.lib()
     if _signed is not L:
         vp, i, f, P = C.c_void_p, C.c_int, C.c_float, C.POINTER
@@ -80,6 +81,7 @@ def lib() -> C.CDLL:
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, i
         _lib = _signed = L
+        _several = torch.cuda.device_count() > 1
     return L
 
 
@@ -89,9 +91,20 @@ def _check(rc: int, where: str) -> None:
         raise KflError(rc, detail if detail.startswith(where) else where)
 
 
-def _at(t):
-    """Address of a CUDA tensor (None: NULL)."""
-    return None if t is None else t.data_ptr()
+def _at(t, where):
+    """Address of a tensor in the memory of the current device, which is where the calls run (None: NULL)."""
+    if t is None:
+        return None
+    if not t.is_cuda or _several and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{where} is not in the memory of the current CUDA device")
+    return t.data_ptr()
+
+
+def _handle(h):
+    """A description whose buffers are the current device's."""
+    if _several and getattr(h, "device", None) not in (None, torch.cuda.current_device()):
+        raise ValueError(f"the buffers of a {type(h).__name__} are not in the memory of the current CUDA device")
+    return C.byref(h)
 
 
 def _int32(t, where, n=None):
@@ -99,7 +112,7 @@ def _int32(t, where, n=None):
         return None
     if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
         raise ValueError(f"{where} is a contiguous int32 tensor" + (f" of {n}" if n is not None else ""))
-    return t.data_ptr()
+    return t.data_ptr() if t.is_cuda and not _several else _at(t, where)  # (a step's call has six of them: no call more)
 
 
 def _heads(t, where, n_tokens=None, head_dim=None):
@@ -115,7 +128,7 @@ def _heads(t, where, n_tokens=None, head_dim=None):
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{where} is bf16, fp16 or fp32")
-    return _pack_heads(t.data_ptr(), per_token, per_head, n_heads, dtype)
+    return _pack_heads(t.data_ptr() if t.is_cuda and not _several else _at(t, where), per_token, per_head, n_heads, dtype)
 
 
 # ---- rotary positions ----------------------------------------------------------------------------
@@ -127,7 +140,7 @@ def kfl_rope_table(n_pos: int, rope_dim: int, theta: float, scaling: str = "plai
     if out is None:
         out = torch.empty(max(n_pos, 0), max(rope_dim // 2, 0), 2, dtype=torch.float32, device="cuda")
     cfg = kfl_rope_cfg(rope_dim, SCALINGS[scaling], theta, factor, low, high, original_ctx, magnitude)
-    _check(lib().kfl_rope_table(C.byref(cfg), n_pos, _at(out), cuda_stream), "kfl_rope_table")
+    _check(lib().kfl_rope_table(C.byref(cfg), n_pos, _at(out, "out"), cuda_stream), "kfl_rope_table")
     return out
 
 
@@ -135,8 +148,9 @@ def rope_plan(table, layout: str = "half") -> kfl_rope_plan:
     """A rotation by a table of kfl_rope_table; keeps the tensor alive."""
     if table.dtype != torch.float32 or not table.is_contiguous() or table.dim() != 3 or table.shape[2] != 2:
         raise ValueError("a rotation's table is a contiguous fp32 [n_pos][rope_dim / 2][2]")
-    plan = kfl_rope_plan(table.data_ptr(), table.shape[0], 2 * table.shape[1], LAYOUTS[layout])
-    plan.table = table
+    code = LAYOUTS[layout]
+    plan = kfl_rope_plan(_at(table, "the table"), table.shape[0], 2 * table.shape[1], code)
+    plan.table, plan.device = table, table.get_device()
     return plan
 
 
@@ -145,7 +159,7 @@ def kfl_rope(plan: kfl_rope_plan, q, q_out, k, k_out, positions, inverse: bool =
     """Rotates q into q_out and k into k_out ([token][head][head_dim]; k and k_out may be None; an output may be
     its input) by int32 positions [token].  Asynchronous."""
     n, _, hd = q.shape
-    _check(lib().kfl_rope(C.byref(plan), _heads(q, "q", n, hd), _heads(q_out, "q_out", n, hd), _heads(k, "k", n, hd),
+    _check(lib().kfl_rope(_handle(plan), _heads(q, "q", n, hd), _heads(q_out, "q_out", n, hd), _heads(k, "k", n, hd),
                           _heads(k_out, "k_out", n, hd), _int32(positions, "positions", n), n, hd, int(inverse), _int32(status, "status", 1),
                           cuda_stream), "kfl_rope")
 
@@ -159,8 +173,8 @@ def pool(pages, page_tokens: int, n_layers: int, n_kv_heads: int, head_dim: int,
         if pages.dtype != torch.uint8 or not pages.is_contiguous() or page_bytes < 1 or pages.numel() % page_bytes:
             raise ValueError(f"the pages are a contiguous uint8 tensor of whole pages ({page_bytes} bytes)")
         n_pages = pages.numel() // page_bytes
-    p = kfl_kv4_pool(_at(pages), n_pages, page_tokens, n_layers, n_kv_heads, head_dim)
-    p.tensor = pages
+    p = kfl_kv4_pool(_at(pages, "the pool"), n_pages, page_tokens, n_layers, n_kv_heads, head_dim)
+    p.tensor, p.device = pages, None if pages is None else pages.get_device()
     return p
 
 
@@ -168,14 +182,14 @@ def page_map(table, lengths, refs) -> kfl_kv4_map:
     """Who holds which pages: int32 table [n_users][max_pages], lengths [n_users], refs [n_pages]."""
     m = kfl_kv4_map(_int32(table, "table"), _int32(lengths, "lengths", table.shape[0]), _int32(refs, "refs"),
                     table.shape[0], table.shape[1])
-    m.tensors = (table, lengths, refs)
+    m.tensors, m.device = (table, lengths, refs), table.get_device()
     return m
 
 
 def _covers(p, m):
     if m.tensors[2].numel() < p.n_pages:
         raise ValueError(f"refs is a contiguous int32 tensor of {p.n_pages}")
-    return C.byref(p), C.byref(m)
+    return _handle(p), _handle(m)
 
 
 def kfl_kv4_page_bytes(p) -> int:
@@ -190,8 +204,8 @@ def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=N
     k rotated first where ``rope`` is a rope_plan.  users None: row t is user t's.  Asynchronous."""
     n = k.shape[0]
     a, b = _heads(k, "k", n, p.head_dim), _heads(v, "v", n, p.head_dim)
-    _check(lib().kfl_kv4_append(C.byref(p), C.byref(m), layer, a, b, _int32(users, "users", n),
-                                _int32(positions, "positions", n), n, rope and C.byref(rope),
+    _check(lib().kfl_kv4_append(_handle(p), _handle(m), layer, a, b, _int32(users, "users", n),
+                                _int32(positions, "positions", n), n, rope and _handle(rope),
                                 _int32(status, "status", 1), cuda_stream), "kfl_kv4_append")
 
 
@@ -199,7 +213,7 @@ def kfl_kv4_read(p, m, layer: int, users, positions, k_out, v_out, status=None, 
     """The values that the cache holds for rows (users[t], positions[t]) of one layer.  Asynchronous."""
     n = k_out.shape[0]
     a, b = _heads(k_out, "k_out", n, p.head_dim), _heads(v_out, "v_out", n, p.head_dim)
-    _check(lib().kfl_kv4_read(C.byref(p), C.byref(m), layer, _int32(users, "users", n),
+    _check(lib().kfl_kv4_read(_handle(p), _handle(m), layer, _int32(users, "users", n),
                               _int32(positions, "positions", n), n, a, b,
                               _int32(status, "status", 1), cuda_stream), "kfl_kv4_read")
 
@@ -234,9 +248,9 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
         raise ValueError("lse is a contiguous fp32 [token][query head]")
     a, b = _heads(q, "q", n, p.head_dim), _heads(out, "out", n, p.head_dim)
-    _check(lib().kfl_kv4_attend(C.byref(p), C.byref(m), layer, a, b, _at(lse),
+    _check(lib().kfl_kv4_attend(_handle(p), _handle(m), layer, a, b, _at(lse, "lse"),
                                 _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
-                                1.0 / math.sqrt(hd) if scale is None else scale, window, workspace.data_ptr(),
+                                1.0 / math.sqrt(hd) if scale is None else scale, window, _at(workspace, "the workspace"),
                                 workspace.numel(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
 
 
@@ -262,7 +276,7 @@ def _scratch(p, workspace):
         p.scratch = (p.n_pages, need)
     if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"the workspace is one of pages_workspace for this pool ({need} bytes)")
-    return workspace.data_ptr()
+    return _at(workspace, "the workspace")
 
 
 def kfl_kv4_reserve(p, m, users, n_new, workspace, status=None, cuda_stream: int | None = None) -> None:
@@ -300,5 +314,5 @@ def kfl_kv4_compact(p, m, table_out, refs_out, n_live, workspace, status=None, c
 def kfl_kv4_copy_pages(p, src, dst, status=None, cuda_stream: int | None = None) -> None:
     """Copies page src[i] to page dst[i] (int32).  Asynchronous."""
     n = src.numel()
-    _check(lib().kfl_kv4_copy_pages(C.byref(p), _int32(src, "src"), _int32(dst, "dst", n), n,
+    _check(lib().kfl_kv4_copy_pages(_handle(p), _int32(src, "src"), _int32(dst, "dst", n), n,
                                     _int32(status, "status", 1), cuda_stream), "kfl_kv4_copy_pages")

@@ -54,3 +54,111 @@ def test_a_pools_own_workspace_is_taken(lib):  # noqa: F811
     p.n_pages = 3000  # (a description that changes is looked at anew)
     with pytest.raises(ValueError, match="pages_workspace"):
         kv4._scratch(p, Fake(need))
+
+
+class OnDevice:
+    """A tensor that says it lies in a device's memory."""
+    is_cuda = True
+
+    def __init__(self, t, device=0):
+        self.t, self.index = t, device
+
+    def get_device(self):
+        return self.index
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def calls(place):
+    """Every call with tensors, as (function, arguments by name) in the binding's own order; place(name, tensor) puts each
+    where it shall be."""
+    def i32(name, n):
+        return place(name, torch.zeros(n, dtype=torch.int32))
+
+    def rows(name, n, heads, dtype=torch.bfloat16):
+        return place(name, torch.zeros(n, heads, 64, dtype=dtype))
+
+    def pool(name="pages"):
+        return kv4.pool(place(name, torch.zeros(5 * 2 * 16 * 72, dtype=torch.uint8)), 16, 1, 2, 64)
+
+    def page_map():
+        return kv4.page_map(place("table", torch.zeros(3, 4, dtype=torch.int32)), i32("lengths", 3), i32("refs", 5))
+
+    def plan():
+        return kv4.rope_plan(place("cos_sin", torch.zeros(9, 32, 2)))
+
+    def scratch():
+        return place("workspace", torch.zeros(1 << 15, dtype=torch.uint8))
+
+    status = i32("status", 1)
+    yield lambda: kv4.kfl_rope_table(9, 64, 1e4, out=place("out", torch.zeros(9, 32, 2)))
+    yield lambda: kv4.kfl_rope(plan(), rows("q", 2, 4), rows("q_out", 2, 4), rows("k", 2, 2), rows("k_out", 2, 2),
+                               i32("positions", 2), status=status)
+    yield lambda: kv4.kfl_kv4_append(pool(), page_map(), 0, rows("k", 2, 2), rows("v", 2, 2), i32("users", 2), i32("positions", 2),
+                                     rope=plan(), status=status)
+    yield lambda: kv4.kfl_kv4_read(pool(), page_map(), 0, i32("users", 2), i32("positions", 2), rows("k_out", 2, 2),
+                                   rows("v_out", 2, 2), status=status)
+    yield lambda: kv4.kfl_kv4_attend(pool(), page_map(), 0, rows("q", 2, 4), rows("out", 2, 4), scratch(), users=i32("users", 1),
+                                     q_start=i32("q_start", 2), max_q=2, lse=place("lse", torch.zeros(2, 4)), status=status)
+    yield lambda: kv4.kfl_kv4_reserve(pool(), page_map(), i32("users", 2), i32("n_new", 2), scratch(), status=status)
+    yield lambda: kv4.kfl_kv4_fork(pool(), page_map(), i32("src", 2), i32("dst", 2), scratch(), status=status)
+    yield lambda: kv4.kfl_kv4_free(pool(), page_map(), i32("users", 2), status=status)
+    yield lambda: kv4.kfl_kv4_compact(pool(), page_map(), i32("table_out", 12), i32("refs_out", 5), i32("n_live", 1), scratch(),
+                                      status=status)
+    yield lambda: kv4.kfl_kv4_copy_pages(pool(), i32("src", 2), i32("dst", 2), status=status)
+
+
+@pytest.fixture
+def recorded(monkeypatch, lib):  # noqa: F811
+    """The library's calls do nothing and succeed; a list of their names."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return getattr(lib, name)
+            return lambda *a: made.append(name) or 0
+
+    monkeypatch.setattr(kv4, "lib", lambda: Library())
+    monkeypatch.setattr(kv4, "_several", False)
+    return made
+
+
+def test_host_tensors_are_refused(recorded):
+    """Each tensor of each call: its address would go to a kernel as it is."""
+    names = []
+    for call in calls(lambda name, t: names.append(name) or OnDevice(t)):
+        call()
+    assert len(recorded) == 10
+    for host in sorted(set(names)):
+        del recorded[:]
+        refused = 0
+        for call in calls(lambda name, t: t if name == host else OnDevice(t)):  # noqa: B023
+            try:
+                call()
+            except ValueError as e:
+                assert "current CUDA device" in str(e)
+                refused += 1
+        assert refused > 0 and refused + len(recorded) == 10, host
+
+
+def test_tensors_of_another_device_are_refused(recorded, monkeypatch):
+    monkeypatch.setattr(kv4, "_several", True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in calls(lambda name, t: OnDevice(t, 1)):
+        call()
+    assert len(recorded) == 10
+    del recorded[:]
+    for call in calls(lambda name, t: OnDevice(t, 0)):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
+    assert recorded == []
+    # descriptions that were made while another device was the current one
+    p = kv4.pool(OnDevice(torch.zeros(5 * 16 * 72, dtype=torch.uint8), 1), 16, 1, 1, 64)
+    m = kv4.page_map(*(OnDevice(torch.zeros(s, dtype=torch.int32), 1) for s in ((3, 4), 3, 5)))
+    plan = kv4.rope_plan(OnDevice(torch.zeros(9, 32, 2), 1))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for h in (p, m, plan):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            kv4._handle(h)
