@@ -247,11 +247,13 @@ def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None
         raise ValueError("more sequences than users")
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
         raise ValueError("lse is a contiguous fp32 [token][query head]")
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace is contiguous")
     a, b = _heads(q, "q", n, p.head_dim), _heads(out, "out", n, p.head_dim)
     _check(lib().kfl_kv4_attend(_handle(p), _handle(m), layer, a, b, _at(lse, "lse"),
                                 _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
                                 1.0 / math.sqrt(hd) if scale is None else scale, window, _at(workspace, "the workspace"),
-                                workspace.numel(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
+                                workspace.numel() * workspace.element_size(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
 
 
 # ---- pages ---------------------------------------------------------------------------------------

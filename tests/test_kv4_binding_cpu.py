@@ -109,16 +109,22 @@ def calls(place):
     yield lambda: kv4.kfl_kv4_copy_pages(pool(), i32("src", 2), i32("dst", 2), status=status)
 
 
+class Names(list):
+    def __init__(self):
+        super().__init__()
+        self.args = []
+
+
 @pytest.fixture
 def recorded(monkeypatch, lib):  # noqa: F811
     """The library's calls do nothing and succeed; a list of their names."""
-    made = []
+    made = Names()
 
     class Library:
         def __getattr__(self, name):
             if name.endswith("_bytes"):
                 return getattr(lib, name)
-            return lambda *a: made.append(name) or 0
+            return lambda *a: made.append(name) or made.args.append(a) or 0
 
     monkeypatch.setattr(kv4, "lib", lambda: Library())
     monkeypatch.setattr(kv4, "_several", False)
@@ -162,3 +168,17 @@ def test_tensors_of_another_device_are_refused(recorded, monkeypatch):
     for h in (p, m, plan):
         with pytest.raises(ValueError, match="current CUDA device"):
             kv4._handle(h)
+
+
+def test_the_attentions_workspace_is_memory_of_its_size(recorded):
+    """What is handed on as its size is the bytes behind its address: not an expanded tensor's count, nor that of its elements."""
+    pool = kv4.pool(OnDevice(torch.zeros(5 * 16 * 72, dtype=torch.uint8)), 16, 1, 1, 64)
+    m = kv4.page_map(*(OnDevice(torch.zeros(s, dtype=torch.int32)) for s in ((3, 4), 3, 5)))
+    q, out = (OnDevice(torch.zeros(2, 4, 64, dtype=torch.bfloat16)) for _ in range(2))
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(1 << 24), torch.zeros(1 << 16, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            kv4.kfl_kv4_attend(pool, m, 0, q, out, OnDevice(bad))
+    assert recorded == []
+    for ok in (torch.zeros(1 << 16, dtype=torch.uint8), torch.zeros(1 << 14, dtype=torch.float32)):
+        kv4.kfl_kv4_attend(pool, m, 0, q, out, OnDevice(ok))
+        assert recorded.args[-1][-3] == 1 << 16
