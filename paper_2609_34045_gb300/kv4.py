@@ -139,6 +139,8 @@ def kfl_rope_table(n_pos: int, rope_dim: int, theta: float, scaling: str = "plai
     """cos and sin of positions [0, n_pos): fp32 [n_pos][rope_dim / 2][2] (``out``, or a new tensor)."""
     if out is None:
         out = torch.empty(max(n_pos, 0), max(rope_dim // 2, 0), 2, dtype=torch.float32, device="cuda")
+    elif out.dtype != torch.float32 or not out.is_contiguous() or out.numel() < n_pos * rope_dim:
+        raise ValueError("out is a contiguous fp32 [n_pos][rope_dim / 2][2]")
     cfg = kfl_rope_cfg(rope_dim, SCALINGS[scaling], theta, factor, low, high, original_ctx, magnitude)
     _check(lib().kfl_rope_table(C.byref(cfg), n_pos, _at(out, "out"), cuda_stream), "kfl_rope_table")
     return out

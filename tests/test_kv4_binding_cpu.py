@@ -182,3 +182,14 @@ def test_the_attentions_workspace_is_memory_of_its_size(recorded):
     for ok in (torch.zeros(1 << 16, dtype=torch.uint8), torch.zeros(1 << 14, dtype=torch.float32)):
         kv4.kfl_kv4_attend(pool, m, 0, q, out, OnDevice(ok))
         assert recorded.args[-1][-3] == 1 << 16
+
+
+def test_a_table_has_room_for_its_angles(recorded):
+    for bad in (torch.zeros(8, 32, 2), torch.zeros(9, 32, 2, dtype=torch.float64), torch.zeros(9, 32, 4)[..., ::2],
+                torch.zeros(1).expand(9, 32, 2)):
+        with pytest.raises(ValueError, match="out is"):
+            kv4.kfl_rope_table(9, 64, 1e4, out=OnDevice(bad))
+    assert recorded == []
+    for ok in (torch.zeros(9, 32, 2), torch.zeros(600)):
+        kv4.kfl_rope_table(9, 64, 1e4, out=OnDevice(ok))
+    assert recorded == ["kfl_rope_table"] * 2
