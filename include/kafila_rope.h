@@ -63,8 +63,8 @@ typedef struct {
   double magnitude;    /* cos and sin times this; 0: 1, or RAMP's own */
 } kfl_rope_cfg;
 
-/* cos and sin of the angles of positions [0, n_pos): device fp32 [n_pos][rope_dim / 2][2], computed in fp64.
- * Enqueued on cuda_stream.  Errors: KFL_ERR_ARG, KFL_ERR_CUDA. */
+/* cos and sin of the angles of positions [0, n_pos): device fp32 [n_pos][rope_dim / 2][2], 8-byte aligned (a
+ * kfl_rope_plan wants 16), computed in fp64.  Enqueued on cuda_stream.  Errors: KFL_ERR_ARG, KFL_ERR_CUDA. */
 int kfl_rope_table(const kfl_rope_cfg *cfg, int n_pos, float *cos_sin, void *cuda_stream);
 
 /* A rotation: a table of kfl_rope_table (16-byte aligned) and how its pairs lie in a head. */

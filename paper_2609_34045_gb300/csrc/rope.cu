@@ -165,6 +165,7 @@ extern "C" int kfl_rope_table(const kfl_rope_cfg *cfg, int n_pos, float *cos_sin
   using namespace kfl;
   const char *me = "kfl_rope_table";
   if (!cfg || !cos_sin || n_pos < 1) return bad_arg(me, "NULL pointer or no positions");
+  if (reinterpret_cast<uintptr_t>(cos_sin) & 7) return bad_arg(me, "the table is 8-byte aligned (16 for a rotation)");
   if (cfg->rope_dim < 2 || cfg->rope_dim > 512 || cfg->rope_dim % 2) return bad_arg(me, "rope_dim is even, 2..512");
   if (!(cfg->theta > 1.0) || !std::isfinite(cfg->theta)) return bad_arg(me, "theta is above 1");
   if (cfg->scaling < KFL_ROPE_PLAIN || cfg->scaling > KFL_ROPE_RAMP) return bad_arg(me, "unknown scaling");

@@ -1,8 +1,11 @@
 """What the binding of the 4-bit cache refuses before a call reaches the library, and what it lets through."""
+import ctypes as C
+
 import pytest
 import torch
 
 from paper_2609_34045_gb300 import kv4
+from paper_2609_34045_gb300 import stage as K
 from test_kv4_cpu import lib  # noqa: F401
 
 
@@ -193,3 +196,11 @@ def test_a_table_has_room_for_its_angles(recorded):
     for ok in (torch.zeros(9, 32, 2), torch.zeros(600)):
         kv4.kfl_rope_table(9, 64, 1e4, out=OnDevice(ok))
     assert recorded == ["kfl_rope_table"] * 2
+
+
+@pytest.mark.parametrize("off", [1, 2, 4, 12])
+def test_a_table_off_its_pairs_alignment_is_refused(lib, off):  # noqa: F811
+    """cos and sin are stored as a pair of 8 bytes."""
+    cfg = kv4.kfl_rope_cfg(64, 0, 1e4, 1.0, 0.0, 0.0, 0.0, 0.0)
+    assert lib.kfl_rope_table(C.byref(cfg), 10, (1 << 20) + off, None) == K.KFL_ERR_ARG
+    assert "aligned" in K.kfl_last_error_detail()
