@@ -89,7 +89,9 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.n_seqs = n_seqs, p.n_tokens = n_tokens, p.max_q = q_start ? max_q : 1;
   p.n_heads = q->n_heads, p.group = q->n_heads / pool->n_kv_heads;
   p.group_inv = (65536 + p.group - 1) / p.group;
-  p.scale = scale, p.window = window, p.status = status;
+  p.scale = scale, p.status = status;
+  // (a window that no context fills is none; the kernels take it off places below 2^26, in 32 bits)
+  p.window = window >= map->max_pages * pool->page_tokens ? 0 : window;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)p.max_q * p.group;
   const bool few = is_few(pool, map, n_seqs, rows);
