@@ -222,11 +222,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv4_fork_kernel(const PlanParams
     } else if (src == dst) {
       dst = -1;
     } else {
-      length = min(max(0, p.map.lengths[src]), p.map.max_pages << P);
+      // (max_pages 2^24 of 128 tokens are 2^31 of them)
+      const int64_t most = (int64_t)p.map.max_pages << P;
+      length = (int)min((int64_t)max(0, p.map.lengths[src]), most);
       full = length >> P;
       need = (length & (p.pool.page_tokens() - 1)) != 0;
-      const int before = min(max(0, p.map.lengths[dst]), p.map.max_pages << P);
-      columns = max(full + need, (before + p.pool.page_tokens() - 1) >> P);
+      const int64_t before = min((int64_t)max(0, p.map.lengths[dst]), most);
+      columns = max(full + need, (int)((before + p.pool.page_tokens() - 1) >> P));
     }
   }
   int total;
