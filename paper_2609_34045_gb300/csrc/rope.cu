@@ -146,7 +146,8 @@ cudaError_t launch_rope(RopeParams &p, bool wide, bool half, int n_tokens, cudaS
   // blocks).  Many: a block per token with up to four heads per thread, whose loads are in flight together.
   const bool few = n_tokens < 304;
   const int most = std::max(1, (few ? 64 : ROPE_THREADS) / p.n_items);
-  p.heads_per_block = few ? std::min(p.n_heads, most) : p.n_heads;
+  // (a grid has at most 65535 rows of blocks: of 2 x 65536 heads a block may take more than its threads do at once)
+  p.heads_per_block = few ? std::min(p.n_heads, std::max(most, (p.n_heads + 65534) / 65535)) : p.n_heads;
   const int steps = std::max((p.heads_per_block + most - 1) / most, few ? 1 : std::min(p.heads_per_block, ROPE_AHEAD));
   p.heads_per_step = (p.heads_per_block + steps - 1) / steps;
   const dim3 grid(n_tokens, (p.n_heads + p.heads_per_block - 1) / p.heads_per_block);
