@@ -18,6 +18,10 @@ import torch
 from . import kv4
 
 
+class NoRoom(RuntimeError):
+    """The pool or a user's row of the table has no room for a pass; nothing was reserved."""
+
+
 class Session:
     """Buffers of a stage's 4-bit cache: ``n_users`` users of up to ``max_ctx`` tokens sharing ``n_pages`` pages.
 
@@ -26,6 +30,7 @@ class Session:
     def __init__(self, n_layers, n_heads, n_kv_heads, head_dim, n_users, max_ctx, n_pages, page_tokens=64,
                  dtype=torch.bfloat16, theta=1e6, rope_dim=None, layout="half", max_tokens=2048):
         self.n_heads, self.head_dim, self.dtype, self.n_users = n_heads, head_dim, dtype, n_users
+        self.max_ctx, self.page_tokens = max_ctx, page_tokens
         page_bytes = n_layers * n_kv_heads * (page_tokens * head_dim * 9 // 8)
         int32 = dict(dtype=torch.int32, device="cuda")
         self.pages = torch.empty(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
@@ -48,11 +53,26 @@ class Session:
         """torch's current stream: the inputs, the lists made here and the outputs' memory are ordered on it, and on no other."""
         return torch.cuda.current_stream().cuda_stream
 
+    def _room(self, pages):
+        if pages > 0:
+            free = int((self.refs == 0).sum())
+            if pages > free:
+                raise NoRoom(f"{pages} new pages are needed, {free} of {self.refs.numel()} are free")
+
     def begin(self, counts: dict) -> dict:
-        """Room for counts[user] more tokens of each user, and what the layers of the pass need to know of them.  The
-        lengths are read once here (a server knows them); a captured step would keep these tensors."""
+        """Room for counts[user] more tokens of each user, and what the layers of the pass need to know of them.  Waits for
+        the device once, to read the lengths, and once more in passes that need new pages, to count the free ones: the
+        operators themselves only report a full pool in `status`, by which time a pass that goes on has attended at the
+        wrong positions.  Raises NoRoom before anything is changed."""
         users, n = list(counts), [counts[u] for u in counts]
+        if any(not 0 <= u < self.n_users for u in users) or any(c < 0 for c in n):
+            raise ValueError(f"counts of users below {self.n_users}, none negative")
         before = self.lengths.tolist()
+        for u, c in zip(users, n):
+            if before[u] + c > self.max_ctx:
+                raise NoRoom(f"user {u} has {before[u]} tokens and takes {c} more, of {self.max_ctx}")
+        pages = [-(-(before[u] + c) // self.page_tokens) - -(-before[u] // self.page_tokens) for u, c in zip(users, n)]
+        self._room(sum(pages))
         ids = self._int32(users)
         kv4.kfl_kv4_reserve(self.pool, self.map, ids, self._int32(n), self.scratch, status=self.status,
                             cuda_stream=self._stream())

@@ -84,3 +84,27 @@ def test_a_captured_layer_of_a_pass():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want) and s.status.item() == 0
+
+
+def test_a_full_pool_stops_a_pass_before_it_begins():
+    """Users go on where they were once there is room again, with the outputs of a session that was never short."""
+    from paper_2609_34045_gb300.kv4_session import NoRoom
+
+    def passes(s, short):
+        out = []
+        for i, counts in enumerate(({0: 30, 1: 17, 2: 16}, {0: 2, 1: 1}, {0: 1, 2: 3})):
+            if i == 2 and short:
+                tables = s.table.clone(), s.lengths.clone(), s.refs.clone()
+                for bad in (counts, {1: 1, 0: 17}, {2: 1}):
+                    with pytest.raises(NoRoom):
+                        s.begin(bad)
+                assert all(torch.equal(a, b) for a, b in zip(tables, (s.table, s.lengths, s.refs)))
+            if i == 2:
+                s.free([1])
+            step = s.begin(counts)
+            out.append([s.attend(layer, step, *rows(sum(counts.values()), 3 * i + layer)) for layer in range(LAYERS)])
+        assert s.status.item() == 0
+        return out
+
+    full, roomy = session(n_pages=5), session()
+    assert all(torch.equal(a, b) for x, y in zip(passes(full, True), passes(roomy, False)) for a, b in zip(x, y))

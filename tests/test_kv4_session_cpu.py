@@ -45,3 +45,34 @@ def test_every_call_is_on_torchs_current_stream(session):
     session.compact()
     assert {name for name, _ in session.calls} == set(CALLS)
     assert [name for name, kw in session.calls if kw.get("cuda_stream") != STREAM] == []
+
+
+def reserved(s):
+    return [name for name, _ in s.calls].count("kfl_kv4_reserve")
+
+
+def test_a_pass_that_has_no_room_is_refused_before_it_begins(session):
+    """8 pages of 16 tokens, 5 of them held: by user 0 with 60 tokens (4 pages) and user 1 with 16 (1)."""
+    session.lengths[:2] = torch.tensor([60, 16], dtype=torch.int32)
+    session.refs[:5] = 1
+    for ok in ({0: 4}, {1: 48}, {0: 4, 1: 17, 2: 16}, {2: 48}, {0: 0, 1: 0}):
+        session.begin(ok)
+    assert reserved(session) == 5
+    for bad in ({2: 49}, {0: 4, 1: 17, 2: 17}, {1: 33, 2: 17}):  # four pages, of three
+        with pytest.raises(kv4_session.NoRoom, match="free"):
+            session.begin(bad)
+    for bad in ({0: 5}, {2: 1, 0: 100}):  # 64 tokens a user
+        with pytest.raises(kv4_session.NoRoom, match="user 0"):
+            session.begin(bad)
+    for bad in ({3: 1}, {-1: 1}, {0: -1, 1: 1}):
+        with pytest.raises(ValueError):
+            session.begin(bad)
+    assert reserved(session) == 5
+
+
+def test_a_row_that_ends_behind_the_longest_context(session):
+    """A table's row may have room behind max_ctx, for which there are no angles."""
+    session.max_ctx = 60
+    session.begin({0: 60})
+    with pytest.raises(kv4_session.NoRoom):
+        session.begin({0: 61})
