@@ -19,7 +19,7 @@ from . import kv4
 
 
 class NoRoom(RuntimeError):
-    """The pool or a user's row of the table has no room for a pass; nothing was reserved."""
+    """The pool or a user's row of the table has no room for a pass or a fork; nothing was changed."""
 
 
 class Session:
@@ -96,7 +96,13 @@ class Session:
         return out
 
     def fork(self, src, dst):
-        """User dst[i] goes on from where src[i] is, all at once."""
+        """User dst[i] goes on from where src[i] is, all at once.  Waits for the device, to read the lengths: raises
+        NoRoom where the pool has no page for a copied end (the operator would leave that user as it was)."""
+        src, dst = list(src), list(dst)
+        if len(src) != len(dst) or len(set(dst)) != len(dst) or any(not 0 <= u < self.n_users for u in src + dst):
+            raise ValueError(f"as many users below {self.n_users} in src and dst, in dst none twice")
+        lengths = self.lengths.tolist()
+        self._room(sum(a != b and lengths[a] % self.page_tokens != 0 for a, b in zip(src, dst)))
         kv4.kfl_kv4_fork(self.pool, self.map, self._int32(src), self._int32(dst), self.scratch, status=self.status,
                          cuda_stream=self._stream())
 

@@ -108,3 +108,16 @@ def test_a_full_pool_stops_a_pass_before_it_begins():
 
     full, roomy = session(n_pages=5), session()
     assert all(torch.equal(a, b) for x, y in zip(passes(full, True), passes(roomy, False)) for a, b in zip(x, y))
+
+
+def test_a_full_pool_stops_a_fork():
+    from paper_2609_34045_gb300.kv4_session import NoRoom
+    s = session(n_pages=4)
+    s.begin({0: 40, 1: 3})
+    before = s.table.clone(), s.lengths.clone(), s.refs.clone()
+    with pytest.raises(NoRoom):
+        s.fork([0], [1])  # (new pages are taken before old ones are given back)
+    assert all(torch.equal(a, b) for a, b in zip(before, (s.table, s.lengths, s.refs)))
+    s.free([1])
+    s.fork([0], [1])
+    assert s.lengths.tolist()[:2] == [40, 40] and s.refs.tolist() == [2, 2, 1, 1] and s.status.item() == 0

@@ -76,3 +76,21 @@ def test_a_row_that_ends_behind_the_longest_context(session):
     session.begin({0: 60})
     with pytest.raises(kv4_session.NoRoom):
         session.begin({0: 61})
+
+
+def test_a_fork_that_has_no_room_is_refused(session):
+    """Two free pages, and users whose last page is full (0), not full (1) and not there (2)."""
+    session.lengths[:2] = torch.tensor([16, 20], dtype=torch.int32)
+    session.refs[:6] = 1
+    for ok in (([1, 1], [0, 2]), ([0, 1, 1], [2, 1, 0]), ([0, 0], [1, 2]), ([2], [0]), ([], [])):
+        session.fork(*ok)
+    forks = [name for name, _ in session.calls].count("kfl_kv4_fork")
+    assert forks == 5
+    session.refs[6] = 2
+    session.fork([1], [0])
+    with pytest.raises(kv4_session.NoRoom, match="2 new pages are needed, 1 "):
+        session.fork([1, 1], [0, 2])
+    for bad in (([1], [3]), ([-1], [0]), ([1, 1], [0, 0]), ([1, 0], [2])):
+        with pytest.raises(ValueError):
+            session.fork(*bad)
+    assert [name for name, _ in session.calls].count("kfl_kv4_fork") == forks + 1
