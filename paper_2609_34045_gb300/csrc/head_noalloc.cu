@@ -7,9 +7,9 @@
 // until the process exits, and every call on that GPU shares it.
 //
 // Set-up happens on the first call on each device (with that device current): the array's
-// device address is looked up with cudaGetSymbolAddress, its ticket cleared with cudaMemset
-// and the device synchronized (the memset is ordered only on the legacy default stream), so that
-// first call belongs before any stream capture.  The last
+// device address is looked up with cudaGetSymbolAddress, the kernels of all batches are loaded, the ticket is
+// cleared with cudaMemset and the device synchronized (the memset is ordered only on the legacy default
+// stream), so that first call belongs before any stream capture.  The last
 // block of each launch puts the ticket back to zero; the candidates are rewritten by every
 // launch before they are read.  The array keeps the last call's contents, and calls that
 // overlap on the GPU (different streams with no ordering between them) race on it.
@@ -40,6 +40,24 @@ constexpr size_t NA_SCRATCH_BYTES = NA_CAND_BYTES + 256;   // + the ticket: 131,
 // must not pass this symbol to a kernel: on the host it names a stand-in, not device memory.
 static __device__ __align__(256) unsigned char g_head_noalloc_scratch[NA_SCRATCH_BYTES];
 
+template <int B>
+__global__ void head_argmax_noalloc_kernel(const float *hidden, const uint16_t *g, const uint16_t *w, int d, int vocab,
+                                           float eps, int32_t *next_ids, unsigned char *scratch);
+
+// The driver loads a kernel where it is first launched, and may allocate device memory for its code then: all four batches'
+// kernels are loaded with the first call, so that no later one allocates.
+cudaError_t load_kernels() {
+  const void *kernels[] = {
+      reinterpret_cast<const void *>(&head_argmax_noalloc_kernel<1>), reinterpret_cast<const void *>(&head_argmax_noalloc_kernel<2>),
+      reinterpret_cast<const void *>(&head_argmax_noalloc_kernel<3>), reinterpret_cast<const void *>(&head_argmax_noalloc_kernel<4>)};
+  cudaFuncAttributes attr;
+  for (const void *k : kernels) {
+    const cudaError_t e = cudaFuncGetAttributes(&attr, k);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 constexpr int NA_MAX_DEVICES = 64;
 std::mutex g_setup_mutex;
 unsigned char *g_scratch_dev[NA_MAX_DEVICES] = {};
@@ -63,7 +81,8 @@ int scratch_for_current_device(unsigned char **out) {
     }
     // cudaMemset is ordered only on the legacy default stream and may return before it is done;
     // waiting for the device makes the clear complete before a call on any stream reads it
-    e = cudaMemset(static_cast<unsigned char *>(p) + NA_CAND_BYTES, 0, 256);
+    e = load_kernels();
+    if (e == cudaSuccess) e = cudaMemset(static_cast<unsigned char *>(p) + NA_CAND_BYTES, 0, 256);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
       cudaGetLastError();
