@@ -86,8 +86,10 @@ int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, co
  *             aligned, zeroed before its first use and left as it has to be found.  Calls that may overlap
  *             (other streams, no ordering) need one each; after KFL_TIMED_OUT it is zeroed again.
  * A page out of range is reported in status and its rows count as not cached.
- * Precision: fp16 products of the exact codes with fp32 sums for few query rows per KV head; values rounded to
- * fp16 for prompts; softmax weights rounded to fp16; sums and softmax statistics in fp32.
+ * Precision: fp16 products with fp32 sums; softmax weights rounded to fp16; sums and softmax statistics in fp32.
+ * The cached values enter exactly, as codes (few query rows per KV head) or as sums of two fp16 numbers (many, fp16
+ * outputs), or rounded to fp16 (many, bf16 outputs).  Root mean square error of the outputs against 64 bits,
+ * their own rounding among it: 1.7e-3 with bf16, 2.9e-4 with fp16.
  * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer), KFL_ERR_CUDA. */
 int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
                    const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start, int n_seqs,

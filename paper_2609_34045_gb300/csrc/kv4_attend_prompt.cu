@@ -2,23 +2,29 @@
 //
 // Mathematics.  The query rows (token, head of the group) of a KV head are the M of two matrix products,
 //   S = Q K^T (128 rows x 128 keys), O += P V,  P = 2^(c S - m),
-// with fp32 accumulators in tensor memory.  K and V are decoded once per block into fp16 operands in shared memory,
-// value = centre + (code - 8) scale rounded once; P takes the place of S as the second product's fp16 operand.  The
-// reference m of a row is the maximum of its first tiles and moves only when a tile's weights sum to more than 2^14 (P stays
-// inside fp16), so that O is rarely rescaled and the maximum not looked for.  A row of Q is brought into fp16's range by a
-// power of two that its scores are multiplied back by.
+// with fp32 accumulators in tensor memory.  K and V are decoded once per block into fp16 operands in shared memory; P takes
+// the place of S as the second product's fp16 operand.  The reference m of a row is the maximum of its first tiles and moves only
+// when a tile's weights sum to more than 2^14 (P stays inside fp16), so that O is rarely rescaled and the maximum not looked for.
+// A row of Q is brought into fp16's range by a power of two that its scores are multiplied back by.
+//
+// Roundings.  A number rounded to fp16 is 2.1e-4 of it off (root mean square).  The weights are, in P.  With bf16 outputs, whose own
+// rounding is 1.66e-3, so are K and V: 4.3e-4 to 5e-4 in all, which the output's hides.  With fp16 outputs (2.1e-4) it would
+// double their error: there a decoded value is the sum of two fp16 numbers (decode_row) and each product is taken twice; 2.8e-4
+// in all, for 1.01 to 1.55 times the time.
 //
 // What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe, 2048 clocks for 256 rows by 128
-// keys at head_dim 128.  A half's softmax (64 scores a thread, 2.5 instructions each and as much again around them, some 1900
-// clocks beside the decoding warps) and the products behind it take longer than that: 2048 tokens over 8192 keys,
-// 64/8 heads of 128, 453 us, 1.06 PFLOP/s of the 1.89 that a plain bf16 product reaches.
+// keys at head_dim 128.  2048 tokens over 8192 keys, 64/8 heads of 128, bf16: 453 us, 1.06 PFLOP/s of the 1.89 that a plain bf16
+// product reaches, some 4670 clocks a tile.  Of these a half's softmax (64 scores a thread, 2.5 instructions each and as much again
+// around them) takes about 1900 and its own products 1024, one after the other; the rest is not accounted for (waits
+// between the roles, decoding: eight turns a tile of some 350 instructions on seven warps).  fp16: 700 us.  There the second
+// terms' products cost 45 us, their decoding 40, both together 170, and the shorter tiles 90.
 //
-// Roles.  Warps 0-7 and 8-15: softmax of the two 128-row halves, two threads per row with 64 keys each, and their Q and
-// output; 16-22: decoding, a thread per key, 32 keys of K or V at a time in turn, raw codes straight from global memory
+// Roles.  Warps 0-7 and 8-15: softmax of the two 128-row halves, two threads per row with half of a tile's keys each, and their Q
+// and output; 16-22: decoding, a thread per key, 32 keys of K or V at a time in turn, raw codes straight from global memory
 // ahead of their turn; 23: products.  While one half's softmax runs, the other half's products do.  (One thread per row:
 // 531 us.  Four decoding warps: decoding takes as long as the rest.)
 //
-// Work split.  The (sequence, KV head, 256 rows) x (128 keys) tiles in sight form one list that the blocks share
+// Work split.  The (sequence, KV head, 256 rows) x (128 or 64 keys) tiles in sight form one list that the blocks share
 // equally; a row block cut between thread blocks is merged by the last to arrive, in list order.
 #include <algorithm>
 
@@ -28,21 +34,27 @@
 namespace kfl {
 namespace {
 
-constexpr int PT_KEYS = 128;                 // keys of a tile
 constexpr int PT_PARTS = 2;                  // threads of a row
 constexpr int PT_SOFTMAX = 8 * PT_PARTS;     // warps 0 to 15
 constexpr int PT_DECODERS = 7;               // 16 to 22
-constexpr int PT_COLS = PT_KEYS / PT_PARTS;   // scores of a thread
 constexpr int PT_MMA_WARP = PT_SOFTMAX + PT_DECODERS;
 constexpr int PT_THREADS = (PT_MMA_WARP + 1) * 32;
 constexpr float PT_MOST = 16384.f;           // a row's weights in a tile may sum up to this: none is near fp16's end
 
-template <int HD>
+// TERMS: fp16 numbers that a decoded value is the sum of.  One, rounded, on 128 keys a tile; or two, on 64, in the same bytes: with
+// Q in the tensor memory that their narrower scores leave free (read from shared memory by each of twice as many products it
+// held them up: 789 us for 700).
+template <int HD, int TERMS>
 struct Prompt {
+  static constexpr int KEYS = 128 / TERMS;                 // of a tile
+  static constexpr int COLS = KEYS / PT_PARTS;             // scores of a thread
+  static constexpr int QUARTERS = KEYS / 32;               // what a decoding warp takes at once is one
+  static constexpr int Q_COL = KEYS;                       // two terms: of Q, behind a half's scores
   static constexpr int KB = HD / 64;                       // 64-channel blocks of 128-byte rows
-  static constexpr int TILE = 128 * HD * 2;                // bytes of 128 rows in fp16
-  static constexpr int Q_AT = 0, K_AT = 2 * TILE, V_AT = 4 * TILE;
-  static constexpr int INFO_AT = 6 * TILE;                 // int4[FEW_SEQS], then int prefix[FEW_SEQS + 4]
+  static constexpr int TILE = 128 * HD * 2;                // bytes of 128 rows of Q in fp16, and of a tile's K or V
+  static constexpr int TERM = TILE / TERMS;                // from a value's first term to its second
+  static constexpr int Q_AT = 0, K_AT = TERMS == 1 ? 2 * TILE : 0, V_AT = K_AT + 2 * TILE;
+  static constexpr int INFO_AT = V_AT + 2 * TILE;          // int4[FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int FLAG_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;  // uint4 [4][1 + KB]: keys of a tile
   static constexpr int ODD_AT = FLAG_AT + 4 * (1 + KB) * 16;    // uint32 [4][2]: a byte per 32 keys, K and V: not as usual
   static constexpr int PAIR_AT = ODD_AT + 4 * 2 * 4;  // float [2 halves][2][128]: what a row's two threads exchange
@@ -107,14 +119,16 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// 64 scores of a row: w the weights 2^(score cf - top) in fp16 pairs; returns their sum (taken in fp32 before the rounding:
-// above PT_MOST one of them may have outgrown fp16).  Sixteen at a time: a load from tensor memory takes some 50 clocks, which
-// the other warps fill, and more of them in flight would cost registers that the tile loop has not got.
-__device__ __forceinline__ float weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[PT_COLS / 2]) {
+// A thread's scores of a row: w the weights 2^(score cf - top) in fp16 pairs, the second product's operand (bf16 would be eight
+// times the rounding); returns their sum (taken in fp32 before the rounding: above PT_MOST one of them may have outgrown
+// fp16).  Sixteen at a time: a load from tensor memory takes some 50 clocks, which the other warps fill, and more of them in
+// flight would cost registers that the tile loop has not got.
+template <int COLS>
+__device__ __forceinline__ float weigh_scores(uint32_t t_s, float cf, float top, uint32_t (&w)[COLS / 2]) {
   const float2 scale = {cf, cf}, from = {-top, -top};
   float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-  for (int c = 0; c < PT_COLS / 16; ++c) {
+  for (int c = 0; c < COLS / 16; ++c) {
     uint32_t v[16];
     tmem_ld16(t_s + 16 * c, v);
     tmem_wait_ld();
@@ -147,28 +161,31 @@ struct Piece {
   int seq, head, block;          // block: of rows_per_block query rows
   int user, length, first, count;
   int row0, rows;                // its query rows
-  int tile0, n_tiles;            // its first tile (of 128 keys) and how many it sees (at least one)
+  int tile0, n_tiles;            // its first tile (of KEYS keys) and how many it sees (at least one)
   int from, to;                  // this thread block's run of them
   int64_t flat;                  // place of its first tile in the list
 };
 
+template <int KEYS>
 struct List {
   const int4 *info;
   const int *prefix;
   int n_seqs, heads, group, window, rows_per_block;
 };
 
-__device__ __forceinline__ void tiles_of_block(int length, int count, int block, const List &l, int &tile0, int &n) {
+template <int KEYS>
+__device__ __forceinline__ void tiles_of_block(int length, int count, int block, const List<KEYS> &l, int &tile0, int &n) {
   const int rows = count * l.group;
   const int tok0 = block * l.rows_per_block / l.group;
   const int tok1 = (min(rows, (block + 1) * l.rows_per_block) - 1) / l.group;
   const int end = length - count + tok1 + 1;
   const int begin = l.window > 0 ? max(0, length - count + tok0 + 1 - l.window) : 0;
-  tile0 = begin / PT_KEYS;
-  n = max(1, (max(end, 0) + PT_KEYS - 1) / PT_KEYS - tile0);
+  tile0 = begin / KEYS;
+  n = max(1, (max(end, 0) + KEYS - 1) / KEYS - tile0);
 }
 
-__device__ __forceinline__ void open_piece(Piece &pc, const List &l, int skip, int64_t limit) {
+template <int KEYS>
+__device__ __forceinline__ void open_piece(Piece &pc, const List<KEYS> &l, int skip, int64_t limit) {
   // the block's tiles from `skip` on, as far as the list's place `limit`
   pc.row0 = pc.block * l.rows_per_block;
   pc.rows = min(l.rows_per_block, pc.count * l.group - pc.row0);
@@ -177,13 +194,15 @@ __device__ __forceinline__ void open_piece(Piece &pc, const List &l, int skip, i
   pc.to = (int)min((int64_t)pc.n_tiles, limit - pc.flat);
 }
 
-__device__ __forceinline__ void open_sequence(Piece &pc, const List &l) {
+template <int KEYS>
+__device__ __forceinline__ void open_sequence(Piece &pc, const List<KEYS> &l) {
   const int4 v = l.info[pc.seq];
   pc.user = v.x, pc.length = v.y, pc.first = v.z, pc.count = v.w;
 }
 
 // The piece at place `at` of the list (at < limit).  The whole warp calls it: lanes count the tiles of a block each.
-__device__ void find_piece(Piece &pc, const List &l, int64_t at, int64_t limit) {
+template <int KEYS>
+__device__ void find_piece(Piece &pc, const List<KEYS> &l, int64_t at, int64_t limit) {
   const int lane = threadIdx.x & 31;
   int lo = 0, hi = l.n_seqs - 1;
   while (lo < hi) {
@@ -222,7 +241,8 @@ __device__ void find_piece(Piece &pc, const List &l, int64_t at, int64_t limit) 
   open_piece(pc, l, (int)(at - pc.flat), limit);
 }
 
-__device__ void next_piece(Piece &pc, const List &l, int64_t limit) {  // (the list goes on to `limit`)
+template <int KEYS>
+__device__ void next_piece(Piece &pc, const List<KEYS> &l, int64_t limit) {  // (the list goes on to `limit`)
   pc.flat += pc.n_tiles;
   if (++pc.block * l.rows_per_block >= pc.count * l.group) {
     pc.block = 0;
@@ -237,30 +257,66 @@ __device__ void next_piece(Piece &pc, const List &l, int64_t limit) {  // (the l
   open_piece(pc, l, 0, limit);
 }
 
+__device__ __forceinline__ uint32_t neg2(uint32_t x) {
+  uint32_t r;
+  asm("neg.f16x2 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
 // Codes and parameters of one row in fp16 [channel], in the order that the words' nibbles come in (0 4 1 5 2 6 3 7 of
-// every eight), as a row of the swizzled operand.
-template <int HD>
+// every eight), as a row of the swizzled operand.  One term: v = centre + (code - 8) scale, rounded once to fp16's 11 bits, 2.1e-4 of
+// it (root mean square).  With two the second is what that rounding lost, to 2^-12 of a step: with the whole number k that leaves
+// r = centre + k scale at half a step, and t = code - 8 - k, it is (t scale - v) + r, whose first difference
+// is about -r and keeps its bits.  Where k would not fit (a group more than 1900 steps from zero) it is 0, and the
+// second term t scale + (centre - v), whose difference is exact.
+template <int HD, int TERMS>
 __device__ __forceinline__ void decode_row(const uint4 (&raw)[HD / 32], const uint32_t (&par)[HD / 64], uint32_t tile, int row) {
+  using F = Prompt<HD, TERMS>;
 #pragma unroll
-  for (int j = 0; j < HD / 8; ++j) {
-    const uint32_t w = j % 4 == 0 ? raw[j / 4].x : j % 4 == 1 ? raw[j / 4].y : j % 4 == 2 ? raw[j / 4].z : raw[j / 4].w;
-    const uint32_t s = __byte_perm(par[j / 8], 0, 0x1010), c = __byte_perm(par[j / 8], 0, 0x3232);
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = i == 0 ? w << 4 : i == 1 ? w : i == 2 ? w >> 4 : w >> 8;
-      asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v[i]) : "r"(x), "r"(0x00F000F0u), "r"(0x64006400u));  // 16 (64 + u)
-      v[i] = hfma2(hfma2(v[i], 0x2C002C00u, 0xD480D480u), s, c);                                          // / 16 - 72: exact
+  for (int g = 0; g < HD / 64; ++g) {
+    const uint32_t s = __byte_perm(par[g], 0, 0x1010);
+    uint32_t c = __byte_perm(par[g], 0, 0x3232), from = 0xD480D480u;  // -72
+    bool far = false, any_far = false;
+    if constexpr (TERMS == 2) {
+      const float scale = f16_to_f32((uint16_t)par[g]), centre = f16_to_f32((uint16_t)(par[g] >> 16));
+      const float steps = scale > 0.f ? __fdividef(-centre, scale) : 0.f;
+      far = !(fabsf(steps) <= 1900.f);  // (or NaN.  Whole numbers up to 2048 are exact in fp16)
+      const float k = far ? 0.f : rintf(steps), r = far ? centre : fmaf(k, scale, centre);
+      c = pt_pack(r, r), from = pt_pack(-72.f - k, -72.f - k);
+      any_far = __any_sync(0xffffffffu, far);
     }
-    const uint32_t at = tile + (j / 8) * (128 * 128) + row * 128 + (((j & 7) ^ (row & 7)) << 4);
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+#pragma unroll
+    for (int j = g * 8; j < g * 8 + 8; ++j) {
+      const uint32_t w = j % 4 == 0 ? raw[j / 4].x : j % 4 == 1 ? raw[j / 4].y : j % 4 == 2 ? raw[j / 4].z : raw[j / 4].w;
+      uint32_t v[4], rest[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = i == 0 ? w << 4 : i == 1 ? w : i == 2 ? w >> 4 : w >> 8;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v[i]) : "r"(x), "r"(0x00F000F0u), "r"(0x64006400u));  // 16 (64 + u)
+        const uint32_t t = hfma2(v[i], 0x2C002C00u, from);                                                  // / 16 - 72 (- k): exact
+        v[i] = hfma2(t, s, c);
+        if constexpr (TERMS == 2) {
+          rest[i] = hfma2(hfma2(t, s, neg2(v[i])), 0x3C003C00u, c);
+          if (any_far) {
+            const uint32_t other = hfma2(t, s, hfma2(v[i], 0xBC00BC00u, c));
+            if (far) rest[i] = other;
+          }
+        }
+      }
+      const uint32_t at = tile + g * (F::KEYS * 128) + row * 128 + (((j & 7) ^ (row & 7)) << 4);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+      if constexpr (TERMS == 2)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + F::TERM), "r"(rest[0]), "r"(rest[1]), "r"(rest[2]),
+                     "r"(rest[3])
+                     : "memory");
+    }
   }
 }
 
-template <int HD>
+template <int HD, int TERMS>
 __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const AttendParams p, int rows_per_block) {
-  using F = Prompt<HD>;
-  constexpr int KB = F::KB;
+  using F = Prompt<HD, TERMS>;
+  constexpr int KB = F::KB, KEYS = F::KEYS, COLS = F::COLS, QUARTERS = F::QUARTERS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
   const uint32_t base = smem_addr(smem);
@@ -273,12 +329,12 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   const auto bar = [&](int b) { return bars + 8 * b; };
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
-  const List list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
+  const List<KEYS> list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
   pdl_launch_dependents();
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(B_KFULL + i), 4);
-      mbar_init(bar(B_VFULL + i), 4);
+      mbar_init(bar(B_KFULL + i), QUARTERS);
+      mbar_init(bar(B_VFULL + i), QUARTERS);
       mbar_init(bar(B_KFREE + i), 1);
       mbar_init(bar(B_VFREE + i), 1);
       mbar_init(bar(B_Q + i), 4 * PT_PARTS);
@@ -352,13 +408,13 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   };
 
   if (c0 < c1 && warp < PT_SOFTMAX) {
-    // ---- softmax: two threads per query row, each with 64 of a tile's keys and half of the row's channels.  They meet in
+    // ---- softmax: two threads per query row, each with half of a tile's keys and half of the row's channels.  They meet in
     // barriers of the half, so where a wait has given up they go on to the list's end (no wait lasts then), their
     // results being of no account
     const int half = warp / (4 * PT_PARTS), part = warp / 4 % PT_PARTS, row = tid & 127;
     constexpr int CH = HD / PT_PARTS;                          // channels of a thread
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
-    const uint32_t t_s = tmem + lanes + half * 128 + part * PT_COLS;
+    const uint32_t t_s = tmem + lanes + half * 128 + part * COLS;
     const uint32_t t_o = tmem + lanes + 256 + half * 128 + part * CH;
     const uint32_t q_tile = base + F::Q_AT + half * F::TILE;
     const int twins = half * 4 + (warp & 3);
@@ -372,6 +428,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       return x;
     };
     const float log2_scale = fabsf(p.scale) * 1.44269504089f;
+    constexpr uint32_t ODD = QUARTERS == 4 ? 0xffffffffu : 0xffffu;  // (a byte a quarter)
     uint32_t done = 0;  // tiles of this half so far
     unsigned tile = 0;  // tiles of the thread block so far (places of the flags)
     Piece pc;
@@ -422,26 +479,37 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             if (p.scale == 0.f)
 #pragma unroll
               for (int j = 0; j < 8; ++j) f[j] = 0.f;
-            const int chunk = part * (CH / 8) + i;
-            const uint32_t at = q_tile + (chunk / 8) * (128 * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(pt_pack(f[0], f[4])),
-                         "r"(pt_pack(f[1], f[5])), "r"(pt_pack(f[2], f[6])), "r"(pt_pack(f[3], f[7]))
-                         : "memory");
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = pt_pack(f[j], f[j + 4]);
+            if constexpr (TERMS == 1) {
+              const int chunk = part * (CH / 8) + i;
+              const uint32_t at = q_tile + (chunk / 8) * (128 * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[4 * i]), "r"(w[4 * i + 1]),
+                           "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                           : "memory");
+            }
+          }
+          if constexpr (TERMS == 2) {
+#pragma unroll
+            for (int c = 0; c < CH / 32; ++c)
+              tmem_st16(tmem + lanes + half * 128 + F::Q_COL + part * (CH / 2) + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
+            tmem_wait_st();
+            tc_fence_before();
           }
         }
-        fence_async_proxy();
+        if (TERMS == 1) fence_async_proxy();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_Q + half));
         const float cf = p.scale == 0.f ? 1.f : fmaxf(unit * log2_scale, 1e-37f);
         float top = -INFINITY, sum = 0.f;  // top: the reference, in scores times cf; sum: of this thread's weights
         unsigned poison = 0;               // groups of which this row sees a NaN
         const auto see_poison = [&](int t) {
-          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS;
+          const int key0 = (pc.tile0 + pc.from + t) * KEYS;
 #pragma unroll 1
           for (int g = 0; g < KB; ++g) {
             const uint4 v = flags[((tile + t) & 3) * (1 + KB) + 1 + g];
 #pragma unroll 1
-            for (int k = 0; k < PT_KEYS; ++k) {
+            for (int k = 0; k < KEYS; ++k) {
               const uint32_t bits = k < 32 ? v.x : k < 64 ? v.y : k < 96 ? v.z : v.w;
               if ((bits >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison |= 1u << g;
             }
@@ -451,33 +519,33 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         const int least = __reduce_min_sync(0xffffffffu, end);
         const int greatest = __reduce_max_sync(0xffffffffu, begin);
         for (int t = 0; t < n; ++t) {
-          const int key0 = (pc.tile0 + pc.from + t) * PT_KEYS + part * PT_COLS;  // of this thread's keys
+          const int key0 = (pc.tile0 + pc.from + t) * KEYS + part * COLS;  // of this thread's keys
           wait(B_S + half, done & 1);
           __syncwarp();
           tc_fence_after();
-          const bool masked = key0 + PT_COLS > least || (p.window > 0 && key0 < greatest);
+          const bool masked = key0 + COLS > least || (p.window > 0 && key0 < greatest);
           // (what the decoding has to say of the tiles comes while the scores are weighed: shared memory, busy with the
           // products' operands, takes hundreds of clocks)
-          const uint32_t odd_k = odd[2 * ((tile + t) & 3)], odd_v = t > 0 ? odd[2 * ((tile + t - 1) & 3) + 1] : 0;
+          const uint32_t odd_k = odd[2 * ((tile + t) & 3)] & ODD, odd_v = t > 0 ? odd[2 * ((tile + t - 1) & 3) + 1] & ODD : 0;
           // The weights are taken against the reference that the row has; they stay in registers until both threads of the
           // row find that it holds.  Where it does not (the first tile, a row that outgrew it, scores that
           // are masked) the scores, still in place, are read again.
-          uint32_t w[PT_COLS / 2];
+          uint32_t w[COLS / 2];
           float part_sum = 0.f;
-          if (!masked && t > 0) part_sum = weigh_scores(t_s, cf, top, w);
+          if (!masked && t > 0) part_sum = weigh_scores<COLS>(t_s, cf, top, w);
           if (odd_v) see_poison(t - 1);
           if (pair_any(twins, masked || odd_k || t == 0 || part_sum > PT_MOST || top == -INFINITY)) {
             const bool pick = masked || odd_k;
             const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
             const auto sees = [&](int c, int i) {  // column 16 c + i
               const int key = key0 + 16 * c + i;
-              const int k = part * PT_COLS + 16 * c;
+              const int k = part * COLS + 16 * c;
               const uint32_t pages = k < 32 ? there4.x : k < 64 ? there4.y : k < 96 ? there4.z : there4.w;
               return key < end && key >= begin && (pages >> ((c & 1) * 16 + i) & 1);
             };
             float most = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < PT_COLS / 16; ++c) {
+            for (int c = 0; c < COLS / 16; ++c) {
               uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
@@ -511,7 +579,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
             const float ref = top == -INFINITY ? 0.f : top;
             part_sum = 0.f;
 #pragma unroll
-            for (int c = 0; c < PT_COLS / 16; ++c) {
+            for (int c = 0; c < COLS / 16; ++c) {
               uint32_t x[16];
               tmem_ld16(t_s + 16 * c, x);
               tmem_wait_ld();
@@ -530,7 +598,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           }
           sum += part_sum;
 #pragma unroll
-          for (int c = 0; c < PT_COLS / 32; ++c) tmem_st16(t_s + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
+          for (int c = 0; c < COLS / 32; ++c) tmem_st16(t_s + 16 * c, reinterpret_cast<uint32_t(&)[16]>(w[16 * c]));
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -541,7 +609,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         wait(B_O + half, (done - 1) & 1);
         __syncwarp();
         tc_fence_after();
-        if (odd[2 * ((tile + n - 1) & 3) + 1]) see_poison(n - 1);
+        if (odd[2 * ((tile + n - 1) & 3) + 1] & ODD) see_poison(n - 1);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_READ + half));  // (the tiles' flags have been read)
         sum = shared_by_row(sum, [](float a, float b) { return a + b; });
@@ -600,19 +668,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   } else if (c0 < c1 && warp < PT_MMA_WARP) {
     // ---- decoding: a warp takes 32 keys of a tile's K or V, the warps in turn.  Its next keys' rows are loaded while
     // it decodes these, their page numbers one turn earlier still
-    const unsigned n = (unsigned)(c1 - c0) * 8;  // turns: (tile, K or V, quarter)
+    constexpr unsigned TURNS = 2 * QUARTERS;              // of a tile: (K or V, quarter)
+    const unsigned n = (unsigned)(c1 - c0) * TURNS;
     Piece pc;
     find_piece(pc, list, c0, c1);
     int t_next = pc.from;
     unsigned tile_next = 0;
     int page = -2, slot = 0, head = 0;  // of the row of this warp's next turn (a page of -2: behind the user's rows)
     const auto find_page = [&](unsigned turn) {
-      for (; tile_next < turn >> 3; ++tile_next)
+      for (; tile_next < turn / TURNS; ++tile_next)
         if (++t_next == pc.to) {
           next_piece(pc, list, c1);
           t_next = pc.from;
         }
-      const int key = (pc.tile0 + t_next) * PT_KEYS + (turn & 3) * 32 + lane;
+      const int key = (pc.tile0 + t_next) * KEYS + (turn % QUARTERS) * 32 + lane;
       page = key < pc.length ? p.map.table[(int64_t)pc.user * p.map.max_pages + (key >> lp)] : -2;
       slot = key & (p.pool.page_tokens() - 1), head = pc.head;
     };
@@ -640,7 +709,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     const auto load_turn = [&](unsigned t) {  // its page is known
       there = page >= 0 && page < p.pool.n_pages;
       if (page != -2 && !there) report(p.status, KFL_BAD_PAGE);
-      load_row(t >> 2 & 1, there);
+      load_row(t / QUARTERS & 1, there);
     };
     if (turn < n) {
       find_page(turn);
@@ -649,8 +718,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     }
 #pragma unroll 1
     for (; turn < n; turn += PT_DECODERS) {
-      const unsigned tile = turn >> 3;
-      const int which = turn >> 2 & 1, buf = tile & 1, quarter = turn & 3;
+      const unsigned tile = turn / TURNS;
+      const int which = turn / QUARTERS & 1, buf = tile & 1, quarter = turn % QUARTERS;
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) now[j] = later[j];
 #pragma unroll
@@ -676,7 +745,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         flag[0] = have;
       }
       if (lane == 0) reinterpret_cast<volatile uint8_t *>(odd + 2 * (tile & 3) + which)[quarter] = any != 0;
-      decode_row<HD>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, quarter * 32 + lane);
+      decode_row<HD, TERMS>(now, now_p, base + (which ? F::V_AT : F::K_AT) + buf * F::TILE, quarter * 32 + lane);
       fence_async_proxy();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar((which ? B_VFULL : B_KFULL) + buf));
@@ -684,7 +753,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   } else if (c0 < c1) {
     // ---- products, issued by an elected lane.  Descriptors are the same in every lane and known to be: through
     // shuffles, or the compiler moves them lane by lane, which takes longer than a product
-    constexpr uint32_t idesc_s = idesc_kind_f16(128, PT_KEYS, false);
+    constexpr uint32_t idesc_s = idesc_kind_f16(128, KEYS, false);
     constexpr uint32_t idesc_o = idesc_kind_f16(128, HD, false) | (1u << 16);  // B is N-major
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), at = __shfl_sync(0xffffffffu, base, 0);
     unsigned tile = 0, done[2] = {}, pieces[2] = {};
@@ -696,22 +765,28 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
       const uint64_t q = sdesc_k_sw128(at + F::Q_AT + half * F::TILE), k = sdesc_k_sw128(at + F::K_AT + buf * F::TILE);
       if (elect_one()) {
 #pragma unroll
-        for (int i = 0; i < HD / 16; ++i) {
-          constexpr int BLOCK = 128 * 128 >> 4;
-          const int off = (i / 4) * BLOCK + (i % 4) * 2;  // (descriptors count 16 bytes)
-          mma_bf16_ss(tm + half * 128, q + off, k + off, idesc_s, i > 0);
-        }
+        for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i) {  // (descriptors count 16 bytes)
+            const int at_q = (i / 4) * (128 * 128 >> 4) + (i % 4) * 2, at_k = (i / 4) * (KEYS * 128 >> 4) + (i % 4) * 2;
+            if (TERMS == 1)
+              mma_bf16_ss(tm + half * 128, q + at_q, k + at_k, idesc_s, i > 0);
+            else
+              mma_ts(tm + half * 128, tm + half * 128 + F::Q_COL + i * 8, k + (term * F::TERM >> 4) + at_k, idesc_s, term > 0 || i > 0);
+          }
         mma_commit(bar(B_S + half));
       }
       __syncwarp();
     };
     const auto values = [&](int half, int buf, bool first) {
-      const uint64_t v = sdesc_mn_sw128(at + F::V_AT + buf * F::TILE, KB == 2 ? 128 * 128 : 1024);
+      const uint64_t v = sdesc_mn_sw128(at + F::V_AT + buf * F::TILE, KB == 2 ? KEYS * 128 : 1024);
       if (elect_one()) {
 #pragma unroll
-        for (int i = 0; i < PT_KEYS / 16; ++i)
-          mma_ts(tm + 256 + half * 128, tm + half * 128 + i / (PT_COLS / 16) * PT_COLS + i % (PT_COLS / 16) * 8, v + i * 128,
-                 idesc_o, !first || i > 0);
+        for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+          for (int i = 0; i < KEYS / 16; ++i)
+            mma_ts(tm + 256 + half * 128, tm + half * 128 + i / (COLS / 16) * COLS + i % (COLS / 16) * 8,
+                   v + (term * F::TERM >> 4) + i * 128, idesc_o, !first || term > 0 || i > 0);
         mma_commit(bar(B_O + half));
       }
       __syncwarp();
@@ -839,14 +914,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   }
 }
 
-template <int HD>
+template <int HD, int TERMS>
 cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   static SmemOptIn opt_in;
-  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_prompt_kernel<HD>);
-  const int smem = Prompt<HD>::SMEM + 1024;
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_prompt_kernel<HD, TERMS>);
+  const int smem = Prompt<HD, TERMS>::SMEM + 1024;
   const cudaError_t e = opt_in(kernel, smem);
   if (e != cudaSuccess) return e;
-  return launch_chained(kv4_attend_prompt_kernel<HD>, std::min(n_sm, FEW_BLOCKS), PT_THREADS, smem, s, p,
+  return launch_chained(kv4_attend_prompt_kernel<HD, TERMS>, std::min(n_sm, FEW_BLOCKS), PT_THREADS, smem, s, p,
                         prompt_rows(p.max_q * p.group));
 }
 
@@ -857,7 +932,9 @@ size_t attend_prompt_partials(int head_dim, int64_t rows) {
 }
 
 cudaError_t launch_attend_prompt(const AttendParams &p, int n_sm, cudaStream_t s) {
-  return p.pool.head_dim == 128 ? launch<128>(p, n_sm, s) : launch<64>(p, n_sm, s);
+  // (two terms for fp16 outputs, whose own rounding is no larger than that of a decoded value; bf16's is eight times it)
+  if (p.pool.head_dim == 128) return p.bf16 ? launch<128, 1>(p, n_sm, s) : launch<128, 2>(p, n_sm, s);
+  return p.bf16 ? launch<64, 1>(p, n_sm, s) : launch<64, 2>(p, n_sm, s);
 }
 
 }  // namespace kfl
