@@ -81,7 +81,9 @@ int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, co
  *             KV head h / (n_heads / n_kv_heads), at most 128 heads per KV head; out does not overlap q
  *   scale     of the scores (normally 1 / sqrt(head_dim))
  *   lse       NULL, or device fp32 [n_tokens][n_heads]: the natural log of the sum of exp(scores)
- *   max_pages * page_tokens at most 2^26
+ *   max_pages * page_tokens at most 2^26; a sequence's query rows per KV head at most 2^30.  Prompts that see more
+ *             than 2^31 tiles (of 256 rows by 64 keys, per KV head, summed over 512 neighbouring sequences: one
+ *             prompt of 2^22 tokens of 8 heads per KV head) are reported (KFL_BAD_POSITION) and not computed
  *   workspace device memory of kfl_kv4_attend_workspace_bytes for the same sizes (or larger ones), 16-byte
  *             aligned, zeroed before its first use and left as it has to be found.  Calls that may overlap
  *             (other streams, no ordering) need one each; after KFL_TIMED_OUT it is zeroed again.
@@ -90,7 +92,7 @@ int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, co
  * The cached values enter exactly, as codes (few query rows per KV head) or as sums of two fp16 numbers (many, fp16
  * outputs), or rounded to fp16 (many, bf16 outputs).  Root mean square error of the outputs against 64 bits,
  * their own rounding among it: 1.7e-3 with bf16, 2.9e-4 with fp16.
- * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer), KFL_ERR_CUDA. */
+ * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer, query rows), KFL_ERR_CUDA. */
 int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
                    const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start, int n_seqs,
                    int n_tokens, int max_q, float scale, int window, void *workspace, size_t workspace_bytes,

@@ -365,30 +365,37 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
     } else {
       length = min(max(0, p.map.lengths[user]), p.map.max_pages << lp);
     }
-    int tiles = 0;
+    int64_t tiles = 0;
     for (int b = lane; b * rows_per_block < count * p.group; b += 32) {
       int tile0, n;
       tiles_of_block(length, count, b, list, tile0, n);
       tiles += n;
     }
-    tiles = __reduce_add_sync(0xffffffffu, tiles);
-    if (lane == 0) info[s] = make_int4(user, length, first, count), prefix[s + 1] = tiles;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, off);
+    if (lane == 0) info[s] = make_int4(user, length, first, count), prefix[s + 1] = (int)min(tiles, (int64_t)0x7fffffff);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = words[0];
   if (warp == 0) {
-    int before = 0;
+    int64_t before = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-      int v = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0;
+      int64_t v = s0 + lane < p.n_seqs ? prefix[s0 + lane + 1] : 0;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, v, off);
+        const int64_t o = __shfl_up_sync(0xffffffffu, v, off);
         if (lane >= off) v += o;
       }
-      if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = before + v;
+      if (s0 + lane < p.n_seqs) prefix[s0 + lane + 1] = (int)(before + v);
       before += __shfl_sync(0xffffffffu, v, 31);
+    }
+    // (a list of that many tiles would run for half a minute: refused)
+    if (before >= 0x7fffffff) {
+      __syncwarp();
+      if (lane == 0) prefix[p.n_seqs] = 0;
+      if (blockIdx.x == 0 && lane == 0) report(p.status, KFL_BAD_POSITION);
     }
   }
   __syncthreads();

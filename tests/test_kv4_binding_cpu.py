@@ -204,3 +204,17 @@ def test_a_table_off_its_pairs_alignment_is_refused(lib, off):  # noqa: F811
     cfg = kv4.kfl_rope_cfg(64, 0, 1e4, 1.0, 0.0, 0.0, 0.0, 0.0)
     assert lib.kfl_rope_table(C.byref(cfg), 10, (1 << 20) + off, None) == K.KFL_ERR_ARG
     assert "aligned" in K.kfl_last_error_detail()
+
+
+def test_more_query_rows_than_are_counted_are_refused(lib):  # noqa: F811
+    """2^24 tokens of 128 heads per KV head: their count would pass 31 bits on the device."""
+    def attend(n, max_q, n_seqs=1):
+        q = kv4.kfl_heads(1 << 20, 256 * 64, 64, 256, 0)
+        p = kv4.kfl_kv4_pool(1 << 20, 10, 16, 1, 2, 64)
+        m = kv4.kfl_kv4_map(1 << 20, 1 << 20, 1 << 20, 3, 4)
+        return lib.kfl_kv4_attend(C.byref(p), C.byref(m), 0, C.byref(q), C.byref(q), None, None, 1 << 20, n_seqs, n, max_q, 1.0, 0,
+                                  1 << 20, 1 << 50, None, None)
+
+    for n, max_q in ((1 << 24, 1 << 24), ((1 << 23) + 1, 2 ** 31 - 1), (2 ** 31 - 1, (1 << 23) + 1)):
+        assert attend(n, max_q) == K.KFL_ERR_RANGE
+        assert "query rows" in K.kfl_last_error_detail()
