@@ -330,7 +330,6 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
   const List<KEYS> list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
-  pdl_launch_dependents();
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(B_KFULL + i), QUARTERS);
@@ -379,6 +378,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = words[0];
+  // (not before this block has its tensor memory: a block of the next kernel that took it first would wait for this grid's end,
+  // and this block for that one's)
+  pdl_launch_dependents();
   if (warp == 0) {
     int64_t before = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
