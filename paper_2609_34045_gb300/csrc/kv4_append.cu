@@ -5,7 +5,8 @@
 // of 8 heads took 49 us against 13 for their bytes.  So sixteen channels of a k row and of its v row to a thread, four
 // threads to a group of 64, whose ends meet in two shuffles; a code is four operations, its place in the word the last of
 // them, and two more where a group's ends need a clamp.  19 us for these rows unrotated, 25 rotated in neighbouring
-// pairs, 31 in halves, 18 for reading them back.  The difference is the angles: 8 bytes for each pair, which the L1 looks up a
+// pairs, 31 in halves, 18 for reading them back, all with rows that the L2 still holds; rows of four prompts that come from HBM, rotated in
+// halves, 34 to 36 and 20.  The difference is the angles: 8 bytes for each pair, which the L1 looks up a
 // line at a time.  Through shared memory they cost a barrier that waits for them (29 and 28 us); with the next rows' loads
 // under way in a loop the registers leave half the warps (34 us).  The rotation's partner channels are read once more,
 // from L1, rather than exchanged: the partner may lie in any other thread or in the same one, depending on layout and rope_dim.

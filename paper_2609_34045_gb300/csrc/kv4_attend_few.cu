@@ -46,7 +46,8 @@ constexpr int SUB = 2;
 
 template <int HD, int NT>
 struct Few {
-  // 12 warps of at most 168 registers (11: 2 us more for 32 ragged users; 16 spill); with 16 query rows 8 warps of 255
+  // 12 warps of at most 168 registers (11: 2 us more for 32 ragged users; 16 spill in the tile loop); with 16 query rows 8 warps of
+  // 255.  At head_dim 128 both keep 16 bytes of a thread in local memory
   static constexpr int WARPS = NT == 1 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int COLS = 8 * NT;

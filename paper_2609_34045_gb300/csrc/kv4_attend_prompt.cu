@@ -13,7 +13,7 @@
 // in all, for 1.01 to 1.55 times the time.
 //
 // What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe, 2048 clocks for 256 rows by 128
-// keys at head_dim 128.  2048 tokens over 8192 keys, 64/8 heads of 128, bf16: 453 us, 1.06 PFLOP/s of the 1.89 that a plain bf16
+// keys at head_dim 128.  2048 tokens over 8192 keys, 64/8 heads of 128, bf16: 452 us, 1.06 PFLOP/s of the 1.89 that a plain bf16
 // product reaches, some 4670 clocks a tile.  Of these a half's softmax (64 scores a thread, 2.5 instructions each and as much again
 // around them) takes about 1900 and its own products 1024, one after the other; the rest is not accounted for (waits
 // between the roles, decoding: eight turns a tile of some 350 instructions on seven warps).  fp16: 700 us.  There the second
