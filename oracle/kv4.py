@@ -83,6 +83,84 @@ def attend(q, k, v, positions, scale, window=0):
     return out, size, lse
 
 
+def tree_seen(parents):
+    """Which nodes each node of a tree sees [node][node], and how many ancestors it has."""
+    seen = np.zeros((len(parents), len(parents)), dtype=bool)
+    for i, up in enumerate(parents):
+        if up >= 0:
+            seen[i] = seen[up]
+        seen[i, i] = True
+    return seen, seen.sum(1) - 1
+
+
+def tree_words(seen, max_q):
+    """Rows of `seen` as 32-bit words, node j in bit j % 32 of word j / 32."""
+    out = np.zeros((len(seen), -(-max_q // 32)), dtype=np.uint32)
+    for i, j in zip(*np.nonzero(seen)):
+        out[i, j // 32] |= np.uint32(1 << (j % 32))
+    return out
+
+
+def tree_keys(seen, n, window=0):
+    """Which of n cached rows, the last of which are the nodes, each node sees."""
+    c = len(seen)
+    keys = np.zeros((c, n), dtype=bool)
+    for i in range(c):
+        begin = n - c - max(0, window - int(seen[i].sum())) if window else 0
+        keys[i, max(0, begin):max(0, n - c)] = True
+        for j in range(c):
+            if seen[i, j] and n - c + j >= 0:
+                keys[i, n - c + j] = True
+    return keys
+
+
+def causal_keys(count, n, window=0):
+    """The same of tokens that see the rows up to their own."""
+    pos, key = np.arange(n - count, n)[:, None], np.arange(n)
+    return (key <= pos) & ((key > pos - window) if window else True)
+
+
+def attend_keys(q, k, v, seen, scale):
+    """attend over the keys that `seen` [t][n] says."""
+    out, size, lse = np.zeros(q.shape), np.zeros(q.shape), np.full(len(q), -np.inf)
+    for i in range(len(q)):
+        if seen[i].any():
+            x = k[seen[i]] @ q[i].astype(np.float64) * scale
+            w = np.exp(x - x.max())
+            out[i], size[i] = w @ v[seen[i]] / w.sum(), w @ np.abs(v[seen[i]]) / w.sum()
+            lse[i] = x.max() + np.log(w.sum())
+    return out, size, lse
+
+
+def weights(q, k, lse, seen, scale):
+    """exp(scale q k - lse) [t][n] where seen, else 0."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.exp(q.astype(np.float64) @ k.T * scale - lse.astype(np.float64)[:, None])
+    return np.where(seen & (lse != -np.inf)[:, None], w, 0.0)
+
+
+def select(mass, n, budget, first, recent):
+    """The slots that stay of n, ascending."""
+    if n <= budget:
+        return np.arange(n)
+    middle = np.arange(first, n - recent)
+    order = sorted(middle, key=lambda t: (0 if np.isnan(mass[t]) else 1, 0.0 if np.isnan(mass[t]) else -mass[t], t))
+    return np.array(sorted([*range(first), *order[:budget - first - recent], *range(n - recent, n)]))
+
+
+def keep_bytes(pool, table_row, new_row, layer, head, lists, first, page, hd):
+    """One block's rows of kfl_kv4_keep: slots first + j from lists[j], and what stands before them in a new page, into a
+    copy of the pool."""
+    n, m = page * hd // 2, page * hd // 16
+    src = pool.copy()
+    begin = first // page * page if new_row[first // page] != table_row[first // page] else first
+    for s in range(begin, first + len(lists)):
+        e = s if s < first else int(lists[s - first])
+        a, b = src[table_row[e // page], layer, head], pool[new_row[s // page], layer, head]
+        for at, size in ((0, hd // 2), (n, hd // 2), (2 * n, hd // 16), (2 * n + m, hd // 16)):
+            b[at + s % page * size:at + (s % page + 1) * size] = a[at + e % page * size:at + (e % page + 1) * size]
+
+
 class Pages:
     """Tables of users' pages, as kfl_kv4_reserve, _fork, _free and _compact leave them."""
 
@@ -132,6 +210,33 @@ class Pages:
                 self.refs[page] -= 1
             self.table[b], self.lengths[b] = row, lengths[a]
         return copies
+
+    def keep(self, users, first, counts):
+        """The users' old rows of the table (None: not touched)."""
+        free, old, refs, gone = self._free_pages(), [], self.refs.copy(), []
+        used = 0
+        for u, f, c in zip(users, first, counts):
+            n = int(self.lengths[u])
+            if f + c == n:
+                old.append(None)
+                continue
+            row, need, held = self.table[u].copy(), -(-(f + c) // self.page), -(-n // self.page)
+            shared = [j for j in range(f // self.page, need) if refs[row[j]] > 1]
+            used += len(shared)
+            if shared and used > len(free):
+                old.append(None)
+                continue
+            for r, j in enumerate(shared):
+                new = free[used - len(shared) + r]
+                gone.append(row[j])
+                self.table[u, j], self.refs[new] = new, 1
+            gone += [int(p) for p in row[need:held]]
+            self.table[u, need:held] = -1
+            self.lengths[u] = f + c
+            old.append(row)
+        for p in gone:
+            self.refs[p] -= 1
+        return old
 
     def compact(self):
         live = np.nonzero(self.refs)[0]

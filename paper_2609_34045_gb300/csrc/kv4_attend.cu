@@ -6,6 +6,7 @@
 
 #include <algorithm>
 
+#include "../../include/kafila_kv4_tree.h"
 #include "kv4_attend.cuh"
 
 namespace kfl {
@@ -62,11 +63,11 @@ extern "C" int kfl_kv4_attend_workspace_bytes(const kfl_kv4_pool *pool, int n_he
   return KFL_OK;
 }
 
-extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
-                              const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start,
-                              int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace,
-                              size_t workspace_bytes, int32_t *status, void *cuda_stream) {
-  const char *me = "kfl_kv4_attend";
+// views NULL: each token sees the rows up to its own.
+static int attend(const char *me, const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
+                  const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start, const uint32_t *views,
+                  int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace, size_t workspace_bytes,
+                  int32_t *status, void *cuda_stream) {
   if (!heads_valid(q, n_tokens) || !heads_valid(out, n_tokens)) return bad_arg(me, "q and out are needed");
   int rc = check_attend(me, pool, q->n_heads, n_seqs, n_tokens, max_q, true);
   if (rc == KFL_OK) rc = check_map(map, me);
@@ -88,6 +89,7 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.q = view_of(*q), p.out = view_of(*out);
   p.q_wide = rows_aligned16(*q), p.out_wide = rows_aligned16(*out), p.bf16 = q->dtype == KFL_DT_BF16;
   p.lse = lse, p.users = users, p.q_start = q_start;
+  p.views = views, p.words = (max_q + 31) / 32;
   p.n_seqs = n_seqs, p.n_tokens = n_tokens, p.max_q = q_start ? max_q : 1;
   p.n_heads = q->n_heads, p.group = q->n_heads / pool->n_kv_heads;
   p.group_inv = (65536 + p.group - 1) / p.group;
@@ -113,4 +115,26 @@ extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
     e = few ? launch_attend_few(p, few_cols(rows), n_sm, s) : launch_attend_prompt(p, n_sm, s);
   }
   return cuda_result(e, me);
+}
+
+extern "C" int kfl_kv4_attend(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
+                              const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start,
+                              int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace,
+                              size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  return attend("kfl_kv4_attend", pool, map, layer, q, out, lse, users, q_start, nullptr, n_seqs, n_tokens, max_q, scale, window,
+                workspace, workspace_bytes, status, cuda_stream);
+}
+
+extern "C" int kfl_kv4_attend_tree(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
+                                   const kfl_heads *out, float *lse, const int32_t *users, const int32_t *q_start,
+                                   const uint32_t *views, int n_seqs, int n_tokens, int max_q, float scale, int window,
+                                   void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  const char *me = "kfl_kv4_attend_tree";
+  if (max_q > KFL_KV4_TREE_MOST) {
+    bad_arg(me, "a sequence has at most 1024 nodes");
+    return KFL_ERR_RANGE;
+  }
+  if ((!views && n_tokens > 0) || (reinterpret_cast<uintptr_t>(views) & 3)) return bad_arg(me, "views are needed");
+  return attend(me, pool, map, layer, q, out, lse, users, q_start, views, n_seqs, n_tokens, max_q, scale, window, workspace,
+                workspace_bytes, status, cuda_stream);
 }

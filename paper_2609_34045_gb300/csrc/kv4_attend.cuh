@@ -18,6 +18,8 @@ struct AttendParams {
   int q_wide, out_wide, bf16;
   float *lse;
   const int32_t *users, *q_start;
+  const uint32_t *views;  // trees: which of the last tokens each token sees, [n_tokens][words]; else NULL
+  int words;
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
   float scale;
   int window;
@@ -37,6 +39,31 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
+}
+
+// Trees.  Rows of context that a token which sees `nodes` of the last tokens still sees with a window.
+__device__ __forceinline__ int tree_nodes(const AttendParams &p, int token, int count) {
+  const uint32_t *view = p.views + (int64_t)token * p.words;
+  int n = 0;
+  for (int w = 0; 32 * w < count; ++w) n += __popc(view[w] & (count - 32 * w >= 32 ? 0xffffffffu : (1u << (count - 32 * w)) - 1));
+  return n;
+}
+// Which of the 32 keys from key0 on a token sees, a bit each; its sequence has `count` nodes from key `base` on (below 0
+// where a user has fewer rows than nodes: those nodes' keys are not there).
+__device__ __forceinline__ uint32_t tree_view(const AttendParams &p, int token, int key0, int base, int count) {
+  const uint32_t *view = p.views + (int64_t)token * p.words;
+  const int node0 = key0 - base, w = node0 >> 5;  // (of the context: negative)
+  const auto word = [&](int i) { return i < 0 ? 0xffffffffu : i < p.words ? view[i] : 0u; };
+  uint32_t seen = __funnelshift_r(word(w), word(w + 1), node0 & 31);
+  if (node0 + 32 > count) seen &= node0 >= count ? 0u : (1u << (count - node0)) - 1;
+  if (p.window > 0 && node0 < 0) {
+    const int begin = base - max(0, p.window - tree_nodes(p, token, count)) - key0;  // (at most the nodes' own start)
+    if (begin >= 32)
+      seen = 0;
+    else if (begin > 0)
+      seen &= ~((1u << begin) - 1);
+  }
+  return seen;
 }
 
 // Waits for an mbarrier phase for two seconds at most (by the clock: a poll may itself be held for microseconds).

@@ -33,6 +33,7 @@
 
 #include "attn_core.cuh"  // cp_async16
 #include "kv4_attend.cuh"
+#include "kv4_stream.cuh"
 
 namespace kfl {
 namespace {
@@ -63,58 +64,6 @@ struct Few {
   static_assert(SMEM <= 232448, "shared memory of a block");
 };
 
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// The same from a start value of its own.
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1, const float (&c)[4]) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
-}
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ float half_lo(uint32_t x) { return __low2float(*reinterpret_cast<const __half2 *>(&x)); }
-__device__ __forceinline__ float half_hi(uint32_t x) { return __high2float(*reinterpret_cast<const __half2 *>(&x)); }
-
-// The nibbles of a word's bytes 0 and 2 as two fp16 pairs, as they stand: whole numbers below 2048 in the bits of an fp16
-// are that many times 2^-24 (its subnormal numbers and the first binade above), exactly, and the matrix unit takes them as
-// any others.  The low nibbles are u 2^-24, the high ones u 2^-20.
-__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t &low, uint32_t &high) {
-  low = w & 0x000F000Fu;
-  high = w & 0x00F000F0u;
-}
-constexpr float LOW = 0x1p-24f, HIGH = 0x1p-20f;
-__device__ __forceinline__ uint2 lds64(uint32_t addr) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-  return v;
-}
-
 // 1 / x, and 0 of 0: a sum of weights, which is 0 where nothing is seen, else no smaller than its reference's weight
 __device__ __forceinline__ float inverse(float x) {
   float r;
@@ -130,11 +79,6 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
   return r;
 }
 
-// a / b, in 32 bits where they fit: one chain of instructions instead of three.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  return (a | b) >> 32 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
-}
-
 // A place in the list of tiles.
 struct Cursor {
   int seq, head, block, tile;  // block: of COLS query rows; tile: within the segment (sequence, KV head, block)
@@ -143,11 +87,12 @@ struct Cursor {
 };
 
 // (user, length, first token, tokens) of a sequence; its tiles start at key first_tile * 64
+template <bool TREE>
 __device__ __forceinline__ int first_tile_of(int length, int count, int window) {
-  return window > 0 ? max(0, length - count + 1 - window) / TILE : 0;
+  return window > 0 ? max(0, length - count + !TREE - window) / TILE : 0;
 }
 
-template <int COLS>
+template <int COLS, bool TREE>
 __device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, const int *prefix, const AttendParams &p) {
   const int4 v = info[c.seq];
   c.user = v.x, c.length = v.y, c.first = v.z, c.count = v.w;
@@ -155,11 +100,11 @@ __device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, cons
   int units = prefix[c.seq + 1] - prefix[c.seq];
   if (c.blocks > 1) units /= c.blocks;
   c.n_tiles = units - 1;
-  c.first_tile = first_tile_of(v.y, v.w, p.window);
+  c.first_tile = first_tile_of<TREE>(v.y, v.w, p.window);
 }
 
 // The tile of unit `flat` of the list, -1 for what comes before a segment's first (a segment of n tiles is n + 1 units).
-template <int COLS>
+template <int COLS, bool TREE>
 __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 *info, const int *prefix,
                                             const AttendParams &p) {
   int lo = 0, hi = p.n_seqs - 1;
@@ -171,7 +116,7 @@ __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 
       lo = mid + 1;
   }
   c.seq = lo;
-  enter_sequence<COLS>(c, info, prefix, p);
+  enter_sequence<COLS, TREE>(c, info, prefix, p);
   const int rest = (int)(flat - (int64_t)prefix[lo] * p.pool.n_kv_heads);  // (below heads * blocks * 2^20)
   const int segment = rest / (c.n_tiles + 1);
   c.tile = rest - segment * (c.n_tiles + 1) - 1;
@@ -179,7 +124,7 @@ __device__ __forceinline__ void locate_tile(Cursor &c, int64_t flat, const int4 
   c.block = segment - c.head * c.blocks;
 }
 
-template <int COLS>
+template <int COLS, bool TREE>
 __device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const int *prefix, const AttendParams &p) {
   if (++c.tile < c.n_tiles) return;
   c.tile = 0;
@@ -189,7 +134,7 @@ __device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const int
   c.head = 0;
   do {
     if (++c.seq >= p.n_seqs) return;
-    enter_sequence<COLS>(c, info, prefix, p);
+    enter_sequence<COLS, TREE>(c, info, prefix, p);
   } while (c.n_tiles <= 0);
 }
 
@@ -303,7 +248,7 @@ __device__ __forceinline__ void merge_columns(int n, int col, int lane, const At
     for (int off = 16; off > 0; off >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], off);
 }
 
-template <int HD, int NT, bool BF16>
+template <int HD, int NT, bool BF16, bool TREE>
 __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel(const AttendParams p) {
   using F = Few<HD, NT>;
   constexpr int G = F::GROUPS, COLS = F::COLS, W = F::WARPS;
@@ -339,7 +284,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     if (bad && blockIdx.x == 0) report(p.status, bad);
     info[s] = make_int4(user, length, first, count);
     return (count * p.group + COLS - 1) / COLS *
-           (max(1, (length + TILE - 1) / TILE - first_tile_of(length, count, p.window)) + 1);
+           (max(1, (length + TILE - 1) / TILE - first_tile_of<TREE>(length, count, p.window)) + 1);
   };
   const auto warp_sum = [&](int v) {  // up to and with this lane's
 #pragma unroll
@@ -408,7 +353,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   const bool copies = lane < (lp == LOG_TILE ? 1 : 4 * TILE >> lb);
   const int32_t *fetch_row = nullptr;
   if (w0 < w1) {
-    locate_tile<COLS>(fetch, w0, info, prefix, p);
+    locate_tile<COLS, TREE>(fetch, w0, info, prefix, p);
     if (fetch.tile < 0) fetch.tile = 0, ++w0;
     fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
   }
@@ -459,7 +404,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
     const int seq = fetch.seq;
     fetch_flat += fetch.tile + 1 == fetch.n_tiles ? 2 : 1;
     if (fetch_flat < w1) {
-      next_tile<COLS>(fetch, info, prefix, p);
+      next_tile<COLS, TREE>(fetch, info, prefix, p);
       if (fetch.seq != seq) fetch_row = p.map.table + (int64_t)fetch.user * p.map.max_pages;
       load_page();
     }
@@ -589,9 +534,10 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       const uint32_t base_p = ring + slot * F::TILE_BYTES + 2 * CODES + 16 * s0 * (G * 4);
       const int key0 = (at.first_tile + at.tile) * TILE + 16 * s0;
       // some rows do not see all of the tile: its last keys, a window's first ones, a missing page
-      const int all_end = at.length - at.count + 1;
+      const int all_end = at.length - at.count + !TREE;
+      const int last_begin = TREE ? all_end - max(0, p.window - at.count) : at.length - p.window;  // with a window: of any row
       const bool masked = key0 + 16 * SUB > all_end || (have & ((1 << SUB) - 1)) != (1 << SUB) - 1 ||
-                          (p.window > 0 && key0 < at.length - p.window);
+                          (p.window > 0 && key0 < last_begin);
       float x[NT][SUB][4];
       uint32_t vpar[SUB][2][G];  // (scale, centre) of the lane's two keys of each subtile, as they are stored
       const int key_lane = (gid >> 1) + 4 * (gid & 1);  // matrix row gid is this key of a subtile, row gid + 8 key_lane + 8
@@ -651,6 +597,25 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
       }
       if (masked) {
         unsigned hidden[NT] = {};  // a bit per score of this lane
+        if constexpr (TREE) {
+          static_assert(16 * SUB == 32, "a step's keys are a word's bits");
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int t = min(token_of(at.block * COLS + n * 8 + 2 * tig + c, p), at.count - 1);
+              unsigned seen = tree_view(p, at.first + t, key0, all_end, at.count);
+#pragma unroll
+              for (int st = 0; st < SUB; ++st)
+                if (!(have >> st & 1)) seen &= ~(0xffffu << 16 * st);
+              seen >>= key_lane;
+#pragma unroll
+              for (int st = 0; st < SUB; ++st)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  if (!(seen >> (16 * st + 8 * h) & 1)) x[n][st][2 * h + c] = -INFINITY, hidden[n] |= 1u << (4 * st + 2 * h + c);
+            }
+        } else {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -662,6 +627,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
               const bool sees = key0 + k < end && (p.window == 0 || key0 + k >= end - p.window) && (have >> st & 1);
               if (!sees) x[n][st][i] = -INFINITY, hidden[n] |= 1u << (4 * st + i);
             }
+        }
         // Parameters that no row sees may be anything.  A NaN that some rows see and others do not: theirs at once
         // (through the group's centres), and gone for the products, where it would meet the others' zeros
 #pragma unroll
@@ -902,7 +868,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
           }
       }
     }
-    if (next < w1) next_tile<COLS>(at, info, prefix, p);
+    if (next < w1) next_tile<COLS, TREE>(at, info, prefix, p);
     flat = next;
   }
 
@@ -927,7 +893,7 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   // a segment's places in the list, and how it stands to this block's: whole, or begun (0) or continued (1) elsewhere
   const auto segment = [&](int id, Cursor &c, int64_t &sa, int64_t &sb) {
     c.seq = id >> 10, c.head = id >> 2 & 255, c.block = id & 3;
-    enter_sequence<COLS>(c, info, prefix, p);
+    enter_sequence<COLS, TREE>(c, info, prefix, p);
     sa = (int64_t)prefix[c.seq] * heads + (c.head * c.blocks + c.block) * (c.n_tiles + 1) + 1, sb = sa + c.n_tiles;
   };
   Cursor seg;
@@ -1023,18 +989,18 @@ __global__ void __launch_bounds__(Few<HD, NT>::THREADS, 1) kv4_attend_few_kernel
   }
 }
 
-template <int HD, int NT, bool BF16>
+template <int HD, int NT, bool BF16, bool TREE>
 cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   using F = Few<HD, NT>;
   static SmemOptIn opt_in;
-  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_few_kernel<HD, NT, BF16>);
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_few_kernel<HD, NT, BF16, TREE>);
   const cudaError_t e = opt_in(kernel, F::SMEM);
   if (e != cudaSuccess) return e;
   // as many blocks as the longest contexts could fill
   const int64_t most = (int64_t)p.n_seqs * p.pool.n_kv_heads * p.most_blocks *
                        (((int64_t)p.map.max_pages << p.pool.log2_tokens) / TILE + 2);
   const unsigned grid = (unsigned)std::min<int64_t>(std::min(n_sm, FEW_BLOCKS), (most + F::WARPS - 1) / F::WARPS);
-  return launch_chained(kv4_attend_few_kernel<HD, NT, BF16>, grid, F::THREADS, F::SMEM, s, p);
+  return launch_chained(kv4_attend_few_kernel<HD, NT, BF16, TREE>, grid, F::THREADS, F::SMEM, s, p);
 }
 
 }  // namespace
@@ -1047,13 +1013,14 @@ size_t attend_few_partials(int head_dim, int cols) {
   return FEW_BLOCKS * floats * sizeof(float);
 }
 
-template <bool BF16>
+template <bool BF16, bool TREE>
 static cudaError_t launch_type(const AttendParams &p, int cols, int n_sm, cudaStream_t s) {
-  if (p.pool.head_dim == 128) return cols <= 8 ? launch<128, 1, BF16>(p, n_sm, s) : launch<128, 2, BF16>(p, n_sm, s);
-  return cols <= 8 ? launch<64, 1, BF16>(p, n_sm, s) : launch<64, 2, BF16>(p, n_sm, s);
+  if (p.pool.head_dim == 128) return cols <= 8 ? launch<128, 1, BF16, TREE>(p, n_sm, s) : launch<128, 2, BF16, TREE>(p, n_sm, s);
+  return cols <= 8 ? launch<64, 1, BF16, TREE>(p, n_sm, s) : launch<64, 2, BF16, TREE>(p, n_sm, s);
 }
 cudaError_t launch_attend_few(const AttendParams &p, int cols, int n_sm, cudaStream_t s) {
-  return p.bf16 ? launch_type<true>(p, cols, n_sm, s) : launch_type<false>(p, cols, n_sm, s);
+  if (p.views) return p.bf16 ? launch_type<true, true>(p, cols, n_sm, s) : launch_type<false, true>(p, cols, n_sm, s);
+  return p.bf16 ? launch_type<true, false>(p, cols, n_sm, s) : launch_type<false, false>(p, cols, n_sm, s);
 }
 
 }  // namespace kfl

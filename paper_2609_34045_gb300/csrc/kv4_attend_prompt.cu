@@ -166,26 +166,29 @@ struct Piece {
   int64_t flat;                  // place of its first tile in the list
 };
 
-template <int KEYS>
+template <int KEYS_, bool TREE_>
 struct List {
+  static constexpr int KEYS = KEYS_;
+  static constexpr bool TREE = TREE_;
   const int4 *info;
   const int *prefix;
   int n_seqs, heads, group, window, rows_per_block;
 };
 
-template <int KEYS>
-__device__ __forceinline__ void tiles_of_block(int length, int count, int block, const List<KEYS> &l, int &tile0, int &n) {
+template <class L>
+__device__ __forceinline__ void tiles_of_block(int length, int count, int block, const L &l, int &tile0, int &n) {
   const int rows = count * l.group;
   const int tok0 = block * l.rows_per_block / l.group;
   const int tok1 = (min(rows, (block + 1) * l.rows_per_block) - 1) / l.group;
-  const int end = length - count + tok1 + 1;
-  const int begin = l.window > 0 ? max(0, length - count + tok0 + 1 - l.window) : 0;
-  tile0 = begin / KEYS;
-  n = max(1, (max(end, 0) + KEYS - 1) / KEYS - tile0);
+  // (a tree's nodes may see any of the last tokens, and of the context a window's rows at most)
+  const int end = L::TREE ? length : length - count + tok1 + 1;
+  const int begin = l.window > 0 ? max(0, length - count + (L::TREE ? 0 : tok0 + 1) - l.window) : 0;
+  tile0 = begin / L::KEYS;
+  n = max(1, (max(end, 0) + L::KEYS - 1) / L::KEYS - tile0);
 }
 
-template <int KEYS>
-__device__ __forceinline__ void open_piece(Piece &pc, const List<KEYS> &l, int skip, int64_t limit) {
+template <class L>
+__device__ __forceinline__ void open_piece(Piece &pc, const L &l, int skip, int64_t limit) {
   // the block's tiles from `skip` on, as far as the list's place `limit`
   pc.row0 = pc.block * l.rows_per_block;
   pc.rows = min(l.rows_per_block, pc.count * l.group - pc.row0);
@@ -194,15 +197,15 @@ __device__ __forceinline__ void open_piece(Piece &pc, const List<KEYS> &l, int s
   pc.to = (int)min((int64_t)pc.n_tiles, limit - pc.flat);
 }
 
-template <int KEYS>
-__device__ __forceinline__ void open_sequence(Piece &pc, const List<KEYS> &l) {
+template <class L>
+__device__ __forceinline__ void open_sequence(Piece &pc, const L &l) {
   const int4 v = l.info[pc.seq];
   pc.user = v.x, pc.length = v.y, pc.first = v.z, pc.count = v.w;
 }
 
 // The piece at place `at` of the list (at < limit).  The whole warp calls it: lanes count the tiles of a block each.
-template <int KEYS>
-__device__ void find_piece(Piece &pc, const List<KEYS> &l, int64_t at, int64_t limit) {
+template <class L>
+__device__ void find_piece(Piece &pc, const L &l, int64_t at, int64_t limit) {
   const int lane = threadIdx.x & 31;
   int lo = 0, hi = l.n_seqs - 1;
   while (lo < hi) {
@@ -241,8 +244,8 @@ __device__ void find_piece(Piece &pc, const List<KEYS> &l, int64_t at, int64_t l
   open_piece(pc, l, (int)(at - pc.flat), limit);
 }
 
-template <int KEYS>
-__device__ void next_piece(Piece &pc, const List<KEYS> &l, int64_t limit) {  // (the list goes on to `limit`)
+template <class L>
+__device__ void next_piece(Piece &pc, const L &l, int64_t limit) {  // (the list goes on to `limit`)
   pc.flat += pc.n_tiles;
   if (++pc.block * l.rows_per_block >= pc.count * l.group) {
     pc.block = 0;
@@ -313,7 +316,7 @@ __device__ __forceinline__ void decode_row(const uint4 (&raw)[HD / 32], const ui
   }
 }
 
-template <int HD, int TERMS>
+template <int HD, int TERMS, bool TREE>
 __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const AttendParams p, int rows_per_block) {
   using F = Prompt<HD, TERMS>;
   constexpr int KB = F::KB, KEYS = F::KEYS, COLS = F::COLS, QUARTERS = F::QUARTERS;
@@ -329,7 +332,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   const auto bar = [&](int b) { return bars + 8 * b; };
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
-  const List<KEYS> list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
+  const List<KEYS, TREE> list = {info, prefix, p.n_seqs, heads, p.group, p.window, rows_per_block};
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(B_KFULL + i), QUARTERS);
@@ -448,8 +451,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
         const int r = half * 128 + row;
         const bool there = r < pc.rows;
         const int token = (pc.row0 + (there ? r : 0)) / p.group, head = pc.head * p.group + (pc.row0 + (there ? r : 0)) % p.group;
-        const int end = there ? pc.length - pc.count + token + 1 : pc.length;  // keys below it are seen
-        const int begin = p.window > 0 ? end - p.window : 0;
+        // keys below `end` are seen, from `begin` on (a tree: all context, and by their bits the nodes behind it)
+        const int end = TREE ? pc.length - pc.count : there ? pc.length - pc.count + token + 1 : pc.length;
+        const int begin = p.window == 0 ? 0
+                          : TREE        ? end - max(0, p.window - tree_nodes(p, pc.first + token, pc.count))
+                                        : end - p.window;
         // its query, in fp16 and the words' channel order
         float unit, inv;
         {
@@ -520,7 +526,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
 #pragma unroll 1
             for (int k = 0; k < KEYS; ++k) {
               const uint32_t bits = k < 32 ? v.x : k < 64 ? v.y : k < 96 ? v.z : v.w;
-              if ((bits >> (k & 31) & 1) && key0 + k < end && key0 + k >= begin) poison |= 1u << g;
+              if (!(bits >> (k & 31) & 1)) continue;
+              if (TREE ? tree_view(p, pc.first + token, key0 + k, end, pc.count) & 1 : key0 + k < end && key0 + k >= begin)
+                poison |= 1u << g;
             }
           }
         };
@@ -546,11 +554,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
           if (pair_any(twins, masked || odd_k || t == 0 || part_sum > PT_MOST || top == -INFINITY)) {
             const bool pick = masked || odd_k;
             const uint4 there4 = flags[((tile + t) & 3) * (1 + KB)];
+            uint32_t view[COLS / 32] = {};  // a tree's: a bit per key of this thread's
+            if (TREE && pick)
+#pragma unroll
+              for (int i = 0; i < COLS / 32; ++i) {
+                const int k = part * COLS + 32 * i;
+                view[i] = tree_view(p, pc.first + token, key0 + 32 * i, end, pc.count) &
+                          (k < 32 ? there4.x : k < 64 ? there4.y : k < 96 ? there4.z : there4.w);
+              }
             const auto sees = [&](int c, int i) {  // column 16 c + i
+              if constexpr (TREE) return (bool)((COLS > 32 && c >= 2 ? view[COLS / 32 - 1] : view[0]) >> ((c & 1) * 16 + i) & 1);
               const int key = key0 + 16 * c + i;
               const int k = part * COLS + 16 * c;
               const uint32_t pages = k < 32 ? there4.x : k < 64 ? there4.y : k < 96 ? there4.z : there4.w;
-              return key < end && key >= begin && (pages >> ((c & 1) * 16 + i) & 1);
+              return key < end && key >= begin && (bool)(pages >> ((c & 1) * 16 + i) & 1);
             };
             float most = -INFINITY;
 #pragma unroll 1
@@ -923,14 +940,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) kv4_attend_prompt_kernel(const 
   }
 }
 
-template <int HD, int TERMS>
+template <int HD, int TERMS, bool TREE>
 cudaError_t launch(const AttendParams &p, int n_sm, cudaStream_t s) {
   static SmemOptIn opt_in;
-  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_prompt_kernel<HD, TERMS>);
+  const void *kernel = reinterpret_cast<const void *>(&kv4_attend_prompt_kernel<HD, TERMS, TREE>);
   const int smem = Prompt<HD, TERMS>::SMEM + 1024;
   const cudaError_t e = opt_in(kernel, smem);
   if (e != cudaSuccess) return e;
-  return launch_chained(kv4_attend_prompt_kernel<HD, TERMS>, std::min(n_sm, FEW_BLOCKS), PT_THREADS, smem, s, p,
+  return launch_chained(kv4_attend_prompt_kernel<HD, TERMS, TREE>, std::min(n_sm, FEW_BLOCKS), PT_THREADS, smem, s, p,
                         prompt_rows(p.max_q * p.group));
 }
 
@@ -940,10 +957,14 @@ size_t attend_prompt_partials(int head_dim, int64_t rows) {
   return (size_t)FEW_BLOCKS * 2 * prompt_rows(rows) * (head_dim + 2) * sizeof(float);
 }
 
-cudaError_t launch_attend_prompt(const AttendParams &p, int n_sm, cudaStream_t s) {
+template <bool TREE>
+static cudaError_t launch_type(const AttendParams &p, int n_sm, cudaStream_t s) {
   // (two terms for fp16 outputs, whose own rounding is no larger than that of a decoded value; bf16's is eight times it)
-  if (p.pool.head_dim == 128) return p.bf16 ? launch<128, 1>(p, n_sm, s) : launch<128, 2>(p, n_sm, s);
-  return p.bf16 ? launch<64, 1>(p, n_sm, s) : launch<64, 2>(p, n_sm, s);
+  if (p.pool.head_dim == 128) return p.bf16 ? launch<128, 1, TREE>(p, n_sm, s) : launch<128, 2, TREE>(p, n_sm, s);
+  return p.bf16 ? launch<64, 1, TREE>(p, n_sm, s) : launch<64, 2, TREE>(p, n_sm, s);
+}
+cudaError_t launch_attend_prompt(const AttendParams &p, int n_sm, cudaStream_t s) {
+  return p.views ? launch_type<true>(p, n_sm, s) : launch_type<false>(p, n_sm, s);
 }
 
 }  // namespace kfl

@@ -1,0 +1,62 @@
+// The attention weight of cached rows (include/kafila_kv4_evict.h): kfl_kv4_weights.
+#include <math.h>
+
+#include <algorithm>
+
+#include "kv4_weights.cuh"
+
+using namespace kfl;
+
+extern "C" int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
+                               const float *lse, const kfl_kv4_mass *mass, const int32_t *users, const int32_t *q_start,
+                               int n_seqs, int n_tokens, int max_q, float scale, int window, void *workspace,
+                               size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  const char *me = "kfl_kv4_weights";
+  if (!heads_valid(q, n_tokens)) return bad_arg(me, "q is needed");
+  int rc = check_pool(pool, true, me);
+  if (rc == KFL_OK) rc = check_map(map, me);
+  if (rc == KFL_OK) rc = check_layer(pool, layer, me);
+  if (rc != KFL_OK) return rc;
+  if (q->dtype == KFL_DT_FP32) return bad_arg(me, "q is bf16 or fp16");
+  if (!std::isfinite(scale) || window < 0) return bad_arg(me, "scale is finite, window not negative");
+  if (!q_start && n_tokens != n_seqs) return bad_arg(me, "without q_start every sequence has one token");
+  size_t need = 0;
+  rc = kfl_kv4_attend_workspace_bytes(pool, q->n_heads, n_seqs, n_tokens, max_q, &need);  // (checks heads and counts)
+  if (rc != KFL_OK) return rc;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < need)
+    return bad_arg(me, "a 16-byte aligned workspace of kfl_kv4_attend_workspace_bytes is needed");
+  if (n_seqs > WEIGHT_SEQS) {
+    bad_arg(me, "more than 1024 sequences in one call");
+    return KFL_ERR_RANGE;
+  }
+  if (n_seqs == 0 || n_tokens == 0) return KFL_OK;
+  if (!mass_valid(mass) || !lse || (reinterpret_cast<uintptr_t>(lse) & 3)) return bad_arg(me, "lse and mass are needed");
+  if (((int64_t)map->max_pages * pool->page_tokens) > (1 << 26)) return bad_arg(me, "max_pages * page_tokens is at most 2^26");
+  WeightParams p = {};
+  p.pool = pool_of(*pool), p.map = map_of(*map), p.layer = layer;
+  p.q = view_of(*q), p.q_wide = rows_aligned16(*q), p.bf16 = q->dtype == KFL_DT_BF16;
+  p.lse = lse, p.mass = view_of(*mass), p.all_users = users;
+  p.n_tokens = n_tokens, p.max_q = q_start ? max_q : 1;
+  p.n_heads = q->n_heads, p.group = q->n_heads / pool->n_kv_heads;
+  p.scale = scale, p.status = status;
+  // (a window that no context fills is none; the kernels take it off places below 2^26, in 32 bits)
+  p.window = window >= map->max_pages * pool->page_tokens ? 0 : window;
+  const int64_t rows = (int64_t)std::min(p.max_q, n_tokens) * p.group;
+  if (rows > (1 << 30)) {
+    bad_arg(me, "more than 2^30 query rows of a sequence per KV head");
+    return KFL_ERR_RANGE;
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  int dev = 0, n_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+  for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
+    p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
+    p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
+    for (int64_t r = 0; e == cudaSuccess && r < rows; r += WEIGHT_FEW) {
+      p.row0 = (int)r;
+      e = launch_weights_few(p, weight_cols(rows - r), n_sm, s);
+    }
+  }
+  return cuda_result(e, me);
+}

@@ -1,5 +1,6 @@
-"""Python binding of ``include/kafila_rope.h`` and ``include/kafila_kv4.h``: rotary positions and the 4-bit
-paged KV cache (argument marshalling only, as in ``stage``).
+"""Python binding of ``include/kafila_rope.h``, ``include/kafila_kv4.h``, ``include/kafila_kv4_tree.h`` and
+``include/kafila_kv4_evict.h``: rotary positions, the 4-bit paged KV cache, trees of drafted tokens over it and rows that leave
+it (argument marshalling only, as in ``stage``).
 
 Functions named ``kfl_*`` call the C entry point of that name on CUDA tensors.  ``rope_plan``, ``pool`` and
 ``page_map`` describe buffers that the caller keeps; ``attend_workspace`` and ``pages_workspace`` allocate the
@@ -52,6 +53,15 @@ class kfl_kv4_map(C.Structure):
                 ("max_pages", C.c_int)]
 
 
+class kfl_kv4_mass(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("layer_stride", "user_stride", "head_stride")]
+
+
+class kfl_kv4_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("layer_stride", "seq_stride", "head_stride")] + [
+        ("most", C.c_int)]
+
+
 _lib = _signed = None
 _several = True  # whether a tensor may be another device's (until the library is loaded: perhaps)
 
@@ -63,6 +73,7 @@ def lib() -> C.CDLL:
     if _signed is not L:
         vp, i, f, P = C.c_void_p, C.c_int, C.c_float, C.POINTER
         heads, plan, pl, mp, sz = vp, P(kfl_rope_plan), P(kfl_kv4_pool), P(kfl_kv4_map), P(C.c_size_t)
+        mass = P(kfl_kv4_mass)
         for name, args in {
             "kfl_rope_table": [P(kfl_rope_cfg), i, vp, vp],
             "kfl_rope": [plan, heads, heads, heads, heads, vp, i, i, i, vp, vp],
@@ -77,6 +88,11 @@ def lib() -> C.CDLL:
             "kfl_kv4_free": [pl, mp, vp, i, vp, vp],
             "kfl_kv4_compact": [pl, mp, vp, vp, vp, vp, vp, vp],
             "kfl_kv4_copy_pages": [pl, vp, vp, i, vp, vp],
+            "kfl_kv4_tree": [vp, vp, vp, i, i, i, vp, vp, vp, vp],
+            "kfl_kv4_attend_tree": [pl, mp, i, heads, heads, vp, vp, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
+            "kfl_kv4_weights": [pl, mp, i, heads, vp, mass, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
+            "kfl_kv4_select": [pl, mp, mass, vp, i, i, i, i, vp, vp, vp, vp],
+            "kfl_kv4_keep": [pl, mp, vp, P(kfl_kv4_rows), vp, vp, mass, i, vp, vp, vp],
         }.items():
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, i
@@ -233,29 +249,131 @@ def attend_workspace(p, n_heads: int, n_seqs: int, n_tokens: int, max_q: int = 1
                        device="cuda")
 
 
+def _sequences(m, q, users, q_start, lse, workspace):
+    """How many sequences a call's rows are."""
+    n = q.shape[0]
+    n_seqs = users.numel() if users is not None else q_start.numel() - 1 if q_start is not None else n
+    if users is None and n_seqs > m.n_users:
+        raise ValueError("more sequences than users")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * q.shape[1]):
+        raise ValueError("lse is a contiguous fp32 [token][query head]")
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace is contiguous")
+    return n_seqs
+
+
 def kfl_kv4_attend(p, m, layer: int, q, out, workspace, users=None, q_start=None, max_q: int = 1, scale=None,
                    window: int = 0, lse=None, status=None, cuda_stream: int | None = None) -> None:
     """Attention of q's rows over the users' cached rows of one layer, into out (bf16 or fp16
     [token][query head][head_dim]).  Without q_start (int32 [sequence + 1]) every row is a sequence; without users
     (int32 [sequence]) sequence s is user s.  lse: fp32 [token][query head].  Asynchronous."""
-    n, n_heads, hd = q.shape
-    if users is not None:
-        n_seqs = users.numel()
-    elif q_start is not None:
-        n_seqs = q_start.numel() - 1
-    else:
-        n_seqs = n
-    if users is None and n_seqs > m.n_users:
-        raise ValueError("more sequences than users")
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < n * n_heads):
-        raise ValueError("lse is a contiguous fp32 [token][query head]")
-    if not workspace.is_contiguous():
-        raise ValueError("the workspace is contiguous")
+    n, _, hd = q.shape
+    n_seqs = _sequences(m, q, users, q_start, lse, workspace)
     a, b = _heads(q, "q", n, p.head_dim), _heads(out, "out", n, p.head_dim)
     _check(lib().kfl_kv4_attend(_handle(p), _handle(m), layer, a, b, _at(lse, "lse"),
                                 _int32(users, "users"), _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
                                 1.0 / math.sqrt(hd) if scale is None else scale, window, _at(workspace, "the workspace"),
                                 workspace.numel() * workspace.element_size(), _int32(status, "status", 1), cuda_stream), "kfl_kv4_attend")
+
+
+# ---- trees of drafted tokens ---------------------------------------------------------------------
+
+def _views(views, n, max_q, where="views"):
+    words = -(-max_q // 32)
+    if views.dim() != 2 or views.shape[0] < n or views.shape[1] != words:
+        raise ValueError(f"{where} is a contiguous int32 [token][{words}]")
+    return _int32(views, where)
+
+
+def kfl_kv4_tree(parents, views, positions=None, q_start=None, first=None, max_q: int = 1, status=None,
+                 cuda_stream: int | None = None) -> None:
+    """Which of their sequence's nodes the nodes of drafted trees see, into views (int32 [token][ceil(max_q / 32)], a bit a
+    node), and their positions, first (int32 [sequence], None: 0) + ancestors, into positions (int32 [token], may be
+    None).  parents: int32 [token], counted within the sequence, -1 for none; q_start as in kfl_kv4_attend.  Asynchronous."""
+    n = parents.numel()
+    n_seqs = q_start.numel() - 1 if q_start is not None else n
+    _check(lib().kfl_kv4_tree(_int32(parents, "parents"), _int32(q_start, "q_start"), _int32(first, "first", n_seqs), n_seqs, n,
+                              max_q, _views(views, n, max_q), _int32(positions, "positions", n), _int32(status, "status", 1),
+                              cuda_stream), "kfl_kv4_tree")
+
+
+def kfl_kv4_attend_tree(p, m, layer: int, q, out, views, workspace, users=None, q_start=None, max_q: int = 1, scale=None,
+                        window: int = 0, lse=None, status=None, cuda_stream: int | None = None) -> None:
+    """kfl_kv4_attend of the nodes of trees: of its sequence's last tokens each sees those of its row of views
+    (kfl_kv4_tree).  Asynchronous."""
+    n, _, hd = q.shape
+    n_seqs = _sequences(m, q, users, q_start, lse, workspace)
+    a, b = _heads(q, "q", n, p.head_dim), _heads(out, "out", n, p.head_dim)
+    _check(lib().kfl_kv4_attend_tree(_handle(p), _handle(m), layer, a, b, _at(lse, "lse"), _int32(users, "users"),
+                                     _int32(q_start, "q_start", n_seqs + 1), _views(views, n, max_q), n_seqs, n, max_q,
+                                     1.0 / math.sqrt(hd) if scale is None else scale, window, _at(workspace, "the workspace"),
+                                     workspace.numel() * workspace.element_size(), _int32(status, "status", 1), cuda_stream),
+           "kfl_kv4_attend_tree")
+
+
+# ---- rows that leave the cache -------------------------------------------------------------------
+
+def _mass(mass, p, m):
+    """kfl_kv4_mass of a tensor [layer][user][KV head][slot] whose slots are neighbours and whose rows do not overlap."""
+    if mass is None:
+        return None
+    want = (p.n_layers, m.n_users, p.n_kv_heads, m.max_pages * p.page_tokens)
+    if mass.dtype != torch.float32 or mass.dim() != 4 or mass.shape[0] != want[0] or mass.shape[1] < want[1] \
+            or mass.shape[2] != want[2] or mass.shape[3] < want[3]:
+        raise ValueError(f"mass is fp32 [layer][user][KV head][slot] of {list(want)}")
+    if not mass.is_contiguous():
+        span = 1
+        for size, stride in sorted(zip(mass.shape, mass.stride()), key=lambda v: v[1]):
+            if size > 1 and stride < span:
+                raise ValueError("the rows of mass do not overlap")
+            span += (size - 1) * stride
+        if mass.stride(3) != 1:
+            raise ValueError("the slots of mass are neighbours")
+    a, b, c, _ = mass.stride()
+    return C.byref(kfl_kv4_mass(_at(mass, "mass"), a, b, c))
+
+
+def kfl_kv4_weights(p, m, layer: int, q, lse, mass, workspace, users=None, q_start=None, max_q: int = 1, scale=None,
+                    window: int = 0, status=None, cuda_stream: int | None = None) -> None:
+    """Adds to mass (fp32 [layer][user][KV head][slot]) of one layer the weight that q's rows give every cached row, with the
+    lse that kfl_kv4_attend or kfl_kv4_attend_tree wrote for them; the other arguments as theirs.  Asynchronous."""
+    n, _, hd = q.shape
+    n_seqs = _sequences(m, q, users, q_start, lse, workspace)
+    a = _heads(q, "q", n, p.head_dim)
+    _check(lib().kfl_kv4_weights(_handle(p), _handle(m), layer, a, _at(lse, "lse"), _mass(mass, p, m), _int32(users, "users"),
+                                 _int32(q_start, "q_start", n_seqs + 1), n_seqs, n, max_q,
+                                 1.0 / math.sqrt(hd) if scale is None else scale, window, _at(workspace, "the workspace"),
+                                 workspace.numel() * workspace.element_size(), _int32(status, "status", 1), cuda_stream),
+           "kfl_kv4_weights")
+
+
+def kfl_kv4_select(p, m, mass, users, budget: int, rows, counts, first: int = 0, recent: int = 0, status=None,
+                   cuda_stream: int | None = None) -> None:
+    """The rows that stay of the users (int32) cut to `budget`: the first, the most recent, and of the others those with the
+    greatest mass; slots into rows (int32 [layer][user of the list][KV head][budget], -1 behind the last), how many into
+    counts (int32 [user of the list]).  Asynchronous."""
+    n = users.numel()
+    if tuple(rows.shape) != (p.n_layers, n, p.n_kv_heads, budget):
+        raise ValueError(f"rows is int32 [layer][user of the list][KV head][budget], {[p.n_layers, n, p.n_kv_heads, budget]}")
+    _check(lib().kfl_kv4_select(_handle(p), _handle(m), _mass(mass, p, m), _int32(users, "users"), n, budget, first, recent,
+                                _int32(rows, "rows"), _int32(counts, "counts", n), _int32(status, "status", 1), cuda_stream),
+           "kfl_kv4_select")
+
+
+def kfl_kv4_keep(p, m, users, rows, counts, workspace, first=None, mass=None, status=None,
+                 cuda_stream: int | None = None) -> None:
+    """Cuts the users (int32) to their rows below first (int32 [user of the list], None: 0) and the counts (int32) rows of
+    their lists: rows is int32 [layer][user of the list][KV head][most], of any strides whose last is 1 (expanded where
+    layers or heads are alike).  mass moves with the rows.  Asynchronous."""
+    n = users.numel()
+    if rows.dtype != torch.int32 or rows.dim() != 4 or tuple(rows.shape[:3]) != (p.n_layers, n, p.n_kv_heads) \
+            or rows.stride(3) != 1 and rows.shape[3] > 1:
+        raise ValueError(f"rows is int32 [layer][user of the list][KV head][most], {[p.n_layers, n, p.n_kv_heads]}, its last stride 1")
+    a, b = _covers(p, m)
+    r = kfl_kv4_rows(_at(rows, "rows"), *rows.stride()[:3], rows.shape[3])
+    _check(lib().kfl_kv4_keep(a, b, _int32(users, "users"), C.byref(r), _int32(first, "first", n), _int32(counts, "counts", n),
+                              _mass(mass, p, m), n, _scratch(p, workspace), _int32(status, "status", 1), cuda_stream),
+           "kfl_kv4_keep")
 
 
 # ---- pages ---------------------------------------------------------------------------------------
