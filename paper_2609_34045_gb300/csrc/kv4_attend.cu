@@ -40,11 +40,6 @@ int check_attend(const char *me, const kfl_kv4_pool *pool, int n_heads, int n_se
   return KFL_OK;
 }
 
-// The workspace: tickets (zero between calls), then partial results.  The tickets' part is the same for every call, so
-// that no call's partial results lie where another one's tickets are.
-constexpr size_t TICKET_BYTES = (size_t)FEW_SEQS * KV4_MOST_HEADS * ((FEW_ROWS + 15) / 16) * 4;
-static_assert(TICKET_BYTES >= FEW_BLOCKS * 4 && TICKET_BYTES % 128 == 0, "tickets");
-
 }  // namespace
 }  // namespace kfl
 

@@ -10,6 +10,11 @@ constexpr int FEW_ROWS = 64;     // most query rows per KV head of the few-row k
 constexpr int FEW_SEQS = 512;    // sequences of one of its launches (their places lie in shared memory)
 constexpr int FEW_BLOCKS = 152;  // most blocks of one of its launches
 
+// The workspace: tickets (zero between calls), then partial results.  The tickets' part is the same for every call, so
+// that no call's partial results lie where another one's tickets are.
+constexpr size_t TICKET_BYTES = (size_t)FEW_SEQS * KV4_MOST_HEADS * ((FEW_ROWS + 15) / 16) * 4;
+static_assert(TICKET_BYTES >= FEW_BLOCKS * 4 && TICKET_BYTES % 128 == 0, "tickets");
+
 struct AttendParams {
   Kv4Pool pool;
   Kv4Map map;

@@ -29,7 +29,7 @@
 #include <algorithm>
 
 #include "kv4_attend.cuh"
-#include "prefill_tc.cuh"
+#include "kv4_tc.cuh"
 
 namespace kfl {
 namespace {
@@ -66,25 +66,6 @@ struct Prompt {
 // Barriers, in 8-byte places behind BAR_AT.
 enum { B_KFULL = 0, B_KFREE = 2, B_VFULL = 4, B_VFREE = 6, B_Q = 8, B_S = 10, B_P = 12, B_O = 14, B_READ = 16, B_DRAIN = 18 };
 
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 // Shared-memory descriptor of an operand whose N (channels) lies contiguous, 128-byte swizzled: rows of 64 channels, one
 // per K (key), groups of 8 rows 1024 bytes apart (the stride byte offset), the next 64 channels `next` bytes on (the
 // leading byte offset).
@@ -107,16 +88,6 @@ __device__ __forceinline__ uint32_t pt_pack(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
-}
-
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, d;\n\t"
-      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
 }
 
 // A thread's scores of a row: w the weights 2^(score cf - top) in fp16 pairs, the second product's operand (bf16 would be eight

@@ -46,6 +46,8 @@ extern "C" int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map,
     bad_arg(me, "more than 2^30 query rows of a sequence per KV head");
     return KFL_ERR_RANGE;
   }
+  p.tickets = static_cast<unsigned *>(workspace);
+  p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + TICKET_BYTES);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   int dev = 0, n_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -53,10 +55,7 @@ extern "C" int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map,
   for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
     p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
     p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
-    for (int64_t r = 0; e == cudaSuccess && r < rows; r += WEIGHT_FEW) {
-      p.row0 = (int)r;
-      e = launch_weights_few(p, weight_cols(rows - r), n_sm, s);
-    }
+    e = rows <= WEIGHT_FEW ? launch_weights_few(p, weight_cols(rows), n_sm, s) : launch_weights_many(p, n_sm, s);
   }
   return cuda_result(e, me);
 }

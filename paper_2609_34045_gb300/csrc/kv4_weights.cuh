@@ -7,7 +7,7 @@
 namespace kfl {
 
 constexpr int WEIGHT_SEQS = 1024;  // sequences of a call
-constexpr int WEIGHT_FEW = 32;     // most query rows per KV head that one launch of the streaming kernel takes
+constexpr int WEIGHT_FEW = 32;     // most query rows per KV head of the streaming kernel
 
 struct MassView {
   float *data;
@@ -30,7 +30,6 @@ struct WeightParams {
   const int32_t *all_users;           // the call's list, or NULL
   const int32_t *users, *q_start;     // from sequence seq0 on
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
-  int row0;  // streaming kernel: query rows [row0, row0 + its columns) of a KV head
   float scale;
   int window;
   unsigned *tickets;
@@ -64,5 +63,6 @@ __device__ __forceinline__ bool named_earlier(const WeightParams &p, int s) {
 
 inline int weight_cols(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
 cudaError_t launch_weights_few(const WeightParams &p, int cols, int n_sm, cudaStream_t s);
+cudaError_t launch_weights_many(const WeightParams &p, int n_sm, cudaStream_t s);
 
 }  // namespace kfl
