@@ -7,17 +7,19 @@
 // bf16, with the queries as they stand, in their own type: nothing is rounded before the fp32 sums.  Scales and centres
 // act on the sums, four fused operations a score with two groups.
 //
-// What bounds it.  An exponential a score: 16 a clock and SM, 1024 clocks for a unit of 256 keys by 64 rows, whose products take
-// some 600 and whose other fp32 work about 700 of the issue slots.
+// What bounds it.  An exponential a score: 16 a clock and SM, 2048 clocks for a unit of 256 keys by 128 rows, whose products
+// take some 1100 and whose other fp32 work about 1400 issue slots of each scheduler.
 //
-// Roles.  Warps 0-15: two threads per key (32 rows of a unit each), keys on the tensor memory's lanes, so that a key's weights
-// are summed in a register.  They also decode their keys, into tensor memory: the products' first operand.  16-19: queries, a
-// thread per row, into swizzled shared memory, with the sums and log-sum-exps; 20: products.
+// Roles.  Warps 0-15: two threads per key (64 rows of a unit each), keys on the tensor memory's lanes, so that a key's weights
+// are summed in a register.  They also decode their keys into swizzled shared memory.  16: tensor copies of the queries, which
+// need no conversion; 17, 18: every other unit's sums of the queries (as products with ones) and log-sum-exps; 19: products.
+// While one half's (128 keys) sums are read, the other half's products run.
 //
-// Work split.  The units (sequence, KV head, 256 keys, 64 rows) in sight form one list that the blocks share equally, rows
-// fastest: a block decodes its keys once.  Keys whose rows are cut between blocks are summed by the last to arrive, in list
-// order, so results do not depend on arrival.
+// Work split.  The units (sequence, KV head, 256 keys, as many tokens as fill 128 rows) in sight form one list that the blocks
+// share equally, rows fastest: a block decodes its keys once.  Keys whose rows are cut between blocks are summed by the last to
+// arrive, in list order, so results do not depend on arrival.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4_tc.cuh"
 #include "kv4_weights.cuh"
@@ -25,53 +27,63 @@
 namespace kfl {
 namespace {
 
-constexpr int WM_KEYS = 256, WM_ROWS = 64;
-constexpr int WM_SUMMERS = 16, WM_LOADERS = 4;  // warps
-constexpr int WM_MMA_WARP = WM_SUMMERS + WM_LOADERS;
+constexpr int WM_KEYS = 256, WM_ROWS = 128;
+constexpr int WM_SUMMERS = 16;  // warps
+constexpr int WM_COPY_WARP = 16, WM_STAT_WARP = 17, WM_MMA_WARP = 19;
 constexpr int WM_THREADS = (WM_MMA_WARP + 1) * 32;
-constexpr int WM_STAGES = 4;  // of queries
+constexpr int WM_STAGES = 4;  // of queries: even, so that a stage is always the same warp's to sum (else it could take an older phase for its own)
 
 template <int HD>
 struct Many {
   static constexpr int GROUPS = HD / 64;
   static constexpr int STAGE = WM_ROWS * HD * 2;   // bytes of a unit's queries
-  static constexpr int A_COLS = HD / 2;            // of a half's keys (128) in tensor memory
-  static constexpr int D_COLS = GROUPS * WM_ROWS;  // of a half's sums
-  static constexpr int BUFFERS = HD == 128 ? 3 : 4;
-  static constexpr int D_AT = 2 * A_COLS;
-  static_assert(D_AT + BUFFERS * D_COLS <= 512, "tensor memory");
-  static constexpr int ROWS_AT = WM_STAGES * STAGE;              // float [stages][4][64]: sums of both groups, -lse, end
+  static constexpr int HALF = 128 * HD * 2;        // of 128 keys
+  static constexpr int D_COLS = GROUPS * WM_ROWS;  // of a half's sums in tensor memory
+  static constexpr int BUFFERS = 256 / D_COLS;     // of each half
+  static constexpr int K_AT = WM_STAGES * STAGE;
+  static constexpr int ROWS_AT = K_AT + 2 * HALF;                      // float [stages][4][128]: sums of both groups, -lse, end
   static constexpr int SUM_AT = ROWS_AT + WM_STAGES * 4 * WM_ROWS * 4;  // float [256]: the second threads' sums
-  static constexpr int INFO_AT = SUM_AT + WM_KEYS * 4;           // int4 [FEW_SEQS], then int prefix[FEW_SEQS + 4]
+  static constexpr int ODD_AT = SUM_AT + WM_KEYS * 4;                  // int [stages]: a row that is not like the others
+  static constexpr int INFO_AT = ODD_AT + 16;                          // int4 [FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int BAR_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;
-  static constexpr int N_BARS = 2 * WM_STAGES + 2 * 4 + 2 + 1;
+  static constexpr int N_BARS = 3 * WM_STAGES + 8 + 3;
   static constexpr int SMEM = BAR_AT + N_BARS * 8 + 32;
+  static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
 };
-// Barriers.  Sums are done by half and by the unit's parity (a half's next-but-one job waits, through the buffers, for this one
-// to be read), buffers and stages are free again by number.
-enum { W_QFULL = 0, W_QFREE = WM_STAGES, W_DFULL = 2 * WM_STAGES, W_DFREE = W_DFULL + 4, W_A = W_DFREE + 4, W_DRAIN = W_A + 2 };
+// Barriers: queries are there, may be overwritten, their sums are there; a half's buffer of sums is full, free; a half's
+// keys are there.
+enum {
+  W_QFULL = 0,
+  W_QFREE = WM_STAGES,
+  W_STATS = 2 * WM_STAGES,
+  W_DFULL = 3 * WM_STAGES,
+  W_DFREE = W_DFULL + 4,
+  W_A = W_DFREE + 4,
+  W_DRAIN = W_A + 2
+};
 
 // A run of one key tile's units.
 struct Keys {
   int seq, head, tile;
   int user, length, first, count;
   int first_tile, n_tiles;  // of the sequence
-  int row_tile, n;          // the tile's first row tile and how many see it
+  int row_tile, n;          // the tile's first tile of tokens and how many see it
   int from, to;             // this block's run of them
   int64_t flat;             // place of its first unit in the list
 };
 struct WmList {
   const int4 *info;
   const int *prefix;
-  int n_seqs, heads, group, window;
+  int n_seqs, heads, window;
+  int tokens;  // of a unit: as many as fill its rows
 };
 
-// Which rows, in tiles of 64, see a key of the tile (at least one does, between a sequence's first tile and its last).
+// Which tokens, in tiles, see a key of the tile (at least one does, between a sequence's first tile and its last).
 __device__ __forceinline__ void rows_of_tile(int length, int count, int tile, const WmList &l, int &row_tile, int &n) {
   const int base = length - count, k0 = tile * WM_KEYS, k1 = min(k0 + WM_KEYS, length);
   const int t0 = max(0, k0 - base), t1 = l.window > 0 ? min(count, k1 - base - 1 + l.window) : count;
-  row_tile = t0 * l.group / WM_ROWS;
-  n = (t1 * l.group + WM_ROWS - 1) / WM_ROWS - row_tile;
+  row_tile = t0 / l.tokens;
+  n = (t1 + l.tokens - 1) / l.tokens - row_tile;
 }
 __device__ __forceinline__ void enter(Keys &k, const WmList &l) {
   const int4 v = l.info[k.seq];
@@ -157,24 +169,46 @@ __device__ __forceinline__ void decode8(uint32_t w, uint32_t (&out)[4]) {
   }
 }
 
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// Sums over 16 channels, as a product with ones: of rows gid (d[0], d[1]) and gid + 8 (d[2], d[3]).
+template <bool BF16>
+__device__ __forceinline__ void mma_ones(float (&d)[4], const uint32_t (&a)[4]) {
+  if (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(0x3F803F80u));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(0x3C003C00u));
+}
+
 template <int HD, bool BF16>
-__global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const WeightParams p) {
+__global__ void __launch_bounds__(WM_THREADS, 1)
+    kv4_weights_many_kernel(const WeightParams p, const __grid_constant__ CUtensorMap q_map, int use_map, int tokens) {
   using F = Many<HD>;
   constexpr int G = F::GROUPS, NB = F::BUFFERS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
   const uint32_t base = smem_addr(smem);
+  volatile int *unlike = reinterpret_cast<volatile int *>(smem + F::ODD_AT);
   int4 *info = reinterpret_cast<int4 *>(smem + F::INFO_AT);
   int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
   volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + F::BAR_AT + F::N_BARS * 8);  // TMEM, abort, last
   const auto bar = [&](int b) { return base + F::BAR_AT + 8 * b; };
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens;
-  const WmList list = {info, prefix, p.n_seqs, heads, p.group, p.window};
+  const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens, group = p.group;
+  const WmList list = {info, prefix, p.n_seqs, heads, p.window, tokens};
   if (tid == 0) {
     for (int i = 0; i < WM_STAGES; ++i) {
-      mbar_init(bar(W_QFULL + i), 2);
+      mbar_init(bar(W_QFULL + i), 1);
       mbar_init(bar(W_QFREE + i), 1 + WM_SUMMERS);
+      mbar_init(bar(W_STATS + i), 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(W_DFULL + i), 1);
@@ -187,6 +221,9 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
   }
   fence_mbar_init();
   if (warp == WM_MMA_WARP) tmem_alloc(base + F::BAR_AT + F::N_BARS * 8, 512);
+  // (rows behind a unit's tokens stay zero)
+  for (int i = tid; i < WM_STAGES * F::STAGE / 16; i += WM_THREADS) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+  fence_async_proxy();
   pdl_wait();
 
   // ---- the list: every sequence's units per head, summed
@@ -236,6 +273,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
   const int64_t total = (int64_t)prefix[p.n_seqs] * heads;
   const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
   const int64_t c0 = min(blockIdx.x * quota, total), c1 = min(c0 + quota, total);
+  const int unit_rows = tokens * group;
 
   // a wait that gives up lets no later one last
   const auto wait = [&](int b, uint32_t parity) {
@@ -248,16 +286,16 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
   };
 
   if (c0 < c1 && warp < WM_SUMMERS) {
-    // ---- keys: two threads each, with 32 of a unit's rows
-    const int half = warp >> 2 & 1, part = warp >> 3, key = half * 128 + (warp & 3) * 32 + lane;
+    // ---- keys: two threads each, with 64 of a unit's rows
+    const int half = warp >> 2 & 1, part = warp >> 3, row = (warp & 3) * 32 + lane, key = half * 128 + row;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // TMEM lane 32 (warp mod 4), in bits 16 up
     float *second = reinterpret_cast<float *>(smem + F::SUM_AT);
     const float factor = p.scale * 1.44269504089f;
-    unsigned unit = 0, tiles = 0;
+    unsigned unit = 0;
     Keys k;
     find_keys(k, list, c0, c1);
     for (;;) {
-      // ---- its codes, into tensor memory (all products with the ones before have been waited for), half of them each
+      // ---- its codes, half of them each (all products with the ones before have been waited for)
       const int slot = k.tile * WM_KEYS + key;
       bool there = false;
       float2 s[G], c[G];
@@ -281,19 +319,18 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
             report(p.status, KFL_BAD_PAGE);
           }
         }
-        uint32_t w[HD / 4];
+        const uint32_t tile = base + F::K_AT + half * F::HALF + row * 128;
 #pragma unroll
-        for (int i = 0; i < HD / 64; ++i) {
-          decode8<BF16>(raw[i].x, reinterpret_cast<uint32_t(&)[4]>(w[16 * i]));
-          decode8<BF16>(raw[i].y, reinterpret_cast<uint32_t(&)[4]>(w[16 * i + 4]));
-          decode8<BF16>(raw[i].z, reinterpret_cast<uint32_t(&)[4]>(w[16 * i + 8]));
-          decode8<BF16>(raw[i].w, reinterpret_cast<uint32_t(&)[4]>(w[16 * i + 12]));
+        for (int i = 0; i < HD / 16; ++i) {  // a word's eight codes are 16 bytes of the row
+          const uint32_t w = i % 4 == 0 ? raw[i / 4].x : i % 4 == 1 ? raw[i / 4].y : i % 4 == 2 ? raw[i / 4].z : raw[i / 4].w;
+          const int chunk = part * (HD / 16) + i;
+          uint32_t v[4];
+          decode8<BF16>(w, v);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + (chunk / 8) * (128 * 128) + (((chunk & 7) ^ (row & 7)) << 4)),
+                       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                       : "memory");
         }
-#pragma unroll
-        for (int i = 0; i < HD / 64; ++i)
-          tmem_st16(tmem + lanes + half * F::A_COLS + part * (HD / 4) + 16 * i, reinterpret_cast<uint32_t(&)[16]>(w[16 * i]));
-        tmem_wait_st();
-        tc_fence_before();
+        fence_async_proxy();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(W_A + half));
 #pragma unroll
@@ -307,54 +344,65 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
       const int key0 = slot - lane, before = k.length - k.count;
       float2 sum = {0.f, 0.f};
       for (int t = k.from; t < k.to; ++t, ++unit) {
-        const unsigned stage = unit % WM_STAGES, job = 2 * unit + half, buf = job % NB;
-        const int row0 = (k.row_tile + t) * WM_ROWS;
-        const int least = before + row0 / p.group + 1, most = before + min(k.count - 1, (row0 + WM_ROWS - 1) / p.group) + 1;
-        const bool masked = any_odd || key0 + 32 > least || (p.window > 0 && key0 < most - p.window);
-        wait(W_QFULL + stage, unit / WM_STAGES & 1);
-        wait(W_DFULL + 2 * half + (unit & 1), unit >> 1 & 1);
+        const unsigned stage = unit % WM_STAGES, buf = half * NB + unit % NB;
+        const int token0 = (k.row_tile + t) * tokens;
+        const int least = before + token0 + 1, most = before + min(k.count, token0 + tokens);
+        wait(W_STATS + stage, unit / WM_STAGES & 1);
+        wait(W_DFULL + buf, unit / NB & 1);
         __syncwarp();
         tc_fence_after();
-        const float *rows = reinterpret_cast<const float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS + part * 32;
-        const uint32_t d = tmem + lanes + F::D_AT + buf * F::D_COLS + part * 32;
+        const bool masked = any_odd || key0 + 32 > least || (p.window > 0 && key0 < most - p.window) || unlike[stage];
+        const float *rows = reinterpret_cast<const float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS + part * 64;
+        const uint32_t d = tmem + lanes + buf * F::D_COLS + part * 64;
+        // Sixteen rows at a time, the next ones' sums under way.  (Two forms: a branch between the rows would keep their
+        // operations apart)
+        const auto weigh = [&](auto some) {
+          uint32_t a[2][G][16];
 #pragma unroll
-        for (int r0 = 0; r0 < 32; r0 += 16) {
-          uint32_t a[G][16];
+          for (int g = 0; g < G; ++g) tmem_ld16(d + g * WM_ROWS, a[0][g]);
 #pragma unroll
-          for (int g = 0; g < G; ++g) tmem_ld16(d + g * WM_ROWS + r0, a[g]);
-          tmem_wait_ld();
+          for (int r0 = 0; r0 < 64; r0 += 16) {
+            tmem_wait_ld();
+            if (r0 + 16 < 64) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            float4 q[G];
-#pragma unroll
-            for (int g = 0; g < G; ++g) q[g] = *reinterpret_cast<const float4 *>(rows + g * WM_ROWS + r0 + i);
-            const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
-            float2 x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-              x0 = fma2(c[g], {q[g].x, q[g].y}, x0), x1 = fma2(c[g], {q[g].z, q[g].w}, x1);
+              for (int g = 0; g < G; ++g) tmem_ld16(d + g * WM_ROWS + r0 + 16, a[(r0 / 16 + 1) & 1][g]);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(W_DFREE + buf));
             }
+            const uint32_t(&x)[G][16] = a[r0 / 16 & 1];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-              x0 = fma2(s[g], {__uint_as_float(a[g][i]), __uint_as_float(a[g][i + 1])}, x0);
-              x1 = fma2(s[g], {__uint_as_float(a[g][i + 2]), __uint_as_float(a[g][i + 3])}, x1);
+            for (int i = 0; i < 16; i += 4) {
+              const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
+              float2 x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
+#pragma unroll
+              for (int g = 0; g < G; ++g) {
+                const float4 q = *reinterpret_cast<const float4 *>(rows + g * WM_ROWS + r0 + i);
+                x0 = fma2(c[g], {q.x, q.y}, x0), x1 = fma2(c[g], {q.z, q.w}, x1);
+              }
+#pragma unroll
+              for (int g = 0; g < G; ++g) {
+                x0 = fma2(s[g], {__uint_as_float(x[g][i]), __uint_as_float(x[g][i + 1])}, x0);
+                x1 = fma2(s[g], {__uint_as_float(x[g][i + 2]), __uint_as_float(x[g][i + 3])}, x1);
+              }
+              float2 w0 = {wm_ex2(x0.x), wm_ex2(x0.y)}, w1 = {wm_ex2(x1.x), wm_ex2(x1.y)};
+              if constexpr (decltype(some)::value) {
+                const int4 e = *reinterpret_cast<const int4 *>(rows + 3 * WM_ROWS + r0 + i);
+                const auto sees = [&](int end) { return slot < end && (p.window == 0 || slot >= end - p.window); };
+                w0 = {sees(e.x) ? w0.x : 0.f, sees(e.y) ? w0.y : 0.f};
+                w1 = {sees(e.z) ? w1.x : 0.f, sees(e.w) ? w1.y : 0.f};
+              }
+              sum = add2(sum, add2(w0, w1));
             }
-            float2 w0 = {wm_ex2(x0.x), wm_ex2(x0.y)}, w1 = {wm_ex2(x1.x), wm_ex2(x1.y)};
-            if (masked) {
-              const int4 e = *reinterpret_cast<const int4 *>(rows + 3 * WM_ROWS + r0 + i);
-              const auto sees = [&](int end) { return slot < end && (p.window == 0 || slot >= end - p.window); };
-              w0 = {sees(e.x) ? w0.x : 0.f, sees(e.y) ? w0.y : 0.f};
-              w1 = {sees(e.z) ? w1.x : 0.f, sees(e.w) ? w1.y : 0.f};
-            }
-            sum = add2(sum, add2(w0, w1));
           }
-        }
-        tc_fence_before();
+        };
+        if (masked)
+          weigh(std::true_type());
+        else
+          weigh(std::false_type());
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar(W_DFREE + buf));
-          mbar_arrive(bar(W_QFREE + stage));
-        }
+        if (lane == 0) mbar_arrive(bar(W_QFREE + stage));
       }
       // ---- the tile's end: both threads' sums, added to the mass or handed on
       const int pair = half * 4 + (warp & 3);
@@ -372,67 +420,112 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
         }
       }
       named_bar_sync(1 + pair, 64);  // (before the second sums are written again)
-      ++tiles;
       if (k.flat + k.to >= c1) break;
       next_keys(k, list, c1);
     }
-  } else if (c0 < c1 && warp < WM_MMA_WARP) {
-    // ---- queries: two warps for every other unit, a thread per row
-    const int mine = (warp - WM_SUMMERS) >> 1, r = (warp & 1) * 32 + lane;
+  } else if (c0 < c1 && warp == WM_COPY_WARP) {
+    // ---- queries: a box of the group's heads by the unit's tokens, 64 channels at a time; rows off 16 bytes by hand
     unsigned unit = 0;
     Keys k;
     find_keys(k, list, c0, c1);
     for (;;) {
       for (int t = k.from; t < k.to; ++t, ++unit) {
-        if ((int)(unit & 1) != mine) continue;
-        const int row = (k.row_tile + t) * WM_ROWS + r, token = row / p.group, head = k.head * p.group + row - token * p.group;
-        const bool there = row < k.count * p.group;
-        uint4 v[HD / 8] = {};
-        float lse = -INFINITY;
-        if (there) {
-          lse = p.lse[((int64_t)k.first + token) * p.n_heads + head];
-          const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q.row((int64_t)k.first + token, head));
-          if (p.q_wide) {
-#pragma unroll
-            for (int i = 0; i < HD / 8; ++i) v[i] = reinterpret_cast<const uint4 *>(src)[i];
-          } else {
-#pragma unroll
-            for (int i = 0; i < HD / 8; ++i) {
-              uint32_t *w = reinterpret_cast<uint32_t *>(&v[i]);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = src[8 * i + 2 * j] | ((uint32_t)src[8 * i + 2 * j + 1] << 16);
-            }
-          }
-        }
-        // (a row that saw nothing adds nothing, whatever it holds)
-        const bool counts = lse != -INFINITY;
-        float sums[2] = {};
-#pragma unroll
-        for (int i = 0; i < HD / 8; ++i) {
-          if (!counts) v[i] = make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-          float e[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            e[j] = BF16 ? bf16_lo(w[j]) + bf16_hi(w[j]) : f16_to_f32((uint16_t)w[j]) + f16_to_f32((uint16_t)(w[j] >> 16));
-          sums[i / 8] += e[0] + e[1] + (e[2] + e[3]);
-        }
         const unsigned stage = unit % WM_STAGES;
+        const int token0 = (k.row_tile + t) * tokens;
         wait(W_QFREE + stage, unit / WM_STAGES & 1 ^ 1);
         __syncwarp();
-        const uint32_t to = base + stage * F::STAGE + r * 128;
+        const uint32_t to = base + stage * F::STAGE;
+        if (use_map) {
+          if (elect_one()) {
+            mbar_arrive_expect_tx(bar(W_QFULL + stage), unit_rows * HD * 2);
 #pragma unroll
-        for (int i = 0; i < HD / 8; ++i)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (i / 8) * (WM_ROWS * 128) + (((i & 7) ^ (r & 7)) << 4)),
-                       "r"(v[i].x), "r"(v[i].y), "r"(v[i].z), "r"(v[i].w)
-                       : "memory");
-        float *rows = reinterpret_cast<float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS + r;
-        rows[0] = sums[0], rows[WM_ROWS] = sums[1];
-        rows[2 * WM_ROWS] = counts ? lse * -1.44269504089f : -INFINITY;
-        reinterpret_cast<int *>(rows)[3 * WM_ROWS] = counts ? k.length - k.count + token + 1 : -1;
-        fence_async_proxy();
+            for (int g = 0; g < G; ++g)
+              tma_load_3d(to + g * (WM_ROWS * 128), &q_map, 64 * g, k.head * group, k.first + token0, bar(W_QFULL + stage));
+          }
+          __syncwarp();
+        } else {
+          for (int r = 0; r < unit_rows; ++r) {
+            const int token = token0 + r / group;
+            uint32_t w[HD / 64] = {};
+            if (token < k.count) {
+              const uint16_t *e = reinterpret_cast<const uint16_t *>(p.q.row((int64_t)k.first + token, k.head * group + r % group));
+#pragma unroll
+              for (int j = 0; j < HD / 64; ++j) w[j] = e[64 * j + 2 * lane] | ((uint32_t)e[64 * j + 2 * lane + 1] << 16);
+            }
+#pragma unroll
+            for (int j = 0; j < HD / 64; ++j)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + j * (WM_ROWS * 128) + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4),
+                           "r"(w[j])
+                           : "memory");
+          }
+          fence_async_proxy();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(W_QFULL + stage));
+        }
+      }
+      if (k.flat + k.to >= c1) break;
+      next_keys(k, list, c1);
+    }
+  } else if (c0 < c1 && warp < WM_MMA_WARP) {
+    // ---- every other unit's rows: their sums over each group's channels, log-sum-exps, and the keys that they see.  A lane
+    // has the rows lane, lane + 32, ...: their tokens and heads are the same in every unit
+    const unsigned mine = warp - WM_STAT_WARP;
+    int row_token[4], row_head[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 32 * i + lane;
+      row_token[i] = r / group, row_head[i] = r % group;
+    }
+    unsigned unit = 0;
+    Keys k;
+    find_keys(k, list, c0, c1);
+    for (;;) {
+      for (int t = k.from; t < k.to; ++t, ++unit) {
+        if ((unit & 1) != mine) continue;
+        const unsigned stage = unit % WM_STAGES;
+        const int token0 = (k.row_tile + t) * tokens;
+        float lse[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = token0 + row_token[i];
+          lse[i] = -INFINITY;
+          if (32 * i + lane < unit_rows && token < k.count)
+            lse[i] = p.lse[((int64_t)k.first + token) * p.n_heads + k.head * group + row_head[i]];
+        }
+        wait(W_QFULL + stage, unit / WM_STAGES & 1);
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(W_QFULL + stage));
+        float *rows = reinterpret_cast<float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS;
+#pragma unroll 2
+        for (int m = 0; m < WM_ROWS / 16; ++m) {
+          const int r = 16 * m + (lane & 15);  // of this lane's address: matrices of rows 0-7, 8-15, then their next 8 channels
+          const uint32_t from = base + stage * F::STAGE + r * 128;
+          uint32_t a[G][4][4];  // (all under way before the first is waited for)
+#pragma unroll
+          for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ldmatrix_x4(a[g][i], from + g * (WM_ROWS * 128) + (((2 * i + (lane >> 4)) ^ (r & 7)) << 4));
+          float d[G][4] = {};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int g = 0; g < G; ++g) mma_ones<BF16>(d[g], a[g][i]);
+#pragma unroll
+          for (int g = 0; g < G; ++g)
+            if ((lane & 3) == 0) rows[g * WM_ROWS + 16 * m + (lane >> 2)] = d[g][0], rows[g * WM_ROWS + 16 * m + 8 + (lane >> 2)] = d[g][2];
+        }
+        bool other = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (a row that saw nothing adds nothing, whatever it holds; one behind the tokens is zero, or another's)
+          const bool counts = lse[i] != -INFINITY;
+          other = other || (!counts && 32 * i + lane < unit_rows);
+          rows[2 * WM_ROWS + 32 * i + lane] = counts ? lse[i] * -1.44269504089f : -INFINITY;
+          reinterpret_cast<int *>(rows)[3 * WM_ROWS + 32 * i + lane] = counts ? k.length - k.count + token0 + row_token[i] + 1 : -1;
+        }
+        other = __any_sync(0xffffffffu, other);
+        if (lane == 0) unlike[stage] = other;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(W_STATS + stage));
       }
       if (k.flat + k.to >= c1) break;
       next_keys(k, list, c1);
@@ -452,20 +545,20 @@ __global__ void __launch_bounds__(WM_THREADS, 1) kv4_weights_many_kernel(const W
         ok = wait(W_QFULL + stage, unit / WM_STAGES & 1);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const unsigned job = 2 * unit + half, buf = __shfl_sync(0xffffffffu, job % NB, 0);
+          const unsigned buf = __shfl_sync(0xffffffffu, half * NB + unit % NB, 0);
           if (t == 0) ok = ok && wait(W_A + half, tiles & 1);
-          ok = ok && wait(W_DFREE + buf, job / NB & 1 ^ 1);
+          ok = ok && wait(W_DFREE + buf, unit / NB & 1 ^ 1);
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           tc_fence_after();
-          const uint64_t q = sdesc_k_sw128(at + stage * F::STAGE);
-          const uint32_t d = tm + F::D_AT + buf * F::D_COLS, a = tm + half * F::A_COLS;
+          const uint64_t q = sdesc_k_sw128(at + stage * F::STAGE), a = sdesc_k_sw128(at + F::K_AT + half * F::HALF);
           if (elect_one()) {
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
               for (int i = 0; i < 4; ++i)  // (descriptors count 16 bytes)
-                mma_ts(d + g * WM_ROWS, a + g * 32 + i * 8, q + g * (WM_ROWS * 128 >> 4) + i * 2, idesc, i > 0);
-            mma_commit(bar(W_DFULL + 2 * half + (unit & 1)));
+                mma_bf16_ss(tm + buf * F::D_COLS + g * WM_ROWS, a + g * (128 * 128 >> 4) + i * 2, q + g * (WM_ROWS * 128 >> 4) + i * 2,
+                            idesc, i > 0);
+            mma_commit(bar(W_DFULL + buf));
             if (half == 1) mma_commit(bar(W_QFREE + stage));
           }
           __syncwarp();
@@ -518,10 +611,13 @@ template <int HD, bool BF16>
 cudaError_t launch(const WeightParams &p, int n_sm, cudaStream_t s) {
   static SmemOptIn opt_in;
   const void *kernel = reinterpret_cast<const void *>(&kv4_weights_many_kernel<HD, BF16>);
-  const int smem = Many<HD>::SMEM + 1024;
+  const int smem = Many<HD>::SMEM + 1024, tokens = WM_ROWS / p.group;
   const cudaError_t e = opt_in(kernel, smem);
   if (e != cudaSuccess) return e;
-  return launch_chained(kv4_weights_many_kernel<HD, BF16>, std::min(n_sm, FEW_BLOCKS), WM_THREADS, smem, s, p);
+  CUtensorMap map = {};
+  const int use_map = p.q_wide && encode_heads_map(&map, p.q.data, HD, p.n_heads, p.n_tokens, p.q.head_bytes, p.q.token_bytes,
+                                                   p.group, tokens) == 0;
+  return launch_chained(kv4_weights_many_kernel<HD, BF16>, std::min(n_sm, FEW_BLOCKS), WM_THREADS, smem, s, p, map, use_map, tokens);
 }
 
 }  // namespace

@@ -1105,6 +1105,21 @@ int encode_rows_map(CUtensorMap *map, const uint16_t *w, int K, int N, int box_r
              : -1;
 }
 
+int encode_heads_map(CUtensorMap *map, const void *base, int hd, int n_heads, int n_tokens, int64_t head_bytes,
+                     int64_t token_bytes, int box_heads, int box_tokens) {
+  auto fn = encode_fn();
+  if (!fn || head_bytes <= 0 || token_bytes <= 0 || (reinterpret_cast<uintptr_t>(base) & 15) != 0) return -1;
+  const cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)head_bytes, (cuuint64_t)token_bytes};
+  const cuuint32_t box[3] = {PG_K, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? 0
+             : -1;
+}
+
 // Weight tiles [n_rb][n_kt][RB][KT] bf16 as a 4-D tensor (column, row, K tile, row block):
 // boxes of 64 columns x RB rows x 1 K tile x box_rb row blocks; row blocks >= n_rb read as zero.
 int encode_tiles_map(CUtensorMap *map, const uint8_t *tiles, int n_kt, int n_rb, int box_rb) {

@@ -131,6 +131,10 @@ int encode_terms_map(CUtensorMap *map, const uint16_t *base, int K, int rows, in
 int encode_tiles_map(CUtensorMap *map, const uint8_t *tiles, int n_kt, int n_rb, int box_rb);
 // A row-major bf16 matrix [N][K] (K a multiple of 8, 16-byte aligned): boxes of 64 columns x box_rows rows.
 int encode_rows_map(CUtensorMap *map, const uint16_t *w, int K, int N, int box_rows);
+// Rows of heads [n_tokens][n_heads][hd] of a 16-bit type, rows and strides (in bytes) multiples of 16: boxes of 64
+// channels x box_heads x box_tokens; heads and tokens behind the last read as zero.
+int encode_heads_map(CUtensorMap *map, const void *base, int hd, int n_heads, int n_tokens, int64_t head_bytes,
+                     int64_t token_bytes, int box_heads, int box_tokens);
 // Opts a kernel in to its dynamic shared memory before a launch.  The attribute holds for the device it
 // was set on, so it is set once on each (a bit per device; beyond 64, at every launch); a failure is not
 // remembered.  One per kernel, shared by every thread.
