@@ -5,21 +5,23 @@
 // narrow down the K-th greatest key T, until a value's keys are all wanted; a last pass writes the slots with a key above T,
 // and the first ones with T itself, each to the place that a running count gives it.
 //
-// What bounds it.  4 bytes a row in and 4 bytes a kept row out; some 30 instructions a key, and a chain of ten barriers.  The
-// keys are read from memory once and stay in registers (a row longer than the registers of eight blocks: in shared memory, and
-// are read again behind it).  A long row, of which there are too few to fill the SMs, is shared by a cluster of up to
-// eight blocks, whose counts meet in distributed shared memory.
+// What bounds it.  4 bytes a row in and 4 bytes a kept row out; the instructions a key, and a chain of ten barriers.  The
+// keys are read from memory once and stay in shared memory, neighbours with one thread, so that a place in the output costs a
+// thread one sum over the block and not a vote a key (128 instructions a key with the votes).  (A row longer than the shared
+// memory of eight blocks is read again in each pass.)  A long row, of which there are too few to fill the SMs, is shared by a
+// cluster of up to eight blocks, whose counts meet in distributed shared memory.
 #include <algorithm>
+#include <type_traits>
 
+#include "attn_core.cuh"  // cp_async16
 #include "kv4_weights.cuh"
 #include "prefill.cuh"
 
 namespace kfl {
 namespace {
 
-constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_BINS = 2048;
-constexpr int SEL_ROOM = 40960;  // keys of a block in shared memory at most; more are read again
+constexpr int SEL_BYTES = 192 << 10;  // of keys in a block's shared memory
 constexpr int SEL_USERS = 1024;
 
 struct SelectParams {
@@ -29,62 +31,70 @@ struct SelectParams {
   const int32_t *users;
   int n, budget, first, recent;
   int32_t *rows, *counts, *status;
-  int room, cluster;  // keys in shared memory (PER 0), blocks of a row
-  int64_t items;      // layers * n * heads
+  int cluster;    // blocks of a row
+  int room;       // keys of a thread that fit shared memory
+  int wide;       // rows of masses start on 16 bytes
+  int64_t items;  // layers * n * heads
 };
 
-// Keys order as the masses do (NaN above all, both zeros alike).
+// Keys order as the masses do.  The sum makes both zeros one, and of every NaN the positive one, above all numbers.  No
+// mass has a key below 2^22.
 __device__ __forceinline__ uint32_t mass_key(float v) {
-  if (v != v) return 0xffffffffu;
   const uint32_t b = __float_as_uint(v + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
-
 __device__ __forceinline__ uint4 ld_cluster4(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
 
-// Exclusive sum over the block of one value per thread; total: the sum.
-__device__ __forceinline__ int scan_block(int v, int &total, int *sums) {
+// One more in a count of shared memory, if so (predicated: a branch a key costs more).
+__device__ __forceinline__ void count_if(uint32_t at, bool so) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p red.shared.add.u32 [%0], 1;\n\t}" ::"r"(at), "r"((uint32_t)so) : "memory");
+}
+
+// Sum of one value per thread over the threads before this one; total: over the block.
+template <int WARPS>
+__device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t &total, uint32_t *sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int s = v;
+  uint32_t s = v;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const int o = __shfl_up_sync(0xffffffffu, s, off);
+    const uint32_t o = __shfl_up_sync(0xffffffffu, s, off);
     if (lane >= off) s += o;
   }
   if (lane == 31) sums[warp] = s;
   __syncthreads();
-  int w = lane < SEL_WARPS ? sums[lane] : 0;
-#pragma unroll
-  for (int off = 1; off < SEL_WARPS; off <<= 1) {
-    const int o = __shfl_up_sync(0xffffffffu, w, off);
-    if (lane >= off) w += o;
-  }
-  total = __shfl_sync(0xffffffffu, w, SEL_WARPS - 1);
-  const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-  return s - v + (warp ? before : 0);
+  const uint32_t w = lane < WARPS ? sums[lane] : 0;
+  total = __reduce_add_sync(0xffffffffu, w);
+  return s - v + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 }
 
-// PER: keys of a thread, in registers; 0: any number, in shared memory and behind it.
-template <int PER>
-__global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(const SelectParams p) {
-  extern __shared__ uint32_t keys[];  // [room]
+// A thread's keys: an odd multiple of four, so that the threads of a warp read theirs from different banks.
+__host__ __device__ inline int64_t keys_per_thread(int64_t n, int64_t threads) { return ((n + threads - 1) / threads + 3) / 4 * 4 | 4; }
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_kernel(const SelectParams p) {
+  extern __shared__ __align__(16) uint32_t keys[];  // [thread][per]
+  constexpr int WARPS = THREADS / 32, BINS = SEL_BINS / THREADS;
   __shared__ alignas(16) uint32_t hist[2][SEL_BINS];  // by turns: the last pass's counts are read while the next one's are made
-  __shared__ int sums[SEL_WARPS], above[SEL_WARPS], ties[SEL_WARPS];
-  __shared__ int found[3];   // the bin, how many of it are wanted, how many there are
-  __shared__ int totals[2];  // of this block: above the threshold, at it
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ uint32_t sums[2][WARPS];
+  __shared__ int found[3];        // the bin, how many of it are wanted, how many there are
+  __shared__ uint32_t totals[2];  // of this block: above the threshold, at it
+  const int tid = threadIdx.x;
   const int rank = p.cluster > 1 ? (int)cluster_ctarank() : 0, C = p.cluster;
   const int heads = p.pool.n_kv_heads;
-  *reinterpret_cast<uint4 *>(&hist[0][4 * tid]) = *reinterpret_cast<uint4 *>(&hist[1][4 * tid]) = make_uint4(0, 0, 0, 0);
+  const auto clear = [&](uint32_t *counts) {
+#pragma unroll
+    for (int j = 0; j < BINS; j += 4) *reinterpret_cast<uint4 *>(&counts[BINS * tid + j]) = make_uint4(0, 0, 0, 0);
+  };
+  clear(hist[0]), clear(hist[1]);
   pdl_launch_dependents();
   pdl_wait();
   const auto sync = [&]() {
@@ -105,132 +115,166 @@ __global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(const SelectPar
       if (!known) report(p.status, KFL_BAD_USER);
     }
     if (length <= p.budget) {  // (the whole cluster alike)
-      for (int j = rank * SEL_THREADS + tid; j < p.budget; j += C * SEL_THREADS) out[j] = j < length ? j : -1;
+      for (int j = rank * THREADS + tid; j < p.budget; j += C * THREADS) out[j] = j < length ? j : -1;
       continue;
     }
-    const int m = length - p.first - p.recent, K = p.budget - p.first - p.recent;
-    // ---- this block's slice of the m rows between, a run of whole 32s for each warp
-    const float *mass = p.mass.row(layer, user, head) + p.first;
-    const int seg = ((m + C * SEL_WARPS - 1) / (C * SEL_WARPS) + 31) / 32 * 32;
-    const int w0 = (int)min(((int64_t)rank * SEL_WARPS + warp) * seg, (int64_t)m), w1 = min(w0 + seg, m);
-    uint32_t mine[PER > 0 ? PER : 1];
-    const int begin = (int)min((int64_t)rank * SEL_WARPS * seg, (int64_t)m);
-    const auto stored = [&](int j) { return j - begin < p.room ? keys[j - begin] : mass_key(mass[j]); };
-    // every key of this thread: f(slot less `first`, key, whether there is one)
-    const auto each = [&](auto f) {
-      if constexpr (PER > 0) {
+    const int stop = length - p.recent, K = p.budget - p.first - p.recent;
+    // ---- this thread's slots, of those from `first` (rounded down to four) to `stop`: `per` neighbours
+    const float *mass = p.mass.row(layer, user, head);
+    const int first4 = p.first & ~3;
+    const int per = (int)keys_per_thread(stop - first4, C * THREADS);
+    const int s0 = (int)min((int64_t)first4 + ((int64_t)rank * THREADS + tid) * per, (int64_t)stop);
+    const bool stays = per <= p.room;
+    const bool inner = s0 >= p.first && s0 + per <= stop;  // all of them are in question
+    const auto key_of = [&](int s, float v) { return inner || (s >= p.first && s < stop) ? mass_key(v) : 0u; };
+    if (stays && K > 0) {  // the masses as they are, a warp's together, its lanes side by side
+      const int lane = tid & 31, sw = (int)min((int64_t)first4 + ((int64_t)rank * THREADS + tid - lane) * per, (int64_t)stop);
+      float *to = reinterpret_cast<float *>(keys) + (tid - lane) * per;
+      for (int o = 4 * lane; o < 32 * per; o += 128) {
+        if (p.wide) {  // (a row's slots are a multiple of 16: what is read behind `stop` is there)
+          if (sw + o < stop) cp_async16(to + o, mass + sw + o);
+        } else {
 #pragma unroll
-        for (int k = 0; k < PER; ++k)
-          if (32 * k < seg) f(w0 + 32 * k + lane, mine[k], w0 + 32 * k + lane < w1);
+          for (int j = 0; j < 4; ++j)
+            if (sw + o + j < stop) to[o + j] = mass[sw + o + j];
+        }
+      }
+      cp_async_commit();
+    }
+    // every key of this thread: f(slot, key); the first time they are made
+    const auto each = [&](auto f, auto made) {
+      if (stays) {
+#pragma unroll 4
+        for (int q = 0; q < per; q += 4) {
+          uint4 *at = reinterpret_cast<uint4 *>(keys + tid * per + q);
+          uint4 k = *at;
+          if constexpr (!decltype(made)::value) {
+            k = {key_of(s0 + q, __uint_as_float(k.x)), key_of(s0 + q + 1, __uint_as_float(k.y)),
+                 key_of(s0 + q + 2, __uint_as_float(k.z)), key_of(s0 + q + 3, __uint_as_float(k.w))};
+            *at = k;
+          }
+          f(s0 + q, k.x), f(s0 + q + 1, k.y), f(s0 + q + 2, k.z), f(s0 + q + 3, k.w);
+        }
       } else {
-        for (int j0 = w0; j0 < w1; j0 += 32) f(j0 + lane, j0 + lane < w1 ? stored(j0 + lane) : 0u, j0 + lane < w1);
+#pragma unroll 4
+        for (int q = 0; q < per; ++q) f(s0 + q, s0 + q < stop ? key_of(s0 + q, mass[s0 + q]) : 0u);
       }
     };
-    if (K > 0) {
-      if constexpr (PER > 0) {
-        float v[PER];
-#pragma unroll
-        for (int k = 0; k < PER; ++k) v[k] = w0 + 32 * k + lane < w1 ? mass[w0 + 32 * k + lane] : 0.f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) mine[k] = mass_key(v[k]);
-      } else {
-#pragma unroll 8
-        for (int j = w0 + lane; j < min(w1, begin + p.room); j += 32) keys[j - begin] = mass_key(mass[j]);
-        __syncwarp();
-      }
-    }
-    for (int j = rank * SEL_THREADS + tid; j < p.first + p.recent; j += C * SEL_THREADS)
-      out[j < p.first ? j : K + j] = j < p.first ? j : m + j;
+    const std::true_type made;
+    for (int j = rank * THREADS + tid; j < p.first + p.recent; j += C * THREADS)
+      out[j < p.first ? j : K + j] = j < p.first ? j : length - p.first - p.recent + j;
     if (K == 0) continue;
     uint32_t T = 0;
     int want = K;
     bool all = false;  // of the last bin
-    __syncthreads();   // (the counts are zero)
-#pragma unroll 1
-    for (int pass = 0; pass < 3 && !all; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      uint32_t *counts = hist[pass & 1];
-      each([&](int, uint32_t k, bool is) {
-        if (is && (pass == 0 || k >> (shift + bits) == T >> (shift + bits))) atomicAdd(&counts[k >> shift & ((1u << bits) - 1)], 1u);
-      });
+    cp_async_wait<0>();
+    __syncthreads();  // (and the counts are zero)
+    const auto narrow = [&](auto which) {
+      constexpr int PASS = decltype(which)::value, SHIFT = PASS == 0 ? 21 : PASS == 1 ? 10 : 0;
+      uint32_t *counts = hist[PASS & 1];
+      const uint32_t base = smem_addr(counts);
+      // (keys of no slot, 0, fall into the first bin, which is never the one)
+      each(
+          [&](int, uint32_t k) {
+            const uint32_t x = k ^ T;  // (T: the bits so far)
+            count_if(base + (x >> SHIFT) * 4, PASS == 0 || x >> (SHIFT + (PASS == 1 ? 11 : 10)) == 0);
+          },
+          std::integral_constant<bool, (PASS > 0)>());
       sync();
-      // four bins a thread, of all blocks; the one in which the `want`-th greatest lies
-      const uint32_t at = smem_addr(&counts[4 * tid]);
-      uint4 b = *reinterpret_cast<const uint4 *>(&counts[4 * tid]);
-      for (int r = 1; r < C; ++r) {
-        const uint4 o = ld_cluster4(map_to_rank(at, (rank + r) & (C - 1)));
-        b.x += o.x, b.y += o.y, b.z += o.z, b.w += o.w;
-      }
-      int total;
-      const int own = b.x + b.y + b.z + b.w, before = scan_block(own, total, sums);
-      int greater = total - before - own;
-      if (greater < want && greater + own >= want) {
-        const int four[4] = {(int)b.x, (int)b.y, (int)b.z, (int)b.w};
+      // a run of bins a thread, of all blocks; the one in which the `want`-th greatest lies
+      uint4 b[BINS / 4];
 #pragma unroll
-        for (int j = 3; j >= 0; --j) {
-          if (greater < want && greater + four[j] >= want) found[0] = 4 * tid + j, found[1] = want - greater, found[2] = four[j];
-          greater += four[j];
+      for (int j = 0; j < BINS / 4; ++j) b[j] = *reinterpret_cast<const uint4 *>(&counts[BINS * tid + 4 * j]);
+      if constexpr (THREADS == 512) {  // (clusters: all blocks' counts under way together)
+        if (C > 1) {
+          uint4 o[7];
+#pragma unroll
+          for (int r = 1; r < 8; ++r)
+            if (r < C) o[r - 1] = ld_cluster4(map_to_rank(base + BINS * tid * 4, (rank + r) & (C - 1)));
+#pragma unroll
+          for (int r = 1; r < 8; ++r)
+            if (r < C) b[0].x += o[r - 1].x, b[0].y += o[r - 1].y, b[0].z += o[r - 1].z, b[0].w += o[r - 1].w;
         }
       }
-      // the other counts are free: every block has been here since it read them (zero again for the next pass, or row)
-      *reinterpret_cast<uint4 *>(&hist[(pass & 1) ^ 1][4 * tid]) = make_uint4(0, 0, 0, 0);
+      uint32_t own = 0, total;
+#pragma unroll
+      for (int j = 0; j < BINS / 4; ++j) own += b[j].x + b[j].y + (b[j].z + b[j].w);
+      const uint32_t before = scan_block<WARPS>(own, total, sums[0]);
+      int greater = (int)(total - before - own);
+      if (greater < want && greater + (int)own >= want) {
+#pragma unroll
+        for (int j = BINS - 1; j >= 0; --j) {
+          const int here = j % 4 == 3 ? b[j / 4].w : j % 4 == 2 ? b[j / 4].z : j % 4 == 1 ? b[j / 4].y : b[j / 4].x;
+          if (greater < want && greater + here >= want) found[0] = BINS * tid + j, found[1] = want - greater, found[2] = here;
+          greater += here;
+        }
+      }
+      // the other counts are free: every block has been here since it read them (zero again for the next pass)
+      clear(hist[(PASS & 1) ^ 1]);
       __syncthreads();
-      T |= (uint32_t)found[0] << shift;
+      T |= (uint32_t)found[0] << SHIFT;
       want = found[1];
       all = want == found[2];
-    }
+    };
+    narrow(std::integral_constant<int, 0>());
+    if (!all) narrow(std::integral_constant<int, 1>());
+    if (!all) narrow(std::integral_constant<int, 2>());
     // (all of the last bin: its keys are those from T on, whatever their other bits)
-    if (all && T > 0) --T, want = 0;
-    // ---- how many of each warp's run are above T, and at it
-    int g = 0, t = 0;
-    each([&](int, uint32_t k, bool is) { g += is && k > T, t += is && k == T; });
-    g = __reduce_add_sync(0xffffffffu, g), t = __reduce_add_sync(0xffffffffu, t);
-    if (lane == 0) above[warp] = g, ties[warp] = t;
-    __syncthreads();
-    if (C > 1 && warp == 0) {
-      const int a = __reduce_add_sync(0xffffffffu, lane < SEL_WARPS ? above[lane] : 0);
-      const int b = __reduce_add_sync(0xffffffffu, lane < SEL_WARPS ? ties[lane] : 0);
-      if (lane == 0) totals[0] = a, totals[1] = b;
+    if (all) --T, want = 0;
+    // ---- each thread's places: how many before it are above T, and at it
+    uint32_t g = 0, t = 0, g0, t0 = 0, all_g, all_t = 0;
+    each([&](int, uint32_t k) { g += k > T; }, made);
+    if (want > 0) each([&](int, uint32_t k) { t += k == T; }, made);
+    g0 = scan_block<WARPS>(g, all_g, sums[1]);
+    if (want > 0) t0 = scan_block<WARPS>(t, all_t, sums[0]);
+    if (C > 1) {
+      if (tid == 0) totals[0] = all_g, totals[1] = all_t;
+      cluster_sync_all();
+      const int lane = tid & 31;
+      const uint32_t a = lane < rank ? ld_cluster(map_to_rank(smem_addr(&totals[0]), lane)) : 0;
+      const uint32_t b = lane < rank ? ld_cluster(map_to_rank(smem_addr(&totals[1]), lane)) : 0;
+      g0 += __reduce_add_sync(0xffffffffu, a), t0 += __reduce_add_sync(0xffffffffu, b);
     }
-    int g0 = lane < warp ? above[lane] : 0, t0 = lane < warp ? ties[lane] : 0;
-    sync();
-    if (C > 1 && lane < rank) {
-      g0 += ld_cluster(map_to_rank(smem_addr(&totals[0]), lane));
-      t0 += ld_cluster(map_to_rank(smem_addr(&totals[1]), lane));
+    // ---- the slots: those above T, and of those at it the first `want`
+    const uint32_t most = want;
+    int32_t *to = out + p.first + g0 + min(t0, most);
+    if (want == 0) {
+      each(
+          [&](int s, uint32_t k) {
+            if (k > T) *to++ = s;
+          },
+          made);
+    } else {
+      uint32_t left = t0 < most ? most - t0 : 0;  // ties that are still wanted
+      each(
+          [&](int s, uint32_t k) {
+            const bool tie = k == T && left > 0;
+            if (k > T || tie) *to++ = s;
+            left -= tie;
+          },
+          made);
     }
-    g0 = __reduce_add_sync(0xffffffffu, g0), t0 = __reduce_add_sync(0xffffffffu, t0);
-    // ---- the slots, each at its place
-    each([&](int j, uint32_t k, bool is) {
-      const unsigned over = __ballot_sync(0xffffffffu, is && k > T), at = __ballot_sync(0xffffffffu, is && k == T);
-      const unsigned below = (1u << lane) - 1;
-      const int tie = t0 + __popc(at & below);
-      if ((over >> lane & 1) || ((at >> lane & 1) && tie < want)) out[p.first + g0 + __popc(over & below) + min(tie, want)] = p.first + j;
-      g0 += __popc(over), t0 += __popc(at);
-    });
-    // the counts of the last pass, too, for the next row (the others have read them, and the totals)
+    // (the others have read this block's counts and totals)
     sync();
-    *reinterpret_cast<uint4 *>(&hist[0][4 * tid]) = *reinterpret_cast<uint4 *>(&hist[1][4 * tid]) = make_uint4(0, 0, 0, 0);
+    clear(hist[0]), clear(hist[1]);
   }
 }
 
-template <int PER>
-cudaError_t launch(const SelectParams &p, cudaStream_t s) {
-  const size_t smem = PER > 0 ? 0 : (size_t)p.room * 4;
-  if (PER == 0) {
-    static SmemOptIn opt_in;
-    const cudaError_t e = opt_in(reinterpret_cast<const void *>(&kv4_select_kernel<PER>), SEL_ROOM * 4);
-    if (e != cudaSuccess) return e;
-  }
+template <int THREADS>
+cudaError_t launch(SelectParams p, int64_t most, cudaStream_t s) {
+  static SmemOptIn opt_in;
+  const cudaError_t e = opt_in(reinterpret_cast<const void *>(&kv4_select_kernel<THREADS>), SEL_BYTES);
+  if (e != cudaSuccess) return e;
+  p.room = (int)std::min<int64_t>(keys_per_thread(most, THREADS * p.cluster), SEL_BYTES / (4 * THREADS));
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = p.cluster, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(std::min<int64_t>(p.items, 1 << 20) * p.cluster)), cfg.blockDim = dim3(SEL_THREADS);
-  cfg.dynamicSmemBytes = smem, cfg.stream = s;
-  cfg.attrs = attr, cfg.numAttrs = p.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kv4_select_kernel<PER>, p);
+  cfg.gridDim = dim3((unsigned)(std::min<int64_t>(p.items, 1 << 20) * p.cluster)), cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = (size_t)p.room * THREADS * 4, cfg.stream = s, cfg.attrs = attr, cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kv4_select_kernel<THREADS>, p);
 }
 
 }  // namespace
@@ -260,14 +304,14 @@ extern "C" int kfl_kv4_select(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.users = users, p.n = n, p.budget = budget, p.first = first, p.recent = recent;
   p.rows = rows, p.counts = counts, p.status = status;
   p.items = (int64_t)pool->n_layers * n * pool->n_kv_heads;
-  // blocks of a row: as many as leave a thread no more than 8 keys, while the rows do not fill the SMs twice; else as few
-  // as hold the keys in registers, 32 a thread at most
-  const int64_t most = std::max<int64_t>((int64_t)map->max_pages * pool->page_tokens - first - recent, 1);
-  const auto per_thread = [&]() { return (most + (int64_t)p.cluster * SEL_THREADS - 1) / (p.cluster * SEL_THREADS); };
+  p.wide = ((reinterpret_cast<uintptr_t>(mass->data) | (uintptr_t)(4 * (mass->layer_stride | mass->user_stride | mass->head_stride))) & 15) == 0;
+  // Many rows: a block of 256 threads each, as long as six of them fit an SM (a table is often a page longer than a round number
+  // of rows).  Few, or longer ones: blocks of 512 threads, as many of them as leave a thread 12 keys, or their shared memory
+  const int64_t most = (int64_t)map->max_pages * pool->page_tokens;
+  const auto per = [&](int threads) { return keys_per_thread(most, (int64_t)p.cluster * threads); };
   p.cluster = 1;
-  while (p.cluster < 8 && per_thread() > (p.items * p.cluster < 2 * 152 ? 8 : 32)) p.cluster *= 2;
-  const int64_t per = per_thread();
-  p.room = SEL_ROOM;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return cuda_result(per <= 8 ? launch<8>(p, s) : per <= 16 ? launch<16>(p, s) : per <= 32 ? launch<32>(p, s) : launch<0>(p, s), me);
+  if (p.items >= 2 * 152 && per(256) <= 36) return cuda_result(launch<256>(p, most, s), me);
+  while (p.cluster < 8 && per(512) > (p.items * p.cluster < 2 * 152 ? 12 : SEL_BYTES / (4 * 512))) p.cluster *= 2;
+  return cuda_result(launch<512>(p, most, s), me);
 }

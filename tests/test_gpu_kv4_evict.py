@@ -229,7 +229,7 @@ def check_select(lengths, budget, first, recent, page=64, layers=1, heads=1, kin
     elif kind == "equal":
         mass[:] = 0.25
     elif kind == "odd":
-        mass = rng.choice(np.array([0.0, -0.0, np.inf, -np.inf, np.nan, 1.0, -1.0, 1e-42, -1e-42, 3.4e38], dtype=np.float32), shape)
+        mass = rng.choice(np.array([0.0, -0.0, np.inf, -np.inf, np.nan, -np.nan, 1.0, -1.0, 1e-42, -1e-42, 3.4e38], dtype=np.float32), shape)
     t = torch.from_numpy(mass).cuda()
     if strided:
         t = torch.zeros(shape[1], shape[0], shape[2], shape[3] + 5, device="cuda")[..., 3:-2].transpose(0, 1).copy_(t)
