@@ -34,7 +34,7 @@ struct SelectParams {
   int cluster;    // blocks of a row
   int room;       // keys of a thread that fit shared memory
   int wide;       // rows of masses start on 16 bytes
-  int64_t items;  // layers * n * heads
+  int log2_cluster;
 };
 
 // Keys order as the masses do.  The sum makes both zeros one, and of every NaN the positive one, above all numbers.  No
@@ -76,13 +76,16 @@ __device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t &total, uint
   return s - v + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 }
 
-// A thread's keys: an odd multiple of four, so that the threads of a warp read theirs from different banks.
-__host__ __device__ inline int64_t keys_per_thread(int64_t n, int64_t threads) { return ((n + threads - 1) / threads + 3) / 4 * 4 | 4; }
+// A thread's keys of n (at most 2^26) for 2^log2_threads: an odd multiple of four, so that the threads of a warp read theirs
+// from different banks.
+__host__ __device__ inline int keys_per_thread(int n, int log2_threads) {
+  return ((((n - 1) >> log2_threads) + 4) & ~3) | 4;
+}
 
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_kernel(const SelectParams p) {
   extern __shared__ __align__(16) uint32_t keys[];  // [thread][per]
-  constexpr int WARPS = THREADS / 32, BINS = SEL_BINS / THREADS;
+  constexpr int WARPS = THREADS / 32, BINS = SEL_BINS / THREADS, LOG2 = THREADS == 256 ? 8 : 9;
   __shared__ alignas(16) uint32_t hist[2][SEL_BINS];  // by turns: the last pass's counts are read while the next one's are made
   __shared__ uint32_t sums[2][WARPS];
   __shared__ int found[3];        // the bin, how many of it are wanted, how many there are
@@ -103,13 +106,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
     else
       __syncthreads();
   };
-  for (int64_t item = blockIdx.x / C; item < p.items; item += gridDim.x / C) {
-    const int64_t row_of = item / heads;
-    const int head = (int)(item - row_of * heads), layer = (int)(row_of / p.n), i = (int)(row_of - (int64_t)layer * p.n);
-    const int user = p.users[i];
+  const unsigned in_layer = blockIdx.x >> p.log2_cluster;  // (user of the list, head)
+  const int i = in_layer / heads, head = in_layer - i * heads;
+  const int user = p.users[i];
+  for (int layer = blockIdx.y; layer < p.pool.n_layers; layer += gridDim.y) {
     const bool known = user >= 0 && user < p.map.n_users;
     const int length = known ? min(max(0, p.map.lengths[user]), p.map.max_pages << p.pool.log2_tokens) : 0;
-    int32_t *out = p.rows + item * p.budget;
+    int32_t *out = p.rows + (((int64_t)layer * p.n + i) * heads + head) * p.budget;
     if (layer == 0 && head == 0 && rank == 0 && tid == 0) {
       p.counts[i] = min(length, p.budget);
       if (!known) report(p.status, KFL_BAD_USER);
@@ -122,13 +125,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
     // ---- this thread's slots, of those from `first` (rounded down to four) to `stop`: `per` neighbours
     const float *mass = p.mass.row(layer, user, head);
     const int first4 = p.first & ~3;
-    const int per = (int)keys_per_thread(stop - first4, C * THREADS);
-    const int s0 = (int)min((int64_t)first4 + ((int64_t)rank * THREADS + tid) * per, (int64_t)stop);
+    const int per = keys_per_thread(stop - first4, LOG2 + p.log2_cluster);
+    const int s0 = min(first4 + (rank * THREADS + tid) * per, stop);  // (below 2^27)
     const bool stays = per <= p.room;
-    const bool inner = s0 >= p.first && s0 + per <= stop;  // all of them are in question
-    const auto key_of = [&](int s, float v) { return inner || (s >= p.first && s < stop) ? mass_key(v) : 0u; };
+    const bool inner = __all_sync(0xffffffffu, s0 >= p.first && s0 + per <= stop);  // all of this warp's are in question
+    const auto key_of = [&](int s, float v) { return s >= p.first && s < stop ? mass_key(v) : 0u; };
     if (stays && K > 0) {  // the masses as they are, a warp's together, its lanes side by side
-      const int lane = tid & 31, sw = (int)min((int64_t)first4 + ((int64_t)rank * THREADS + tid - lane) * per, (int64_t)stop);
+      const int lane = tid & 31, sw = min(first4 + (rank * THREADS + tid - lane) * per, stop);
       float *to = reinterpret_cast<float *>(keys) + (tid - lane) * per;
       for (int o = 4 * lane; o < 32 * per; o += 128) {
         if (p.wide) {  // (a row's slots are a multiple of 16: what is read behind `stop` is there)
@@ -149,8 +152,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
           uint4 *at = reinterpret_cast<uint4 *>(keys + tid * per + q);
           uint4 k = *at;
           if constexpr (!decltype(made)::value) {
-            k = {key_of(s0 + q, __uint_as_float(k.x)), key_of(s0 + q + 1, __uint_as_float(k.y)),
-                 key_of(s0 + q + 2, __uint_as_float(k.z)), key_of(s0 + q + 3, __uint_as_float(k.w))};
+            if (inner)
+              k = {mass_key(__uint_as_float(k.x)), mass_key(__uint_as_float(k.y)), mass_key(__uint_as_float(k.z)),
+                   mass_key(__uint_as_float(k.w))};
+            else
+              k = {key_of(s0 + q, __uint_as_float(k.x)), key_of(s0 + q + 1, __uint_as_float(k.y)),
+                   key_of(s0 + q + 2, __uint_as_float(k.z)), key_of(s0 + q + 3, __uint_as_float(k.w))};
             *at = k;
           }
           f(s0 + q, k.x), f(s0 + q + 1, k.y), f(s0 + q + 2, k.z), f(s0 + q + 3, k.w);
@@ -177,7 +184,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
       each(
           [&](int, uint32_t k) {
             const uint32_t x = k ^ T;  // (T: the bits so far)
-            count_if(base + (x >> SHIFT) * 4, PASS == 0 || x >> (SHIFT + (PASS == 1 ? 11 : 10)) == 0);
+            if constexpr (PASS == 0)
+              asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(base + (x >> SHIFT) * 4) : "memory");
+            else
+              count_if(base + (x >> SHIFT) * 4, x < 1u << (SHIFT + (PASS == 1 ? 11 : 10)));
           },
           std::integral_constant<bool, (PASS > 0)>());
       sync();
@@ -261,18 +271,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
 }
 
 template <int THREADS>
-cudaError_t launch(SelectParams p, int64_t most, cudaStream_t s) {
+cudaError_t launch(SelectParams p, int most, cudaStream_t s) {
   static SmemOptIn opt_in;
   const cudaError_t e = opt_in(reinterpret_cast<const void *>(&kv4_select_kernel<THREADS>), SEL_BYTES);
   if (e != cudaSuccess) return e;
-  p.room = (int)std::min<int64_t>(keys_per_thread(most, THREADS * p.cluster), SEL_BYTES / (4 * THREADS));
+  p.room = std::min(keys_per_thread(most, (THREADS == 256 ? 8 : 9) + p.log2_cluster), SEL_BYTES / (4 * THREADS));
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = p.cluster, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(std::min<int64_t>(p.items, 1 << 20) * p.cluster)), cfg.blockDim = dim3(THREADS);
+  cfg.gridDim = dim3(p.n * p.pool.n_kv_heads * p.cluster, std::min(p.pool.n_layers, 65535)), cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = (size_t)p.room * THREADS * 4, cfg.stream = s, cfg.attrs = attr, cfg.numAttrs = p.cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kv4_select_kernel<THREADS>, p);
 }
@@ -303,15 +313,15 @@ extern "C" int kfl_kv4_select(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.pool = pool_of(*pool), p.map = map_of(*map), p.mass = view_of(*mass);
   p.users = users, p.n = n, p.budget = budget, p.first = first, p.recent = recent;
   p.rows = rows, p.counts = counts, p.status = status;
-  p.items = (int64_t)pool->n_layers * n * pool->n_kv_heads;
   p.wide = ((reinterpret_cast<uintptr_t>(mass->data) | (uintptr_t)(4 * (mass->layer_stride | mass->user_stride | mass->head_stride))) & 15) == 0;
   // Many rows: a block of 256 threads each, as long as six of them fit an SM (a table is often a page longer than a round number
   // of rows).  Few, or longer ones: blocks of 512 threads, as many of them as leave a thread 12 keys, or their shared memory
-  const int64_t most = (int64_t)map->max_pages * pool->page_tokens;
-  const auto per = [&](int threads) { return keys_per_thread(most, (int64_t)p.cluster * threads); };
+  const int most = map->max_pages * pool->page_tokens;
+  const int64_t items = (int64_t)pool->n_layers * n * pool->n_kv_heads;
   p.cluster = 1;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (p.items >= 2 * 152 && per(256) <= 36) return cuda_result(launch<256>(p, most, s), me);
-  while (p.cluster < 8 && per(512) > (p.items * p.cluster < 2 * 152 ? 12 : SEL_BYTES / (4 * 512))) p.cluster *= 2;
+  if (items >= 2 * 152 && keys_per_thread(most, 8) <= 36) return cuda_result(launch<256>(p, most, s), me);
+  while (p.cluster < 8 && keys_per_thread(most, 9 + p.log2_cluster) > (items * p.cluster < 2 * 152 ? 12 : SEL_BYTES / (4 * 512)))
+    p.cluster *= 2, ++p.log2_cluster;
   return cuda_result(launch<512>(p, most, s), me);
 }
