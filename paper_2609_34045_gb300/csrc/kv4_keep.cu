@@ -51,15 +51,16 @@ __device__ __forceinline__ Cut cut_of(const KeepParams &p, int i) {
 
 __global__ void __launch_bounds__(KEEP_PLAN) kv4_keep_plan_kernel(const KeepParams p) {
   __shared__ int user[KEEP_MOST], news[KEEP_MOST], at[KEEP_MOST];
+  __shared__ int3 pages[KEEP_MOST];  // (begin, need, held)
   __shared__ int sums[32];
   pdl_launch_dependents();
   pdl_wait();
   const int i = threadIdx.x, warp = i >> 5, lane = i & 31;
-  if (i < p.n) user[i] = p.users[i];
+  Cut c = {};
+  if (i < p.n) c = cut_of(p, i), user[i] = c.user;
   __syncthreads();
   // ---- which users change at all
   if (i < p.n) {
-    const Cut c = cut_of(p, i);
     bool again = false;
     for (int j = 0; j < i; ++j) again |= user[j] == c.user;
     int bad = 0;
@@ -69,21 +70,23 @@ __global__ void __launch_bounds__(KEEP_PLAN) kv4_keep_plan_kernel(const KeepPara
       bad = KFL_BAD_POSITION;
     if (bad) report(p.status, bad);
     news[i] = bad || c.first + c.count == c.length ? -1 : 0;
+    pages[i] = make_int3(c.begin, c.need, c.held);
   }
   __syncthreads();
   // ---- the pages that rows move into and others hold too, a warp per user
   for (int k = warp; k < p.n; k += KEEP_PLAN / 32) {
     if (news[k] < 0) continue;
-    const Cut c = cut_of(p, k);
-    const int32_t *row = p.map.table + (int64_t)c.user * p.map.max_pages;
+    const int3 c = pages[k];
+    const int32_t *row = p.map.table + (int64_t)user[k] * p.map.max_pages;
     int n = 0;
     bool bad = false;
-    for (int j = c.begin + lane; j < c.held; j += 32) {
+#pragma unroll 4
+    for (int j = c.x + lane; j < c.z; j += 32) {
       const int page = row[j];
       if (page < 0 || page >= p.pool.n_pages)
         bad = true;
       else
-        n += j < c.need && p.map.refs[page] > 1;
+        n += j < c.y && p.map.refs[page] > 1;
     }
     n = __reduce_add_sync(0xffffffffu, n);
     bad = __any_sync(0xffffffffu, bad);
@@ -147,12 +150,12 @@ __global__ void __launch_bounds__(KEEP_PLAN) kv4_keep_plan_kernel(const KeepPara
   // ---- which places they take
   for (int k = warp; k < p.n; k += KEEP_PLAN / 32) {
     if (at[k] < 0 || news[k] == 0) continue;
-    const Cut c = cut_of(p, k);
-    const int32_t *row = p.map.table + (int64_t)c.user * p.map.max_pages;
+    const int3 c = pages[k];
+    const int32_t *row = p.map.table + (int64_t)user[k] * p.map.max_pages;
     int to = at[k];
-    for (int j0 = c.begin; j0 < c.need; j0 += 32) {
+    for (int j0 = c.x; j0 < c.y; j0 += 32) {
       const int j = j0 + lane;
-      const unsigned shared = __ballot_sync(0xffffffffu, j < c.need && p.map.refs[row[min(j, c.need - 1)]] > 1);
+      const unsigned shared = __ballot_sync(0xffffffffu, j < c.y && p.map.refs[row[min(j, c.y - 1)]] > 1);
       if (shared >> lane & 1) p.place[to + __popc(shared & ((1u << lane) - 1))] = j;
       to += __popc(shared);
     }

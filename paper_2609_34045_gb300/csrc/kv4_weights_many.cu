@@ -354,26 +354,25 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
         const bool masked = any_odd || key0 + 32 > least || (p.window > 0 && key0 < most - p.window) || unlike[stage];
         const float *rows = reinterpret_cast<const float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS + part * 64;
         const uint32_t d = tmem + lanes + buf * F::D_COLS + part * 64;
-        // Sixteen rows at a time, the next ones' sums under way.  (Two forms: a branch between the rows would keep their
-        // operations apart)
+        // Half the rows' sums at a time: the buffer is free for the next products while the second half is weighed.  (Two
+        // forms: a branch between the rows would keep their operations apart)
         const auto weigh = [&](auto some) {
-          uint32_t a[2][G][16];
 #pragma unroll
-          for (int g = 0; g < G; ++g) tmem_ld16(d + g * WM_ROWS, a[0][g]);
+          for (int r0 = 0; r0 < 64; r0 += 32) {
+            uint32_t a[G][32];
 #pragma unroll
-          for (int r0 = 0; r0 < 64; r0 += 16) {
+            for (int g = 0; g < G; ++g) {
+              tmem_ld16(d + g * WM_ROWS + r0, reinterpret_cast<uint32_t(&)[16]>(a[g][0]));
+              tmem_ld16(d + g * WM_ROWS + r0 + 16, reinterpret_cast<uint32_t(&)[16]>(a[g][16]));
+            }
             tmem_wait_ld();
-            if (r0 + 16 < 64) {
-#pragma unroll
-              for (int g = 0; g < G; ++g) tmem_ld16(d + g * WM_ROWS + r0 + 16, a[(r0 / 16 + 1) & 1][g]);
-            } else {
+            if (r0 > 0) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(bar(W_DFREE + buf));
             }
-            const uint32_t(&x)[G][16] = a[r0 / 16 & 1];
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
+            for (int i = 0; i < 32; i += 4) {
               const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
               float2 x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
 #pragma unroll
@@ -383,8 +382,8 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
               }
 #pragma unroll
               for (int g = 0; g < G; ++g) {
-                x0 = fma2(s[g], {__uint_as_float(x[g][i]), __uint_as_float(x[g][i + 1])}, x0);
-                x1 = fma2(s[g], {__uint_as_float(x[g][i + 2]), __uint_as_float(x[g][i + 3])}, x1);
+                x0 = fma2(s[g], {__uint_as_float(a[g][i]), __uint_as_float(a[g][i + 1])}, x0);
+                x1 = fma2(s[g], {__uint_as_float(a[g][i + 2]), __uint_as_float(a[g][i + 3])}, x1);
               }
               float2 w0 = {wm_ex2(x0.x), wm_ex2(x0.y)}, w1 = {wm_ex2(x1.x), wm_ex2(x1.y)};
               if constexpr (decltype(some)::value) {
