@@ -32,6 +32,8 @@ class kfl_heads(C.Structure):
 # the same as packed bytes, in a third of a ctypes structure's time: a decode step's kernel is over in less than its
 # arguments take
 _pack_heads = struct.Struct("@Pqqii").pack
+_pack_mass = struct.Struct("@Pqqq").pack
+_pack_rows = struct.Struct("@Pqqqi4x").pack
 
 
 class kfl_rope_cfg(C.Structure):
@@ -73,7 +75,7 @@ def lib() -> C.CDLL:
     if _signed is not L:
         vp, i, f, P = C.c_void_p, C.c_int, C.c_float, C.POINTER
         heads, plan, pl, mp, sz = vp, P(kfl_rope_plan), P(kfl_kv4_pool), P(kfl_kv4_map), P(C.c_size_t)
-        mass = P(kfl_kv4_mass)
+        mass = rows = vp
         for name, args in {
             "kfl_rope_table": [P(kfl_rope_cfg), i, vp, vp],
             "kfl_rope": [plan, heads, heads, heads, heads, vp, i, i, i, vp, vp],
@@ -92,7 +94,7 @@ def lib() -> C.CDLL:
             "kfl_kv4_attend_tree": [pl, mp, i, heads, heads, vp, vp, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
             "kfl_kv4_weights": [pl, mp, i, heads, vp, mass, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
             "kfl_kv4_select": [pl, mp, mass, vp, i, i, i, i, vp, vp, vp, vp],
-            "kfl_kv4_keep": [pl, mp, vp, P(kfl_kv4_rows), vp, vp, mass, i, vp, vp, vp],
+            "kfl_kv4_keep": [pl, mp, vp, rows, vp, vp, mass, i, vp, vp, vp],
         }.items():
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, i
@@ -317,20 +319,21 @@ def _mass(mass, p, m):
     """kfl_kv4_mass of a tensor [layer][user][KV head][slot] whose slots are neighbours and whose rows do not overlap."""
     if mass is None:
         return None
-    want = (p.n_layers, m.n_users, p.n_kv_heads, m.max_pages * p.page_tokens)
-    if mass.dtype != torch.float32 or mass.dim() != 4 or mass.shape[0] != want[0] or mass.shape[1] < want[1] \
-            or mass.shape[2] != want[2] or mass.shape[3] < want[3]:
-        raise ValueError(f"mass is fp32 [layer][user][KV head][slot] of {list(want)}")
-    if not mass.is_contiguous():
+    shape = mass.shape
+    if mass.dtype != torch.float32 or len(shape) != 4 or shape[0] != p.n_layers or shape[1] < m.n_users \
+            or shape[2] != p.n_kv_heads or shape[3] < m.max_pages * p.page_tokens:
+        raise ValueError("mass is fp32 [layer][user][KV head][slot] of "
+                         f"{[p.n_layers, m.n_users, p.n_kv_heads, m.max_pages * p.page_tokens]}")
+    a, b, c, one = mass.stride()
+    if one != 1 or c < shape[3] or b < c * shape[2] or a < b * shape[1]:  # not in this order, with room between
         span = 1
-        for size, stride in sorted(zip(mass.shape, mass.stride()), key=lambda v: v[1]):
+        for size, stride in sorted(zip(shape, (a, b, c, one)), key=lambda v: v[1]):
             if size > 1 and stride < span:
                 raise ValueError("the rows of mass do not overlap")
             span += (size - 1) * stride
-        if mass.stride(3) != 1:
+        if one != 1:
             raise ValueError("the slots of mass are neighbours")
-    a, b, c, _ = mass.stride()
-    return C.byref(kfl_kv4_mass(_at(mass, "mass"), a, b, c))
+    return _pack_mass(_at(mass, "mass"), a, b, c)
 
 
 def kfl_kv4_weights(p, m, layer: int, q, lse, mass, workspace, users=None, q_start=None, max_q: int = 1, scale=None,
@@ -366,12 +369,13 @@ def kfl_kv4_keep(p, m, users, rows, counts, workspace, first=None, mass=None, st
     their lists: rows is int32 [layer][user of the list][KV head][most], of any strides whose last is 1 (expanded where
     layers or heads are alike).  mass moves with the rows.  Asynchronous."""
     n = users.numel()
-    if rows.dtype != torch.int32 or rows.dim() != 4 or tuple(rows.shape[:3]) != (p.n_layers, n, p.n_kv_heads) \
-            or rows.stride(3) != 1 and rows.shape[3] > 1:
+    shape, strides = rows.shape, rows.stride()
+    if rows.dtype != torch.int32 or len(shape) != 4 or shape[0] != p.n_layers or shape[1] != n or shape[2] != p.n_kv_heads \
+            or strides[3] != 1 and shape[3] > 1:
         raise ValueError(f"rows is int32 [layer][user of the list][KV head][most], {[p.n_layers, n, p.n_kv_heads]}, its last stride 1")
     a, b = _covers(p, m)
-    r = kfl_kv4_rows(_at(rows, "rows"), *rows.stride()[:3], rows.shape[3])
-    _check(lib().kfl_kv4_keep(a, b, _int32(users, "users"), C.byref(r), _int32(first, "first", n), _int32(counts, "counts", n),
+    r = _pack_rows(_at(rows, "rows"), strides[0], strides[1], strides[2], shape[3])
+    _check(lib().kfl_kv4_keep(a, b, _int32(users, "users"), r, _int32(first, "first", n), _int32(counts, "counts", n),
                               _mass(mass, p, m), n, _scratch(p, workspace), _int32(status, "status", 1), cuda_stream),
            "kfl_kv4_keep")
 
