@@ -16,6 +16,7 @@
 // (sequence, head), whose query rows take about a tile's time; warps take equal pieces and stream them through
 // slots of their own (bulk copies of the pages' K parts), with no barrier between warps.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4_stream.cuh"
 #include "kv4_weights.cuh"
@@ -29,7 +30,7 @@ template <int HD, int NT>
 struct Weigh {
   static constexpr int WARPS = NT <= 2 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
-  static constexpr int COLS = 8 * NT;
+  static constexpr int UNROLL = NT == 1 ? 4 : 2;  // groups of 16 keys in a body
   static constexpr int GROUPS = HD / KV4_GROUP;
   static constexpr int CODES = TILE * HD / 2, PARAMS = TILE * HD / 16;
   static constexpr int TILE_BYTES = CODES + PARAMS;
@@ -87,7 +88,7 @@ __device__ __forceinline__ void next_tile(Cursor &c, const int4 *info, const Wei
 template <int HD, int NT, bool BF16>
 __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_kernel(const WeightParams p) {
   using F = Weigh<HD, NT>;
-  constexpr int G = F::GROUPS, W = F::WARPS;
+  constexpr int G = F::GROUPS, W = F::WARPS, UNROLL = F::UNROLL;
   extern __shared__ __align__(128) uint8_t smem[];
   int4 *info = reinterpret_cast<int4 *>(smem + F::RING_BYTES);
   int *prefix = reinterpret_cast<int *>(info + FEW_SEQS);
@@ -201,9 +202,9 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
   load_page();
 
   uint32_t q[NT][G][2][2][2];  // B fragments: [group][word of a lane][half of its pairs][register]
-  float qs[NT][G][2], cf[NT][2], nl[NT][2];
+  float2 qs[NT][G], seed[NT][G], cf[NT], nl[NT];  // (columns 2 tig and 2 tig + 1)
   int end[NT][2];  // keys below it are seen
-  bool without = false;  // a row of this lane's saw nothing
+  bool without = false, absent = false;  // a row of this lane's saw nothing; a column is no row, or such a one
   unsigned slot = 0, phase = 0;
   float *mass = nullptr;
   const float log2_scale = fabsf(p.scale) * 1.44269504089f;
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
       // but for the smallest of fp16)
       uint32_t raw[NT][G][8];
       const int rows = at.count * p.group;
-      without = false;
+      without = absent = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int row = min(n * 8 + gid, rows - 1), t = row / p.group;
@@ -245,7 +246,8 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
           // (a row that saw nothing adds nothing, and rows that are not there neither)
           const bool counts = col < rows && lse != -INFINITY;
           without = without || (col < rows && !counts);
-          nl[n][c] = counts ? lse * -1.44269504089f : -INFINITY;
+          absent = absent || !counts;
+          (c ? nl[n].y : nl[n].x) = counts ? lse * -1.44269504089f : -INFINITY;
           end[n][c] = counts ? at.length - at.count + t + 1 : -1;
         }
       if (flat == w0) issue();
@@ -282,15 +284,13 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
               mma16816(even, 0x3C003C00u, 0x3C003C00u, 0, 0, q[n][g][j][h][0], q[n][g][j][h][1]);
               mma16816(odd, 0, 0, 0x3C003C00u, 0x3C003C00u, q[n][g][j][h][0], q[n][g][j][h][1]);
             }
-#pragma unroll
-          for (int c = 0; c < 2; ++c) qs[n][g][c] = LOW * fmaf(16.f, odd[c], even[c]);
+          qs[n][g] = {LOW * fmaf(16.f, odd[0], even[0]), LOW * fmaf(16.f, odd[1], even[1])};
+          seed[n][g] = {-8.f * qs[n][g].x, -8.f * qs[n][g].y};
         }
         const float factor = unit * log2_scale * (1.f / LOW);  // (columns of the accumulators: 2 tig, 2 tig + 1)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          cf[n][c] = __shfl_sync(0xffffffffu, factor, (2 * tig + c) * 4);
-          if (nl[n][c] == -INFINITY) cf[n][c] = 0.f;  // (no score makes up for it)
-        }
+        cf[n] = {__shfl_sync(0xffffffffu, factor, 8 * tig), __shfl_sync(0xffffffffu, factor, 8 * tig + 4)};
+        if (nl[n].x == -INFINITY) cf[n].x = 0.f;  // (no score makes up for it)
+        if (nl[n].y == -INFINITY) cf[n].y = 0.f;
       }
       if (flat == w0)
 #pragma unroll
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
     // ---- one tile.  A lane keeps the sums of two keys, of the 16 keys that bear its place's number
     const int tile0 = (at.first_tile + at.tile) * TILE;
     const int key_a = tile0 + 16 * tig + key_lane, key_b = key_a + 8;
-    float old_a = 0.f, old_b = 0.f, sum_a = 0.f, sum_b = 0.f;
+    float old_a = 0.f, old_b = 0.f;
     if (key_a < at.length) old_a = mass[key_a];
     if (key_b < at.length) old_b = mass[key_b];
     if (!dead && !wait_2s(bar0 + slot * 8, phase)) {
@@ -315,88 +315,100 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
 #pragma unroll
     for (int i = 0; i < F::SLOTS; ++i)
       if (i == (int)slot) have = valid[i];
-    const bool partly = without || tile0 + TILE > at.length - at.count + 1 || have != ALL ||
+    const bool partly = __any_sync(0xffffffffu, without) || tile0 + TILE > at.length - at.count + 1 || have != ALL ||
                         (p.window > 0 && tile0 < at.length - p.window);
-#pragma unroll 2
-    for (int st = 0; st < TILE / 16; ++st) {
-      const uint32_t kb = ring + slot * F::TILE_BYTES + 16 * st * (HD / 2);
-      const uint32_t kp = ring + slot * F::TILE_BYTES + F::CODES + 16 * st * (G * 4);
-      uint2 kw[2][G];
-      float ks[2][G], kc[2][G];
-      bool odd = false;
+    float2 sum[TILE / 16] = {};  // of the lane's columns, for its two keys of every 16
+    const auto weigh = [&](auto careful) {
+      constexpr bool CAREFUL = decltype(careful)::value;
+#pragma unroll(CAREFUL ? 1 : UNROLL)
+      for (int st = 0; st < TILE / 16; ++st) {
+        const uint32_t kb = ring + slot * F::TILE_BYTES + 16 * st * (HD / 2);
+        const uint32_t kp = ring + slot * F::TILE_BYTES + F::CODES + 16 * st * (G * 4);
+        uint2 kw[2][G];
+        float ks[2][G], kc[2][G];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) kw[h][g] = lds64(kb + (key_lane + 8 * h) * (HD / 2) + g * 32 + tig * 8);
-        const uint32_t off = (key_lane + 8 * h) * (G * 4);
-        uint32_t pk[G];
-        if constexpr (G == 2) {
-          const uint2 a = lds64(kp + off);
-          pk[0] = a.x, pk[G - 1] = a.y;
-        } else {
-          pk[0] = lds32(kp + off);
+          for (int g = 0; g < G; ++g) kw[h][g] = lds64(kb + (key_lane + 8 * h) * (HD / 2) + g * 32 + tig * 8);
+          const uint32_t off = (key_lane + 8 * h) * (G * 4);
+          uint32_t pk[G];
+          if constexpr (G == 2) {
+            const uint2 a = lds64(kp + off);
+            pk[0] = a.x, pk[G - 1] = a.y;
+          } else {
+            pk[0] = lds32(kp + off);
+          }
+#pragma unroll
+          for (int g = 0; g < G; ++g) ks[h][g] = half_lo(pk[g]), kc[h][g] = half_hi(pk[g]);
         }
+        float2 x[NT][2];  // of a key, both columns
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          ks[h][g] = half_lo(pk[g]), kc[h][g] = half_hi(pk[g]);
-          odd = odd || (pk[g] & 0x7c00u) == 0x7c00u || (pk[g] & 0x7c000000u) == 0x7c000000u;
-        }
-      }
-      float x[NT][4];
+          float acc[NT][4];
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        float acc[NT][4];
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t lo = j ? kw[0][g].y : kw[0][g].x, hi = j ? kw[1][g].y : kw[1][g].x;
+            uint32_t a0, a1, a2, a3, a4, a5, a6, a7;
+            code_pairs(lo, a0, a2), code_pairs(hi, a1, a3);
+            code_pairs(lo >> 8, a4, a6), code_pairs(hi >> 8, a5, a7);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t lo = j ? kw[0][g].y : kw[0][g].x, hi = j ? kw[1][g].y : kw[1][g].x;
-          uint32_t a0, a1, a2, a3, a4, a5, a6, a7;
-          code_pairs(lo, a0, a2), code_pairs(hi, a1, a3);
-          code_pairs(lo >> 8, a4, a6), code_pairs(hi >> 8, a5, a7);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            if (j == 0) {
-              const float seed[4] = {-8.f * qs[n][g][0], -8.f * qs[n][g][1], -8.f * qs[n][g][0], -8.f * qs[n][g][1]};
-              mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1], seed);
-            } else {
-              mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
+            for (int n = 0; n < NT; ++n) {
+              if (j == 0) {
+                const float from[4] = {seed[n][g].x, seed[n][g].y, seed[n][g].x, seed[n][g].y};
+                mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1], from);
+              } else {
+                mma16816(acc[n], a0, a1, a2, a3, q[n][g][j][0][0], q[n][g][j][0][1]);
+              }
+              mma16816(acc[n], a4, a5, a6, a7, q[n][g][j][1][0], q[n][g][j][1][1]);
             }
-            mma16816(acc[n], a4, a5, a6, a7, q[n][g][j][1][0], q[n][g][j][1][1]);
           }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              x[n][h] = fma2({ks[h][g], ks[h][g]}, {acc[n][2 * h], acc[n][2 * h + 1]},
+                             fma2({kc[h][g], kc[h][g]}, qs[n][g], g == 0 ? float2{0.f, 0.f} : x[n][h]));
         }
+        float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            x[n][i] = fmaf(ks[i >> 1][g], acc[n][i], g == 0 ? kc[i >> 1][g] * qs[n][g][i & 1] : fmaf(kc[i >> 1][g], qs[n][g][i & 1], x[n][i]));
-      }
-      float s0 = 0.f, s1 = 0.f;
-      if (!__any_sync(0xffffffffu, partly || odd)) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float2 scale = {cf[n][0], cf[n][1]}, from = {nl[n][0], nl[n][1]};
-          const float2 a = fma2({x[n][0], x[n][1]}, scale, from), b = fma2({x[n][2], x[n][3]}, scale, from);
-          s0 += ex2(a.x) + ex2(a.y), s1 += ex2(b.x) + ex2(b.y);
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = tile0 + 16 * st + key_lane + 8 * (i >> 1), c = i & 1;
-            const bool sees = key < end[n][c] && (p.window == 0 || key >= end[n][c] - p.window) && (have >> st & 1);
-            w[i] = sees ? ex2(fmaf(x[n][i], cf[n][c], nl[n][c])) : 0.f;
+          for (int h = 0; h < 2; ++h) {
+            float2 w = fma2(x[n][h], cf[n], nl[n]);
+            w = {ex2(w.x), ex2(w.y)};
+            if (CAREFUL) {
+              const int key = tile0 + 16 * st + key_lane + 8 * h;
+              const auto sees = [&](int e) { return key < e && (p.window == 0 || key >= e - p.window) && (have >> st & 1); };
+              w = {sees(end[n][0]) ? w.x : 0.f, sees(end[n][1]) ? w.y : 0.f};
+            }
+            s[h] += w.x + w.y;  // (in the same order: what is seen does not hang on what is not)
           }
-          s0 += w[0] + w[1], s1 += w[2] + w[3];  // (in the same order: what is seen does not hang on what is not)
-        }
-      }
 #pragma unroll
-      for (int off = 1; off < 4; off <<= 1) {
-        s0 += __shfl_xor_sync(0xffffffffu, s0, off);
-        s1 += __shfl_xor_sync(0xffffffffu, s1, off);
+        for (int i = 0; i < TILE / 16; ++i)  // (not by index: the sums stay in registers)
+          if (i == st) sum[i] = {s[0], s[1]};
       }
-      if (st == tig) sum_a = s0, sum_b = s1;
+    };
+    bool again = partly;
+    if (!partly) {
+      weigh(std::false_type());
+      // (a key that is no number has no weight for columns that are no rows)
+      if (__any_sync(0xffffffffu, absent)) {
+        float all = 0.f;
+#pragma unroll
+        for (int st = 0; st < TILE / 16; ++st) all += sum[st].x + sum[st].y;
+        again = __any_sync(0xffffffffu, all != all);
+      }
     }
+    if (again) weigh(std::true_type());
+    // sums over the four lanes of a key, in two exchanges: each lane ends with the 16 keys of its own number
+    float2 half[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 mine = tig & 2 ? sum[2 + i] : sum[i], other = tig & 2 ? sum[i] : sum[2 + i];
+      half[i] = {mine.x + __shfl_xor_sync(0xffffffffu, other.x, 2), mine.y + __shfl_xor_sync(0xffffffffu, other.y, 2)};
+    }
+    const float2 mine = tig & 1 ? half[1] : half[0], other = tig & 1 ? half[0] : half[1];
+    const float sum_a = mine.x + __shfl_xor_sync(0xffffffffu, other.x, 1), sum_b = mine.y + __shfl_xor_sync(0xffffffffu, other.y, 1);
     __syncwarp();  // (every lane has read the slot)
     if (fetch_flat < w1) issue();
     if (++slot == F::SLOTS) slot = 0, phase ^= 1;
