@@ -2,13 +2,15 @@
 // (include/kafila_kv4_evict.h).
 //
 // Mathematics.  A key t and a query row j, in groups g of 64 channels:
-//   a_tjg = sum_c (u_tc - 8) q_jc,   mass_t += sum_j 2^( sum_g s_tg a_tjg + sum_g c_tg sum_c q_jc - log2(e) lse_j )
+//   a_tjg = sum_c (u_tc - 8) q_jc,   mass_t += sum_j 2^( sum_g s_tg a_tjg + sum_g c_tg Q_jg - log2(e) lse_j ),  Q_jg = sum_c q_jc
 // (s, c: the key's scale and centre times scale log2(e)).  The a are matrix products of the codes, which are exact as fp16 or
-// bf16, with the queries as they stand, in their own type: nothing is rounded before the fp32 sums.  Scales and centres
-// act on the sums, four fused operations a score with two groups.
+// bf16, with the queries as they stand, in their own type: nothing is rounded before the fp32 sums.  Scales act on the sums.
+// bf16 takes the centres along in the products: s (a + (c / s) Q), c / s and Q as sums of three bf16 numbers each, whose
+// six larger products are sixteen more channels (2^-24 is left out).  That is 11 instructions for four scores in place of 17.
+// (fp16 has not got the exponents for it; nor has a key with scale 0, which takes the long way.)
 //
-// What bounds it.  An exponential a score: 16 a clock and SM, 2048 clocks for a unit of 256 keys by 128 rows, whose products
-// take some 1100 and whose other fp32 work about 1400 issue slots of each scheduler.
+// What bounds it.  FMA and issue slots: a pair of fp32 operations in one instruction takes two of a scheduler's.  (An exponential a score
+// is 1024 clocks for a unit of 256 keys by 128 rows, its products 1450.)
 //
 // Roles.  Warps 0-15: two threads per key (64 rows of a unit each), keys on the tensor memory's lanes, so that a key's weights
 // are summed in a register.  They also decode their keys into swizzled shared memory.  16: tensor copies of the queries, which
@@ -31,7 +33,8 @@ constexpr int WM_KEYS = 256, WM_ROWS = 128;
 constexpr int WM_SUMMERS = 16;  // warps
 constexpr int WM_COPY_WARP = 16, WM_STAT_WARP = 17, WM_MMA_WARP = 19;
 constexpr int WM_THREADS = (WM_MMA_WARP + 1) * 32;
-constexpr int WM_STAGES = 4;  // of queries: even, so that a stage is always the same warp's to sum (else it could take an older phase for its own)
+constexpr int WM_STAGES = 3;   // of queries, free again when summed and multiplied
+constexpr int WM_RECORDS = 4;  // of what is known of the queries' rows, which the sums' readers need for longer
 
 template <int HD>
 struct Many {
@@ -40,27 +43,50 @@ struct Many {
   static constexpr int HALF = 128 * HD * 2;        // of 128 keys
   static constexpr int D_COLS = GROUPS * WM_ROWS;  // of a half's sums in tensor memory
   static constexpr int BUFFERS = 256 / D_COLS;     // of each half
+  static constexpr int FOLD = 128 * 32;            // of sixteen more channels of 128 keys or rows: [2][row] of 16 bytes
   static constexpr int K_AT = WM_STAGES * STAGE;
-  static constexpr int ROWS_AT = K_AT + 2 * HALF;                      // float [stages][4][128]: sums of both groups, -lse, end
-  static constexpr int SUM_AT = ROWS_AT + WM_STAGES * 4 * WM_ROWS * 4;  // float [256]: the second threads' sums
-  static constexpr int ODD_AT = SUM_AT + WM_KEYS * 4;                  // int [stages]: a row that is not like the others
+  static constexpr int KF_AT = K_AT + 2 * HALF;                        // [half][group]
+  static constexpr int QF_AT = KF_AT + 2 * GROUPS * FOLD;              // [stages][group]
+  static constexpr int ROWS_AT = QF_AT + WM_STAGES * GROUPS * FOLD;    // float [records][4][128]: sums of both groups, -lse, end
+  static constexpr int SUM_AT = ROWS_AT + WM_RECORDS * 4 * WM_ROWS * 4;  // float [256]: the second threads' sums
+  static constexpr int ODD_AT = SUM_AT + WM_KEYS * 4;                  // int [records]: a row that is not like the others
   static constexpr int INFO_AT = ODD_AT + 16;                          // int4 [FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int BAR_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;
-  static constexpr int N_BARS = 3 * WM_STAGES + 8 + 3;
+  static constexpr int N_BARS = 2 * WM_STAGES + 2 * WM_RECORDS + 8 + 3;
   static constexpr int SMEM = BAR_AT + N_BARS * 8 + 32;
   static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
 };
-// Barriers: queries are there, may be overwritten, their sums are there; a half's buffer of sums is full, free; a half's
-// keys are there.
+// Barriers: queries are there, may be overwritten; their rows' records are there, may be overwritten; a half's sums are there,
+// have been read; a half's keys are there.
 enum {
   W_QFULL = 0,
-  W_QFREE = WM_STAGES,
-  W_STATS = 2 * WM_STAGES,
-  W_DFULL = 3 * WM_STAGES,
+  W_QFREE = W_QFULL + WM_STAGES,
+  W_STATS = W_QFREE + WM_STAGES,
+  W_RFREE = W_STATS + WM_RECORDS,
+  W_DFULL = W_RFREE + WM_RECORDS,
   W_DFREE = W_DFULL + 4,
   W_A = W_DFREE + 4,
   W_DRAIN = W_A + 2
 };
+
+// Shared-memory descriptor of a K-major operand of sixteen channels without a swizzle: 8 rows of 16 bytes are 128 bytes, the next 8
+// rows follow, their other 8 channels lie `next` bytes on.
+__device__ __forceinline__ uint64_t sdesc_k_plain(uint32_t addr, uint32_t next) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(next >> 4) << 16;
+  d |= (uint64_t)(128 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  return d;
+}
+// A number as three bf16 terms, each the rounding of what the ones before left.
+__device__ __forceinline__ void three_terms(float x, uint32_t (&t)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    t[i] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+    x -= __uint_as_float(t[i] << 16);
+  }
+}
 
 // A run of one key tile's units.
 struct Keys {
@@ -207,8 +233,11 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
   if (tid == 0) {
     for (int i = 0; i < WM_STAGES; ++i) {
       mbar_init(bar(W_QFULL + i), 1);
-      mbar_init(bar(W_QFREE + i), 1 + WM_SUMMERS);
+      mbar_init(bar(W_QFREE + i), 2);
+    }
+    for (int i = 0; i < WM_RECORDS; ++i) {
       mbar_init(bar(W_STATS + i), 1);
+      mbar_init(bar(W_RFREE + i), WM_SUMMERS);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(W_DFULL + i), 1);
@@ -221,8 +250,8 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
   }
   fence_mbar_init();
   if (warp == WM_MMA_WARP) tmem_alloc(base + F::BAR_AT + F::N_BARS * 8, 512);
-  // (rows behind a unit's tokens stay zero)
-  for (int i = tid; i < WM_STAGES * F::STAGE / 16; i += WM_THREADS) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+  // (rows behind a unit's tokens stay zero, and the second half of the sixteen channels)
+  for (int i = tid; i < F::ROWS_AT / 16; i += WM_THREADS) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
   fence_async_proxy();
   pdl_wait();
 
@@ -330,29 +359,42 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
                        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                        : "memory");
         }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float a = f16_to_f32((uint16_t)par[g]), b = f16_to_f32((uint16_t)(par[g] >> 16));
+          s[g] = {a * factor, a * factor}, c[g] = {b * factor, b * factor};
+          bool alone = (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u;  // (no number)
+          if constexpr (BF16) {
+            alone = alone || a == 0.f;
+            if (!alone) c[g] = {0.f, 0.f};  // (its centre goes along in the products)
+            if (part == (G == 2 ? g : 0)) {
+              uint32_t r[3];
+              three_terms(alone ? 0.f : b / a, r);
+              const uint32_t at = base + F::KF_AT + (half * G + g) * F::FOLD + row * 16;
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0] | r[0] << 16), "r"(r[1] | r[0] << 16),
+                           "r"(r[1] | r[2] << 16), "r"(0)
+                           : "memory");
+            }
+          }
+          odd = odd || alone;
+        }
         fence_async_proxy();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(W_A + half));
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const float a = f16_to_f32((uint16_t)par[g]) * factor, b = f16_to_f32((uint16_t)(par[g] >> 16)) * factor;
-          s[g] = {a, a}, c[g] = {b, b};
-          odd = odd || (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u;
-        }
       }
       const bool any_odd = __any_sync(0xffffffffu, odd);
       const int key0 = slot - lane, before = k.length - k.count;
       float2 sum = {0.f, 0.f};
       for (int t = k.from; t < k.to; ++t, ++unit) {
-        const unsigned stage = unit % WM_STAGES, buf = half * NB + unit % NB;
+        const unsigned record = unit % WM_RECORDS, buf = half * NB + unit % NB;
         const int token0 = (k.row_tile + t) * tokens;
         const int least = before + token0 + 1, most = before + min(k.count, token0 + tokens);
-        wait(W_STATS + stage, unit / WM_STAGES & 1);
+        wait(W_STATS + record, unit / WM_RECORDS & 1);
         wait(W_DFULL + buf, unit / NB & 1);
         __syncwarp();
         tc_fence_after();
-        const bool masked = any_odd || key0 + 32 > least || (p.window > 0 && key0 < most - p.window) || unlike[stage];
-        const float *rows = reinterpret_cast<const float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS + part * 64;
+        const bool masked = any_odd || key0 + 32 > least || (p.window > 0 && key0 < most - p.window) || unlike[record];
+        const float *rows = reinterpret_cast<const float *>(smem + F::ROWS_AT) + record * 4 * WM_ROWS + part * 64;
         const uint32_t d = tmem + lanes + buf * F::D_COLS + part * 64;
         // Half the rows' sums at a time: the buffer is free for the next products while the second half is weighed.  (Two
         // forms: a branch between the rows would keep their operations apart)
@@ -375,10 +417,12 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
             for (int i = 0; i < 32; i += 4) {
               const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
               float2 x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
+              if constexpr (!BF16 || decltype(some)::value) {
 #pragma unroll
-              for (int g = 0; g < G; ++g) {
-                const float4 q = *reinterpret_cast<const float4 *>(rows + g * WM_ROWS + r0 + i);
-                x0 = fma2(c[g], {q.x, q.y}, x0), x1 = fma2(c[g], {q.z, q.w}, x1);
+                for (int g = 0; g < G; ++g) {
+                  const float4 q = *reinterpret_cast<const float4 *>(rows + g * WM_ROWS + r0 + i);
+                  x0 = fma2(c[g], {q.x, q.y}, x0), x1 = fma2(c[g], {q.z, q.w}, x1);
+                }
               }
 #pragma unroll
               for (int g = 0; g < G; ++g) {
@@ -401,7 +445,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
         else
           weigh(std::false_type());
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(W_QFREE + stage));
+        if (lane == 0) mbar_arrive(bar(W_RFREE + record));
       }
       // ---- the tile's end: both threads' sums, added to the mass or handed on
       const int pair = half * 4 + (warp & 3);
@@ -480,8 +524,11 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
     find_keys(k, list, c0, c1);
     for (;;) {
       for (int t = k.from; t < k.to; ++t, ++unit) {
-        if ((unit & 1) != mine) continue;
-        const unsigned stage = unit % WM_STAGES;
+        const unsigned stage = unit % WM_STAGES, record = unit % WM_RECORDS;
+        if ((unit & 1) != mine) {  // (the other warp's: waited for all the same, or an older phase of the stage could be taken for it)
+          wait(W_QFULL + stage, unit / WM_STAGES & 1);
+          continue;
+        }
         const int token0 = (k.row_tile + t) * tokens;
         float lse[4];
 #pragma unroll
@@ -491,26 +538,46 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
           if (32 * i + lane < unit_rows && token < k.count)
             lse[i] = p.lse[((int64_t)k.first + token) * p.n_heads + k.head * group + row_head[i]];
         }
+        wait(W_RFREE + record, unit / WM_RECORDS & 1 ^ 1);
         wait(W_QFULL + stage, unit / WM_STAGES & 1);
         __syncwarp();
-        float *rows = reinterpret_cast<float *>(smem + F::ROWS_AT) + stage * 4 * WM_ROWS;
-#pragma unroll 2
-        for (int m = 0; m < WM_ROWS / 16; ++m) {
-          const int r = 16 * m + (lane & 15);  // of this lane's address: matrices of rows 0-7, 8-15, then their next 8 channels
-          const uint32_t from = base + stage * F::STAGE + r * 128;
-          uint32_t a[G][4][4];  // (all under way before the first is waited for)
+        float *rows = reinterpret_cast<float *>(smem + F::ROWS_AT) + record * 4 * WM_ROWS;
+        // (every lane of four has the sums of two rows of each 16: one of them, of one group, is its own to write.  Two such
+        // tiles at a time: a warp's chains of products, sums and roundings are its time)
+#pragma unroll 1
+        for (int m0 = 0; m0 < WM_ROWS / 16; m0 += 2) {
+          uint32_t a[2][G][4][4];
 #pragma unroll
-          for (int g = 0; g < G; ++g)
+          for (int m = 0; m < 2; ++m) {
+            const int r = 16 * (m0 + m) + (lane & 15);  // of this lane's address: matrices of rows 0-7, 8-15, then their next 8 channels
+            const uint32_t from = base + stage * F::STAGE + r * 128;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ldmatrix_x4(a[g][i], from + g * (WM_ROWS * 128) + (((2 * i + (lane >> 4)) ^ (r & 7)) << 4));
-          float d[G][4] = {};
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) ldmatrix_x4(a[m][g][i], from + g * (WM_ROWS * 128) + (((2 * i + (lane >> 4)) ^ (r & 7)) << 4));
+          }
+          float d[2][G][4] = {};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int g = 0; g < G; ++g) mma_ones<BF16>(d[g], a[g][i]);
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int g = 0; g < G; ++g)
-            if ((lane & 3) == 0) rows[g * WM_ROWS + 16 * m + (lane >> 2)] = d[g][0], rows[g * WM_ROWS + 16 * m + 8 + (lane >> 2)] = d[g][2];
+              for (int g = 0; g < G; ++g) mma_ones<BF16>(d[m][g], a[m][g][i]);
+          const int g = lane & 1;
+          if (g < G)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              const float low = g ? d[m][G - 1][0] : d[m][0][0], high = g ? d[m][G - 1][2] : d[m][0][2], sum = lane & 2 ? high : low;
+              const int of = 16 * (m0 + m) + (lane >> 2) + 4 * (lane & 2);
+              rows[g * WM_ROWS + of] = sum;
+              if constexpr (BF16) {
+                uint32_t s[3];
+                three_terms(sum, s);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + F::QF_AT + (stage * G + g) * F::FOLD + of * 16),
+                             "r"(s[0] | s[1] << 16), "r"(s[0] | s[2] << 16), "r"(s[1] | s[0] << 16), "r"(0)
+                             : "memory");
+              }
+            }
         }
         bool other = false;
 #pragma unroll
@@ -522,9 +589,13 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
           reinterpret_cast<int *>(rows)[3 * WM_ROWS + 32 * i + lane] = counts ? k.length - k.count + token0 + row_token[i] + 1 : -1;
         }
         other = __any_sync(0xffffffffu, other);
-        if (lane == 0) unlike[stage] = other;
+        if (lane == 0) unlike[record] = other;
+        if (BF16) fence_async_proxy();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(W_STATS + stage));
+        if (lane == 0) {
+          mbar_arrive(bar(W_STATS + record));
+          mbar_arrive(bar(W_QFREE + stage));
+        }
       }
       if (k.flat + k.to >= c1) break;
       next_keys(k, list, c1);
@@ -540,7 +611,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
     for (;; ++tiles) {
       const int n = __shfl_sync(0xffffffffu, k.to - k.from, 0);
       for (int t = 0; t < n; ++t, ++unit) {
-        const unsigned stage = __shfl_sync(0xffffffffu, unit % WM_STAGES, 0);
+        const unsigned stage = __shfl_sync(0xffffffffu, unit % WM_STAGES, 0), record = __shfl_sync(0xffffffffu, unit % WM_RECORDS, 0);
         ok = wait(W_QFULL + stage, unit / WM_STAGES & 1);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -550,13 +621,25 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           tc_fence_after();
           const uint64_t q = sdesc_k_sw128(at + stage * F::STAGE), a = sdesc_k_sw128(at + F::K_AT + half * F::HALF);
-          if (elect_one()) {
+          const uint64_t qf = sdesc_k_plain(at + F::QF_AT + stage * G * F::FOLD, F::FOLD / 2);
+          const uint64_t af = sdesc_k_plain(at + F::KF_AT + half * G * F::FOLD, F::FOLD / 2);
+          if (elect_one())
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
               for (int i = 0; i < 4; ++i)  // (descriptors count 16 bytes)
                 mma_bf16_ss(tm + buf * F::D_COLS + g * WM_ROWS, a + g * (128 * 128 >> 4) + i * 2, q + g * (WM_ROWS * 128 >> 4) + i * 2,
                             idesc, i > 0);
+          __syncwarp();
+          if (BF16 && half == 0) {  // (the rows' sums are not needed before)
+            if (!(ok = __all_sync(0xffffffffu, wait(W_STATS + record, unit / WM_RECORDS & 1)))) break;
+            tc_fence_after();
+          }
+          if (elect_one()) {
+            if (BF16)
+#pragma unroll
+              for (int g = 0; g < G; ++g)
+                mma_bf16_ss(tm + buf * F::D_COLS + g * WM_ROWS, af + g * (F::FOLD >> 4), qf + g * (F::FOLD >> 4), idesc, 1);
             mma_commit(bar(W_DFULL + buf));
             if (half == 1) mma_commit(bar(W_QFREE + stage));
           }
