@@ -5,9 +5,10 @@
 //   a_tjg = sum_c (u_tc - 8) q_jc,   mass_t += sum_j 2^( sum_g s_tg a_tjg + sum_g c_tg Q_jg - log2(e) lse_j ),  Q_jg = sum_c q_jc
 // (s, c: the key's scale and centre times scale log2(e)).  The a are matrix products of the codes, which are exact as fp16 or
 // bf16, with the queries as they stand, in their own type: nothing is rounded before the fp32 sums.  Scales act on the sums.
-// bf16 takes the centres along in the products: s (a + (c / s) Q), c / s and Q as sums of three bf16 numbers each, whose
-// six larger products are sixteen more channels (2^-24 is left out).  That is 11 instructions for four scores in place of 17.
-// (fp16 has not got the exponents for it; nor has a key with scale 0, which takes the long way.)
+// bf16 takes all but the scales along in the products: s_0 (a_0 + (c_0 / s_0) Q_0 - (1 / s_0) log2(e) lse) + s_1 (a_1 + (c_1 /
+// s_1) Q_1), each factor as a sum of three bf16 numbers, of whose products the six larger ones are channels more (2^-24 is left
+// out): ten instructions for four scores in place of 17, and no load.  (fp16 has not got the exponents for it; nor has a
+// key with scale 0, which takes the long way.)
 //
 // What bounds it.  FMA and issue slots: a pair of fp32 operations in one instruction takes two of a scheduler's.  (An exponential a score
 // is 1024 clocks for a unit of 256 keys by 128 rows, its products 1450.)
@@ -43,7 +44,7 @@ struct Many {
   static constexpr int HALF = 128 * HD * 2;        // of 128 keys
   static constexpr int D_COLS = GROUPS * WM_ROWS;  // of a half's sums in tensor memory
   static constexpr int BUFFERS = 256 / D_COLS;     // of each half
-  static constexpr int FOLD = 128 * 32;            // of sixteen more channels of 128 keys or rows: [2][row] of 16 bytes
+  static constexpr int FOLD = 128 * 32;            // of sixteen more channels of 128 keys or rows: [2][row] of 8
   static constexpr int K_AT = WM_STAGES * STAGE;
   static constexpr int KF_AT = K_AT + 2 * HALF;                        // [half][group]
   static constexpr int QF_AT = KF_AT + 2 * GROUPS * FOLD;              // [stages][group]
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
       const int slot = k.tile * WM_KEYS + key;
       bool there = false;
       float2 s[G], c[G];
-      bool odd = false;  // a scale or centre that is no number
+      bool odd = false;  // a scale or centre that is no number, or (bf16) not to be divided by
       {
         uint32_t par[G] = {};
         uint4 raw[HD / 64] = {};
@@ -359,24 +360,30 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
                        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                        : "memory");
         }
+        float ratio[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const float a = f16_to_f32((uint16_t)par[g]), b = f16_to_f32((uint16_t)(par[g] >> 16));
           s[g] = {a * factor, a * factor}, c[g] = {b * factor, b * factor};
-          bool alone = (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u;  // (no number)
-          if constexpr (BF16) {
-            alone = alone || a == 0.f;
-            if (!alone) c[g] = {0.f, 0.f};  // (its centre goes along in the products)
-            if (part == (G == 2 ? g : 0)) {
-              uint32_t r[3];
-              three_terms(alone ? 0.f : b / a, r);
-              const uint32_t at = base + F::KF_AT + (half * G + g) * F::FOLD + row * 16;
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0] | r[0] << 16), "r"(r[1] | r[0] << 16),
-                           "r"(r[1] | r[2] << 16), "r"(0)
-                           : "memory");
-            }
+          ratio[g] = b / a;
+          odd = odd || (par[g] & 0x7c00u) == 0x7c00u || (par[g] & 0x7c000000u) == 0x7c000000u || (BF16 && a == 0.f);
+        }
+        if constexpr (BF16) {
+          const float inv = 1.f / s[0].x;
+          odd = odd || !(fabsf(inv) < 1e30f);
+          // (the first thread's are the channels of the first group, the second's of the second)
+          if (part < G) {
+            const int g = G == 2 ? part : 0;
+            uint32_t r[3], n[3];
+            three_terms(odd ? 0.f : ratio[g], r);
+            three_terms(odd || g > 0 ? 0.f : inv, n);
+            const uint32_t at = base + F::KF_AT + (half * G + g) * F::FOLD + row * 16;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0] | r[0] << 16), "r"(r[1] | r[0] << 16),
+                         "r"(r[1] | r[2] << 16), "r"(n[0] | n[0] << 16)
+                         : "memory");
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + F::FOLD / 2), "r"(n[1] | n[0] << 16), "r"(n[1] | n[2] << 16)
+                         : "memory");
           }
-          odd = odd || alone;
         }
         fence_async_proxy();
         __syncwarp();
@@ -415,9 +422,10 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
             }
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
-              const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
-              float2 x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
-              if constexpr (!BF16 || decltype(some)::value) {
+              float2 x0 = {0.f, 0.f}, x1 = {0.f, 0.f};
+              if (!BF16 || (decltype(some)::value && odd)) {
+                const float4 nl = *reinterpret_cast<const float4 *>(rows + 2 * WM_ROWS + r0 + i);
+                x0 = {nl.x, nl.y}, x1 = {nl.z, nl.w};
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                   const float4 q = *reinterpret_cast<const float4 *>(rows + g * WM_ROWS + r0 + i);
@@ -573,9 +581,9 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
               if constexpr (BF16) {
                 uint32_t s[3];
                 three_terms(sum, s);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + F::QF_AT + (stage * G + g) * F::FOLD + of * 16),
-                             "r"(s[0] | s[1] << 16), "r"(s[0] | s[2] << 16), "r"(s[1] | s[0] << 16), "r"(0)
-                             : "memory");
+                const uint32_t to = base + F::QF_AT + (stage * G + g) * F::FOLD + of * 16;
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(s[0] | s[1] << 16), "r"(s[0] | s[2] << 16) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 8), "r"(s[1] | s[0] << 16) : "memory");
               }
             }
         }
@@ -587,6 +595,15 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
           other = other || (!counts && 32 * i + lane < unit_rows);
           rows[2 * WM_ROWS + 32 * i + lane] = counts ? lse[i] * -1.44269504089f : -INFINITY;
           reinterpret_cast<int *>(rows)[3 * WM_ROWS + 32 * i + lane] = counts ? k.length - k.count + token0 + row_token[i] + 1 : -1;
+          if constexpr (BF16) {
+            // (no weight: one term, whose products with finite numbers are none that others cannot be added to)
+            uint32_t n[3];
+            three_terms(counts && lse[i] != INFINITY ? lse[i] * -1.44269504089f : -0x1p100f, n);
+            const uint32_t to = base + F::QF_AT + stage * G * F::FOLD + (32 * i + lane) * 16;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 12), "r"(n[0] | n[1] << 16) : "memory");
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + F::FOLD / 2), "r"(n[0] | n[2] << 16), "r"(n[1] | n[0] << 16)
+                         : "memory");
+          }
         }
         other = __any_sync(0xffffffffu, other);
         if (lane == 0) unlike[record] = other;
