@@ -86,7 +86,9 @@ template <int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_kernel(const SelectParams p) {
   extern __shared__ __align__(16) uint32_t keys[];  // [thread][per]
   constexpr int WARPS = THREADS / 32, BINS = SEL_BINS / THREADS, LOG2 = THREADS == 256 ? 8 : 9;
-  __shared__ alignas(16) uint32_t hist[2][SEL_BINS];  // by turns: the last pass's counts are read while the next one's are made
+  // of clusters by turns: the last pass's counts are read by other blocks while the next one's are made
+  constexpr int TURNS = THREADS == 512 ? 2 : 1;
+  __shared__ alignas(16) uint32_t hist[TURNS][SEL_BINS];
   __shared__ uint32_t sums[2][WARPS];
   __shared__ int found[3];        // the bin, how many of it are wanted, how many there are
   __shared__ uint32_t totals[2];  // of this block: above the threshold, at it
@@ -97,7 +99,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
 #pragma unroll
     for (int j = 0; j < BINS; j += 4) *reinterpret_cast<uint4 *>(&counts[BINS * tid + j]) = make_uint4(0, 0, 0, 0);
   };
-  clear(hist[0]), clear(hist[1]);
+  clear(hist[0]), clear(hist[TURNS - 1]);
   pdl_launch_dependents();
   pdl_wait();
   const auto sync = [&]() {
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
     __syncthreads();  // (and the counts are zero)
     const auto narrow = [&](auto which) {
       constexpr int PASS = decltype(which)::value, SHIFT = PASS == 0 ? 21 : PASS == 1 ? 10 : 0;
-      uint32_t *counts = hist[PASS & 1];
+      uint32_t *counts = hist[PASS & (TURNS - 1)];
       const uint32_t base = smem_addr(counts);
       // (keys of no slot, 0, fall into the first bin, which is never the one)
       each(
@@ -219,8 +221,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
           greater += here;
         }
       }
-      // the other counts are free: every block has been here since it read them (zero again for the next pass)
-      clear(hist[(PASS & 1) ^ 1]);
+      // zero again for the next pass: the other counts, free since every block has been here after it read them; or these, each
+      // thread its own
+      clear(hist[TURNS == 2 ? (PASS & 1) ^ 1 : 0]);
       __syncthreads();
       T |= (uint32_t)found[0] << SHIFT;
       want = found[1];
@@ -266,7 +269,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 5 : 1) kv4_select_ke
     }
     // (the others have read this block's counts and totals)
     sync();
-    clear(hist[0]), clear(hist[1]);
+    if (TURNS == 2) clear(hist[0]), clear(hist[TURNS - 1]);
   }
 }
 
