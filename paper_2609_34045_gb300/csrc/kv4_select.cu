@@ -317,14 +317,25 @@ extern "C" int kfl_kv4_select(const kfl_kv4_pool *pool, const kfl_kv4_map *map, 
   p.users = users, p.n = n, p.budget = budget, p.first = first, p.recent = recent;
   p.rows = rows, p.counts = counts, p.status = status;
   p.wide = ((reinterpret_cast<uintptr_t>(mass->data) | (uintptr_t)(4 * (mass->layer_stride | mass->user_stride | mass->head_stride))) & 15) == 0;
-  // Many rows: a block of 256 threads each, as long as six of them fit an SM (a table is often a page longer than a round number
-  // of rows).  Few, or longer ones: blocks of 512 threads, as many of them as leave a thread 12 keys, or their shared memory
+  // Rows for every SM: a block of 256 threads each, if 36 keys a thread hold them (a table is often a page longer than a round
+  // number of rows).  Fewer, or longer ones: blocks of 512 threads, and clusters of them while a thread has more than 12 keys and
+  // all are at work at once, or where one block's shared memory does not hold a row.  us in a graph, by rows x length:
+  //                  256 threads   512   2 x 512   4 x 512   8 x 512
+  //     4 x  4096       5.0        4.5     5.8       6.6       8.7
+  //    64 x  4096       6.0        5.3     6.8      13.4      41.9
+  //   256 x  4096       7.6        9.1    22.3      49.8
+  //   896 x  4096      14.0       24.4    64.1
+  //     8 x 16384                  9.9     9.7       9.7      11.6
+  //   128 x 16384                 10.1    17.7      32.0      80.3
+  //     8 x 65536                 (171)   16.4      12.1      11.9
+  //   224 x 65536                 (406)   54.5      85.6     180.9
   const int most = map->max_pages * pool->page_tokens;
   const int64_t items = (int64_t)pool->n_layers * n * pool->n_kv_heads;
   p.cluster = 1;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (items >= 2 * 152 && keys_per_thread(most, 8) <= 36) return cuda_result(launch<256>(p, most, s), me);
-  while (p.cluster < 8 && keys_per_thread(most, 9 + p.log2_cluster) > (items * p.cluster < 2 * 152 ? 12 : SEL_BYTES / (4 * 512)))
+  if (items >= 152 && keys_per_thread(most, 8) <= 36) return cuda_result(launch<256>(p, most, s), me);
+  while (p.cluster < 8 &&
+         keys_per_thread(most, 9 + p.log2_cluster) > (items * p.cluster * 2 <= 152 ? 12 : SEL_BYTES / (4 * 512)))
     p.cluster *= 2, ++p.log2_cluster;
   return cuda_result(launch<512>(p, most, s), me);
 }

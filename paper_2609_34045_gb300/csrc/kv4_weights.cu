@@ -48,6 +48,16 @@ extern "C" int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map,
   }
   p.tickets = static_cast<unsigned *>(workspace);
   p.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + TICKET_BYTES);
+  // The streaming kernel takes up to 32 query rows per KV head at once, and twice as many in two launches; the other one's time is
+  // that of its 256-key tiles, much the same up to 128 rows: little as long as every SM has one at most (by what the tables could
+  // hold: the lengths are on the device).  us in a graph, heads of 128, 8 KV heads, bf16:
+  //   sequences x keys   streaming: 8 rows   16     32     48     64   |   the other: 72    128    256
+  //    1 x 1000                    5.6      7.0    9.3   16.9   18.2              11.0   10.7   12.0
+  //    4 x 3000                    6.4      8.2   10.7   19.1   21.1              21.8   19.9   23.7
+  //    8 x 8192                   12.7     17.0   23.7   40.9   47.0              73.4   62.1   80.3
+  //   32 x 4096                   21.1     28.9   41.6   74.4   83.0               143    124    159
+  const int64_t tiles = (int64_t)n_seqs * pool->n_kv_heads * (((int64_t)map->max_pages * pool->page_tokens + 255) / 256);
+  const bool few = rows <= WEIGHT_COLS || (rows <= 2 * WEIGHT_COLS && tiles > 152);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   int dev = 0, n_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -55,7 +65,11 @@ extern "C" int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map,
   for (int s0 = 0; e == cudaSuccess && s0 < n_seqs; s0 += FEW_SEQS) {
     p.seq0 = s0, p.n_seqs = std::min(FEW_SEQS, n_seqs - s0);
     p.users = users ? users + s0 : nullptr, p.q_start = q_start ? q_start + s0 : nullptr;
-    e = rows <= WEIGHT_FEW ? launch_weights_few(p, weight_cols(rows), n_sm, s) : launch_weights_many(p, n_sm, s);
+    if (few)
+      for (p.row0 = 0; e == cudaSuccess && p.row0 < rows; p.row0 += WEIGHT_COLS)
+        e = launch_weights_few(p, weight_cols(rows - p.row0), n_sm, s);
+    else
+      e = launch_weights_many(p, n_sm, s);
   }
   return cuda_result(e, me);
 }

@@ -7,7 +7,7 @@
 namespace kfl {
 
 constexpr int WEIGHT_SEQS = 1024;  // sequences of a call
-constexpr int WEIGHT_FEW = 32;     // most query rows per KV head of the streaming kernel
+constexpr int WEIGHT_COLS = 32;    // most query rows per KV head of one launch of the streaming kernel
 
 struct MassView {
   float *data;
@@ -30,6 +30,7 @@ struct WeightParams {
   const int32_t *all_users;           // the call's list, or NULL
   const int32_t *users, *q_start;     // from sequence seq0 on
   int seq0, n_seqs, n_tokens, max_q, n_heads, group;
+  int row0;  // streaming kernel: query rows [row0, row0 + its columns) of a KV head
   float scale;
   int window;
   unsigned *tickets;

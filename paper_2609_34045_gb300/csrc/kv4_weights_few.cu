@@ -45,10 +45,10 @@ struct Cursor {
   int user, length, first, count;
 };
 
-// Tiles of a sequence for a KV head.
+// Tiles of a sequence for a KV head: none if it has no query rows here.
 __device__ __forceinline__ int tiles_of(const int4 &v, const WeightParams &p, int &first_tile) {
   first_tile = p.window > 0 ? max(0, v.y - v.w + 1 - p.window) / TILE : 0;
-  return v.w > 0 ? max(0, (v.y + TILE - 1) / TILE - first_tile) : 0;
+  return v.w * p.group > p.row0 ? max(0, (v.y + TILE - 1) / TILE - first_tile) : 0;
 }
 
 __device__ __forceinline__ void enter_sequence(Cursor &c, const int4 *info, const WeightParams &p) {
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
 
   // ---- the list of tiles: each sequence's, summed.  Up to 32 sequences every warp makes the whole list, alike
   const auto units_of = [&](int s, bool again) {
-    const int4 v = weight_sequence(p, s, again, blockIdx.x == 0);
+    const int4 v = weight_sequence(p, s, again, blockIdx.x == 0 && p.row0 == 0);
     info[s] = v;
     int first_tile;
     const int n = tiles_of(v, p, first_tile);
@@ -214,11 +214,11 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
       // ---- a new (sequence, head): its query rows as fp16 (a power of two per row brings the largest to [2^14, 2^15): exact
       // but for the smallest of fp16)
       uint32_t raw[NT][G][8];
-      const int rows = at.count * p.group;
+      const int rows = at.count * p.group - p.row0;  // (or more than there are columns)
       without = absent = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int row = min(n * 8 + gid, rows - 1), t = row / p.group;
+        const int row = p.row0 + min(n * 8 + gid, rows - 1), t = row / p.group;
         const bool there = n * 8 + gid < rows;
         const uint16_t *e =
             reinterpret_cast<const uint16_t *>(p.q.row((int64_t)at.first + t, at.head * p.group + row - t * p.group)) + tig * 16;
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int col = n * 8 + 2 * tig + c, row = min(col, rows - 1), t = row / p.group;
+          const int col = n * 8 + 2 * tig + c, row = p.row0 + min(col, rows - 1), t = row / p.group;
           const float lse = p.lse[((int64_t)at.first + t) * p.n_heads + at.head * p.group + row - t * p.group];
           // (a row that saw nothing adds nothing, and rows that are not there neither)
           const bool counts = col < rows && lse != -INFINITY;
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(Weigh<HD, NT>::THREADS, 1) kv4_weights_few_ker
 #pragma unroll
     for (int i = 0; i < F::SLOTS; ++i)
       if (i == (int)slot) have = valid[i];
-    const bool partly = __any_sync(0xffffffffu, without) || tile0 + TILE > at.length - at.count + 1 || have != ALL ||
+    const bool partly = __any_sync(0xffffffffu, without) || tile0 + TILE > at.length - at.count + 1 + p.row0 / p.group || have != ALL ||
                         (p.window > 0 && tile0 < at.length - p.window);
     float2 sum[TILE / 16] = {};  // of the lane's columns, for its two keys of every 16
     const auto weigh = [&](auto careful) {
