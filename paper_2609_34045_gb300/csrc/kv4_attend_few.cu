@@ -11,6 +11,9 @@
 // factor per key and group, not per element, a group that reads as NaN reaches exactly the rows that see it, and
 // codes behind a user's end (any bits) are finite.
 //
+// Trees (TREE).  Of its sequence's last tokens a row sees those of its bits, and all before them: a step's 32 keys are one word of
+// them, asked for in the steps that reach those tokens only.
+//
 // What bounds it.  0.56 bytes per cached element and 4 flops per query row: HBM, if the elements' arithmetic
 // keeps up.  At 6.77 TB/s an SM gets 42 elements a clock, its logic units do 64 operations: 0.6 (K) and 0.75 (V) per
 // element for the nibbles and some 0.4 for the rest.  Measured: 32 users at 412 to 8192 keys, 64/8 heads of 128 (160 MB)

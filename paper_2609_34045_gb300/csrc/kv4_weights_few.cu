@@ -6,7 +6,10 @@
 // u 2^-24 or u 2^-20, and the 8 too many come off through the accumulator's start value.  Every step is exact but the
 // fp32 sums, the exponential (2^-22) and the weights' sum.
 //
-// What bounds it.  Half the cache's bytes (K): 0.28 bytes per cached element, 2 flops per query row: HBM.
+// What bounds it.  Half the cache's bytes (K): 0.28 bytes per cached element, 2 flops per query row: HBM, if the codes' instructions
+// keep up.  32 users at 412 to 8192 keys, 64/8 heads of 128 (88 MB): 20.3 us in a graph, 4.3 TB/s; some 500 instructions a tile at half
+// the issue slots, and about 6 us before the first tile and after the last.  (16 warps of 128 registers: 21.1; 14: 24.9; slots
+// of three tiles: the same.)
 //
 // Layout.  S^T = K Q^T with m16n8k16, keys in M, 8 query rows in N (two or four such column blocks).  A key's weights lie in
 // four lanes, which sum them; every cached row belongs to one warp, so nothing is merged and the order of the sums
