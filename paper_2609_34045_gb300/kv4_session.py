@@ -110,9 +110,10 @@ class Session:
             step.update(trees=dict(zip(users, trees)), before={u: before[u] for u in users}, start=start, rows={},
                         views=torch.empty(start[-1], -(-step["max_q"] // 32), dtype=torch.int32, device="cuda"),
                         positions=torch.empty(start[-1], dtype=torch.int32, device="cuda"))
-            kv4.kfl_kv4_tree(self._int32([p for t in trees for p in t]), step["views"], step["positions"],
-                             q_start=step["q_start"], first=self._int32([before[u] + self.evicted[u] for u in users]),
-                             max_q=step["max_q"], status=self.status, cuda_stream=self._stream())
+            if start[-1] > 0:
+                kv4.kfl_kv4_tree(self._int32([p for t in trees for p in t]), step["views"], step["positions"],
+                                 q_start=step["q_start"], first=self._int32([before[u] + self.evicted[u] for u in users]),
+                                 max_q=step["max_q"], status=self.status, cuda_stream=self._stream())
         return step
 
     def attend(self, layer: int, step: dict, q, k, v, window: int = 0):
@@ -188,8 +189,11 @@ class Session:
             raise ValueError("a session with masses evicts")
         if budget < 1 or first < 0 or recent < 0 or first + recent > budget:
             raise ValueError("first and recent are not negative and together at most the budget")
+        users = list(range(self.n_users) if users is None else users)
+        if len(set(users)) != len(users) or any(not 0 <= u < self.n_users for u in users):
+            raise ValueError(f"users below {self.n_users}, none twice")
         lengths = self.lengths.tolist()
-        users = [u for u in (range(self.n_users) if users is None else users) if lengths[u] > budget]
+        users = [u for u in users if lengths[u] > budget]
         if not users:
             return {}
         self._unshared(users, [0] * len(users), [budget] * len(users))

@@ -450,3 +450,94 @@ def test_keep_on_a_side_stream_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert dev[2].tolist() == [200, 90] and int(dev[3].sum()) == int((dev[1] >= 0).sum())
+
+
+def test_weights_of_long_caches_and_many_prompts():
+    """Key tiles whose rows several thread blocks share, and lists of many sequences."""
+    c = Case([5000, 40], 1, 128, 64, seed=3)
+    check_weights(c, queries(2, 8, 128))
+    c = Case([700, 300], 1, 128, 64, seed=3)
+    check_weights(c, queries(700, 4, 128), tokens=[600, 100])
+    lengths = [40 + (i * 13) % 70 for i in range(60)]
+    c = Case(lengths, 1, 64, 16, seed=3)
+    check_weights(c, queries(60 * 35, 2, 64), tokens=[35] * 60)
+
+
+@pytest.mark.parametrize("group", [3, 17, 100, 128])
+def test_weights_of_unusual_groups(group):
+    """Groups that do not divide a unit's rows, up to the largest; one token and several."""
+    c = Case([70, 33], 1, 64, 16, seed=3)
+    check_weights(c, queries(2, group, 64))
+    check_weights(c, queries(9, group, 64), tokens=[7, 2])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("tokens", [[3], [70]])
+def test_weights_of_keys_without_spread_and_far_from_zero(dtype, tokens):
+    """Groups of scale 0 (any code), of a centre thousands of steps from zero, and of next to no scale."""
+    c = Case([170], 1, 128, 32, seed=3)
+    for slot in range(0, 150, 3):
+        p = c.params(0, slot, 0, 0, 0)
+        p[slot % 2] = [(0.0, 0.75), (2.0 ** -24, -0.5), (0.01, 50.0), (0.0, 0.0), (3e-5, 2.0)][slot // 3 % 5]
+    check_weights(c, queries(tokens[0], 4, 128, dtype, std=0.25), tokens=tokens)
+
+
+def test_rows_of_other_sequences_do_not_reach_a_tail():
+    """A unit's rows behind a sequence's last token are the next sequence's, NaN and infinities among them."""
+    c = Case([100, 90], 1, 128, 64, seed=5)
+    q = queries(40 + 30, 4, 128)
+    q[40:, :, 5] = float("nan")
+    q[40:, 1, 7] = float("inf")
+    lse = lse_of(c, torch.nan_to_num(q, 0.0, 0.0), [40, 30], [0, 1], 0, 0, 128 ** -0.5)
+    both = check_weights_raw(c, q, [40, 30], lse)
+    alone = check_weights_raw(c, q[:40].contiguous(), [40], lse[:40].copy())
+    assert np.isfinite(both[0, 0]).all() and (both[0, 0] == alone[0, 0]).all()
+
+
+def test_keep_many_users():
+    rng = np.random.default_rng(1)
+    lengths = [int(v) for v in rng.integers(1, 60, 300)]
+    c = Cache(lengths, 16, 64, 1, 1, 4, shared=[(0, u, 1) for u in range(1, 40)], spare=80)
+    order = [int(u) for u in rng.permutation(300)][:260]
+    first = [int(rng.integers(0, lengths[u] + 1)) for u in order]
+    c.keep(order, first, [int(rng.integers(0, lengths[u] - f + 1)) for u, f in zip(order, first)])
+
+
+def test_select_of_many_users():
+    check_select([1 + (i * 29) % 300 for i in range(1024)], 90, 2, 5, page=16)
+
+
+def test_offsets_behind_4_gib():
+    """Pages, and masses, behind 32-bit byte offsets: weights of both kernels, and rows kept."""
+    from paper_2609_34045_gb300 import kv4
+    page, hd, heads, layers = 128, 128, 8, 40
+    n_pages = (5 << 30) // (page * hd * 9 // 8 * heads * layers)
+    pool_t = torch.zeros(n_pages, layers, heads, page * hd * 9 // 8, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[-1, -1], [n_pages - 1, n_pages - 2]], dtype=torch.int32, device="cuda")
+    lengths, refs = i32([0, 200]), torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    refs[-2:] = 1
+    p, m = kv4.pool(pool_t, page, layers, heads, hd), kv4.page_map(table, lengths, refs)
+    g = torch.Generator().manual_seed(3)
+    k = torch.randn(200, heads, hd, generator=g).to(BF16).cuda()
+    pos, user = torch.arange(200, dtype=torch.int32, device="cuda"), torch.ones(200, dtype=torch.int32, device="cuda")
+    kv4.kfl_kv4_append(p, m, layers - 1, k, k, user, pos)
+    mass = torch.zeros(layers, 2, heads, 14_000_000, device="cuda")[..., :256]  # the last layer's are 36 GB on
+    kd = ora.values(*ora.quantise(k.float().cpu().numpy()))
+    want = np.zeros((heads, 200))
+    for t in (1, 40):
+        q = queries(t, 8 * heads, hd)
+        lse = torch.full((t, 8 * heads), 5.0, device="cuda")
+        kv4.kfl_kv4_weights(p, m, layers - 1, q.cuda(), lse, mass, kv4.attend_workspace(p, 8 * heads, 1, t, t), users=i32([1]),
+                            q_start=i32([0, t]), max_q=t)
+        for h in range(heads):
+            for j in range(8 * h, 8 * h + 8):
+                want[h] += ora.weights(q[:, j].double().numpy(), kd[:, h], np.full(t, 5.0), ora.causal_keys(t, 200), hd ** -0.5).sum(0)
+    got = mass[layers - 1, 1, :, :200].double().cpu().numpy()
+    assert (np.abs(got - want) <= 2.0 ** -14 * want).all()
+    rows = torch.arange(100, 200, dtype=torch.int32, device="cuda").expand(layers, 1, heads, 100)
+    kv4.kfl_kv4_keep(p, m, i32([1]), rows, i32([100]), kv4.pages_workspace(p), mass=mass)
+    k2, v2 = torch.empty_like(k[:100]), torch.empty_like(k[:100])
+    kv4.kfl_kv4_read(p, m, layers - 1, user[:100], pos[:100], k2, v2)
+    assert torch.equal(k2.cpu(), torch.from_numpy(kd[100:].astype(np.float32)).to(BF16)) and torch.equal(v2, k2)
+    assert torch.equal(mass[layers - 1, 1, :, :100].double().cpu(), torch.from_numpy(got[:, 100:]))
+    assert (mass[layers - 1, 1, :, 100:200] == 0).all() and lengths.tolist() == [0, 100] and table[1].tolist() == [n_pages - 1, -1]

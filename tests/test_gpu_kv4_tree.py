@@ -261,3 +261,33 @@ def test_one_workspace_and_captured_calls():
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_more_sequences_than_one_launch_takes():
+    rng = np.random.default_rng(2)
+    tokens = [1 + i % 3 for i in range(600)]
+    c = Case([t + (i * 37) % 60 for i, t in enumerate(tokens)], 1, 64, 32, seed=8)
+    seen = [ora.tree_seen(random_tree(rng, t))[0] for t in tokens]
+    assert_near(*attend_tree(c, queries(sum(tokens), 2, 64), seen))
+    tokens = [20 + i % 7 for i in range(530)]  # the many-row kernel
+    c = Case([t + (i * 11) % 60 for i, t in enumerate(tokens)], 1, 64, 32, seed=9)
+    seen = [ora.tree_seen(random_tree(rng, t))[0] for t in tokens]
+    assert_near(*attend_tree(c, queries(sum(tokens), 4, 64), seen))
+
+
+@pytest.mark.parametrize("hd,group,dtype", [(128, 4, BF16), (64, 2, FP16)])
+def test_the_largest_trees(hd, group, dtype):
+    """1024 nodes: their words fill a row of 32, and several tiles are theirs alone."""
+    rng = np.random.default_rng(7)
+    c = Case([1024 + 77, 1024], 1, hd, 64, seed=2)
+    seen = [ora.tree_seen(random_tree(rng, 1024, s))[0] for s in (40, 3)]
+    assert_near(*attend_tree(c, queries(2048, group, hd, dtype), seen))
+
+
+def test_long_contexts_cut_between_blocks():
+    """Row blocks whose tiles several thread blocks share, the nodes in the last one's."""
+    rng = np.random.default_rng(8)
+    c = Case([9000, 40, 3333], 1, 128, 128, seed=2)
+    for tokens in ([5, 2, 1], [60, 33, 50]):
+        seen = [ora.tree_seen(random_tree(rng, t))[0] for t in tokens]
+        assert_near(*attend_tree(c, queries(sum(tokens), 8, 128), seen))

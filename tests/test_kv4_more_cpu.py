@@ -338,6 +338,9 @@ def test_evictions_that_cannot_be_are_refused(masses, session):  # noqa: F811
             masses.evict(**{**dict(first=0, recent=0), **bad})
     with pytest.raises(ValueError, match="masses"):
         session.evict(10)
+    for users in ([0, 0], [-1], [3]):
+        with pytest.raises(ValueError, match="users"):
+            masses.evict(10, users, first=0, recent=0)
     masses.lengths[:2] = torch.tensor([60, 64], dtype=torch.int32)
     masses.table[:2] = torch.arange(4, dtype=torch.int32)
     masses.refs[:] = 1
@@ -345,3 +348,10 @@ def test_evictions_that_cannot_be_are_refused(masses, session):  # noqa: F811
     with pytest.raises(kv4_session.NoRoom):  # three pages of each are another's too, and none is free
         masses.evict(40, first=1, recent=2)
     assert masses.evicted == [0, 0, 0] and masses.calls[-1][0] == "kfl_rope_table"
+
+
+def test_a_pass_of_trees_without_tokens(masses):
+    s = masses
+    step = s.begin({0: 0, 1: 0}, {})
+    s.accept(step, {})
+    assert "kfl_kv4_tree" not in [name for name, _ in s.calls] and "kfl_kv4_weights" not in [name for name, _ in s.calls]
