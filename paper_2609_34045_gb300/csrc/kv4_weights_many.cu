@@ -42,6 +42,8 @@ constexpr int WM_COPY_WARP = 16, WM_STAT_WARP = 17, WM_MMA_WARP = 19;
 constexpr int WM_THREADS = (WM_MMA_WARP + 1) * 32;
 constexpr int WM_STAGES = 3;   // of queries, free again when summed and multiplied
 constexpr int WM_RECORDS = 4;  // of what is known of the queries' rows, which the sums' readers need for longer
+constexpr int WM_FULL = 2 * WM_STAGES;  // barriers of the copies: an even number, so that each is waited for by one of the two
+                                        // warps that sum, in every phase
 
 template <int HD>
 struct Many {
@@ -59,7 +61,7 @@ struct Many {
   static constexpr int ODD_AT = SUM_AT + WM_KEYS * 4;                  // int [records]: a row that is not like the others
   static constexpr int INFO_AT = ODD_AT + 16;                          // int4 [FEW_SEQS], then int prefix[FEW_SEQS + 4]
   static constexpr int BAR_AT = INFO_AT + FEW_SEQS * 16 + (FEW_SEQS + 4) * 4;
-  static constexpr int N_BARS = 2 * WM_STAGES + 2 * WM_RECORDS + 8 + 3;
+  static constexpr int N_BARS = WM_FULL + WM_STAGES + 2 * WM_RECORDS + 8 + 3;
   static constexpr int SMEM = BAR_AT + N_BARS * 8 + 32;
   static_assert(SMEM + 1024 <= 232448, "shared memory of a block");
 };
@@ -67,7 +69,7 @@ struct Many {
 // have been read; a half's keys are there.
 enum {
   W_QFULL = 0,
-  W_QFREE = W_QFULL + WM_STAGES,
+  W_QFREE = W_QFULL + WM_FULL,
   W_STATS = W_QFREE + WM_STAGES,
   W_RFREE = W_STATS + WM_RECORDS,
   W_DFULL = W_RFREE + WM_RECORDS,
@@ -238,10 +240,8 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
   const int heads = p.pool.n_kv_heads, lp = p.pool.log2_tokens, group = p.group;
   const WmList list = {info, prefix, p.n_seqs, heads, p.window, tokens};
   if (tid == 0) {
-    for (int i = 0; i < WM_STAGES; ++i) {
-      mbar_init(bar(W_QFULL + i), 1);
-      mbar_init(bar(W_QFREE + i), 2);
-    }
+    for (int i = 0; i < WM_FULL; ++i) mbar_init(bar(W_QFULL + i), 1);
+    for (int i = 0; i < WM_STAGES; ++i) mbar_init(bar(W_QFREE + i), 2);
     for (int i = 0; i < WM_RECORDS; ++i) {
       mbar_init(bar(W_STATS + i), 1);
       mbar_init(bar(W_RFREE + i), WM_SUMMERS);
@@ -483,21 +483,21 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
   } else if (c0 < c1 && warp == WM_COPY_WARP) {
     // ---- queries: a box of the group's heads by the unit's tokens, 64 channels at a time; rows off 16 bytes by hand
     unsigned unit = 0;
+    bool ok = true;
     Keys k;
     find_keys(k, list, c0, c1);
     for (;;) {
       for (int t = k.from; t < k.to; ++t, ++unit) {
-        const unsigned stage = unit % WM_STAGES;
+        const unsigned stage = unit % WM_STAGES, full = unit % WM_FULL;
         const int token0 = (k.row_tile + t) * tokens;
-        wait(W_QFREE + stage, unit / WM_STAGES & 1 ^ 1);
-        __syncwarp();
+        if (!(ok = __all_sync(0xffffffffu, wait(W_QFREE + stage, unit / WM_STAGES & 1 ^ 1)))) break;
         const uint32_t to = base + stage * F::STAGE;
         if (use_map) {
           if (elect_one()) {
-            mbar_arrive_expect_tx(bar(W_QFULL + stage), unit_rows * HD * 2);
+            mbar_arrive_expect_tx(bar(W_QFULL + full), unit_rows * HD * 2);
 #pragma unroll
             for (int g = 0; g < G; ++g)
-              tma_load_3d(to + g * (WM_ROWS * 128), &q_map, 64 * g, k.head * group, k.first + token0, bar(W_QFULL + stage));
+              tma_load_3d(to + g * (WM_ROWS * 128), &q_map, 64 * g, k.head * group, k.first + token0, bar(W_QFULL + full));
           }
           __syncwarp();
         } else {
@@ -517,12 +517,14 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
           }
           fence_async_proxy();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(W_QFULL + stage));
+          if (lane == 0) mbar_arrive(bar(W_QFULL + full));
         }
       }
-      if (k.flat + k.to >= c1) break;
+      if (!ok || k.flat + k.to >= c1) break;
       next_keys(k, list, c1);
     }
+    // (no copy outlives the block, whoever has given up)
+    for (unsigned u = unit > WM_STAGES ? unit - WM_STAGES : 0; u < unit; ++u) wait_2s(bar(W_QFULL + u % WM_FULL), u / WM_FULL & 1);
   } else if (c0 < c1 && warp < WM_MMA_WARP) {
     // ---- every other unit's rows: their sums over each group's channels, log-sum-exps, and the keys that they see.  A lane
     // has the rows lane, lane + 32, ...: their tokens and heads are the same in every unit
@@ -539,10 +541,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
     for (;;) {
       for (int t = k.from; t < k.to; ++t, ++unit) {
         const unsigned stage = unit % WM_STAGES, record = unit % WM_RECORDS;
-        if ((unit & 1) != mine) {  // (the other warp's: waited for all the same, or an older phase of the stage could be taken for it)
-          wait(W_QFULL + stage, unit / WM_STAGES & 1);
-          continue;
-        }
+        if ((unit & 1) != mine) continue;
         const int token0 = (k.row_tile + t) * tokens;
         float lse[4];
 #pragma unroll
@@ -553,7 +552,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
             lse[i] = p.lse[((int64_t)k.first + token) * p.n_heads + k.head * group + row_head[i]];
         }
         wait(W_RFREE + record, unit / WM_RECORDS & 1 ^ 1);
-        wait(W_QFULL + stage, unit / WM_STAGES & 1);
+        wait(W_QFULL + unit % WM_FULL, unit / WM_FULL & 1);
         __syncwarp();
         float *rows = reinterpret_cast<float *>(smem + F::ROWS_AT) + record * 4 * WM_ROWS;
         // (every lane of four has the sums of two rows of each 16: one of them, of one group, is its own to write.  Two such
@@ -635,7 +634,7 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
       const int n = __shfl_sync(0xffffffffu, k.to - k.from, 0);
       for (int t = 0; t < n; ++t, ++unit) {
         const unsigned stage = __shfl_sync(0xffffffffu, unit % WM_STAGES, 0), record = __shfl_sync(0xffffffffu, unit % WM_RECORDS, 0);
-        ok = wait(W_QFULL + stage, unit / WM_STAGES & 1);
+        ok = wait(W_QFULL + unit % WM_FULL, unit / WM_FULL & 1);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const unsigned buf = __shfl_sync(0xffffffffu, half * NB + unit % NB, 0);
