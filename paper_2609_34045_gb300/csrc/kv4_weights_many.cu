@@ -11,13 +11,14 @@
 // key with scale 0, which takes the long way.)
 //
 // What bounds it.  2 head_dim flops and an exponential a (query head, visible key).  2048 tokens over 8192 keys, 64/8 heads of 128:
-// 302 us in bf16, 0.80 PFLOP/s of the 1.98 that a plain bf16 product reaches, 356 in fp16.  A unit of 256 keys by 128 rows takes
+// 305 us in bf16, 0.79 PFLOP/s of the 1.98 that a plain bf16 product reaches, 355 in fp16.  A unit of 256 keys by 128 rows takes
 // some 3250 clocks: its products 1400 of the tensor pipe (fed from shared memory at nearly all of its rate), its exponentials 1024, its
 // other fp32 operations about 1000 of a scheduler's slots; a half's products and the reading of their sums follow one another, as
 // two halves of two groups fill the tensor memory.  Few rows: a tile's keys come, are decoded and multiplied one after
 // the other, 5 us a tile of 256 keys however few the rows.
 // (Measured slower: 64 rows a product, two sets of sums a half, 382 us for 349 of the form then; four threads a key with all their
-// sums loaded at once, 374 for 302; a warp for each half's products, 368; the next tile's keys under way in registers, 314.)
+// sums loaded at once, 374, a warp for each half's products, 368, and the next tile's keys under way in registers, 314, each for
+// 302 of the form then; a barrier for each copy that one warp waits for in every phase made 305 of that.)
 //
 // Roles.  Warps 0-15: two threads per key (64 rows of a unit each), keys on the tensor memory's lanes, so that a key's weights
 // are summed in a register.  They also decode their keys into swizzled shared memory.  16: tensor copies of the queries, which
