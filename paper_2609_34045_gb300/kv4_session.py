@@ -226,9 +226,11 @@ class Session:
             self.evicted[u] = n
 
     def free(self, users):
+        users = list(users)
         kv4.kfl_kv4_free(self.pool, self.map, self._int32(users), status=self.status, cuda_stream=self._stream())
-        if self.mass is not None:
-            self.mass[:, list(users)] = 0
+        users = [u for u in users if 0 <= u < self.n_users]  # (the others are reported in `status`)
+        if self.mass is not None and users:
+            self.mass[:, users] = 0
         for u in users:
             self.evicted[u] = 0
 

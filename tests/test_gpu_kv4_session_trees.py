@@ -196,3 +196,20 @@ def test_evictions_without_room_for_shared_pages_are_refused():
         s.evict(40, [1], recent=8)
     assert torch.equal(s.table, table) and torch.equal(s.lengths, lengths) and s.evicted == [0, 0]
     assert s.evict(16, [1], first=0, recent=0) == {1: 48} and s.lengths.tolist() == [64, 16]
+
+
+@pytest.mark.parametrize("masses", [False, True])
+def test_users_that_there_are_none_of_are_reported_when_freed(masses):
+    from paper_2609_34045_gb300.kv4 import KFL_BAD_USER
+    from paper_2609_34045_gb300.kv4_session import Session
+    s = Session(1, 4, 2, 64, n_users=2, max_ctx=64, n_pages=8, page_tokens=16, masses=masses)
+    s.begin({0: 20, 1: 30})
+    s.evicted = [3, 5]
+    if masses:
+        s.mass.fill_(1)
+    s.free([-1, 2, 0])
+    assert s.status.item() == KFL_BAD_USER and s.lengths.tolist() == [0, 30] and s.evicted == [0, 5]
+    if masses:
+        assert not s.mass[:, 0].any() and (s.mass[:, 1] == 1).all()
+    s.free([])
+    assert s.lengths.tolist() == [0, 30]
