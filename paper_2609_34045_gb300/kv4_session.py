@@ -107,7 +107,13 @@ class Session:
         if any(self.evicted[u] for u in users):
             step["positions"] = self._int32([before[u] + self.evicted[u] + i for u in users for i in range(counts[u])])
         if trees is not None:
-            step.update(trees=dict(zip(users, trees)), before={u: before[u] for u in users}, start=start, rows={},
+            deepest = 0
+            for t in trees:
+                depth = []
+                for p in t:
+                    depth.append(1 + (depth[p] if p >= 0 else 0))
+                deepest = max([deepest, *depth])
+            step.update(trees=dict(zip(users, trees)), before={u: before[u] for u in users}, start=start, rows={}, deepest=deepest,
                         views=torch.empty(start[-1], -(-step["max_q"] // 32), dtype=torch.int32, device="cuda"),
                         positions=torch.empty(start[-1], dtype=torch.int32, device="cuda"))
             if start[-1] > 0:
@@ -118,7 +124,9 @@ class Session:
 
     def attend(self, layer: int, step: dict, q, k, v, window: int = 0):
         """One layer's attention of a pass: q [token][query head][head_dim] rotated, k and v appended, the users' rows
-        attended to (with masses, their weights added up: of trees by `accept`)."""
+        attended to (with masses, their weights added up: of trees by `accept`, so that a window holds their longest path)."""
+        if "trees" in step and self.mass is not None and 0 < window < step["deepest"]:
+            raise ValueError(f"a path of {step['deepest']} nodes is longer than the window of {window}")
         turned, out, stream = torch.empty_like(q), torch.empty_like(q), self._stream()
         places = dict(status=self.status, cuda_stream=stream)
         if step["positions"] is step["slots"]:

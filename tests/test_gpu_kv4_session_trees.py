@@ -213,3 +213,25 @@ def test_users_that_there_are_none_of_are_reported_when_freed(masses):
         assert not s.mass[:, 0].any() and (s.mass[:, 1] == 1).all()
     s.free([])
     assert s.lengths.tolist() == [0, 30]
+
+
+def test_a_window_shorter_than_a_path_is_refused_where_masses_are_kept():
+    """(A node sees all of its path, whatever the window; the accepted tokens' weights are those of the window's rows.)"""
+    from paper_2609_34045_gb300.kv4_session import Session
+    for masses in (False, True):
+        s = Session(1, 4, 2, 64, n_users=2, max_ctx=64, n_pages=8, page_tokens=16, masses=masses)
+        q, k = (torch.randn(9, h, 64, device="cuda").to(torch.bfloat16) for h in (4, 2))
+        step = s.begin({0: 5, 1: 4}, {1: [-1, 0, 0, 2]})  # a chain of five, and a path of three
+        if masses:
+            before = s.pages.clone()
+            with pytest.raises(ValueError):
+                s.attend(0, step, q, k, k, window=4)
+            assert torch.equal(s.pages, before)
+        else:
+            s.attend(0, step, q, k, k, window=4)
+        s.attend(0, step, q, k, k, window=5)
+        s.accept(step, {0: [0, 1, 2, 3, 4], 1: [0, 2, 3]})
+        assert s.lengths.tolist() == [5, 3] and s.status.item() == 0
+        if masses:  # an accepted token's weights sum to one in each of four heads, to 1e-5 (lse, weights)
+            got = s.mass[0, :2].sum(dim=(1, 2)).tolist()
+            assert got == pytest.approx([20, 12], abs=1e-3)
