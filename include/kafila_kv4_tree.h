@@ -35,7 +35,7 @@ int kfl_kv4_tree(const int32_t *parents, const int32_t *q_start, const int32_t *
 /* kfl_kv4_attend for trees: token i of c of a sequence sees the rows below length - c and, of the last c, those whose
  * bit is set in its row of `views` ([n_tokens][ceil(max_q / 32)], kfl_kv4_tree's or any others; bits from c on count for
  * nothing).  With window > 0 a token that sees b of the last c sees only the last max(0, window - b) rows of the others:
- * window rows in all.  A token that sees nothing gets zeros, and -inf in lse.
+ * window rows in all, or all its b if those are more.  A token that sees nothing gets zeros, and -inf in lse.
  * Arguments, workspace, precision and errors otherwise as kfl_kv4_attend's; max_q up to KFL_KV4_TREE_MOST
  * (KFL_ERR_RANGE). */
 int kfl_kv4_attend_tree(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,
