@@ -63,6 +63,13 @@ int kfl_kv4_append(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, 
                    const kfl_heads *v, const int32_t *users, const int32_t *positions, int n_tokens,
                    const kfl_rope_plan *rope, int32_t *status, void *cuda_stream);
 
+/* The same for rows whose place is not their position (drafted trees, users that rows were taken from): row t to slot
+ * slots[t] of its user, k rotated by positions[t] (device int32 [n_tokens]; rope is needed).  A slot behind the user's
+ * pages, or a position outside the rotation's table, is reported in status and not written. */
+int kfl_kv4_append_at(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *k,
+                      const kfl_heads *v, const int32_t *users, const int32_t *slots, const int32_t *positions,
+                      int n_tokens, const kfl_rope_plan *rope, int32_t *status, void *cuda_stream);
+
 /* The values that the cache holds for the rows (users[t], positions[t]) of one layer, rounded to the outputs'
  * type.  Rows out of range are reported in status and not written. */
 int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const int32_t *users,

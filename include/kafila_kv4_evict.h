@@ -4,7 +4,7 @@
  * The paper admits a session only if its whole context fits (section V-D).  A user that is cut to a budget of rows
  * goes on beyond it: the first and the last rows stay, and of the others those that queries have looked at most.
  * Keys keep the rotation of the position that they were appended at, so a row may lie at any slot; new
- * tokens are rotated by their true position (kfl_rope) and appended without a rotation.
+ * tokens are rotated by their true position (kfl_kv4_append_at).
  *
  * Conventions as in kafila_kv4.h.
  */

@@ -3,8 +3,8 @@
  *
  * A sequence's drafted tokens are the nodes of a tree (or of several: a node without a parent hangs on the
  * cached context).  A node sees the whole context, its ancestors and itself.  Nodes are appended like other tokens,
- * node i of c at slot length - c + i, but stand at position (context) + (number of ancestors): k is rotated by that
- * (kfl_rope) and appended without a rotation.
+ * node i of c at slot length - c + i, but stand at position (context) + (number of ancestors), which k is rotated by
+ * (kfl_kv4_append_at).
  *
  * Conventions as in kafila_kv4.h.
  */

@@ -1,4 +1,4 @@
-// Rows into and out of the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_append, kfl_kv4_read.
+// Rows into and out of the 4-bit paged KV cache (include/kafila_kv4.h): kfl_kv4_append, kfl_kv4_append_at, kfl_kv4_read.
 //
 // Memory bound in bytes (a 16-bit value read and 4.5 bits written, or the reverse), if the instructions per value stay
 // below some 12: at 41 (eight channels a thread, integer divisions of 64 bits, a code's clamp and shift one by one) 16384 rows
@@ -22,23 +22,25 @@ struct RowsParams {
   Kv4Map map;
   int layer;
   HeadsView k, v;
-  const int32_t *users, *positions;
+  const int32_t *users, *slots;
   int n_tokens;
-  const float2 *cos_sin;  // NULL: no rotation
+  const int32_t *positions;  // to rotate by (NULL: the slots)
+  const float2 *cos_sin;     // NULL: no rotation
   int n_pos, rope_half, rope_layout;
   int32_t *status;
 };
 
-// Where row t goes: its place in the table (NULL: out of range, reported once per row), its slot in the page.
-__device__ __forceinline__ const int32_t *place(const RowsParams &p, int user, int pos, bool reports, int &slot) {
+// Where row t goes: its place in the table (NULL: it or its position is out of range, reported once per row), its slot in
+// the page.
+__device__ __forceinline__ const int32_t *place(const RowsParams &p, int user, int at, int pos, bool reports, int &slot) {
   int bad = 0;
   if (user < 0 || user >= p.map.n_users)
     bad = KFL_BAD_USER;
-  else if (pos < 0 || (pos >> p.pool.log2_tokens) >= p.map.max_pages || (p.cos_sin && pos >= p.n_pos))
+  else if (at < 0 || (at >> p.pool.log2_tokens) >= p.map.max_pages || (p.cos_sin && (pos < 0 || pos >= p.n_pos)))
     bad = KFL_BAD_POSITION;
   if (bad && reports) report(p.status, bad);
-  slot = pos & (p.pool.page_tokens() - 1);
-  return bad ? nullptr : p.map.table + (int64_t)user * p.map.max_pages + (pos >> p.pool.log2_tokens);
+  slot = at & (p.pool.page_tokens() - 1);
+  return bad ? nullptr : p.map.table + (int64_t)user * p.map.max_pages + (at >> p.pool.log2_tokens);
 }
 __device__ __forceinline__ bool page_ok(const RowsParams &p, int page, bool reports) {
   if (page >= 0 && page < p.pool.n_pages) return true;
@@ -203,13 +205,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) kv4_append_kernel(const RowsPa
   // (threads behind the last row repeat it without storing it: the shuffles take whole warps)
   const Unit u = unit_of(p, min(unit, n_units - 1));
   const int c = (threadIdx.x & (lanes - 1)) * CH;
-  const int pos = p.positions[u.t], user = p.users ? p.users[u.t] : (int)u.t;
+  const int to_slot = p.slots[u.t], pos = p.positions ? p.positions[u.t] : to_slot, user = p.users ? p.users[u.t] : (int)u.t;
   const T *k_row = reinterpret_cast<const T *>(p.k.row(u.t, u.head));
   const Raw<T> v_raw = load_raw<T, WIDE>(reinterpret_cast<const T *>(p.v.row(u.t, u.head)) + c);
   const Raw<T> k_raw = load_raw<T, WIDE>(k_row + c);
   const bool reports = u.head == 0 && c == 0 && unit < n_units;
   int slot, page = -2;
-  const int32_t *at = place(p, user, pos, reports, slot);
+  const int32_t *at = place(p, user, to_slot, pos, reports, slot);
   if (at) page = *at;
   float x[CH];
   unpack(k_raw, x);
@@ -263,7 +265,7 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowsParams 
   const int c = (threadIdx.x & (lanes - 1)) * CH;
   const bool reports = u.head == 0 && c == 0;
   int slot;
-  const int32_t *at = place(p, p.users ? p.users[u.t] : (int)u.t, p.positions[u.t], reports, slot);
+  const int32_t *at = place(p, p.users ? p.users[u.t] : (int)u.t, p.slots[u.t], 0, reports, slot);
   if (!at) return;
   const int page = *at;
   if (!page_ok(p, page, reports)) return;
@@ -290,8 +292,8 @@ cudaError_t launch_rows(const RowsParams &p, bool reads, bool wide, cudaStream_t
 }
 
 int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer,
-              const kfl_heads *k, const kfl_heads *v, const int32_t *users, const int32_t *positions, int n_tokens,
-              const kfl_rope_plan *rope, int32_t *status, void *cuda_stream) {
+              const kfl_heads *k, const kfl_heads *v, const int32_t *users, const int32_t *slots, const int32_t *positions,
+              int n_tokens, const kfl_rope_plan *rope, int32_t *status, void *cuda_stream) {
   int rc = check_pool(pool, true, me);
   if (rc == KFL_OK) rc = check_map(map, me);
   if (rc == KFL_OK) rc = check_layer(pool, layer, me);
@@ -300,7 +302,7 @@ int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv
   if (k->n_heads != pool->n_kv_heads || v->n_heads != pool->n_kv_heads || k->dtype != v->dtype)
     return bad_arg(me, "k and v have the pool's heads and one type");
   if (rope && (!rope_valid(rope) || rope->rope_dim > pool->head_dim)) return bad_arg(me, "not a rotation of these heads");
-  if (n_tokens < 0 || (n_tokens > 0 && !positions)) return bad_arg(me, "positions are needed");
+  if (n_tokens < 0 || (n_tokens > 0 && !slots)) return bad_arg(me, "positions are needed");
   if (n_tokens == 0) return KFL_OK;
   if ((int64_t)n_tokens * pool->n_kv_heads > 0x7fffffff) {
     bad_arg(me, "more than 2^31 - 1 rows in one call");
@@ -309,7 +311,7 @@ int rows_call(const char *me, bool reads, const kfl_kv4_pool *pool, const kfl_kv
   RowsParams p = {};
   p.pool = pool_of(*pool), p.map = map_of(*map), p.layer = layer;
   p.k = view_of(*k), p.v = view_of(*v);
-  p.users = users, p.positions = positions, p.n_tokens = n_tokens;
+  p.users = users, p.slots = slots, p.positions = positions, p.n_tokens = n_tokens;
   if (rope) {
     p.cos_sin = reinterpret_cast<const float2 *>(rope->cos_sin);
     p.n_pos = rope->n_pos, p.rope_half = rope->rope_dim / 2, p.rope_layout = rope->layout;
@@ -340,13 +342,21 @@ extern "C" int kfl_kv4_page_bytes(const kfl_kv4_pool *pool, size_t *out) {
 extern "C" int kfl_kv4_append(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *k,
                               const kfl_heads *v, const int32_t *users, const int32_t *positions, int n_tokens,
                               const kfl_rope_plan *rope, int32_t *status, void *cuda_stream) {
-  return kfl::rows_call("kfl_kv4_append", false, pool, map, layer, k, v, users, positions, n_tokens, rope, status,
+  return kfl::rows_call("kfl_kv4_append", false, pool, map, layer, k, v, users, positions, nullptr, n_tokens, rope, status,
                         cuda_stream);
+}
+
+extern "C" int kfl_kv4_append_at(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *k,
+                                 const kfl_heads *v, const int32_t *users, const int32_t *slots, const int32_t *positions,
+                                 int n_tokens, const kfl_rope_plan *rope, int32_t *status, void *cuda_stream) {
+  const char *me = "kfl_kv4_append_at";
+  if (n_tokens > 0 && (!rope || !positions)) return kfl::bad_arg(me, "a rotation and its positions are needed");
+  return kfl::rows_call(me, false, pool, map, layer, k, v, users, slots, positions, n_tokens, rope, status, cuda_stream);
 }
 
 extern "C" int kfl_kv4_read(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const int32_t *users,
                             const int32_t *positions, int n_tokens, const kfl_heads *k_out, const kfl_heads *v_out,
                             int32_t *status, void *cuda_stream) {
-  return kfl::rows_call("kfl_kv4_read", true, pool, map, layer, k_out, v_out, users, positions, n_tokens, nullptr,
+  return kfl::rows_call("kfl_kv4_read", true, pool, map, layer, k_out, v_out, users, positions, nullptr, n_tokens, nullptr,
                         status, cuda_stream);
 }

@@ -81,6 +81,7 @@ def lib() -> C.CDLL:
             "kfl_rope": [plan, heads, heads, heads, heads, vp, i, i, i, vp, vp],
             "kfl_kv4_page_bytes": [pl, sz],
             "kfl_kv4_append": [pl, mp, i, heads, heads, vp, vp, i, plan, vp, vp],
+            "kfl_kv4_append_at": [pl, mp, i, heads, heads, vp, vp, vp, i, plan, vp, vp],
             "kfl_kv4_read": [pl, mp, i, vp, vp, i, heads, heads, vp, vp],
             "kfl_kv4_attend": [pl, mp, i, heads, heads, vp, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
             "kfl_kv4_attend_workspace_bytes": [pl, i, i, i, i, sz],
@@ -219,11 +220,17 @@ def kfl_kv4_page_bytes(p) -> int:
 
 
 def kfl_kv4_append(p, m, layer: int, k, v, users, positions, rope=None, status=None,
-                   cuda_stream: int | None = None) -> None:
+                   cuda_stream: int | None = None, rope_positions=None) -> None:
     """Rows of k and v ([token][KV head][head_dim]) of one layer into the users' pages at int32 positions [token];
-    k rotated first where ``rope`` is a rope_plan.  users None: row t is user t's.  Asynchronous."""
+    k rotated first where ``rope`` is a rope_plan: by the same positions, or (kfl_kv4_append_at) by ``rope_positions`` (int32
+    [token]) where a row's place is not its position.  users None: row t is user t's.  Asynchronous."""
     n = k.shape[0]
     a, b = _heads(k, "k", n, p.head_dim), _heads(v, "v", n, p.head_dim)
+    if rope_positions is not None:
+        _check(lib().kfl_kv4_append_at(_handle(p), _handle(m), layer, a, b, _int32(users, "users", n), _int32(positions, "positions", n),
+                                       _int32(rope_positions, "rope_positions", n), n, rope and _handle(rope),
+                                       _int32(status, "status", 1), cuda_stream), "kfl_kv4_append_at")
+        return
     _check(lib().kfl_kv4_append(_handle(p), _handle(m), layer, a, b, _int32(users, "users", n),
                                 _int32(positions, "positions", n), n, rope and _handle(rope),
                                 _int32(status, "status", 1), cuda_stream), "kfl_kv4_append")

@@ -129,13 +129,9 @@ class Session:
             raise ValueError(f"a path of {step['deepest']} nodes is longer than the window of {window}")
         turned, out, stream = torch.empty_like(q), torch.empty_like(q), self._stream()
         places = dict(status=self.status, cuda_stream=stream)
-        if step["positions"] is step["slots"]:
-            kv4.kfl_rope(self.rope, q, turned, None, None, step["positions"], **places)
-            kv4.kfl_kv4_append(self.pool, self.map, layer, k, v, step["row_users"], step["slots"], rope=self.rope, **places)
-        else:  # a row's slot is not its position
-            turned_k = torch.empty_like(k)
-            kv4.kfl_rope(self.rope, q, turned, k, turned_k, step["positions"], **places)
-            kv4.kfl_kv4_append(self.pool, self.map, layer, turned_k, v, step["row_users"], step["slots"], **places)
+        kv4.kfl_rope(self.rope, q, turned, None, None, step["positions"], **places)
+        kv4.kfl_kv4_append(self.pool, self.map, layer, k, v, step["row_users"], step["slots"], rope=self.rope,
+                           rope_positions=None if step["positions"] is step["slots"] else step["positions"], **places)
         lse = None if self.mass is None else torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
         rows = dict(users=step["users"], q_start=step["q_start"], max_q=step["max_q"], window=window, **places)
         if "views" in step:
