@@ -32,10 +32,17 @@ extern "C" {
 int kfl_kv4_tree(const int32_t *parents, const int32_t *q_start, const int32_t *first, int n_seqs, int n_tokens,
                  int max_q, uint32_t *views, int32_t *positions, int32_t *status, void *cuda_stream);
 
+/* The same for attention with a sliding window of `window` positions (0: none): a node sees itself and the window - 1 nodes
+ * before it on its path.  kfl_kv4_attend_tree with these views and the same window is the sliding window: each node
+ * sees the rows that its token would see behind its path alone.  (With kfl_kv4_tree's views a node sees all of its path,
+ * however short the window.)  Positions count all ancestors. */
+int kfl_kv4_tree_window(const int32_t *parents, const int32_t *q_start, const int32_t *first, int n_seqs, int n_tokens,
+                        int max_q, int window, uint32_t *views, int32_t *positions, int32_t *status, void *cuda_stream);
+
 /* kfl_kv4_attend for trees: token i of c of a sequence sees the rows below length - c and, of the last c, those whose
- * bit is set in its row of `views` ([n_tokens][ceil(max_q / 32)], kfl_kv4_tree's or any others; bits from c on count for
- * nothing).  With window > 0 a token that sees b of the last c sees only the last max(0, window - b) rows of the others:
- * window rows in all, or all its b if those are more.  A token that sees nothing gets zeros, and -inf in lse.
+ * bit is set in its row of `views` ([n_tokens][ceil(max_q / 32)], kfl_kv4_tree's, kfl_kv4_tree_window's or any others; bits
+ * from c on count for nothing).  With window > 0 a token that sees b of the last c sees only the last max(0, window - b) rows of the others:
+ * window rows in all, or all its b if those are more (a sliding window: kfl_kv4_tree_window's views).  A token that sees nothing gets zeros, and -inf in lse.
  * Arguments, workspace, precision and errors otherwise as kfl_kv4_attend's; max_q up to KFL_KV4_TREE_MOST
  * (KFL_ERR_RANGE). */
 int kfl_kv4_attend_tree(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q,

@@ -92,6 +92,7 @@ def lib() -> C.CDLL:
             "kfl_kv4_compact": [pl, mp, vp, vp, vp, vp, vp, vp],
             "kfl_kv4_copy_pages": [pl, vp, vp, i, vp, vp],
             "kfl_kv4_tree": [vp, vp, vp, i, i, i, vp, vp, vp, vp],
+            "kfl_kv4_tree_window": [vp, vp, vp, i, i, i, i, vp, vp, vp, vp],
             "kfl_kv4_attend_tree": [pl, mp, i, heads, heads, vp, vp, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
             "kfl_kv4_weights": [pl, mp, i, heads, vp, mass, vp, vp, i, i, i, f, i, vp, C.c_size_t, vp, vp],
             "kfl_kv4_select": [pl, mp, mass, vp, i, i, i, i, vp, vp, vp, vp],
@@ -295,15 +296,19 @@ def _views(views, n, max_q, where="views"):
 
 
 def kfl_kv4_tree(parents, views, positions=None, q_start=None, first=None, max_q: int = 1, status=None,
-                 cuda_stream: int | None = None) -> None:
+                 cuda_stream: int | None = None, window: int = 0) -> None:
     """Which of their sequence's nodes the nodes of drafted trees see, into views (int32 [token][ceil(max_q / 32)], a bit a
     node), and their positions, first (int32 [sequence], None: 0) + ancestors, into positions (int32 [token], may be
-    None).  parents: int32 [token], counted within the sequence, -1 for none; q_start as in kfl_kv4_attend.  Asynchronous."""
+    None).  parents: int32 [token], counted within the sequence, -1 for none; q_start as in kfl_kv4_attend.  With a window
+    (kfl_kv4_tree_window) a node sees that many of its path at most, the nearest.  Asynchronous."""
     n = parents.numel()
     n_seqs = q_start.numel() - 1 if q_start is not None else n
-    _check(lib().kfl_kv4_tree(_int32(parents, "parents"), _int32(q_start, "q_start"), _int32(first, "first", n_seqs), n_seqs, n,
-                              max_q, _views(views, n, max_q), _int32(positions, "positions", n), _int32(status, "status", 1),
-                              cuda_stream), "kfl_kv4_tree")
+    trees = (_int32(parents, "parents"), _int32(q_start, "q_start"), _int32(first, "first", n_seqs), n_seqs, n, max_q)
+    rest = (_views(views, n, max_q), _int32(positions, "positions", n), _int32(status, "status", 1), cuda_stream)
+    if window:
+        _check(lib().kfl_kv4_tree_window(*trees, window, *rest), "kfl_kv4_tree_window")
+    else:
+        _check(lib().kfl_kv4_tree(*trees, *rest), "kfl_kv4_tree")
 
 
 def kfl_kv4_attend_tree(p, m, layer: int, q, out, views, workspace, users=None, q_start=None, max_q: int = 1, scale=None,

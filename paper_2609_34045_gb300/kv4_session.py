@@ -117,14 +117,25 @@ class Session:
                         views=torch.empty(start[-1], -(-step["max_q"] // 32), dtype=torch.int32, device="cuda"),
                         positions=torch.empty(start[-1], dtype=torch.int32, device="cuda"))
             if start[-1] > 0:
-                kv4.kfl_kv4_tree(self._int32([p for t in trees for p in t]), step["views"], step["positions"],
+                step["parents"] = self._int32([p for t in trees for p in t])
+                kv4.kfl_kv4_tree(step["parents"], step["views"], step["positions"],
                                  q_start=step["q_start"], first=self._int32([before[u] + self.evicted[u] for u in users]),
                                  max_q=step["max_q"], status=self.status, cuda_stream=self._stream())
         return step
 
+    def _views(self, step, window):
+        """What the nodes of a pass see of their trees: their paths, or with a window that is shorter than one, its nodes."""
+        if not 0 < window < step["deepest"]:
+            return step["views"]
+        views = torch.empty_like(step["views"])
+        kv4.kfl_kv4_tree(step["parents"], views, q_start=step["q_start"], max_q=step["max_q"], window=window, status=self.status,
+                         cuda_stream=self._stream())
+        return views
+
     def attend(self, layer: int, step: dict, q, k, v, window: int = 0):
         """One layer's attention of a pass: q [token][query head][head_dim] rotated, k and v appended, the users' rows
-        attended to (with masses, their weights added up: of trees by `accept`, so that a window holds their longest path)."""
+        attended to, with a window the last `window` of them that a token would see behind its path alone.  With masses their weights
+        are added up, of trees by `accept`; a window shorter than the longest path is refused there."""
         if "trees" in step and self.mass is not None and 0 < window < step["deepest"]:
             raise ValueError(f"a path of {step['deepest']} nodes is longer than the window of {window}")
         turned, out, stream = torch.empty_like(q), torch.empty_like(q), self._stream()
@@ -135,7 +146,7 @@ class Session:
         lse = None if self.mass is None else torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
         rows = dict(users=step["users"], q_start=step["q_start"], max_q=step["max_q"], window=window, **places)
         if "views" in step:
-            kv4.kfl_kv4_attend_tree(self.pool, self.map, layer, turned, out, step["views"], self.workspace, lse=lse, **rows)
+            kv4.kfl_kv4_attend_tree(self.pool, self.map, layer, turned, out, self._views(step, window), self.workspace, lse=lse, **rows)
             if lse is not None:
                 step["rows"][layer] = (turned, lse, window)
         elif lse is not None:
