@@ -7,8 +7,8 @@
 // bf16, with the queries as they stand, in their own type: nothing is rounded before the fp32 sums.  Scales act on the sums.
 // bf16 takes all but the scales along in the products: s_0 (a_0 + (c_0 / s_0) Q_0 - (1 / s_0) log2(e) lse) + s_1 (a_1 + (c_1 /
 // s_1) Q_1), each factor as a sum of three bf16 numbers, of whose products the six larger ones are channels more (2^-24 is left
-// out): ten instructions for four scores in place of 17, and no load.  (fp16 has not got the exponents for it; nor has a
-// key with scale 0, which takes the long way.)
+// out): ten instructions for four scores in place of 17, and no load.  (fp16 has not got the exponents for it; a
+// key with scale 0, or so small a one that 1 / s_0 is 2^27 and more, takes the long way.)
 //
 // What bounds it.  2 head_dim flops and an exponential a (query head, visible key).  2048 tokens over 8192 keys, 64/8 heads of 128:
 // 305 us in bf16, 0.79 PFLOP/s of the 1.98 that a plain bf16 product reaches, 355 in fp16.  A unit of 256 keys by 128 rows takes
@@ -377,7 +377,9 @@ __global__ void __launch_bounds__(WM_THREADS, 1)
         }
         if constexpr (BF16) {
           const float inv = 1.f / s[0].x;
-          odd = odd || !(fabsf(inv) < 1e30f);
+          // (a row without weight goes along as -2^100: its products with the terms of 1 / s_0 stay finite below 2^27, which holds
+          // for every scale of a key, 2^-24 and up, under the usual softmax scales)
+          odd = odd || !(fabsf(inv) < 0x1p27f);
           // (the first thread's are the channels of the first group, the second's of the second)
           if (part < G) {
             const int g = G == 2 ? part : 0;
