@@ -33,8 +33,10 @@ typedef struct {
  * workspace as in kfl_kv4_attend: a sequence's tokens are its user's last ones, token i sees the rows up to its own.  A row of
  * q whose lse is -inf (it saw nothing) adds nothing.  n_seqs at most 1024; a user named again is reported
  * (KFL_BAD_USER) and its later sequences are skipped.  Rows on a page out of range are reported and keep what they have.
- * Precision: scores from the exact codes with fp32 sums, weights and their sums in fp32, always in the same
- * order: within 5e-6 of 64 bits (2-norm).
+ * Precision: scores from the exact codes with fp32 sums, weights and their sums in fp32, always in the same order.  The
+ * error of a weight grows with the numbers in its exponent: it is within 2^-19 (M + |lse_ij|) + 2^-22 of itself, M =
+ * |scale| sum_c (16 s_c + |c_c|) |q_c| with the scales and centres of the key's channels, and a sum of r weights within
+ * r 2^-24 of itself more; the mass that it is added to is rounded to fp32.  Measured with normal keys and queries, lse below 12: 1e-7 of 64 bits, up to 1e-6 (2-norm).
  * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer, sequences, query rows), KFL_ERR_CUDA. */
 int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q, const float *lse,
                     const kfl_kv4_mass *mass, const int32_t *users, const int32_t *q_start, int n_seqs, int n_tokens,
