@@ -38,6 +38,7 @@ class Session:
         self.n_layers, self.n_kv_heads = n_layers, n_kv_heads
         self.max_ctx, self.page_tokens, self.max_positions = max_ctx, page_tokens, max_positions or max_ctx
         self.evicted = [0] * n_users  # rows that a user has lost: its next token's position is its length and these
+        self.drafts = [None] * n_users  # the pass whose tree a user's last rows are, until it is accepted
         page_bytes = n_layers * n_kv_heads * (page_tokens * head_dim * 9 // 8)
         int32 = dict(dtype=torch.int32, device="cuda")
         self.pages = torch.empty(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
@@ -64,6 +65,11 @@ class Session:
         """torch's current stream: the inputs, the lists made here and the outputs' memory are ordered on it, and on no other."""
         return torch.cuda.current_stream().cuda_stream
 
+    def _no_drafts(self, users):
+        waiting = [u for u in users if self.drafts[u] is not None]
+        if waiting:
+            raise ValueError(f"a tree of users {waiting} waits: accept it, once, or free them")
+
     def _room(self, pages):
         if pages > 0:
             free = int((self.refs == 0).sum())
@@ -76,10 +82,11 @@ class Session:
         or -1 (a user without an entry drafts a chain).  Waits for
         the device once, to read the lengths, and once more in passes that need new pages, to count the free ones: the
         operators themselves only report a full pool in `status`, by which time a pass that goes on has attended at the
-        wrong positions.  Raises NoRoom before anything is changed."""
+        wrong positions.  Raises NoRoom before anything is changed.  A user whose tree has not been accepted takes no other pass."""
         users, n = list(counts), [counts[u] for u in counts]
         if any(not 0 <= u < self.n_users for u in users) or any(c < 0 for c in n):
             raise ValueError(f"counts of users below {self.n_users}, none negative")
+        self._no_drafts([u for u in users if counts[u] > 0])
         trees = None
         if parents is not None:
             trees = [list(parents.get(u, range(-1, c - 1))) for u, c in zip(users, n)]
@@ -113,7 +120,11 @@ class Session:
                 for p in t:
                     depth.append(1 + (depth[p] if p >= 0 else 0))
                 deepest = max([deepest, *depth])
-            step.update(trees=dict(zip(users, trees)), before={u: before[u] for u in users}, start=start, rows={}, deepest=deepest,
+            mark = object()
+            for u, c in zip(users, n):
+                if c > 0:
+                    self.drafts[u] = mark
+            step.update(mark=mark, trees=dict(zip(users, trees)), before={u: before[u] for u in users}, start=start, rows={}, deepest=deepest,
                         views=torch.empty(start[-1], -(-step["max_q"] // 32), dtype=torch.int32, device="cuda"),
                         positions=torch.empty(start[-1], dtype=torch.int32, device="cuda"))
             if start[-1] > 0:
@@ -165,14 +176,17 @@ class Session:
     def accept(self, step: dict, paths: dict):
         """Of the trees of a pass each user's nodes paths[user] stay, from a root down, each the child of the one before it
         (none, and users that are not named: nothing of the tree stays); the others' rows go.  With masses, the weights that
-        the accepted tokens gave are added up.  Once for a pass, before its users' next one.  Waits for the device, to look for
+        the accepted tokens gave are added up.  Once for a pass, before its users' next one: until then its users take no other
+        pass and are neither cut nor forked from, but may leave (be freed, or forked over).  Waits for the device, to look for
         pages that others hold too, and raises NoRoom where there are none to be had in their place."""
         if "trees" not in step or "accepted" in step:
             raise ValueError("a pass of trees is accepted, once")
-        users = list(step["trees"])
+        users = [u for u in step["trees"] if self.drafts[u] is step["mark"]]
         kept = [list(paths.get(u, [])) for u in users]
-        if set(paths) - set(users) or any(not 0 <= j < len(step["trees"][u]) or step["trees"][u][j] != up
-                                          for u, path in zip(users, kept) for j, up in zip(path, [-1] + path)):
+        if any(u in step["trees"] and u not in users and list(paths[u]) for u in paths):
+            raise ValueError("the trees are no longer their users' last tokens")
+        if set(paths) - set(step["trees"]) or any(not 0 <= j < len(step["trees"][u]) or step["trees"][u][j] != up
+                                                  for u, path in zip(users, kept) for j, up in zip(path, [-1] + path)):
             raise ValueError("paths are of the pass's users, each node the child of the one before it")
         lengths = self.lengths.tolist()
         if any(lengths[u] != step["before"][u] + len(step["trees"][u]) for u in users):
@@ -181,18 +195,24 @@ class Session:
         counts = [len(path) for path in kept]
         self._unshared(users, first, [a + c for a, c in zip(first, counts)])
         step["accepted"] = True
+        for u in users:
+            self.drafts[u] = None
+        if not users:
+            return
+        ids = self._int32(users)
         most = max([1, *counts])
         rows = self._int32([[a + j for j in path] + [-1] * (most - len(path)) for a, path in zip(first, kept)])
-        kv4.kfl_kv4_keep(self.pool, self.map, step["users"], rows[None, :, None].expand(self.n_layers, len(users), self.n_kv_heads, most),
+        kv4.kfl_kv4_keep(self.pool, self.map, ids, rows[None, :, None].expand(self.n_layers, len(users), self.n_kv_heads, most),
                          self._int32(counts), self.scratch, first=self._int32(first), mass=self.mass, status=self.status,
                          cuda_stream=self._stream())
         if self.mass is None or sum(counts) == 0:
             return
-        at = [a + j for a, path in zip(step["start"], kept) for j in path]
+        start = dict(zip(step["trees"], step["start"]))
+        at = [start[u] + j for u, path in zip(users, kept) for j in path]
         pick = torch.tensor(at, device="cuda")
         start = [sum(counts[:i]) for i in range(len(counts) + 1)]
         for layer, (q, lse, window) in step["rows"].items():
-            kv4.kfl_kv4_weights(self.pool, self.map, layer, q[pick], lse[pick], self.mass, self.workspace, users=step["users"],
+            kv4.kfl_kv4_weights(self.pool, self.map, layer, q[pick], lse[pick], self.mass, self.workspace, users=ids,
                                 q_start=self._int32(start), max_q=max(counts), window=window, status=self.status,
                                 cuda_stream=self._stream())
 
@@ -211,6 +231,7 @@ class Session:
         users = [u for u in users if lengths[u] > budget]
         if not users:
             return {}
+        self._no_drafts(users)
         self._unshared(users, [0] * len(users), [budget] * len(users))
         ids, stream = self._int32(users), self._stream()
         rows = torch.empty(self.n_layers, len(users), self.n_kv_heads, budget, dtype=torch.int32, device="cuda")
@@ -230,6 +251,7 @@ class Session:
         src, dst = list(src), list(dst)
         if len(src) != len(dst) or len(set(dst)) != len(dst) or any(not 0 <= u < self.n_users for u in src + dst):
             raise ValueError(f"as many users below {self.n_users} in src and dst, in dst none twice")
+        self._no_drafts([a for a, b in zip(src, dst) if a != b])
         lengths = self.lengths.tolist()
         self._room(sum(a != b and lengths[a] % self.page_tokens != 0 for a, b in zip(src, dst)))
         kv4.kfl_kv4_fork(self.pool, self.map, self._int32(src), self._int32(dst), self.scratch, status=self.status,
@@ -237,8 +259,10 @@ class Session:
         if self.mass is not None:
             self.mass[:, dst] = self.mass[:, src]
         evicted = [self.evicted[u] for u in src]
-        for u, n in zip(dst, evicted):
+        for a, u, n in zip(src, dst, evicted):
             self.evicted[u] = n
+            if a != u:
+                self.drafts[u] = None
 
     def free(self, users):
         users = list(users)
@@ -247,7 +271,7 @@ class Session:
         if self.mass is not None and users:
             self.mass[:, users] = 0
         for u in users:
-            self.evicted[u] = 0
+            self.evicted[u], self.drafts[u] = 0, None
 
     def compact(self):
         """Live pages to the lowest numbers; returns how many there are (on the device)."""

@@ -42,4 +42,4 @@ def test_a_sessions_views(session, monkeypatch):  # noqa: F811
     assert [a[5].data_ptr() for a, _ in views][2::2] == [a[1].data_ptr() for a, _ in trees[1:]]
     assert all(kw["window"] == w for (_, kw), w in zip(views, (0, 3, 2, 100, 1)))
     with pytest.raises(kv4_session.NoRoom):
-        session.begin({0: 65}, {})
+        session.begin({2: 65}, {})
