@@ -36,7 +36,8 @@ typedef struct {
  * Precision: scores from the exact codes with fp32 sums, weights and their sums in fp32, always in the same order.  The
  * error of a weight grows with the numbers in its exponent: it is within 2^-19 (M + |lse_ij|) + 2^-22 of itself, M =
  * |scale| sum_c (16 s_c + |c_c|) |q_c| with the scales and centres of the key's channels, and a sum of r weights within
- * r 2^-24 of itself more; the mass that it is added to is rounded to fp32.  Measured with normal keys and queries, lse below 12: 1e-7 of 64 bits, up to 1e-6 (2-norm).
+ * r 2^-24 of itself more; the mass that it is added to is rounded to fp32.  Measured with normal keys and queries, lse
+ * below 12: 1e-7 of 64 bits, up to 1e-6 (2-norm).
  * Errors: KFL_ERR_ARG, KFL_ERR_RANGE (layer, sequences, query rows), KFL_ERR_CUDA. */
 int kfl_kv4_weights(const kfl_kv4_pool *pool, const kfl_kv4_map *map, int layer, const kfl_heads *q, const float *lse,
                     const kfl_kv4_mass *mass, const int32_t *users, const int32_t *q_start, int n_seqs, int n_tokens,
@@ -69,7 +70,8 @@ typedef struct {
  * given back.  Moved in place: a list's entry j is at least first + j and below the length (as in every ascending list
  * of different slots); another one is reported (KFL_BAD_POSITION) and its row, and mass, stay what the slot held.
  * Pages that other users hold too are not written: the user gets new ones (free before the call, lowest first) for
- * those that rows move in.  A user without room for these is left as it was (KFL_NO_PAGES), and so is one whose
+ * those that rows move in.  From the first user on that there is no room for, those that need new pages are left as they
+ * were (KFL_NO_PAGES), also where the free ones would do for a later one of them.  Left as it was is also one whose
  * first or count is negative, whose count is above `most` or whose rows would be more than its length
  * (KFL_BAD_POSITION), that is named again (KFL_BAD_USER), or with a page out of range (KFL_BAD_PAGE).
  * A user that loses nothing is not touched.  workspace: kfl_kv4_pages_workspace_bytes, its contents of no account.
