@@ -20,7 +20,9 @@ extern "C" {
 /* Attention weight per cached row: device fp32 at data + layer * layer_stride + user * user_stride + head *
  * head_stride + slot (strides in elements; a KV head's slots contiguous, max_pages * page_tokens of them).  Different
  * layers, users and heads do not overlap.  Slots behind a user's length hold 0: new rows start from there
- * (kfl_kv4_keep sees to it; the caller zeroes the buffer first, and a user's slots when kfl_kv4_free ends it). */
+ * (kfl_kv4_keep sees to it; the caller zeroes the buffer first, and a user's slots when kfl_kv4_free ends it).  What
+ * kfl_kv4_fork gives a user is weighed anew by nobody: the caller copies the source's slots, all of them, to the
+ * destination's (of all pairs at once, as the rows are). */
 typedef struct {
   float *data;
   int64_t layer_stride, user_stride, head_stride;
