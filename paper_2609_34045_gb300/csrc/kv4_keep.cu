@@ -8,8 +8,9 @@
 //
 // What bounds it.  The kept rows' bytes, read and written (9/8 head_dim each way), through rows of 64 and 8 bytes: eight users of
 // 8192 rows cut to half, 14 layers of 4 heads of 128, 134 us with the reservation after it, of which the moving takes some 120: 428 MB
-// read (a sector of parameters for every second row of it) and 237 MB written, 5.6 TB/s.  (Two chunks ahead instead of one: the
-// same.)  With a few rows (accepted drafts) the chain of round trips, plan, list, page, row: 11 us with the reservation.  The next chunk's rows are under way, and the one
+// read and 237 MB written, 5.6 TB/s.  Read is what lines of 128 bytes of codes come to, two rows in each (191 bytes a kept row for its
+// 128), with sectors of parameters (30), masses (8) and the lists (4): 427 MB; in sectors of 32 bytes all through it would be 312.  (Two
+// chunks ahead instead of one: the same.)  With a few rows (accepted drafts) the chain of round trips, plan, list, page, row: 11 us with the reservation.  The next chunk's rows are under way, and the one
 // after's addresses looked up, while a chunk is stored.
 #include <algorithm>
 

@@ -6,7 +6,7 @@
 // and the first ones with T itself, each to the place that a running count gives it.
 //
 // What bounds it.  4 bytes a row in and 4 bytes a kept row out; the instructions a key (some 40), and a chain of ten barriers: 896 rows
-// of up to 8192 keys 20 us, one row of 4096 keys 4.4, eight of 131072 16.3 (two thousand clocks each to load, to count a pass, and
+// of up to 8192 keys 20 us (in two waves: five blocks an SM are 760), four rows of 4096 keys 4.4, eight of 131072 16.3 (two thousand clocks each to load, to count a pass, and
 // twice that to read the other blocks' counts).  The
 // keys are read from memory once and stay in shared memory, neighbours with one thread, so that a place in the output costs a
 // thread one sum over the block and not a vote a key (128 instructions a key with the votes).  (A row longer than the shared

@@ -1,4 +1,5 @@
-// What the 4-bit cache's kernels on tcgen05 share beside prefill_tc.cuh: operands in tensor memory.
+// What the 4-bit cache's kernels on tcgen05 share beside prefill_tc.cuh: the fence before the tensor unit reads shared memory, pairs of
+// sums, and (the attention) operands in tensor memory.
 #pragma once
 
 #include "prefill_tc.cuh"
